@@ -13,6 +13,10 @@
  *   - the CoverPrune-Lite selection                      (Sec. 4, Eqs. lite_group, lite_select)
  *   - the compaction of the kept tokens                  (Sec. 3.2 / Sec. 5.1: the kept tokens
  *                                                          are the LLM's visual input)
+ * and, for the language model that decodes on the kept tokens:
+ *   - rotary positions at the kept tokens' own indices, and their gradient
+ *   - the append of keys and values to a paged cache
+ *   - the attention of one new token a sequence over that cache
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -70,7 +74,9 @@ typedef enum {
   CP_EDEVICE = 6       /* a device-side consistency check failed (see coverprune_check) */
 } cp_status;
 
-typedef enum { CP_F32 = 0, CP_BF16 = 1 } cp_dtype;
+/* CP_E4M3 (8 bits: 4 of exponent, 3 of fraction, largest value 448) is a type
+ * of caches only. */
+typedef enum { CP_F32 = 0, CP_BF16 = 1, CP_E4M3 = 2 } cp_dtype;
 
 /* Which entry point a workspace is sized for. */
 typedef enum {
@@ -342,6 +348,177 @@ int coverprune_gather(const void* feats, int dtype, const float* pos, const int3
                       int32_t* status, cp_stream_t stream);
 
 /*
+ * Rotary positions.  A head's first `rot` components are rot / 2 pairs; pair i
+ * of a row at position p is turned by the angle p * inv_freq[i]:
+ *   (a, b) -> scale * (a cos - b sin, b cos + a sin)
+ * Components from rot on pass through unchanged.
+ *   inv_freq  device, [rot / 2] float64, radians a position (finite).  The
+ *             angle is reduced by whole turns in 64-bit fixed point, so it is
+ *             as good at position 2^40 as at 1.
+ *   rot       even, 0..D (0: nothing is turned and inv_freq is not read)
+ *   layout    CP_ROPE_HALF: pair i is components i and i + rot / 2;
+ *             CP_ROPE_INTERLEAVED: components 2 i and 2 i + 1
+ *   scale     factor on the turned components (1; stretched contexts often
+ *             take another), finite
+ */
+typedef enum { CP_ROPE_HALF = 0, CP_ROPE_INTERLEAVED = 1 } cp_rope_layout;
+typedef struct {
+  const double* inv_freq;
+  int32_t rot;
+  int32_t layout;
+  float scale;
+} cp_rope;
+
+/*
+ * coverprune_rotary_frequencies -- inv_freq for a context of another length
+ * than the model was trained on; fills the HOST array inv_freq[rot / 2].
+ *   f_i = base^(-2 i / rot), then with factor s >= 1 and original length L:
+ *   CP_STRETCH_NONE    f_i
+ *   CP_STRETCH_LINEAR  f_i / s (positions interpolated)
+ *   CP_STRETCH_BASE    base replaced by base * s^(rot / (rot - 2)): the fastest
+ *                      pair keeps its speed, the slowest is s times slower
+ *   CP_STRETCH_TURNS   by the turns r_i = L f_i / (2 pi) that a pair makes over
+ *                      L: f_i from `high` turns on, f_i / s up to `low`, linear
+ *                      in r_i between the two (low < high)
+ *   CP_STRETCH_INDEX   the same ends, but linear in i: from
+ *                      floor(index of `high` turns) to ceil(index of `low`),
+ *                      index of t turns = rot ln(L / (2 pi t)) / (2 ln base),
+ *                      both clamped to 0..rot - 1
+ * Returns CP_OK or CP_EINVAL (rot odd or < 2, base <= 1, s < 1, L, low or high
+ * out of range where they are used).  Host only.
+ */
+typedef enum {
+  CP_STRETCH_NONE = 0,
+  CP_STRETCH_LINEAR = 1,
+  CP_STRETCH_BASE = 2,
+  CP_STRETCH_TURNS = 3,
+  CP_STRETCH_INDEX = 4
+} cp_stretch;
+int coverprune_rotary_frequencies(int64_t rot, double base, int stretch, double factor,
+                                  double original, double low, double high, double* inv_freq);
+
+/* A tensor of rows [B, T, heads, D] and where its result goes: D contiguous
+ * elements a row, the other strides in elements (any sign or order; 0 only for
+ * dimensions of one).  `out` may equal `in` with equal strides; otherwise the
+ * two must not overlap. */
+typedef struct {
+  const void* in;
+  void* out;
+  int64_t heads;
+  int64_t in_stride[3];  /* batch, token, head */
+  int64_t out_stride[3];
+} cp_rows;
+
+/*
+ * coverprune_rotary -- rotary positions of n (1..4) tensors that share their
+ * positions (a layer's queries and keys, say) in one launch.
+ *   rows     HOST array of n tensors of `dtype` (CP_F32 or CP_BF16), [B, T,
+ *            heads, D]; pointers aligned to an element.  16-byte aligned
+ *            pointers and strides are fastest.
+ *   pos      device int64, pos[b * pos_stride + t]: any value; kept indices as
+ *            coverprune_select returns them will do (pos_stride = 0 shares
+ *            them between the batch's entries)
+ *   inverse  0: turn; 1: turn back, which is the gradient: given d/d out it
+ *            computes d/d in = scale * R^T d/d out
+ * Each product and sum is float32, rounded once to `dtype`.
+ * B, T <= 2^31 - 1, D <= 4096.  B == 0, T == 0 and heads == 0 are no-ops.
+ */
+int coverprune_rotary(const cp_rows* rows, int n, int dtype, int64_t B, int64_t T, int64_t D,
+                      const int64_t* pos, int64_t pos_stride, const cp_rope* rope, int inverse,
+                      cp_stream_t stream);
+
+/*
+ * A paged cache of keys and values.  Key j of sequence b is row j % page_size
+ * of page table[b * table_stride + j / page_size], at
+ *   page * page_stride + row * slot_stride + head * head_stride
+ * elements from k (and its value equally from v); D contiguous elements.
+ *   dtype       CP_BF16, CP_F32 or CP_E4M3
+ *   k, v        device, 16-byte aligned; the strides and D are multiples of 16
+ *               bytes, D <= 256; strides of both are the same
+ *   pages       pages k and v hold (a table entry outside 0..pages - 1 is a bad
+ *               page: see below)
+ *   k_scale, v_scale  device float32 [heads] or NULL (1): the value of a
+ *               stored element is scale * element (any dtype)
+ *   table       device int32 [B, table_width], rows table_stride apart; entries
+ *               beyond a sequence's length are not read
+ */
+typedef struct {
+  uint32_t struct_size; /* = sizeof(cp_cache) */
+  int32_t dtype;
+  void* k;
+  void* v;
+  int64_t pages, page_size, heads, D;
+  int64_t page_stride, slot_stride, head_stride;
+  const float* k_scale;
+  const float* v_scale;
+  const int32_t* table;
+  int64_t table_width, table_stride;
+} cp_cache;
+
+/*
+ * coverprune_cache_append -- T new tokens of B sequences into the cache, keys
+ * rotated on the way, and optionally the queries of the same tokens rotated.
+ *   k, v      [T, heads, D] of `dtype` (CP_F32 or CP_BF16); k_stride, v_stride
+ *             HOST arrays {token, head} in elements.  A float32 cache takes
+ *             float32 rows, a bfloat16 one bfloat16 rows, an 8-bit one either.
+ *   starts    device int32 [B + 1]: sequence b's new tokens are rows
+ *             starts[b]..starts[b + 1] - 1, ascending from 0 on; rows from starts[B] on are
+ *             padding and left alone.  NULL: T == B, one token a sequence.
+ *   lens      device int32 [B]: keys that each sequence holds before the call;
+ *             token i of sequence b becomes key lens[b] + i
+ *   pos       device int64 [T]: positions of the rotation (a kept token's index
+ *             in its scene); NULL: the key's own index lens[b] + i
+ *   rope      NULL: no rotation
+ *   q         NULL, or the queries: B = 1 and T rows as in coverprune_rotary
+ *             (the batch strides are not read)
+ *   new_lens  device int32 [B] or NULL: lens[b] plus its new tokens, at most what
+ *             the table's row holds; must not overlap lens
+ *   status    device int32 or NULL; set to CP_EINVAL (and otherwise not
+ *             written) if a token's key lies beyond the table's row or on a bad
+ *             page, or lens[b] is negative; that token's key and value are
+ *             skipped.
+ * Rotation in float32, one rounding; an 8-bit cache holds
+ * round(x / scale) to nearest even, saturated at +-448 (infinities too; NaN
+ * stays NaN).  Two tokens on one row of the cache are the caller's mistake.
+ */
+int coverprune_cache_append(const cp_cache* cache, const void* k, const int64_t* k_stride,
+                            const void* v, const int64_t* v_stride, int dtype, int64_t T,
+                            const int32_t* starts, const int32_t* lens, int64_t B,
+                            const int64_t* pos, const cp_rope* rope, const cp_rows* q,
+                            int32_t* new_lens, int32_t* status, cp_stream_t stream);
+
+/*
+ * coverprune_decode_attention -- attention of one query a sequence over the
+ * cache: for query head h of sequence b, with kv head h / (Hq / heads),
+ *   s_j = scale * <q, k_j>,  out = sum_j exp(s_j - lse) v_j,
+ *   lse = log sum_j exp(s_j)
+ * over the visible keys j: j < lens[b], j >= lens[b] - window (window > 0), and
+ * keep[b * keep_stride + j] != 0 (keep not NULL).  With none visible out is 0
+ * and lse -infinity.  Rows that are not visible are not read, whatever they hold.
+ *   q       [B, Hq, D] of `dtype`, q_stride HOST {batch, head} in elements.
+ *           bfloat16 goes with a bfloat16 or 8-bit cache, float32 with a float32 one.
+ *   lens    device int32 [B]; negative is 0, more than the table's row
+ *           holds is what it holds
+ *   keep    device uint8 or NULL, a byte a key
+ *   scale   finite (usually 1 / sqrt(D))
+ *   window  0: all keys
+ *   out     as q with out_stride; lse [B, Hq] float32 or NULL
+ *   ws      coverprune_decode_workspace_size bytes, 256-byte aligned; holds
+ *           nothing between calls
+ *   status  device int32 or NULL; set to CP_EINVAL (and otherwise not written)
+ *           if a visible key lies on a bad page; such keys are left out.
+ * Scores, maxima, sums and outputs are float32; with a bfloat16 (8-bit) cache
+ * the weights exp(s_j - m) enter the second product as bfloat16 (float16).  The
+ * same call gives the same bits.  B * heads <= 2^24, table_width * page_size < 2^31.
+ */
+int coverprune_decode_workspace_size(int64_t B, int64_t Hq, const cp_cache* cache, size_t* bytes);
+int coverprune_decode_attention(const void* q, const int64_t* q_stride, int dtype, int64_t B,
+                                int64_t Hq, const cp_cache* cache, const int32_t* lens,
+                                const uint8_t* keep, int64_t keep_stride, float scale,
+                                int64_t window, void* out, const int64_t* out_stride, float* lse,
+                                void* ws, size_t ws_bytes, int32_t* status, cp_stream_t stream);
+
+/*
  * coverprune_barrier_selftest -- exercises the device-side wait limit
  * without any fault: launches `n_blocks` co-resident blocks that wait for
  * `expected` arrivals on a grid barrier in ws (only n_blocks arrive).  With
@@ -368,7 +545,8 @@ int coverprune_barrier_selftest(int32_t n_blocks, int32_t expected, float timeou
  * (prototypes), CP_STAGE_OUTPUT (sort of kept indices, gather),
  * CP_STAGE_SLAB (local SGS with the bounded feature normaliser: the Morton
  * tile pairs that hold a neighbour pair and their cosines, in place of the
- * all-pairs Gram).
+ * all-pairs Gram), CP_STAGE_ROTARY, CP_STAGE_CACHE (cache append) and
+ * CP_STAGE_ATTEND (attention over the cache).
  * Host only; thread-safe.  Returns CP_OK or CP_ECUDA.
  */
 typedef enum {
@@ -381,7 +559,10 @@ typedef enum {
   CP_STAGE_LITE_PROTO = 6,
   CP_STAGE_OUTPUT = 7,
   CP_STAGE_SLAB = 8,
-  CP_STAGE_COUNT = 9
+  CP_STAGE_ROTARY = 9,
+  CP_STAGE_CACHE = 10,
+  CP_STAGE_ATTEND = 11,
+  CP_STAGE_COUNT = 12
 } cp_stage;
 int coverprune_profile_enable(int on);
 int coverprune_profile_read(double* ms, int64_t* launches, int n);

@@ -17,8 +17,10 @@ import torch
 from . import build as _build
 
 CP_OK, CP_EINVAL, CP_EWORKSPACE, CP_ECUDA, CP_ETIMEOUT, CP_EUNSUPPORTED, CP_EDEVICE = range(7)
-CP_F32, CP_BF16 = 0, 1
+CP_F32, CP_BF16, CP_E4M3 = 0, 1, 2
 CP_OP_COST, CP_OP_SELECT, CP_OP_LITE, CP_OP_KNN = 0, 1, 2, 3
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+STRETCHES = {"none": 0, "linear": 1, "base": 2, "turns": 3, "index": 4}
 
 # every symbol declared in include/coverprune.h
 EXPORTS = ("cp_default_params", "coverprune_budget", "coverprune_workspace_size",
@@ -26,11 +28,13 @@ EXPORTS = ("cp_default_params", "coverprune_budget", "coverprune_workspace_size"
            "coverprune_status_string", "coverprune_check", "coverprune_cost",
            "coverprune_select", "coverprune_lite_select", "coverprune_knn",
            "coverprune_knn_noalloc",
-           "coverprune_gather", "coverprune_barrier_selftest", "coverprune_profile_enable",
+           "coverprune_gather", "coverprune_rotary_frequencies", "coverprune_rotary",
+           "coverprune_cache_append", "coverprune_decode_workspace_size",
+           "coverprune_decode_attention", "coverprune_barrier_selftest", "coverprune_profile_enable",
            "coverprune_profile_read", "coverprune_last_error", "coverprune_call_stats",
            "coverprune_version")
 STAGES = ("prep", "gram", "cost", "capacity", "sgs", "lite_order", "lite_proto", "output",
-          "slab")
+          "slab", "rotary", "cache", "attend")
 
 
 class CoverPruneError(RuntimeError):
@@ -57,6 +61,25 @@ class _CpParams(C.Structure):
 class _CallStats(C.Structure):
     _fields_ = [("gain_evaluations", C.c_uint64), ("rounds", C.c_uint64),
                 ("cost_bytes_read", C.c_uint64)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("rot", C.c_int32), ("layout", C.c_int32),
+                ("scale", C.c_float)]
+
+
+class _Rows(C.Structure):
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("heads", C.c_int64),
+                ("in_stride", C.c_int64 * 3), ("out_stride", C.c_int64 * 3)]
+
+
+class _Cache(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_int32), ("k", C.c_void_p),
+                ("v", C.c_void_p), ("pages", C.c_int64), ("page_size", C.c_int64),
+                ("heads", C.c_int64), ("D", C.c_int64), ("page_stride", C.c_int64),
+                ("slot_stride", C.c_int64), ("head_stride", C.c_int64), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("table", C.c_void_p), ("table_width", C.c_int64),
+                ("table_stride", C.c_int64)]
 
 
 @dataclass
@@ -139,6 +162,12 @@ def _lib():
         lib.coverprune_knn.argtypes = [P, I64, I64, I64, P, P, P, SZ, P]
         lib.coverprune_knn_noalloc.argtypes = [P, I64, I64, I64, P, P, P]
         lib.coverprune_gather.argtypes = [P, I32, P, P, I64, I64, I64, P, I64, P, P, P, P, P]
+        lib.coverprune_rotary_frequencies.argtypes = [I64, C.c_double, I32] + [C.c_double] * 4 + [P]
+        lib.coverprune_rotary.argtypes = [P, I32, I32, I64, I64, I64, P, I64, P, I32, P]
+        lib.coverprune_cache_append.argtypes = [P, P, P, P, P, I32, I64, P, P, I64, P, P, P, P, P, P]
+        lib.coverprune_decode_workspace_size.argtypes = [I64, I64, P, C.POINTER(C.c_size_t)]
+        lib.coverprune_decode_attention.argtypes = [P, P, I32, I64, I64, P, P, P, I64, C.c_float,
+                                                    I64, P, P, P, P, SZ, P, P]
         lib.coverprune_barrier_selftest.argtypes = [C.c_int32, C.c_int32, C.c_float, P, SZ, P]
         lib.coverprune_call_stats.argtypes = [P, P, C.POINTER(_CallStats)]
         lib.coverprune_last_error.argtypes = []
@@ -396,6 +425,231 @@ def coverprune_gather(feats, pos, frame, kept, *, status=None, out=None):
     if unbatched:
         return fo[0], po[0], to[0]
     return fo, po, to
+
+
+# ---------------------------------------------------------------------------
+# What the language model runs on the kept tokens: rotary positions, a paged
+# cache of keys and values, and one token's attention over it.
+# ---------------------------------------------------------------------------
+_I64x2, _I64x3 = C.c_int64 * 2, C.c_int64 * 3
+_CACHE_TYPES = {torch.float32: CP_F32, torch.bfloat16: CP_BF16, torch.float8_e4m3fn: CP_E4M3}
+
+
+def _on_gpu(name, t, dtype, shape=None, *, dense=True):
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+    if dense and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _rows_of(name, t, dims):
+    """Checks a tensor of head rows; only its last dimension has to be dense."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dim() != dims:
+        raise ValueError(f"{name} must have {dims} dimensions, got {t.dim()}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be dense in its last dimension")
+
+
+def _rope(inv_freq, D, layout, scale):
+    if layout not in ROPE_LAYOUTS:
+        raise ValueError(f"layout must be one of {tuple(ROPE_LAYOUTS)}, got {layout!r}")
+    _on_gpu("inv_freq", inv_freq, torch.float64)
+    if inv_freq.dim() != 1 or 2 * inv_freq.numel() > D:
+        raise ValueError(f"inv_freq must hold one frequency for each rotated pair, at most {D // 2}")
+    return _Rope(inv_freq.data_ptr(), 2 * inv_freq.numel(), ROPE_LAYOUTS[layout], scale)
+
+
+def coverprune_rotary_frequencies(rot: int, base: float = 10000.0, *, stretch: str = "none",
+                                  factor: float = 1.0, original: float = 0.0, low: float = 1.0,
+                                  high: float = 32.0, device="cuda") -> torch.Tensor:
+    """inv_freq [rot / 2] float64 for rotary positions over the first ``rot``
+    components of a head, stretched for contexts ``factor`` times the
+    ``original`` length as include/coverprune.h describes ("none", "linear",
+    "base", "turns", "index")."""
+    if stretch not in STRETCHES:
+        raise ValueError(f"stretch must be one of {tuple(STRETCHES)}, got {stretch!r}")
+    f = torch.empty(max(1, rot // 2), dtype=torch.float64)
+    _check(_lib().coverprune_rotary_frequencies(rot, base, STRETCHES[stretch], factor, original,
+                                                low, high, f.data_ptr()),
+           "coverprune_rotary_frequencies")
+    return f.to(device)
+
+
+def coverprune_rotary(x, pos, inv_freq, *, layout: str = "half", scale: float = 1.0,
+                      inverse: bool = False, out=None):
+    """x turned to its positions: [T, heads, D] with pos int64 [T], or
+    [B, T, heads, D] with pos [B, T] (or [T], shared).  x may be a list of up to
+    four tensors of the same tokens (queries and keys, say), which one launch
+    turns; out then is a list too.  Any strides with a dense last dimension;
+    out may be x.  inverse=True gives the gradient with respect to x from the
+    one with respect to the result."""
+    many = isinstance(x, (list, tuple))
+    xs = list(x) if many else [x]
+    if not 1 <= len(xs) <= 4:
+        raise ValueError("x must be a tensor or a list of one to four")
+    dims = xs[0].dim()
+    if dims not in (3, 4):
+        raise ValueError("x must be [T, heads, D] or [B, T, heads, D]")
+    if out is None:
+        outs = [torch.empty_like(t) for t in xs]
+    else:
+        outs = list(out) if many else [out]
+        if len(outs) != len(xs):
+            raise ValueError("out must match x")
+    lead, D, dt = xs[0].shape[:-2], xs[0].shape[-1], _dtype(xs[0])
+    rows = (_Rows * len(xs))()
+    for r, t, o in zip(rows, xs, outs):
+        _rows_of("x", t, dims)
+        if t.shape[:-2] != lead or t.shape[-1] != D or t.dtype != xs[0].dtype:
+            raise ValueError("tensors turned together must share tokens, width and dtype")
+        if o is not t:
+            _rows_of("out", o, dims)
+            if o.shape != t.shape or o.dtype != t.dtype:
+                raise ValueError("out must match x in shape and dtype")
+        r.in_, r.out, r.heads = t.data_ptr(), o.data_ptr(), t.shape[-2]
+        r.in_stride[:] = (0,) * (4 - dims) + t.stride()[:-1]
+        r.out_stride[:] = (0,) * (4 - dims) + o.stride()[:-1]
+    B, T = (1, lead[0]) if dims == 3 else lead
+    _on_gpu("pos", pos, torch.int64)
+    if pos.dim() == dims - 2 and tuple(pos.shape) == tuple(lead):
+        pos_stride = T
+    elif pos.dim() == 1 and pos.shape[0] == T:
+        pos_stride = 0
+    else:
+        raise ValueError(f"pos must be [{T}] or {tuple(lead)}, got {tuple(pos.shape)}")
+    rope = _rope(inv_freq, D, layout, scale)
+    _check(_lib().coverprune_rotary(rows, len(xs), dt, B, T, D, _ptr(pos), pos_stride,
+                                    C.byref(rope), 1 if inverse else 0, _stream()),
+           "coverprune_rotary")
+    return outs if many else outs[0]
+
+
+def _cache(k_cache, v_cache, table, k_scale, v_scale):
+    _rows_of("k_cache", k_cache, 4)
+    if k_cache.dtype not in _CACHE_TYPES:
+        raise TypeError(f"the cache must be float32, bfloat16 or float8_e4m3fn, got {k_cache.dtype}")
+    shape, stride = k_cache.shape, k_cache.stride()
+    if v_cache.shape != shape or v_cache.stride() != stride or v_cache.dtype != k_cache.dtype \
+            or not v_cache.is_cuda:
+        raise ValueError("k_cache and v_cache must share shape, strides and dtype")
+    pages, page_size, heads, D = shape
+    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+        if t is not None:
+            _on_gpu(name, t, torch.float32, (heads,))
+    _on_gpu("table", table, torch.int32, dense=False)
+    if table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("table must be [B, width], dense in its last dimension")
+    return _Cache(C.sizeof(_Cache), _CACHE_TYPES[k_cache.dtype], k_cache.data_ptr(),
+                  v_cache.data_ptr(), pages, page_size, heads, D,
+                  stride[0] if pages > 1 else 0, stride[1] if page_size > 1 else 0,
+                  stride[2] if heads > 1 else 0, k_scale.data_ptr() if k_scale is not None else None,
+                  v_scale.data_ptr() if v_scale is not None else None, table.data_ptr(),
+                  table.shape[1], table.stride(0))
+
+
+def coverprune_cache_append(k, v, k_cache, v_cache, table, lens, *, starts=None, pos=None,
+                            inv_freq=None, layout: str = "half", scale: float = 1.0, q=None,
+                            k_scale=None, v_scale=None, new_lens=None, q_out=None,
+                            status=None) -> dict:
+    """Appends k, v [T, heads, D] to a paged cache [pages, page_size, heads, D],
+    keys turned to pos [T] (int64; default: their place in the sequence) where
+    inv_freq is given.  starts int32 [B + 1] says which rows are which
+    sequence's (default: one row a sequence), lens int32 [B] how many keys each
+    holds already.  q [T, Hq, D] is turned in the same launch.  Returns
+    {"lens": int32 [B] after the call, "q": the turned queries or None}."""
+    _rows_of("k", k, 3)
+    _rows_of("v", v, 3)
+    cache = _cache(k_cache, v_cache, table, k_scale, v_scale)
+    T, D = k.shape[0], cache.D
+    if tuple(k.shape) != (T, cache.heads, D) or v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError(f"k and v must be [T, {cache.heads}, {D}] of one dtype")
+    _on_gpu("lens", lens, torch.int32)
+    B = table.shape[0]
+    if tuple(lens.shape) != (B,):
+        raise ValueError(f"lens must have shape ({B},), got {tuple(lens.shape)}")
+    if starts is not None:
+        _on_gpu("starts", starts, torch.int32, (B + 1,))
+    elif T != B:
+        raise ValueError(f"without starts there is one row a sequence: {T} rows, {B} sequences")
+    if pos is not None:
+        _on_gpu("pos", pos, torch.int64, (T,))
+    rope = None if inv_freq is None else _rope(inv_freq, D, layout, scale)
+    if new_lens is None:
+        new_lens = torch.empty_like(lens)
+    else:
+        _on_gpu("new_lens", new_lens, torch.int32, (B,))
+    rows = None
+    if q is not None:
+        _rows_of("q", q, 3)
+        if q.shape[0] != T or q.shape[2] != D or q.dtype != k.dtype:
+            raise ValueError(f"q must be [{T}, heads, {D}] of k's dtype")
+        if q_out is None:
+            q_out = torch.empty_like(q)
+        elif q_out is not q:
+            _rows_of("q_out", q_out, 3)
+            if q_out.shape != q.shape or q_out.dtype != q.dtype:
+                raise ValueError("q_out must match q in shape and dtype")
+        rows = _Rows(q.data_ptr(), q_out.data_ptr(), q.shape[1], _I64x3(0, *q.stride()[:2]),
+                     _I64x3(0, *q_out.stride()[:2]))
+    if status is not None:
+        _on_gpu("status", status, torch.int32)
+    _check(_lib().coverprune_cache_append(
+        C.byref(cache), _ptr(k), _I64x2(*k.stride()[:2]), _ptr(v), _I64x2(*v.stride()[:2]),
+        _dtype(k), T, _ptr(starts), _ptr(lens), B, _ptr(pos),
+        None if rope is None else C.byref(rope), None if rows is None else C.byref(rows),
+        _ptr(new_lens), _ptr(status), _stream()), "coverprune_cache_append")
+    return {"lens": new_lens, "q": q_out}
+
+
+def coverprune_decode_attention(q, k_cache, v_cache, table, lens, *, scale=None, window: int = 0,
+                                keep=None, k_scale=None, v_scale=None, lse: bool = False,
+                                out=None, ws=None, status=None) -> dict:
+    """Attention of one query a sequence, q [B, Hq, D], over a paged cache of
+    which sequence b holds lens[b] keys.  window > 0: the last ``window`` keys
+    only; keep bool [B, >= keys]: the keys marked only.  scale defaults to
+    1 / sqrt(D).  Returns {"out": [B, Hq, D], "lse": float32 [B, Hq] or None,
+    "ws": the workspace, to pass to the next call}."""
+    _rows_of("q", q, 3)
+    cache = _cache(k_cache, v_cache, table, k_scale, v_scale)
+    B, Hq, D = q.shape
+    if D != cache.D or table.shape[0] != B:
+        raise ValueError(f"q must be [{table.shape[0]}, heads, {cache.D}], got {tuple(q.shape)}")
+    _on_gpu("lens", lens, torch.int32, (B,))
+    keep_stride = 0
+    if keep is not None:
+        _on_gpu("keep", keep, torch.bool, dense=False)
+        if keep.dim() != 2 or keep.shape[0] != B or keep.shape[1] < cache.table_width * cache.page_size \
+                or (keep.shape[1] > 1 and keep.stride(1) != 1):
+            raise ValueError(f"keep must be [{B}, at least {cache.table_width * cache.page_size}], "
+                             "dense in its last dimension")
+        keep_stride = keep.stride(0)
+    if out is None:
+        out = torch.empty((B, Hq, D), dtype=q.dtype, device=q.device)
+    else:
+        _rows_of("out", out, 3)
+        if out.shape != q.shape or out.dtype != q.dtype:
+            raise ValueError("out must match q in shape and dtype")
+    lse_out = torch.empty((B, Hq), dtype=torch.float32, device=q.device) if lse else None
+    if status is not None:
+        _on_gpu("status", status, torch.int32)
+    lib = _lib()
+    if ws is None:
+        n = C.c_size_t()
+        _check(lib.coverprune_decode_workspace_size(B, Hq, C.byref(cache), C.byref(n)),
+               "coverprune_decode_workspace_size")
+        ws = torch.empty(max(n.value, 256), dtype=torch.uint8, device=q.device)
+    _check(lib.coverprune_decode_attention(
+        _ptr(q), _I64x2(*q.stride()[:2]), _dtype(q), B, Hq, C.byref(cache), _ptr(lens), _ptr(keep),
+        keep_stride, D ** -0.5 if scale is None else scale, window, _ptr(out),
+        _I64x2(*out.stride()[:2]), _ptr(lse_out), _ptr(ws), ws.numel(), _ptr(status), _stream()),
+        "coverprune_decode_attention")
+    return {"out": out, "lse": lse_out, "ws": ws}
 
 
 def coverprune_barrier_selftest(n_blocks: int, expected: int, timeout_ms: float, ws) -> int:

@@ -53,38 +53,27 @@ void note_cuda_error(const char* where, cudaError_t e) {
            cudaGetErrorString(e));
 }
 
-// Marks the kernels launched while it lives as belonging to `stage`; with
-// profiling on, brackets them with CUDA events on the call's stream.
-class Stage {
- public:
-  Stage(int stage, cudaStream_t s) : prev_(t_stage), s_(s) {
-    t_stage = stage;
-    ev_.stage = stage;
-    if (g_prof_on.load(std::memory_order_relaxed) &&
-        cudaEventCreate(&ev_.start) == cudaSuccess) {
-      if (cudaEventCreate(&ev_.stop) == cudaSuccess) {
-        cudaEventRecord(ev_.start, s_);
-        active_ = true;
-      } else {
-        cudaEventDestroy(ev_.start);
-      }
+Stage::Stage(int stage, cudaStream_t s) : prev_(t_stage), s_(s) {
+  t_stage = stage;
+  stage_ = stage;
+  if (g_prof_on.load(std::memory_order_relaxed) && cudaEventCreate(&start_) == cudaSuccess) {
+    if (cudaEventCreate(&stop_) == cudaSuccess) {
+      cudaEventRecord(start_, s_);
+      active_ = true;
+    } else {
+      cudaEventDestroy(start_);
     }
   }
-  ~Stage() {
-    if (active_) {
-      cudaEventRecord(ev_.stop, s_);
-      std::lock_guard<std::mutex> lk(g_prof_mu);
-      g_prof_events.push_back(ev_);
-    }
-    t_stage = prev_;
-  }
+}
 
- private:
-  int prev_;
-  cudaStream_t s_;
-  StageEvents ev_{};
-  bool active_ = false;
-};
+Stage::~Stage() {
+  if (active_) {
+    cudaEventRecord(stop_, s_);
+    std::lock_guard<std::mutex> lk(g_prof_mu);
+    g_prof_events.push_back({stage_, start_, stop_});
+  }
+  t_stage = prev_;
+}
 
 // ---------------------------------------------------------------------------
 // Device attribute cache.

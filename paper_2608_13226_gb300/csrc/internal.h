@@ -260,6 +260,20 @@ inline int launch_status(const char* where) {
 // Records a plain message as the calling thread's last error.
 void note_message(const char* msg);
 
+// Marks the kernels launched while it lives as belonging to `stage`; with
+// profiling on, brackets them with CUDA events on the call's stream.
+class Stage {
+ public:
+  Stage(int stage, cudaStream_t s);
+  ~Stage();
+
+ private:
+  int prev_, stage_;
+  cudaStream_t s_;
+  cudaEvent_t start_{}, stop_{};
+  bool active_ = false;
+};
+
 #define CP_TRY_STATUS(x)          \
   do {                            \
     int _st = (x);                \

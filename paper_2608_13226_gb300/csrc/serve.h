@@ -1,0 +1,82 @@
+// Declarations shared by the operators of the decoding model (rotary.cu,
+// decode.cu) and their host side (api_serve.cu).  Not part of the public ABI.
+#pragma once
+
+#include "internal.h"
+
+namespace cp {
+
+constexpr int kMaxRows = 4;  // tensors of one rotary call
+
+struct Rope {
+  const double* inv_freq;
+  int half;  // rotated pairs
+  int interleaved;
+  float scale;
+  int back;  // 1: the transpose
+};
+
+struct RowSet {
+  const void* in;
+  void* out;
+  int64_t in_b, in_t, in_h, out_b, out_t, out_h;  // strides, elements
+  int heads;
+};
+
+struct RotaryArgs {
+  RowSet set[kMaxRows];
+  int n;
+  int64_t B, T;
+  int D;
+  const int64_t* pos;
+  int64_t pos_stride;
+  Rope rope;
+};
+int launch_rotary(const RotaryArgs& a, int dtype, cudaStream_t s);
+
+struct Cache {
+  void *k, *v;
+  int64_t pages;
+  int64_t page_stride, slot_stride, head_stride;  // elements
+  const float *k_scale, *v_scale;
+  const int32_t* table;
+  int64_t table_stride;
+  int32_t page_size;
+  int32_t capacity;  // keys a table row holds
+  int heads, D;
+};
+
+struct AppendArgs {
+  Cache cache;
+  const void *k, *v;
+  int64_t k_t, k_h, v_t, v_h;
+  RowSet q;  // heads = 0: none
+  int64_t T;
+  const int32_t *starts, *lens;
+  int B;
+  const int64_t* pos;
+  Rope rope;
+  int32_t *new_lens, *status;
+};
+int launch_cache_append(const AppendArgs& a, int dtype, int cache_dtype, cudaStream_t s);
+
+struct DecodeArgs {
+  Cache cache;
+  const void* q;
+  int64_t q_b, q_h;
+  void* out;
+  int64_t o_b, o_h;
+  int B, Hq;
+  const int32_t* lens;
+  const uint8_t* keep;
+  int64_t keep_stride;
+  float scale;
+  int64_t window;
+  float* lse;
+  void* ws;
+  int32_t* status;
+};
+size_t decode_ws_bytes(int64_t B, int64_t Hq, int64_t heads, int64_t D, int cache_dtype);
+int launch_decode(const DecodeArgs& a, int cache_dtype, cudaStream_t s);
+
+}  // namespace cp
