@@ -509,7 +509,8 @@ int coverprune_cache_append(const cp_cache* cache, const void* k, const int64_t*
  *           if a visible key lies on a bad page; such keys are left out.
  * Scores, maxima, sums and outputs are float32; with a bfloat16 (8-bit) cache
  * the weights exp(s_j - m) enter the second product as bfloat16 (float16).  The
- * same call gives the same bits.  B * heads <= 2^24, table_width * page_size < 2^31.
+ * same call gives the same bits.  B * heads <= 2^24; a table's row holds at most
+ * 2^30 keys (everywhere).
  */
 int coverprune_decode_workspace_size(int64_t B, int64_t Hq, const cp_cache* cache, size_t* bytes);
 int coverprune_decode_attention(const void* q, const int64_t* q_stride, int dtype, int64_t B,

@@ -12,6 +12,8 @@ static size_t size_of(int dtype) { return dtype == CP_F32 ? 4 : dtype == CP_BF16
 
 // Room for a call's element offsets (a stride times a size) in 64 bits.
 constexpr int64_t kMaxSize = 0x7FFFFFFF;
+// Keys of a sequence: an index a little past the last is still an int.
+constexpr int64_t kMaxKeys = (int64_t)1 << 30;
 
 static int rope_of(const cp_rope* r, int64_t D, int back, Rope* out) {
   *out = Rope{nullptr, 0, 0, 1.0f, back};
@@ -44,7 +46,7 @@ static int cache_of(const cp_cache* c, bool with_memory, Cache* out) {
   const int64_t e = (int64_t)size_of(c->dtype);
   if (c->page_size > kMaxSize || c->table_width > kMaxSize || c->pages > kMaxSize)
     return CP_EINVAL;
-  if (c->table_width * c->page_size > kMaxSize) return CP_EUNSUPPORTED;
+  if (c->table_width * c->page_size > kMaxKeys) return CP_EUNSUPPORTED;
   if (c->D > 256 || c->D * e % 16 != 0) return CP_EUNSUPPORTED;
   if (c->page_stride * e % 16 != 0 || c->slot_stride * e % 16 != 0 || c->head_stride * e % 16 != 0)
     return CP_EINVAL;

@@ -1,78 +1,816 @@
-// Attention of one query a sequence over a paged cache.
+// Attention of one query a sequence over a paged cache: out = softmax(scale q K^T) V
+// for every query head, where a group of query heads shares a kv head's keys
+// and values.
+//
+// Each visible key and value row is read once for up to 16 query heads, and a
+// bf16 cache gives 1 flop a byte and query head: the kernel is bound by HBM as
+// long as enough bytes are in flight (about 1 us of it, 45 KB an SM) whatever
+// the lengths.  So
+//  - the keys of all sequences and kv heads are one line of units of 64 keys,
+//    cut evenly among as many blocks as the device holds at a time: a single
+//    long sequence and a batch of ragged ones fill it alike, and no lengths have
+//    to be known on the host;
+//  - in a block every warp runs on its own: it copies tiles of 16 keys (16 rows
+//    of K and of V, wherever their pages are) into a ring in shared memory by
+//    16-byte asynchronous copies, several tiles ahead, and keeps its own running
+//    maximum, sum and output; no barrier between warps until a segment (the
+//    block's part of one sequence and kv head) ends;
+//  - a segment that is a whole sequence is written out, a part of one goes to
+//    the workspace and k_decode_join adds the parts in the order of the blocks.
+// The products run on mma.sync with keys as rows: S^T = K Q^T (16 keys x 8
+// queries) and O^T = V^T P^T, so a group of 8 query heads wastes nothing and
+// the columns of S and O lie in the same lanes.  One tile of 16 keys costs 16
+// MMAs of a warp (head 128, 8 queries) for 8 KB: a tenth of the tensor pipe at
+// the full rate of HBM, where tcgen05's 128 rows would be 7 of 8 empty.
 #include "rope.cuh"
 
 namespace cp {
 
-constexpr int kTile = 128;
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kUnit = 64;   // keys of a unit
+constexpr int kChunk = 64;  // keys whose marks a warp looks at together
+constexpr int kQueue = 128;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
 
-// A block per query head: tiles of 128 keys, a running maximum and sum.
-template <typename T, typename C>
-__global__ void __launch_bounds__(kTile) k_decode(DecodeArgs a) {
-  const Cache& ch = a.cache;
-  const int b = blockIdx.y, h = blockIdx.x, hk = h / (a.Hq / ch.heads), D = ch.D, tid = threadIdx.x;
-  __shared__ float q[256], p[kTile], red[4];
-  __shared__ int64_t at[kTile];
-  for (int d = tid; d < D; d += kTile) q[d] = to_f32(((const T*)a.q)[b * a.q_b + h * a.q_h + d]);
-  const int len = min(max(a.lens[b], 0), ch.capacity);
-  const int first = a.window > 0 && a.window < len ? len - (int)a.window : 0;
-  const float scale = a.scale * (ch.k_scale ? ch.k_scale[hk] : 1.0f);
-  float m = -INFINITY, l = 0.0f, o[2] = {0.0f, 0.0f};
-  for (int j0 = first; j0 < len; j0 += kTile) {
-    const int j = j0 + tid;
-    float x = -INFINITY;
-    int64_t row = -1;
-    if (j < len && (!a.keep || a.keep[b * a.keep_stride + j])) {
-      const int page = ch.table[b * ch.table_stride + j / ch.page_size];
-      if (page < 0 || page >= ch.pages) {
-        if (a.status) set_status(a.status, CP_EINVAL);
-      } else {
-        row = page * ch.page_stride + j % ch.page_size * ch.slot_stride + hk * ch.head_stride;
-      }
-    }
-    __syncthreads();
-    if (row >= 0) {
-      x = 0.0f;
-      for (int d = 0; d < D; ++d) x += q[d] * to_f32(((const C*)ch.k)[row + d]);
-      x *= scale;
-    }
-    float top = x;
-    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-    if (tid % 32 == 0) red[tid / 32] = top;
-    at[tid] = row;
-    __syncthreads();
-    top = fmaxf(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])), m);
-    const float base = top == -INFINITY ? 0.0f : top, f = expf(m - base);
-    p[tid] = row >= 0 ? expf(x - base) : 0.0f;
-    m = top;
-    l *= f;
-    o[0] *= f;
-    o[1] *= f;
-    __syncthreads();
-    for (int i = 0; i < kTile; ++i) {
-      if (at[i] < 0) continue;
-      l += p[i];
-      for (int n = 0; n < 2; ++n)
-        if (tid + n * kTile < D) o[n] += p[i] * to_f32(((const C*)ch.v)[at[i] + tid + n * kTile]);
-    }
-  }
-  const float inv = l == 0.0f ? 0.0f : (ch.v_scale ? ch.v_scale[hk] : 1.0f) / l;
-  for (int n = 0; n < 2; ++n)
-    if (tid + n * kTile < D)
-      ((T*)a.out)[b * a.o_b + h * a.o_h + tid + n * kTile] = from_f32<T>(o[n] * inv);
-  if (a.lse && tid == 0) a.lse[(int64_t)b * a.Hq + h] = l == 0.0f ? -INFINITY : logf(l) + m;
+// What a cache's type changes: bytes an element, keys a tile.
+template <int CT> struct Type;
+template <> struct Type<CP_BF16> { static constexpr int e = 2, tk = 16; using Row = __nv_bfloat16; };
+template <> struct Type<CP_E4M3> { static constexpr int e = 1, tk = 16; using Row = __nv_bfloat16; };
+template <> struct Type<CP_F32> { static constexpr int e = 4, tk = 8; using Row = float; };
+
+// Shape of one variant: CT cache type, DP head width it is laid out for, QT query
+// heads a pass.
+template <int CT, int DP, int QT>
+struct Shape {
+  static constexpr int e = Type<CT>::e, tk = Type<CT>::tk;
+  static constexpr int row = DP * e;                  // bytes of a row in shared memory
+  static constexpr int cpr = row / 16;                // 16-byte chunks of it
+  static constexpr int tile = 2 * tk * row;           // K and V of a tile
+  // ring: as many tiles as keep two blocks on an SM, 3 at least
+  static constexpr int fit = 100 * 1024 / (kWarps * tile);
+  static constexpr int stages = fit < 3 ? 3 : fit > 8 ? 8 : fit;
+  static constexpr int ring = kWarps * stages * tile;
+  static constexpr int extra = CT == CP_F32 ? (QT * DP + kWarps * tk * QT) * 4 : 0;
+  static constexpr int smem = ring + extra;
+  static constexpr int per_sm = smem <= 110 * 1024 ? 2 : 1;
+  static constexpr int part = QT * (DP + 2);  // floats of a partial result
+  static_assert(kWarps * QT * DP * 4 <= ring, "the merge reuses the ring");
+};
+
+// What the blocks leave for the join: the part that begins in block i (a query
+// tile's first units) and over how many blocks it goes on.
+struct Begin {
+  int b, col, blocks, pad;
+};
+
+// Where a chunk of a row lies: rows that are read together fall on other banks.
+template <int CT, int CPR>
+__device__ __forceinline__ int swizzle(int r, int c) {
+  if (CT == CP_F32) return c ^ ((r & 1) << 2);
+  return CPR >= 8 ? c ^ (r & 7) : c ^ ((r >> 1) & 3);
 }
 
-size_t decode_ws_bytes(int64_t, int64_t, int64_t, int64_t, int) { return 256; }
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+  const int n = there ? 16 : 0;  // 0: nothing is read, zeros are written
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n)
+               : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at)
+               : "memory");
+}
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                              uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 "
+      "{%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// Two 8-bit elements as two float16 (exact), from the low or the high half.
+__device__ __forceinline__ uint32_t e4m3_f16x2(uint32_t x) {
+  uint32_t y;
+  asm("{\n\t.reg .b16 l;\n\tcvt.u16.u32 l, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  uint32_t y;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t y;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
+  return y;
+}
+
+// Keys of sequence b: [first, len).
+__device__ __forceinline__ void keys_of(const DecodeArgs& a, int b, int* first, int* len) {
+  const int n = min(max(a.lens[b], 0), a.cache.capacity);
+  *len = n;
+  *first = a.window > 0 && a.window < n ? n - (int)a.window : 0;
+}
+__device__ __forceinline__ int units_of(const DecodeArgs& a, int b, int unit) {
+  int first, len;
+  keys_of(a, b, &first, &len);
+  return max(1, (int)(((int64_t)(len - first) + unit - 1) / unit));
+}
+
+// The keys that a warp takes from its part [lo, hi) of a segment, a tile at a
+// time: every kWarps-th run of `tk` keys, or of the marked ones among them.
+template <int TK>
+struct Keys {
+  int next, hi, lane;
+  const uint8_t* keep;  // the sequence's marks, or null
+  int* queue;           // marked keys that are still to be taken
+  int head, count;
+  uint32_t mark[2][2];  // of the next two chunks
+
+  __device__ void load(int i, int at) {
+    mark[i][0] = at + lane < hi ? keep[at + lane] : 0;
+    mark[i][1] = at + 32 + lane < hi ? keep[at + 32 + lane] : 0;
+  }
+  __device__ void start(int lo, int hi_, int warp) {
+    hi = hi_;
+    head = count = 0;
+    next = lo + warp * (keep ? kChunk : TK);
+    if (keep) {
+      load(0, next);
+      load(1, next + kWarps * kChunk);
+    }
+  }
+  // How many keys the next tile has (0: no more); this lane's, or -1.
+  __device__ int take(int* key) {
+    if (!keep) {
+      const int n = min(max(hi - next, 0), TK);
+      *key = lane < n ? next + lane : -1;
+      next += kWarps * TK;
+      return n;
+    }
+    while (count < TK && next < hi) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t all = __ballot_sync(~0u, mark[0][h] != 0);
+        if (mark[0][h])
+          queue[(head + count + __popc(all & ((1u << lane) - 1))) % kQueue] = next + 32 * h + lane;
+        count += __popc(all);
+      }
+      mark[0][0] = mark[1][0];
+      mark[0][1] = mark[1][1];
+      next += kWarps * kChunk;
+      load(1, next + kWarps * kChunk);
+    }
+    __syncwarp();
+    const int n = min(count, TK);
+    *key = lane < n ? queue[(head + lane) % kQueue] : -1;
+    head = (head + n) % kQueue;
+    count -= n;
+    __syncwarp();
+    return n;
+  }
+};
+
+// A warp's running softmax and output of one segment on the tensor cores.
+// Lane (g, t) = (lane / 4, lane % 4) has the scores of keys g and g + 8 and
+// queries 2 t, 2 t + 1 of each group of 8, and the same queries' outputs at
+// components 16 i + g, + 8 (8-bit caches: 16 i + 2 g, + 1).
+template <int CT, int DP, int QT>
+struct Math {
+  using S = Shape<CT, DP, QT>;
+  static constexpr int NT = QT / 8, KS = DP / 16;
+  uint32_t q[NT][KS][2];
+  float o[NT][KS][4];
+  float m[NT][2], l[NT][2];
+  float sc[NT][2];  // score = sc * product, in units of log 2
+  int g, t;
+
+  __device__ __forceinline__ void start(const DecodeArgs& a, int b, int hk, int h0, int nq, char*,
+                                        int, int lane) {
+    g = lane / 4;
+    t = lane % 4;
+    const int D = a.cache.D;
+    const float scale = a.scale * (a.cache.k_scale ? a.cache.k_scale[hk] : 1.0f) * kLog2e;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int row = 8 * n + g;
+      const uint16_t* src = (const uint16_t*)a.q + b * a.q_b + (int64_t)(h0 + row) * a.q_h;
+      auto at = [&](int d) -> uint32_t { return row < nq && d < D ? src[d] : 0; };
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        // bf16: components 2 t, 2 t + 1 and the same + 8; 8 bits: 4 t .. 4 t + 3, as its keys come
+        const int d0 = 16 * s + (CT == CP_E4M3 ? 4 * t : 2 * t), d1 = d0 + (CT == CP_E4M3 ? 2 : 8);
+        q[n][s][0] = at(d0) | at(d0 + 1) << 16;
+        q[n][s][1] = at(d1) | at(d1 + 1) << 16;
+      }
+      float back = 1.0f;
+      if (CT == CP_E4M3) {
+        // keys enter as float16, exactly, and so do queries once their largest
+        // component is brought to [2^8, 2^9) by a power of two (bf16 has fewer bits;
+        // what lies 2^22 below the largest component loses some)
+        float top = 0.0f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            top = fmaxf(top, fmaxf(fabsf(__uint_as_float(q[n][s][i] << 16)),
+                                   fabsf(__uint_as_float(q[n][s][i] & 0xFFFF0000u))));
+        top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
+        int ex = 0;
+        if (top > 0.0f && top < INFINITY) ex = ilogbf(top) - 8;
+        const float f1 = ldexpf(1.0f, -ex / 2), f2 = ldexpf(1.0f, -(ex - ex / 2));
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            q[n][s][i] = pack_f16(__uint_as_float(q[n][s][i] << 16) * f1 * f2,
+                                  __uint_as_float(q[n][s][i] & 0xFFFF0000u) * f1 * f2);
+        back = (float)ex;
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        // the two queries whose scores this lane has
+        sc[n][i] = scale;
+        if (CT == CP_E4M3) {
+          const int ex = (int)__shfl_sync(~0u, back, 4 * (2 * t + i));
+          sc[n][i] = ldexpf(ldexpf(scale, ex / 2), ex - ex / 2);
+        }
+        m[n][i] = -INFINITY;
+        l[n][i] = 0.0f;
+      }
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[n][s][i] = 0.0f;
+    }
+  }
+
+  __device__ __forceinline__ void tile(uint32_t at, uint32_t valid, char*, int, int lane) {
+    float s[NT][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
+    const int r = lane % 16, half = lane / 16;
+    if (CT == CP_BF16) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        uint32_t x[4];
+        ldmatrix4(x, at + r * S::row + 16 * swizzle<CT, S::cpr>(r, 2 * k + half));
+#pragma unroll
+        for (int n = 0; n < NT; ++n) mma_bf16_16816(s[n], x[0], x[1], x[2], x[3], q[n][k][0], q[n][k][1]);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < KS; k += 2) {
+        uint32_t x[4];
+        ldmatrix4(x, at + r * S::row + 16 * swizzle<CT, S::cpr>(r, k + half));
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t u = x[2 * j], w = x[2 * j + 1];
+          const uint32_t a0 = e4m3_f16x2(u), a1 = e4m3_f16x2(w), a2 = e4m3_f16x2(u >> 16), a3 = e4m3_f16x2(w >> 16);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma_f16_16816(s[n], a0, a1, a2, a3, q[n][k + j][0], q[n][k + j][1]);
+        }
+      }
+    }
+    const bool v0 = valid >> g & 1, v1 = valid >> (g + 8) & 1;
+    uint32_t p[NT][2];
+    bool moved = false;
+    float f[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = (i < 2 ? v0 : v1) ? s[n][i] * sc[n][i & 1] : -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float top = fmaxf(x[i], x[i + 2]);
+#pragma unroll
+        for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+        top = fmaxf(top, m[n][i]);
+        const float base = top == -INFINITY ? 0.0f : top;
+        f[n][i] = exp2_fast(m[n][i] - base);
+        moved |= top != m[n][i];
+        m[n][i] = top;
+        x[i] = v0 ? exp2_fast(fmaf(s[n][i], sc[n][i], -base)) : 0.0f;
+        x[i + 2] = v1 ? exp2_fast(fmaf(s[n][i + 2], sc[n][i], -base)) : 0.0f;
+        l[n][i] = l[n][i] * f[n][i] + (x[i] + x[i + 2]);
+      }
+      // 8 (11) bits of each weight go on: under 2^-8 (2^-11) of the output, which
+      // is rounded to bfloat16 itself; the sum l has all 24
+      const uint32_t lo = CT == CP_BF16 ? pack_bf16(x[0], x[1]) : pack_f16(x[0], x[1]);
+      const uint32_t hi = CT == CP_BF16 ? pack_bf16(x[2], x[3]) : pack_f16(x[2], x[3]);
+      p[n][0] = movmatrix_trans(lo);
+      p[n][1] = movmatrix_trans(hi);
+    }
+    if (__any_sync(~0u, moved)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[n][k][i] *= f[n][i & 1];
+    }
+    at += S::tk * S::row;
+    if (CT == CP_BF16) {
+      const int key = lane % 8 + (lane / 16) * 8, c = lane / 8 % 2;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        uint32_t x[4];
+        ldmatrix4_trans(x, at + key * S::row + 16 * swizzle<CT, S::cpr>(key, 2 * k + c));
+#pragma unroll
+        for (int n = 0; n < NT; ++n) mma_bf16_16816(o[n][k], x[0], x[1], x[2], x[3], p[n][0], p[n][1]);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < KS; k += 2) {
+        uint32_t x[4];
+        ldmatrix4_trans(x, at + r * S::row + 16 * swizzle<CT, S::cpr>(r, k + half));
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          // bytes: key 2 t's components 2 g, 2 g + 1, then key 2 t + 1's
+          const uint32_t u = __byte_perm(x[2 * j], 0, 0x3120), w = __byte_perm(x[2 * j + 1], 0, 0x3120);
+          const uint32_t a0 = e4m3_f16x2(u), a1 = e4m3_f16x2(u >> 16), a2 = e4m3_f16x2(w), a3 = e4m3_f16x2(w >> 16);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma_f16_16816(o[n][k + j], a0, a1, a2, a3, p[n][0], p[n][1]);
+        }
+      }
+    }
+  }
+
+  // This warp's maximum and sum of each query.
+  __device__ __forceinline__ void finish(float* sm, float* sl) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int d = 4; d < 32; d *= 2) l[n][i] += __shfl_xor_sync(~0u, l[n][i], d);
+        if (g == 0) {
+          sm[8 * n + 2 * t + i] = m[n][i];
+          sl[8 * n + 2 * t + i] = l[n][i];
+        }
+      }
+  }
+  // Its outputs by the common maximum: buf[query][component] = o * f[query].
+  __device__ __forceinline__ void put(float* buf, const float* f) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int query = 8 * n + 2 * t + (i & 1);
+          const int d = 16 * k + (CT == CP_E4M3 ? 2 * g + i / 2 : g + 8 * (i / 2));
+          buf[query * DP + d] = o[n][k][i] * f[query];
+        }
+  }
+};
+
+// The same in float32 on the FMA units: 4 lanes a key for the scores, then the
+// components spread over the lanes.
+template <int DP, int QT>
+struct Math<CP_F32, DP, QT> {
+  using S = Shape<CP_F32, DP, QT>;
+  static constexpr int V = DP / 32;  // components of a lane
+  float o[QT][V];
+  float m[QT], l[QT];
+  float sc;
+
+  __device__ __forceinline__ void start(const DecodeArgs& a, int b, int hk, int h0, int nq, char* extra,
+                                        int warp, int lane) {
+    float* sq = (float*)extra;  // the block's queries; each warp fills a part
+    for (int i = warp * 32 + lane; i < QT * DP; i += kThreads) {
+      const int n = i / DP, d = i % DP;
+      sq[i] = n < nq && d < a.cache.D ? ((const float*)a.q)[b * a.q_b + (int64_t)(h0 + n) * a.q_h + d] : 0.0f;
+    }
+    __syncthreads();
+    sc = a.scale * (a.cache.k_scale ? a.cache.k_scale[hk] : 1.0f) * kLog2e;
+#pragma unroll
+    for (int n = 0; n < QT; ++n) {
+      m[n] = -INFINITY;
+      l[n] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < V; ++i) o[n][i] = 0.0f;
+    }
+  }
+
+  // Component of this lane's i-th: consecutive float4 (float2 for heads of 64).
+  __device__ static int component(int i, int lane) {
+    return V == 2 ? 2 * lane + i : 128 * (i / 4) + 4 * lane + i % 4;
+  }
+
+  __device__ __forceinline__ void tile(uint32_t at, uint32_t valid, char* extra, int warp,
+                                       int lane) {
+    const float* sq = (const float*)extra;
+    float* sp = (float*)extra + QT * DP + warp * S::tk * QT;
+    const int r = lane / 4, sub = lane % 4;
+    float s[QT];
+#pragma unroll
+    for (int n = 0; n < QT; ++n) s[n] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < S::cpr / 4; ++j) {
+      const int c = 4 * j + sub;
+      float4 k;
+      asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                   : "=f"(k.x), "=f"(k.y), "=f"(k.z), "=f"(k.w)
+                   : "r"(at + r * S::row + 16 * swizzle<CP_F32, S::cpr>(r, c)));
+#pragma unroll
+      for (int n = 0; n < QT; ++n) {
+        const float4 x = *(const float4*)(sq + n * DP + 4 * c);
+        s[n] = fmaf(x.x, k.x, fmaf(x.y, k.y, fmaf(x.z, k.z, fmaf(x.w, k.w, s[n]))));
+      }
+    }
+    const bool there = valid >> r & 1;
+#pragma unroll
+    for (int n = 0; n < QT; ++n) {
+      s[n] += __shfl_xor_sync(~0u, s[n], 1);
+      s[n] += __shfl_xor_sync(~0u, s[n], 2);
+      const float x = there ? s[n] * sc : -INFINITY;
+      float top = x;
+#pragma unroll
+      for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+      top = fmaxf(top, m[n]);
+      const float base = top == -INFINITY ? 0.0f : top;
+      const float f = exp2f(m[n] - base), p = there ? exp2f(fmaf(s[n], sc, -base)) : 0.0f;
+      m[n] = top;
+      l[n] = l[n] * f + p;
+#pragma unroll
+      for (int i = 0; i < V; ++i) o[n][i] *= f;
+      if (sub == 0) sp[r * QT + n] = p;
+    }
+    __syncwarp();
+    at += S::tk * S::row;
+#pragma unroll
+    for (int k = 0; k < S::tk; ++k) {
+      float v[V];
+      if (V == 2) {
+        asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];"
+                     : "=f"(v[0]), "=f"(v[V > 1 ? 1 : 0])
+                     : "r"(at + k * S::row + 16 * swizzle<CP_F32, S::cpr>(k, lane / 2) + 8 * (lane % 2)));
+      } else {
+#pragma unroll
+        for (int j = 0; j < V / 4; ++j)
+          asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                       : "=f"(v[4 * j]), "=f"(v[4 * j + 1]), "=f"(v[4 * j + 2]), "=f"(v[4 * j + 3])
+                       : "r"(at + k * S::row + 16 * swizzle<CP_F32, S::cpr>(k, 32 * j + lane)));
+      }
+#pragma unroll
+      for (int n = 0; n < QT; ++n) {
+        const float p = sp[k * QT + n];
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[n][i] = fmaf(p, v[i], o[n][i]);
+      }
+    }
+    __syncwarp();
+  }
+
+  __device__ __forceinline__ void finish(float* sm, float* sl) {
+#pragma unroll
+    for (int n = 0; n < QT; ++n) {
+#pragma unroll
+      for (int d = 4; d < 32; d *= 2) l[n] += __shfl_xor_sync(~0u, l[n], d);
+      if (threadIdx.x % 32 == 0) {
+        sm[n] = m[n];
+        sl[n] = l[n];
+      }
+    }
+  }
+  __device__ __forceinline__ void put(float* buf, const float* f) {
+#pragma unroll
+    for (int n = 0; n < QT; ++n)
+#pragma unroll
+      for (int i = 0; i < V; ++i) buf[n * DP + component(i, threadIdx.x % 32)] = o[n][i] * f[n];
+  }
+};
+
+template <int CT, int DP, int QT>
+__global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, int unit, int tiles, float* parts,
+                                                     Begin* begins) {
+  using S = Shape<CT, DP, QT>;
+  using Row = typename Type<CT>::Row;
+  extern __shared__ __align__(128) char smem[];
+  __shared__ int s_queue[kWarps][kQueue];
+  __shared__ uint32_t s_valid[kWarps][S::stages];
+  __shared__ float s_m[kWarps][QT], s_l[kWarps][QT], s_f[kWarps][QT], s_top[QT], s_sum[QT];
+  asm volatile("griddepcontrol.launch_dependents;");
+  const Cache& ch = a.cache;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int G = a.Hq / ch.heads, cols = ch.heads * tiles;
+  const int chunks = ch.D * S::e / 16;  // of a row that is there
+
+  // this block's units of the line
+  int64_t total = 0;
+  for (int b = lane; b < a.B; b += 32) total += units_of(a, b, unit);
+#pragma unroll
+  for (int d = 16; d; d /= 2) total += __shfl_xor_sync(~0u, total, d);
+  total *= cols;
+  const int64_t blocks = min((int64_t)gridDim.x, total);  // each of these has a unit at least
+  if (begins && threadIdx.x == 0) begins[blockIdx.x] = Begin{0, 0, 0, 0};
+  if (blockIdx.x >= blocks) return;
+  int64_t u = total * blockIdx.x / blocks;
+  const int64_t end = total * (blockIdx.x + 1) / blocks;
+  // the sequence they start in
+  int b = 0;
+  int64_t before = 0;
+  for (int b0 = 0;; b0 += 32) {
+    const int64_t own = b0 + lane < a.B ? (int64_t)units_of(a, b0 + lane, unit) * cols : 0;
+    int64_t upto = own;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const int64_t x = __shfl_up_sync(~0u, upto, d);
+      if (lane >= d) upto += x;
+    }
+    const uint32_t past = __ballot_sync(~0u, before + upto > u);
+    if (past) {
+      const int i = __ffs(past) - 1;
+      b = b0 + i;
+      before += __shfl_sync(~0u, upto - own, i);
+      break;
+    }
+    before += __shfl_sync(~0u, upto, 31);
+  }
+
+  const uint32_t ring = smem_addr(smem) + warp * S::stages * S::tile;
+  char* extra = smem + S::ring;
+  Keys<S::tk> keys;
+  keys.lane = lane;
+  keys.queue = s_queue[warp];
+
+  for (; u < end; ++b) {
+    int first, len;
+    keys_of(a, b, &first, &len);
+    const int nu = max(1, (int)(((int64_t)(len - first) + unit - 1) / unit));
+    const int32_t* table = ch.table + (int64_t)b * ch.table_stride;
+    keys.keep = a.keep ? a.keep + (int64_t)b * a.keep_stride : nullptr;
+    for (; u < end && u < before + (int64_t)nu * cols;) {
+      // the segment: units [k0, k1) of sequence b, query tile `col`
+      const int col = (int)((u - before) / nu), k0 = (int)((u - before) % nu);
+      const int k1 = (int)min((int64_t)nu, k0 + (end - u));
+      const int hk = col / tiles, h0 = hk * G + col % tiles * QT;
+      const int nq = min(QT, G - col % tiles * QT);
+      const int lo = first + k0 * unit, hi = (int)min((int64_t)len, first + (int64_t)k1 * unit);
+      const char* kp = (const char*)ch.k + (int64_t)hk * ch.head_stride * S::e;
+      const char* vp = (const char*)ch.v + (int64_t)hk * ch.head_stride * S::e;
+
+      if (chunks < S::cpr)  // components beyond the head's: the products run over zeros
+        for (int i = lane; i < S::stages * S::tk * (S::cpr - chunks); i += 32) {
+          const int c = chunks + i % (S::cpr - chunks), r = i / (S::cpr - chunks);
+          const uint32_t at = ring + r / S::tk * S::tile + r % S::tk * S::row + 16 * swizzle<CT, S::cpr>(r % S::tk, c);
+          asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
+        }
+
+      keys.start(lo, hi, warp);
+      int key, n_next = keys.take(&key), page = -1, issued = 0;
+      auto look = [&] {
+        page = key >= 0 ? table[(uint32_t)key / (uint32_t)ch.page_size] : -1;
+      };
+      auto issue = [&] {
+        if (n_next > 0) {
+          const int slot = issued % S::stages;
+          const uint32_t to = ring + slot * S::tile;
+          bool ok = key >= 0;
+          if (ok && (page < 0 || page >= ch.pages)) {
+            if (a.status) set_status(a.status, CP_EINVAL);
+            ok = false;
+          }
+          const int64_t mine = ok ? page * ch.page_stride + (int64_t)((uint32_t)key % (uint32_t)ch.page_size) * ch.slot_stride : 0;
+          const uint32_t valid = __ballot_sync(~0u, ok);
+          if (lane == 0) s_valid[warp][slot] = valid;
+#pragma unroll
+          for (int i = 0; i < S::tk * S::cpr / 32; ++i) {
+            const int x = 32 * i + lane, r = x / S::cpr, c = x % S::cpr;
+            const int64_t off = __shfl_sync(~0u, mine, r) * S::e + 16 * c;
+            const bool there = valid >> r & 1;
+            if (c < chunks) {
+              const uint32_t at = to + r * S::row + 16 * swizzle<CT, S::cpr>(r, c);
+              copy16(at, kp + (there ? off : 0), there);
+              copy16(at + S::tk * S::row, vp + (there ? off : 0), there);
+            }
+          }
+          ++issued;
+          n_next = keys.take(&key);
+          look();
+        }
+        copy_commit();
+      };
+      look();
+      __syncwarp();
+#pragma unroll 1
+      for (int i = 0; i < S::stages - 1; ++i) issue();
+      Math<CT, DP, QT> math;
+      math.start(a, b, hk, h0, nq, extra, warp, lane);
+      for (int i = 0; i < issued; ++i) {
+        copy_wait<S::stages - 2>();
+        __syncwarp();  // tile i is there for every lane, and tile i - 1 done with
+        issue();
+        const int slot = i % S::stages;
+        math.tile(ring + slot * S::tile, s_valid[warp][slot], extra, warp, lane);
+      }
+      math.finish(s_m[warp], s_l[warp]);
+      copy_wait<0>();
+      __syncthreads();
+      // the warps' results by a common maximum
+      if (threadIdx.x < QT) {
+        const int n = threadIdx.x;
+        float top = -INFINITY, sum = 0.0f;
+        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_m[w][n]);
+        const float base = top == -INFINITY ? 0.0f : top;
+        for (int w = 0; w < kWarps; ++w) {
+          const float f = exp2f(s_m[w][n] - base);
+          s_f[w][n] = f;
+          sum += s_l[w][n] * f;
+        }
+        s_top[n] = top;
+        s_sum[n] = sum;
+      }
+      __syncthreads();
+      float* buf = (float*)smem;
+      math.put(buf + warp * QT * DP, s_f[warp]);
+      __syncthreads();
+      const bool whole = k0 == 0 && k1 == nu;
+      const float vs = ch.v_scale ? ch.v_scale[hk] : 1.0f;
+      float* part = whole ? nullptr : parts + (2 * (int64_t)blockIdx.x + (k0 == 0)) * S::part;
+      for (int i = threadIdx.x; i < nq * DP; i += kThreads) {
+        const int n = i / DP, d = i % DP;
+        float x = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) x += buf[w * QT * DP + i];
+        if (!whole)
+          part[2 * QT + i] = x;
+        else if (d < ch.D)
+          ((Row*)a.out)[b * a.o_b + (int64_t)(h0 + n) * a.o_h + d] =
+              from_f32<Row>(s_sum[n] == 0.0f ? 0.0f : x * (vs / s_sum[n]));
+      }
+      if (threadIdx.x < nq) {
+        const int n = threadIdx.x;
+        if (!whole) {
+          part[n] = s_top[n];
+          part[QT + n] = s_sum[n];
+        } else if (a.lse) {
+          a.lse[(int64_t)b * a.Hq + h0 + n] = s_sum[n] == 0.0f ? -INFINITY : (s_top[n] + log2f(s_sum[n])) * kLn2;
+        }
+      }
+      if (!whole && k0 == 0 && threadIdx.x == 0) {
+        // the block that has the query tile's last unit: unit x is in the largest
+        // block i with i * total / blocks <= x
+        const int64_t last = u + nu - 1;
+        const int at = (int)(((last + 1) * blocks - 1) / total);
+        begins[blockIdx.x] = Begin{b, col, at - (int)blockIdx.x + 1, 0};
+      }
+      u += k1 - k0;
+      __syncthreads();  // the ring and the sums are free
+    }
+    before += (int64_t)nu * cols;
+  }
+}
+
+// Adds the parts of the query tiles that several blocks shared, a block for 4
+// queries of the tile that begins in block blockIdx.x: part 1 of that block, then
+// part 0 of the following ones, weighed by a common maximum.
+constexpr int kJoinThreads = 256, kJoinQueries = 4;
+template <int CT, int DP, int QT>
+__global__ void __launch_bounds__(kJoinThreads) k_decode_join(DecodeArgs a, int tiles, const float* parts,
+                                                              const Begin* begins) {
+  using S = Shape<CT, DP, QT>;
+  using Row = typename Type<CT>::Row;
+  constexpr int kCols = DP / 4, kGroups = kJoinThreads / kCols;  // float4 columns, parts at a time
+  __shared__ float4 s_o[kGroups][kCols];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const Begin x = begins[blockIdx.x];
+  if (x.blocks == 0) return;
+  const int G = a.Hq / a.cache.heads, hk = x.col / tiles, h0 = hk * G + x.col % tiles * QT;
+  const int nq = min(QT, G - x.col % tiles * QT);
+  const float vs = a.cache.v_scale ? a.cache.v_scale[hk] : 1.0f;
+  const int lane = threadIdx.x % 32;
+  auto part = [&](int i) { return parts + (2 * ((int64_t)blockIdx.x + i) + (i == 0)) * S::part; };
+  for (int n = blockIdx.y * kJoinQueries; n < min(nq, (int)(blockIdx.y + 1) * kJoinQueries); ++n) {
+    float top = -INFINITY;
+    for (int i = lane; i < x.blocks; i += 32) top = fmaxf(top, part(i)[n]);
+#pragma unroll
+    for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+    const float base = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f;
+    for (int i = lane; i < x.blocks; i += 32) sum += part(i)[QT + n] * exp2f(part(i)[n] - base);
+    sum = warp_sum(sum);  // the same in every warp
+    float4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int col = threadIdx.x % kCols, group = threadIdx.x / kCols;
+#pragma unroll 4
+    for (int i = group; i < x.blocks; i += kGroups) {
+      const float* p = part(i);
+      const float f = exp2f(p[n] - base);
+      const float4 y = *(const float4*)(p + 2 * QT + n * DP + 4 * col);
+      o.x = fmaf(f, y.x, o.x);
+      o.y = fmaf(f, y.y, o.y);
+      o.z = fmaf(f, y.z, o.z);
+      o.w = fmaf(f, y.w, o.w);
+    }
+    s_o[group][col] = o;
+    __syncthreads();
+    if (threadIdx.x < DP && threadIdx.x < a.cache.D) {
+      float y = 0.0f;
+      for (int i = 0; i < kGroups; ++i) y += ((const float*)s_o[i])[threadIdx.x];
+      ((Row*)a.out)[x.b * a.o_b + (int64_t)(h0 + n) * a.o_h + threadIdx.x] =
+          from_f32<Row>(sum == 0.0f ? 0.0f : y * (vs / sum));
+    }
+    if (threadIdx.x == 0 && a.lse)
+      a.lse[(int64_t)x.b * a.Hq + h0 + n] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
+    __syncthreads();
+  }
+}
+
+// Query heads a pass takes and the width a head is laid out for.
+static int pass_of(int cache_dtype, int64_t G) {
+  if (cache_dtype == CP_F32) return G <= 4 ? 4 : 8;
+  return G <= 8 ? 8 : 16;
+}
+static int width_of(int64_t D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
+constexpr int kMaxBlocks = 1024;
+
+size_t decode_ws_bytes(int64_t B, int64_t Hq, int64_t heads, int64_t D, int cache_dtype) {
+  (void)B;
+  const int QT = pass_of(cache_dtype, Hq / heads), DP = width_of(D);
+  return kMaxBlocks * (sizeof(Begin) + 2 * sizeof(float) * (size_t)QT * (DP + 2));
+}
+
+template <int CT, int DP, int QT>
+static int launch(const DecodeArgs& a, cudaStream_t s) {
+  using S = Shape<CT, DP, QT>;
+  DeviceInfo di;
+  CP_TRY_STATUS(device_info(&di));
+  const int G = a.Hq / a.cache.heads, tiles = (G + QT - 1) / QT;
+  // Sequences of at most 4 units are not cut: the join would cost more.
+  const bool cut = a.cache.capacity > 4 * kUnit;
+  const int unit = cut ? kUnit : 4 * kUnit;
+  const int64_t line = (int64_t)a.B * a.cache.heads * tiles *
+                       (a.cache.capacity < 1 ? 1 : ((int64_t)a.cache.capacity + unit - 1) / unit);
+  if (line > (int64_t)1 << 52) return CP_EUNSUPPORTED;  // units times blocks stay within 64 bits
+  int64_t grid = (int64_t)di.sm_count * S::per_sm;
+  if (grid > kMaxBlocks) grid = kMaxBlocks;
+  if (grid > line) grid = line;
+  Begin* begins = (Begin*)a.ws;
+  float* parts = (float*)((char*)a.ws + kMaxBlocks * sizeof(Begin));
+  CP_TRY_STATUS(allow_smem((const void*)k_decode<CT, DP, QT>, S::smem, "decode: shared memory"));
+  k_decode<CT, DP, QT><<<(unsigned)grid, kThreads, S::smem, s>>>(a, unit, tiles, parts, cut ? begins : nullptr);
+  CP_TRY_STATUS(launch_status("decode"));
+  if (!cut) return CP_OK;
+  // its blocks wait on the device for the parts, not for a launch after them
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)grid, (unsigned)((G < QT ? G : QT) + kJoinQueries - 1) / kJoinQueries);
+  cfg.blockDim = dim3(kJoinThreads);
+  cfg.stream = s;
+  cudaLaunchAttribute early{};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &early;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_decode_join<CT, DP, QT>, a, tiles, (const float*)parts,
+                                           (const Begin*)begins);
+  note_launch();
+  return cuda_status(e, "decode: join");
+}
+
+template <int CT, int DP>
+static int launch_pass(const DecodeArgs& a, cudaStream_t s) {
+  constexpr int one = CT == CP_F32 ? 4 : 8;
+  return pass_of(CT, a.Hq / a.cache.heads) == one ? launch<CT, DP, one>(a, s) : launch<CT, DP, 2 * one>(a, s);
+}
+template <int CT>
+static int launch_type(const DecodeArgs& a, cudaStream_t s) {
+  switch (width_of(a.cache.D)) {
+    case 64: return launch_pass<CT, 64>(a, s);
+    case 128: return launch_pass<CT, 128>(a, s);
+    default: return launch_pass<CT, 256>(a, s);
+  }
+}
 
 int launch_decode(const DecodeArgs& a, int cache_dtype, cudaStream_t s) {
-  const dim3 grid(a.Hq, a.B);
-  if (cache_dtype == CP_F32)
-    k_decode<float, float><<<grid, kTile, 0, s>>>(a);
-  else if (cache_dtype == CP_BF16)
-    k_decode<__nv_bfloat16, __nv_bfloat16><<<grid, kTile, 0, s>>>(a);
-  else
-    k_decode<__nv_bfloat16, __nv_fp8_e4m3><<<grid, kTile, 0, s>>>(a);
-  return last_launch_status();
+  if (cache_dtype == CP_F32) return launch_type<CP_F32>(a, s);
+  if (cache_dtype == CP_BF16) return launch_type<CP_BF16>(a, s);
+  return launch_type<CP_E4M3>(a, s);
 }
 
 }  // namespace cp
