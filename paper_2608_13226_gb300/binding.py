@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 import threading
 from dataclasses import dataclass, fields
 
@@ -431,38 +432,70 @@ def coverprune_gather(feats, pos, frame, kept, *, status=None, out=None):
 # What the language model runs on the kept tokens: rotary positions, a paged
 # cache of keys and values, and one token's attention over it.
 # ---------------------------------------------------------------------------
-_I64x2, _I64x3 = C.c_int64 * 2, C.c_int64 * 3
+# These calls come once a layer and token, so the host's part of them counts:
+# the C structs are packed into bytes in one go, and a tensor is asked for
+# each of its properties once.
 _CACHE_TYPES = {torch.float32: CP_F32, torch.bfloat16: CP_BF16, torch.float8_e4m3fn: CP_E4M3}
+_pack_rows = struct.Struct("@PPq3q3q").pack      # cp_rows
+_pack_rope = struct.Struct("@Piif4x").pack       # cp_rope
+_pack_cache = struct.Struct("@IiPPqqqqqqqPPPqq").pack  # cp_cache
+_pack_pair = struct.Struct("@qq").pack
+_CACHE_BYTES = C.sizeof(_Cache)
 
 
-def _on_gpu(name, t, dtype, shape=None, *, dense=True):
+def _raw_stream(t) -> int:
+    """The current stream of the tensor's device."""
+    return torch.cuda.current_stream(t.device).cuda_stream
+
+
+if hasattr(torch._C, "_cuda_getCurrentRawStream"):  # the same without a Stream object (2 us)
+    def _raw_stream(t) -> int:  # noqa: F811
+        return torch._C._cuda_getCurrentRawStream(t.get_device())
+
+
+def _on_gpu(name, t, dtype, shape=None, dense=True):
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != shape:
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
     if dense and not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _optional(name, t, dtype, shape=None):
+    return None if t is None else _on_gpu(name, t, dtype, shape)
 
 
 def _rows_of(name, t, dims):
-    """Checks a tensor of head rows; only its last dimension has to be dense."""
+    """Shape and strides of a tensor of head rows; only its last dimension has to be dense."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != dims:
+        raise ValueError(f"{name} must have {dims} dimensions, got {len(shape)}")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    if t.dim() != dims:
-        raise ValueError(f"{name} must have {dims} dimensions, got {t.dim()}")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if stride[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{name} must be dense in its last dimension")
+    return shape, stride
+
+
+def _result_like(name, t, shape, dtype, dims):
+    """Strides of a result given by the caller."""
+    got, stride = _rows_of(name, t, dims)
+    if got != shape or t.dtype is not dtype:
+        raise ValueError(f"{name} must be {tuple(shape)} of {dtype}")
+    return stride
 
 
 def _rope(inv_freq, D, layout, scale):
     if layout not in ROPE_LAYOUTS:
         raise ValueError(f"layout must be one of {tuple(ROPE_LAYOUTS)}, got {layout!r}")
-    _on_gpu("inv_freq", inv_freq, torch.float64)
-    if inv_freq.dim() != 1 or 2 * inv_freq.numel() > D:
+    at, n = _on_gpu("inv_freq", inv_freq, torch.float64), inv_freq.shape
+    if len(n) != 1 or 2 * n[0] > D:
         raise ValueError(f"inv_freq must hold one frequency for each rotated pair, at most {D // 2}")
-    return _Rope(inv_freq.data_ptr(), 2 * inv_freq.numel(), ROPE_LAYOUTS[layout], scale)
+    return _pack_rope(at, 2 * n[0], ROPE_LAYOUTS[layout], scale)
 
 
 def coverprune_rotary_frequencies(rot: int, base: float = 10000.0, *, stretch: str = "none",
@@ -490,11 +523,12 @@ def coverprune_rotary(x, pos, inv_freq, *, layout: str = "half", scale: float = 
     out may be x.  inverse=True gives the gradient with respect to x from the
     one with respect to the result."""
     many = isinstance(x, (list, tuple))
-    xs = list(x) if many else [x]
+    xs = x if many else (x,)
     if not 1 <= len(xs) <= 4:
         raise ValueError("x must be a tensor or a list of one to four")
-    dims = xs[0].dim()
-    if dims not in (3, 4):
+    first = xs[0]
+    dims, dtype = first.dim(), first.dtype
+    if dims != 3 and dims != 4:
         raise ValueError("x must be [T, heads, D] or [B, T, heads, D]")
     if out is None:
         outs = [torch.empty_like(t) for t in xs]
@@ -502,55 +536,56 @@ def coverprune_rotary(x, pos, inv_freq, *, layout: str = "half", scale: float = 
         outs = list(out) if many else [out]
         if len(outs) != len(xs):
             raise ValueError("out must match x")
-    lead, D, dt = xs[0].shape[:-2], xs[0].shape[-1], _dtype(xs[0])
-    rows = (_Rows * len(xs))()
-    for r, t, o in zip(rows, xs, outs):
-        _rows_of("x", t, dims)
-        if t.shape[:-2] != lead or t.shape[-1] != D or t.dtype != xs[0].dtype:
+    dt, shape, rows = _dtype(first), first.shape, b""
+    lead, D = shape[:-2], shape[-1]
+    for t, o in zip(xs, outs):
+        shape, stride = _rows_of("x", t, dims)
+        if t is not first and (shape[:-2] != lead or shape[-1] != D or t.dtype is not dtype):
             raise ValueError("tensors turned together must share tokens, width and dtype")
-        if o is not t:
-            _rows_of("out", o, dims)
-            if o.shape != t.shape or o.dtype != t.dtype:
-                raise ValueError("out must match x in shape and dtype")
-        r.in_, r.out, r.heads = t.data_ptr(), o.data_ptr(), t.shape[-2]
-        r.in_stride[:] = (0,) * (4 - dims) + t.stride()[:-1]
-        r.out_stride[:] = (0,) * (4 - dims) + o.stride()[:-1]
+        to = stride if o is t else _result_like("out", o, shape, dtype, dims)
+        if dims == 3:
+            rows += _pack_rows(t.data_ptr(), o.data_ptr(), shape[1], 0, stride[0], stride[1], 0,
+                               to[0], to[1])
+        else:
+            rows += _pack_rows(t.data_ptr(), o.data_ptr(), shape[2], stride[0], stride[1],
+                               stride[2], to[0], to[1], to[2])
     B, T = (1, lead[0]) if dims == 3 else lead
-    _on_gpu("pos", pos, torch.int64)
-    if pos.dim() == dims - 2 and tuple(pos.shape) == tuple(lead):
+    at = _on_gpu("pos", pos, torch.int64)
+    if pos.shape == lead:
         pos_stride = T
     elif pos.dim() == 1 and pos.shape[0] == T:
         pos_stride = 0
     else:
         raise ValueError(f"pos must be [{T}] or {tuple(lead)}, got {tuple(pos.shape)}")
-    rope = _rope(inv_freq, D, layout, scale)
-    _check(_lib().coverprune_rotary(rows, len(xs), dt, B, T, D, _ptr(pos), pos_stride,
-                                    C.byref(rope), 1 if inverse else 0, _stream()),
-           "coverprune_rotary")
+    st = _lib().coverprune_rotary(rows, len(xs), dt, B, T, D, at, pos_stride,
+                                  _rope(inv_freq, D, layout, scale), 1 if inverse else 0,
+                                  _raw_stream(first))
+    if st:
+        _check(st, "coverprune_rotary")
     return outs if many else outs[0]
 
 
 def _cache(k_cache, v_cache, table, k_scale, v_scale):
-    _rows_of("k_cache", k_cache, 4)
-    if k_cache.dtype not in _CACHE_TYPES:
-        raise TypeError(f"the cache must be float32, bfloat16 or float8_e4m3fn, got {k_cache.dtype}")
-    shape, stride = k_cache.shape, k_cache.stride()
-    if v_cache.shape != shape or v_cache.stride() != stride or v_cache.dtype != k_cache.dtype \
+    """cp_cache as bytes, and the cache's heads, width and keys a sequence."""
+    shape, stride = _rows_of("k_cache", k_cache, 4)
+    dtype = k_cache.dtype
+    if dtype not in _CACHE_TYPES:
+        raise TypeError(f"the cache must be float32, bfloat16 or float8_e4m3fn, got {dtype}")
+    if v_cache.shape != shape or v_cache.stride() != stride or v_cache.dtype is not dtype \
             or not v_cache.is_cuda:
         raise ValueError("k_cache and v_cache must share shape, strides and dtype")
     pages, page_size, heads, D = shape
-    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
-        if t is not None:
-            _on_gpu(name, t, torch.float32, (heads,))
-    _on_gpu("table", table, torch.int32, dense=False)
-    if table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
+    ks = _optional("k_scale", k_scale, torch.float32, (heads,))
+    vs = _optional("v_scale", v_scale, torch.float32, (heads,))
+    at, of = _on_gpu("table", table, torch.int32, dense=False), table.shape
+    if len(of) != 2 or (of[1] > 1 and table.stride(1) != 1):
         raise ValueError("table must be [B, width], dense in its last dimension")
-    return _Cache(C.sizeof(_Cache), _CACHE_TYPES[k_cache.dtype], k_cache.data_ptr(),
-                  v_cache.data_ptr(), pages, page_size, heads, D,
-                  stride[0] if pages > 1 else 0, stride[1] if page_size > 1 else 0,
-                  stride[2] if heads > 1 else 0, k_scale.data_ptr() if k_scale is not None else None,
-                  v_scale.data_ptr() if v_scale is not None else None, table.data_ptr(),
-                  table.shape[1], table.stride(0))
+    # strides of dimensions of one do not matter, whatever the tensor says
+    c = _pack_cache(_CACHE_BYTES, _CACHE_TYPES[dtype], k_cache.data_ptr(), v_cache.data_ptr(),
+                    pages, page_size, heads, D, stride[0] if pages > 1 else 0,
+                    stride[1] if page_size > 1 else 0, stride[2] if heads > 1 else 0, ks or 0,
+                    vs or 0, at, of[1], table.stride(0))
+    return c, heads, D, of[1] * page_size
 
 
 def coverprune_cache_append(k, v, k_cache, v_cache, table, lens, *, starts=None, pos=None,
@@ -563,47 +598,35 @@ def coverprune_cache_append(k, v, k_cache, v_cache, table, lens, *, starts=None,
     sequence's (default: one row a sequence), lens int32 [B] how many keys each
     holds already.  q [T, Hq, D] is turned in the same launch.  Returns
     {"lens": int32 [B] after the call, "q": the turned queries or None}."""
-    _rows_of("k", k, 3)
-    _rows_of("v", v, 3)
-    cache = _cache(k_cache, v_cache, table, k_scale, v_scale)
-    T, D = k.shape[0], cache.D
-    if tuple(k.shape) != (T, cache.heads, D) or v.shape != k.shape or v.dtype != k.dtype:
-        raise ValueError(f"k and v must be [T, {cache.heads}, {D}] of one dtype")
-    _on_gpu("lens", lens, torch.int32)
-    B = table.shape[0]
-    if tuple(lens.shape) != (B,):
-        raise ValueError(f"lens must have shape ({B},), got {tuple(lens.shape)}")
-    if starts is not None:
-        _on_gpu("starts", starts, torch.int32, (B + 1,))
-    elif T != B:
+    cache, heads, D, _ = _cache(k_cache, v_cache, table, k_scale, v_scale)
+    shape, ks = _rows_of("k", k, 3)
+    of, vs = _rows_of("v", v, 3)
+    T, B, dtype = shape[0], table.shape[0], k.dtype
+    if shape[1] != heads or shape[2] != D or of != shape or v.dtype is not dtype:
+        raise ValueError(f"k and v must be [T, {heads}, {D}] of one dtype")
+    before = _on_gpu("lens", lens, torch.int32, (B,))
+    if starts is None and T != B:
         raise ValueError(f"without starts there is one row a sequence: {T} rows, {B} sequences")
-    if pos is not None:
-        _on_gpu("pos", pos, torch.int64, (T,))
     rope = None if inv_freq is None else _rope(inv_freq, D, layout, scale)
     if new_lens is None:
         new_lens = torch.empty_like(lens)
-    else:
-        _on_gpu("new_lens", new_lens, torch.int32, (B,))
     rows = None
     if q is not None:
-        _rows_of("q", q, 3)
-        if q.shape[0] != T or q.shape[2] != D or q.dtype != k.dtype:
+        of, st = _rows_of("q", q, 3)
+        if of[0] != T or of[2] != D or q.dtype is not dtype:
             raise ValueError(f"q must be [{T}, heads, {D}] of k's dtype")
         if q_out is None:
             q_out = torch.empty_like(q)
-        elif q_out is not q:
-            _rows_of("q_out", q_out, 3)
-            if q_out.shape != q.shape or q_out.dtype != q.dtype:
-                raise ValueError("q_out must match q in shape and dtype")
-        rows = _Rows(q.data_ptr(), q_out.data_ptr(), q.shape[1], _I64x3(0, *q.stride()[:2]),
-                     _I64x3(0, *q_out.stride()[:2]))
-    if status is not None:
-        _on_gpu("status", status, torch.int32)
-    _check(_lib().coverprune_cache_append(
-        C.byref(cache), _ptr(k), _I64x2(*k.stride()[:2]), _ptr(v), _I64x2(*v.stride()[:2]),
-        _dtype(k), T, _ptr(starts), _ptr(lens), B, _ptr(pos),
-        None if rope is None else C.byref(rope), None if rows is None else C.byref(rows),
-        _ptr(new_lens), _ptr(status), _stream()), "coverprune_cache_append")
+        to = st if q_out is q else _result_like("q_out", q_out, of, dtype, 3)
+        rows = _pack_rows(q.data_ptr(), q_out.data_ptr(), of[1], 0, st[0], st[1], 0, to[0], to[1])
+    st = _lib().coverprune_cache_append(
+        cache, k.data_ptr(), _pack_pair(ks[0], ks[1]), v.data_ptr(), _pack_pair(vs[0], vs[1]),
+        _dtype(k), T, _optional("starts", starts, torch.int32, (B + 1,)), before, B,
+        _optional("pos", pos, torch.int64, (T,)), rope, rows,
+        _on_gpu("new_lens", new_lens, torch.int32, (B,)), _optional("status", status, torch.int32),
+        _raw_stream(k))
+    if st:
+        _check(st, "coverprune_cache_append")
     return {"lens": new_lens, "q": q_out}
 
 
@@ -615,40 +638,38 @@ def coverprune_decode_attention(q, k_cache, v_cache, table, lens, *, scale=None,
     only; keep bool [B, >= keys]: the keys marked only.  scale defaults to
     1 / sqrt(D).  Returns {"out": [B, Hq, D], "lse": float32 [B, Hq] or None,
     "ws": the workspace, to pass to the next call}."""
-    _rows_of("q", q, 3)
-    cache = _cache(k_cache, v_cache, table, k_scale, v_scale)
-    B, Hq, D = q.shape
-    if D != cache.D or table.shape[0] != B:
-        raise ValueError(f"q must be [{table.shape[0]}, heads, {cache.D}], got {tuple(q.shape)}")
-    _on_gpu("lens", lens, torch.int32, (B,))
-    keep_stride = 0
+    cache, heads, D, keys = _cache(k_cache, v_cache, table, k_scale, v_scale)
+    shape, qs = _rows_of("q", q, 3)
+    B, Hq, dtype = shape[0], shape[1], q.dtype
+    if shape[2] != D or table.shape[0] != B:
+        raise ValueError(f"q must be [{table.shape[0]}, heads, {D}], got {tuple(shape)}")
+    n = _on_gpu("lens", lens, torch.int32, (B,))
+    marks, marks_stride = None, 0
     if keep is not None:
-        _on_gpu("keep", keep, torch.bool, dense=False)
-        if keep.dim() != 2 or keep.shape[0] != B or keep.shape[1] < cache.table_width * cache.page_size \
-                or (keep.shape[1] > 1 and keep.stride(1) != 1):
-            raise ValueError(f"keep must be [{B}, at least {cache.table_width * cache.page_size}], "
-                             "dense in its last dimension")
-        keep_stride = keep.stride(0)
+        marks, of = _on_gpu("keep", keep, torch.bool, dense=False), keep.shape
+        if len(of) != 2 or of[0] != B or of[1] < keys or (of[1] > 1 and keep.stride(1) != 1):
+            raise ValueError(f"keep must be [{B}, at least {keys}], dense in its last dimension")
+        marks_stride = keep.stride(0)
+    dt = _dtype(q)
     if out is None:
-        out = torch.empty((B, Hq, D), dtype=q.dtype, device=q.device)
+        out = torch.empty(shape, dtype=dtype, device=q.device)
+        to = (Hq * D, D)
     else:
-        _rows_of("out", out, 3)
-        if out.shape != q.shape or out.dtype != q.dtype:
-            raise ValueError("out must match q in shape and dtype")
+        to = _result_like("out", out, shape, dtype, 3)
     lse_out = torch.empty((B, Hq), dtype=torch.float32, device=q.device) if lse else None
-    if status is not None:
-        _on_gpu("status", status, torch.int32)
     lib = _lib()
     if ws is None:
-        n = C.c_size_t()
-        _check(lib.coverprune_decode_workspace_size(B, Hq, C.byref(cache), C.byref(n)),
+        size = C.c_size_t()
+        _check(lib.coverprune_decode_workspace_size(B, Hq, cache, C.byref(size)),
                "coverprune_decode_workspace_size")
-        ws = torch.empty(max(n.value, 256), dtype=torch.uint8, device=q.device)
-    _check(lib.coverprune_decode_attention(
-        _ptr(q), _I64x2(*q.stride()[:2]), _dtype(q), B, Hq, C.byref(cache), _ptr(lens), _ptr(keep),
-        keep_stride, D ** -0.5 if scale is None else scale, window, _ptr(out),
-        _I64x2(*out.stride()[:2]), _ptr(lse_out), _ptr(ws), ws.numel(), _ptr(status), _stream()),
-        "coverprune_decode_attention")
+        ws = torch.empty(max(size.value, 256), dtype=torch.uint8, device=q.device)
+    st = lib.coverprune_decode_attention(
+        q.data_ptr(), _pack_pair(qs[0], qs[1]), dt, B, Hq, cache, n, marks, marks_stride,
+        D ** -0.5 if scale is None else scale, window, out.data_ptr(), _pack_pair(to[0], to[1]),
+        None if lse_out is None else lse_out.data_ptr(), ws.data_ptr(), ws.numel(),
+        _optional("status", status, torch.int32), _raw_stream(q))
+    if st:
+        _check(st, "coverprune_decode_attention")
     return {"out": out, "lse": lse_out, "ws": ws}
 
 

@@ -112,6 +112,16 @@ int allow_smem(const void* fn, size_t smem, const char* where) {
                      where);
 }
 
+int allow_smem_once(const void* fn, size_t smem, const char* where, std::atomic<uint64_t>* done) {
+  int dev = 0;
+  CP_TRY_STATUS(cuda_status(cudaGetDevice(&dev), where));
+  const uint64_t bit = (uint64_t)1 << (dev & 63);  // device_info refuses devices past 63
+  if (done->load(std::memory_order_acquire) & bit) return CP_OK;
+  CP_TRY_STATUS(allow_smem(fn, smem, where));
+  done->fetch_or(bit, std::memory_order_release);
+  return CP_OK;
+}
+
 // bf16 features: tcgen05 tensor cores; fp32 features: fp32 FMA tiles (TF32
 // would round the features to 10 mantissa bits).  cos_out (may be null):
 // every cosine (bf16) or dot product (fp32) of a pair i <= j stored

@@ -773,7 +773,8 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   if (grid > line) grid = line;
   Begin* begins = (Begin*)a.ws;
   float* parts = (float*)((char*)a.ws + kMaxBlocks * sizeof(Begin));
-  CP_TRY_STATUS(allow_smem((const void*)k_decode<CT, DP, QT>, S::smem, "decode: shared memory"));
+  static std::atomic<uint64_t> allowed{0};
+  CP_TRY_STATUS(allow_smem_once((const void*)k_decode<CT, DP, QT>, S::smem, "decode: shared memory", &allowed));
   k_decode<CT, DP, QT><<<(unsigned)grid, kThreads, S::smem, s>>>(a, unit, tiles, parts, cut ? begins : nullptr);
   CP_TRY_STATUS(launch_status("decode"));
   if (!cut) return CP_OK;

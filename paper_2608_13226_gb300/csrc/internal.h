@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "coverprune.h"
 
 namespace cp {
@@ -93,6 +95,9 @@ int device_info(DeviceInfo* out);
 // the kernel's static part, so that a call with fewer tokens on another host
 // thread does not lower it between here and the launch.
 int allow_smem(const void* fn, size_t smem, const char* where);
+// The same once a device: `*done` is the kernel's own word, a bit a device.  For
+// calls so short that the two runtime calls would count.
+int allow_smem_once(const void* fn, size_t smem, const char* where, std::atomic<uint64_t>* done);
 
 // ---------------------------------------------------------------------------
 // Launchers (each returns a cp_status; all enqueue on `s`).
