@@ -1,25 +1,50 @@
 // Rotary positions, and the append of keys and values to a paged cache.
 //
 // Both read every row once and write it once, a few operations an element: HBM
-// bounds them.  A block takes a few tokens at a time.  First its threads
-// compute the tokens' cosines and sines into shared memory, one pair each, so that
-// a token's angles are computed once for all of its heads; then a thread keeps
-// the V pairs of one place of a row in registers and turns that place in row
-// after row, two 16-byte loads and stores a row where alignment allows.
-// Blocks stay for the whole call: the speeds' float64 arithmetic (1/64 of the
-// float32 rate) is done once a block.
+// bounds them, if about 50 KB an SM of it are on their way all the time.  So
+//  - a block has a run of tokens for the whole call.  The speeds' float64 arithmetic
+//    (1/64 of the float32 rate) is done once a block, and where the tokens go
+//    is looked up kChunk of them at a time, a thread each;
+//  - the rows of its tokens are one line, taken a stage of up to 2 rows a lane
+//    at a time.  Between two barriers the block notes where the rows of the
+//    stage after next lie (a thread a row), computes the angles of the next
+//    stage's tokens (a thread a pair, once for all heads), starts the next
+//    stage's copies and turns this one's rows;
+//  - a lane turns two places of a row, each V pairs in two 16-byte vectors where
+//    alignment allows.  It copies them into slots of its own, so a copy is
+//    waited for by the lane that made it and the barrier never waits for one.
+// The products are packed pairs of float32 (half the FMA instructions).
+#include <type_traits>
+
 #include "rope.cuh"
 
 namespace cp {
 
 constexpr int kThreads = 256;
-constexpr int kGroup = 16;  // tokens of a block at most
-constexpr int kRows = 4;  // rows whose loads a thread has in flight
+// Blocks of an SM and rows of a stage that a lane has at most.  39,328 tokens of
+// 28 + 4 bf16 heads of 128, us for rotary / append: 2 and 2 101 / 112, 2 and 1
+// 105 / 130, 3 and 1 110 / 118, 4 and 1 116 / 122 (fewer bytes under way), 3 and 2
+// 112 / 132 (two blocks fit).
+constexpr int kBlocks = 2;
+constexpr int kItems = 2;
+constexpr int kChunk = 256;  // tokens looked up at a time
+constexpr size_t kMostSmem = 160 * 1024;  // more than any launch takes
+
+// n / d for 0 <= n < 2^31 by a product: with 2^l >= d, mul = ceil(2^(31 + l) / d)
+// is off by less than d / 2^(31 + l), and n times that by less than 1 / d.
+struct Divisor {
+  uint32_t d, mul, shift;
+  __device__ __forceinline__ int of(int n) const { return (int)((uint64_t)(uint32_t)n * mul >> 31 >> shift); }
+};
 
 // Sizes of a launch that the kernels share.
 struct Tiling {
-  int nv, nvt;       // places of V pairs (and then of V components that pass) in a row; threads for them
-  int lanes, group;  // rows side by side, tokens side by side: nvt * lanes * group threads at most
+  int places, wide;  // of V pairs (and then of 2 V components that pass) in a row; threads for them, two each
+  int parts;         // of a row: places / (2 wide), rounded up
+  Divisor rows_of, half_of;  // by the parts of a token's rows, by half
+  int lanes;         // rows side by side: wide * lanes threads at most
+  int stage;         // parts of rows of a stage
+  int held;          // tokens whose angles are held: those of two stages
   int half;
 };
 
@@ -82,36 +107,82 @@ __device__ __forceinline__ void store(C* p, int at, const float (&x)[V]) {
   *reinterpret_cast<W*>(p + at) = y;
 }
 
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  return (uint64_t)__float_as_uint(hi) << 32 | __float_as_uint(lo);
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+
 // The two vectors of a place turned by its pairs: in the half layout a[i] with
 // b[i], interleaved neighbours within a and within b.
-template <typename T, int V>
-__device__ __forceinline__ void turn(const Pack<T, V>& a, const Pack<T, V>& b, const float2 (&cs)[V],
-                                     bool interleaved, float (&x)[V], float (&y)[V]) {
-  if (interleaved) {
-    float z[2 * V];
+template <typename T, int V, bool INTERLEAVED>
+__device__ __forceinline__ void turn(const Pack<T, V>& a, const Pack<T, V>& b, const float (&c)[V], const float (&s)[V],
+                                     float (&x)[V], float (&y)[V]) {
+  float u[V], w[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      z[i] = a[i];
-      z[V + i] = b[i];
+  for (int i = 0; i < V; ++i) {
+    if (INTERLEAVED) {
+      u[i] = 2 * i < V ? a[2 * i % V] : b[2 * i % V];
+      w[i] = 2 * i + 1 < V ? a[(2 * i + 1) % V] : b[(2 * i + 1) % V];
+    } else {
+      u[i] = a[i];
+      w[i] = b[i];
     }
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float u = z[2 * i], w = z[2 * i + 1];
-      z[2 * i] = fmaf(u, cs[i].x, -__fmul_rn(w, cs[i].y));
-      z[2 * i + 1] = fmaf(w, cs[i].x, __fmul_rn(u, cs[i].y));
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      x[i] = z[i];
-      y[i] = z[V + i];
-    }
+  }
+  float p[V], q[V];
+  if constexpr (V == 1) {
+    p[0] = fmaf(w[0], -s[0], __fmul_rn(u[0], c[0]));
+    q[0] = fmaf(u[0], s[0], __fmul_rn(w[0], c[0]));
   } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float u = a[i], w = b[i];
-      x[i] = fmaf(u, cs[i].x, -__fmul_rn(w, cs[i].y));
-      y[i] = fmaf(w, cs[i].x, __fmul_rn(u, cs[i].y));
+    for (int i = 0; i < V; i += 2) {
+      const uint64_t u2 = pair(u[i], u[i + 1]), w2 = pair(w[i], w[i + 1]), c2 = pair(c[i], c[i + 1]);
+      const uint64_t p2 = fma2(w2, pair(-s[i], -s[i + 1]), mul2(u2, c2));
+      const uint64_t q2 = fma2(u2, pair(s[i], s[i + 1]), mul2(w2, c2));
+      p[i] = __uint_as_float((uint32_t)p2);
+      p[i + 1] = __uint_as_float((uint32_t)(p2 >> 32));
+      q[i] = __uint_as_float((uint32_t)q2);
+      q[i + 1] = __uint_as_float((uint32_t)(q2 >> 32));
     }
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    if (INTERLEAVED) {
+      (2 * i < V ? x : y)[2 * i % V] = p[i];
+      (2 * i + 1 < V ? x : y)[(2 * i + 1) % V] = q[i];
+    } else {
+      x[i] = p[i];
+      y[i] = q[i];
+    }
+  }
+}
+
+// V consecutive floats of shared memory, aligned to them.
+template <int V>
+__device__ __forceinline__ void load_floats(const float* p, float* x) {
+  if constexpr (V >= 4) {
+#pragma unroll
+    for (int i = 0; i < V; i += 4) {
+      const float4 y = *reinterpret_cast<const float4*>(p + i);
+      x[i] = y.x;
+      x[i + 1] = y.y;
+      x[i + 2] = y.z;
+      x[i + 3] = y.w;
+    }
+  } else if constexpr (V == 2) {
+    const float2 y = *reinterpret_cast<const float2*>(p);
+    x[0] = y.x;
+    x[1] = y.y;
+  } else {
+    x[0] = p[0];
   }
 }
 
@@ -120,187 +191,300 @@ __device__ __forceinline__ void speeds(const Rope& r, uint64_t* s_turns) {
   for (int i = threadIdx.x; i < r.half; i += kThreads) s_turns[i] = rope_turns(r.inv_freq[i]);
 }
 
-// The turned rows lane, lane + lanes, ... of one token.  `row(r, &in, &out,
-// &scale)` says where row r lies and goes; a null `out` skips it.
-template <typename T, typename C, int V, bool SCALED, int ROWS, typename Row>
-__device__ __forceinline__ void turn_rows(const Tiling& tl, const Rope& rope, const float2* cs_of, int vec0, int lane,
-                                          int rows, Row row) {
-  for (int vec = vec0; vec < tl.nv; vec += tl.nvt) {
-    const int turned = tl.half / V;
-    const bool pass = vec >= turned;
-    float2 cs[V];
-    int at0, at1;
-    if (pass) {
-      at0 = at1 = 2 * tl.half + (vec - turned) * V;
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) cs[i] = cs_of[vec * V + i];
-      at0 = rope.interleaved ? 2 * vec * V : vec * V;
-      at1 = rope.interleaved ? at0 + V : at0 + tl.half;
+// BYTES (4, 8 or 16) from global to shared memory, not waited for.
+template <int BYTES>
+__device__ __forceinline__ void copy_ahead(uint32_t to, const void* from) {
+  if (BYTES == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(BYTES) : "memory");
+}
+
+// A part of a token's row, as a thread notes it for the lanes.
+constexpr int kThere = 1, kTurned = 2, kCached = 4;  // kCached: goes to the cache, in its type
+struct Note {
+  const void* in;
+  void* out;
+  int kind;    // 0: nothing to do
+  int angles;  // where its token's angles are
+  float scale;
+  int part;
+};
+
+// A block's run of tokens.  The job says how many rows a token has (`rows`) and
+// what row r of token tok is (`note`); `locate` looks up a chunk of tokens, a
+// thread each, and gives a token's position.
+template <typename T, typename C, int V, bool SCALED, typename Job>
+__device__ __forceinline__ void run_rows(Job& job, const Rope& rope, const Tiling& tl, int D, int64_t tokens) {
+  extern __shared__ __align__(16) char smem[];  // slots, notes of three stages, angles, speeds
+  __shared__ int64_t s_pos[kChunk];
+  constexpr int kBytes = V * (int)sizeof(T);
+  constexpr bool kSlots = kBytes >= 4;  // smaller vectors are loaded when they are turned
+  using Vec = Pack<T, V>;
+  Vec* slots = reinterpret_cast<Vec*>(smem);
+  Note* notes = reinterpret_cast<Note*>(smem + (kSlots ? 8 * kItems * kThreads * kBytes : 0));
+  float* s_cos = reinterpret_cast<float*>(notes + 3 * tl.stage);
+  float* s_sin = s_cos + tl.held * tl.half;
+  uint64_t* s_turns = reinterpret_cast<uint64_t*>(s_sin + tl.held * tl.half);
+  speeds(rope, s_turns);
+
+  const int64_t first = tokens * blockIdx.x / gridDim.x, last = tokens * (blockIdx.x + 1) / gridDim.x;
+  const int vec0 = threadIdx.x % tl.wide, lane = threadIdx.x / tl.wide;
+  const int rows = job.rows * tl.parts, turned_places = tl.half / V;
+  const bool works = lane < tl.lanes;
+  // The components of this lane's places in a row, two vectors each (`n` of them
+  // there): of a row that turns and of one that passes whole, in the row's first
+  // part.  Rows of several parts are rare and work theirs out.
+  struct Place {
+    int at0, at1, n;
+    bool turned;
+  };
+  auto place_of = [&](bool turns, int part, int sub) {
+    int vec = vec0 + (2 * part + sub) * tl.wide;
+    Place p;
+    p.turned = turns && vec < turned_places;
+    // neighbouring lanes have neighbouring vectors, of the first and of the second
+    // half of what turns or passes
+    int from = 0, to = D;
+    if (p.turned) {
+      to = 2 * tl.half;
+    } else if (turns) {
+      from = 2 * tl.half;
+      vec -= turned_places;
     }
-    for (int r0 = lane; r0 < rows; r0 += ROWS * tl.lanes) {
-      Pack<T, V> a[ROWS], b[ROWS];
-      const T* in[ROWS];
-      C* out[ROWS];
-      float scale[ROWS];
-#pragma unroll
-      for (int i = 0; i < ROWS; ++i) {
-        const int r = r0 + i * tl.lanes;
-        in[i] = nullptr;
-        out[i] = nullptr;
-        scale[i] = 1.0f;
-        if (r < rows) row(r, &in[i], &out[i], &scale[i]);
-        if (out[i]) {
-          a[i] = load<T, V>(in[i], at0);
-          if (!pass) b[i] = load<T, V>(in[i], at1);
+    const int apart = (to - from + 2 * V - 1) / (2 * V);
+    p.at0 = vec < apart ? from + vec * V : D;
+    p.at1 = p.at0 + apart * V;
+    if (V == 1 && p.turned && rope.interleaved) {  // a pair is not to be parted
+      p.at0 = 2 * vec;
+      p.at1 = p.at0 + 1;
+    }
+    p.n = !works || p.at0 >= D ? 0 : p.at1 < to ? 2 : 1;
+    return p;
+  };
+  const Place turning[2] = {place_of(true, 0, 0), place_of(true, 0, 1)};
+  const Place passing[2] = {place_of(false, 0, 0), place_of(false, 0, 1)};
+  auto place = [&](int kind, int part, int sub) {
+    if (tl.parts > 1 && part) return place_of(kind & kTurned, part, sub);
+    return kind & kTurned ? turning[sub] : passing[sub];
+  };
+
+  for (int64_t c = first; c < last; c += kChunk) {
+    const int n = (int)min((int64_t)kChunk, last - c);
+    const int line = n * rows, stages = (line + tl.stage - 1) / tl.stage;
+    __syncthreads();  // the chunk before is done with
+    if (threadIdx.x < n) s_pos[threadIdx.x] = job.locate(c + threadIdx.x);
+    __syncthreads();
+    int known = 0, known_at = 0;  // tokens whose angles have been computed, where the next one's go
+    for (int s = -2; s < stages; ++s) {
+      if (s + 2 < stages) {  // notes of the stage after next
+        Note* to = notes + (s + 2) % 3 * tl.stage;
+        const int j = threadIdx.x;
+        if (j < tl.stage) {
+          const int f = (s + 2) * tl.stage + j, tok = tl.rows_of.of(f);
+          Note x{};
+          if (f < line) {
+            const int rp = f - tok * rows, r = tl.parts == 1 ? rp : rp / tl.parts;
+            x = job.note(r, c + tok, tok);
+            x.part = rp - r * tl.parts;
+            x.angles = tok % tl.held * tl.half;
+          }
+          to[j] = x;
         }
       }
-#pragma unroll
-      for (int i = 0; i < ROWS; ++i) {
-        if (!out[i]) continue;
-        float x[V], y[V];
-        if (pass) {
-#pragma unroll
-          for (int j = 0; j < V; ++j) x[j] = a[i][j];
-        } else {
-          turn<T, V>(a[i], b[i], cs, rope.interleaved, x, y);
+      if (s >= -1 && s + 1 < stages) {
+        // angles of the next stage's tokens
+        const int upto = min(n, tl.rows_of.of((s + 2) * tl.stage + rows - 1));
+        for (int i = threadIdx.x; i < (upto - known) * tl.half; i += kThreads) {
+          const int k = tl.half_of.of(i), p = i - k * tl.half;
+          const int at = (known_at + k >= tl.held ? known_at + k - tl.held : known_at + k) * tl.half + p;
+          rope_unit(s_turns[p], s_pos[known + k], rope, s_cos + at, s_sin + at);
         }
-        if (SCALED) {
+        known_at += upto - known;
+        if (known_at >= tl.held) known_at -= tl.held;
+        known = upto;
+        // and its copies
+        if (kSlots && works) {
+          const Note* of = notes + (s + 1) % 3 * tl.stage;
+          Vec* to = slots + (s + 1) % 2 * (kItems * 4 * kThreads) + threadIdx.x;
 #pragma unroll
-          for (int j = 0; j < V; ++j) {
-            x[j] = __fdiv_rn(x[j], scale[i]);
-            if (!pass) y[j] = __fdiv_rn(y[j], scale[i]);
+          for (int k = 0; k < kItems; ++k) {
+            const int j = lane + k * tl.lanes;
+            const int kind = j < tl.stage ? of[j].kind : 0;
+            if (!kind) continue;
+            const T* in = (const T*)of[j].in;
+#pragma unroll
+            for (int sub = 0; sub < 2; ++sub) {
+              const Place p = place(kind, of[j].part, sub);
+              const uint32_t at = smem_addr(to + (2 * k + sub) * 2 * kThreads);
+              if (p.n > 0) copy_ahead<kSlots ? kBytes : 4>(at, in + p.at0);
+              if (p.n > 1) copy_ahead<kSlots ? kBytes : 4>(at + kThreads * kBytes, in + p.at1);
+            }
           }
         }
-        store<C, V>(out[i], at0, x);
-        if (!pass) store<C, V>(out[i], at1, y);
       }
+      if (kSlots) asm volatile("cp.async.commit_group;" ::: "memory");
+      if (s >= 0 && works) {
+        if (kSlots) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        const Note* of = notes + s % 3 * tl.stage;
+        const Vec* from = slots + s % 2 * (kItems * 4 * kThreads) + threadIdx.x;
+#pragma unroll
+        for (int k = 0; k < kItems; ++k) {
+          const int j = lane + k * tl.lanes;
+          const int kind = j < tl.stage ? of[j].kind : 0;
+          if (!kind) continue;
+          const Note x = of[j];
+#pragma unroll
+          for (int sub = 0; sub < 2; ++sub) {
+            const Place p = place(kind, x.part, sub);
+            if (p.n == 0) continue;
+            Vec a{}, b{};
+            if (kSlots) {
+              a = from[(2 * k + sub) * 2 * kThreads];
+              b = from[((2 * k + sub) * 2 + 1) * kThreads];
+            } else {
+              a = load<T, V>((const T*)x.in, p.at0);
+              if (p.n > 1) b = load<T, V>((const T*)x.in, p.at1);
+            }
+            float u[V], w[V];
+            if (p.turned) {
+              float co[V], si[V];
+              if (rope.interleaved) {
+                constexpr int H = V > 1 ? V / 2 : 1;  // pairs of a vector
+                const int at = x.angles + p.at0 / 2, bt = x.angles + p.at1 / 2;
+                load_floats<H>(s_cos + at, co);
+                load_floats<H>(s_sin + at, si);
+                load_floats<H>(s_cos + bt, co + V - H);
+                load_floats<H>(s_sin + bt, si + V - H);
+                turn<T, V, true>(a, b, co, si, u, w);
+              } else {
+                load_floats<V>(s_cos + x.angles + p.at0, co);
+                load_floats<V>(s_sin + x.angles + p.at0, si);
+                turn<T, V, false>(a, b, co, si, u, w);
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < V; ++i) {
+                u[i] = a[i];
+                w[i] = p.n > 1 ? b[i] : 0.0f;
+              }
+            }
+            if (!(kind & kCached)) {
+              store<T, V>((T*)x.out, p.at0, u);
+              if (p.n > 1) store<T, V>((T*)x.out, p.at1, w);
+            } else {
+              if (SCALED) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                  u[i] = __fdiv_rn(u[i], x.scale);
+                  w[i] = __fdiv_rn(w[i], x.scale);
+                }
+              }
+              store<C, V>((C*)x.out, p.at0, u);
+              if (p.n > 1) store<C, V>((C*)x.out, p.at1, w);
+            }
+          }
+        }
+      }
+      __syncthreads();
     }
   }
 }
+
+template <typename T>
+struct RotaryJob {
+  const RotaryArgs& a;
+  int rows;
+  __device__ int64_t locate(int64_t tok) const {
+    const int64_t b = a.B == 1 ? 0 : tok / a.T;
+    return a.pos[b * a.pos_stride + (tok - b * a.T)];
+  }
+  __device__ Note note(int r, int64_t tok, int) const {
+    const int64_t b = a.B == 1 ? 0 : tok / a.T, t = tok - b * a.T;
+    int i = 0;
+    while (r >= a.set[i].heads) r -= a.set[i++].heads;
+    const RowSet& x = a.set[i];
+    return Note{(const T*)x.in + b * x.in_b + t * x.in_t + r * x.in_h,
+                (T*)x.out + b * x.out_b + t * x.out_t + r * x.out_h, kThere | kTurned, 0, 1.0f, 0};
+  }
+};
 
 template <typename T, int V>
-__global__ void __launch_bounds__(kThreads, 2) k_rotary(RotaryArgs a, Tiling tl, int rows) {
-  extern __shared__ __align__(16) uint64_t s_turns[];  // [half], then the groups' (cos, sin), two of them
-  float2* s_cs = (float2*)(s_turns + tl.half);
-  speeds(a.rope, s_turns);
-  const int vec = threadIdx.x % tl.nvt, lane = threadIdx.x / tl.nvt % tl.lanes;
-  const int mine = threadIdx.x / tl.nvt / tl.lanes;
-  const int64_t tokens = a.B * a.T;
-  int flip = 0;
-  __syncthreads();
-  for (int64_t g = (int64_t)blockIdx.x * tl.group; g < tokens; g += (int64_t)gridDim.x * tl.group, flip ^= 1) {
-    float2* cs = s_cs + flip * tl.group * tl.half;  // the other one may still be read
-    for (int i = threadIdx.x; i < tl.group * tl.half; i += kThreads) {
-      const int64_t tok = g + i / tl.half;
-      if (tok >= tokens) break;
-      const int64_t b = a.B == 1 ? 0 : tok / a.T;
-      rope_unit(s_turns[i % tl.half], a.pos[b * a.pos_stride + (tok - b * a.T)], a.rope, &cs[i].x, &cs[i].y);
-    }
-    __syncthreads();
-    const int64_t tok = g + mine;
-    if (mine >= tl.group || tok >= tokens) continue;
-    const int64_t b = a.B == 1 ? 0 : tok / a.T, t = tok - b * a.T;
-    turn_rows<T, T, V, false, kRows>(tl, a.rope, cs + mine * tl.half, vec, lane, rows, [&](int r, const T** in, T** out, float*) {
-      int n = 0;
-      while (r >= a.set[n].heads) r -= a.set[n++].heads;
-      const RowSet& x = a.set[n];
-      *in = (const T*)x.in + b * x.in_b + t * x.in_t + r * x.in_h;
-      *out = (T*)x.out + b * x.out_b + t * x.out_t + r * x.out_h;
-    });
-  }
+__global__ void __launch_bounds__(kThreads, kBlocks) k_rotary(RotaryArgs a, Tiling tl, int rows) {
+  RotaryJob<T> job{a, rows};
+  run_rows<T, T, V, false>(job, a.rope, tl, a.D, a.B * a.T);
 }
 
-// The sequence that row t belongs to: how many of starts[1..B] are <= t.  A
-// warp's lanes look at 32 places at a time: two rounds for 1024 sequences.
-__device__ __forceinline__ int sequence_of(const int32_t* starts, int B, int64_t t, int lane) {
-  int lo = 0, n = B;
+// The sequence that row t belongs to: how many of starts[1..B] are <= t.
+__device__ __forceinline__ int sequence_of(const int32_t* starts, int B, int64_t t) {
+  int lo = 0, n = B;  // the first lo are, those from lo + n on are not
   while (n > 0) {
-    const int step = (n + 31) / 32, at = lo + (lane + 1) * step - 1;
-    const bool before = at < lo + n && starts[1 + at] <= t;
-    const int k = __popc(__ballot_sync(~0u, before));  // ascending: the first k lanes
-    const int left = lo + n;
-    lo += k * step;
-    n = min(step - 1, left - lo);  // all places up to lo are <= t, the next probed one is not
+    const int h = n / 2;
+    if (starts[1 + lo + h] <= t) {
+      lo += h + 1;
+      n -= h + 1;
+    } else {
+      n = h;
+    }
   }
   return lo;
 }
 
+// Rows of a token: its queries, keys and values.
+template <typename T, typename C>
+struct AppendJob {
+  const AppendArgs& a;
+  int rows;
+  int64_t* s_row;  // [kChunk]: a token's row of the cache; -1 none, -2 it is padding
+  __device__ int64_t locate(int64_t t) const {
+    const Cache& ch = a.cache;
+    const int b = a.starts ? sequence_of(a.starts, a.B, t) : (int)t;
+    int64_t row = -2, pos = 0;
+    if (b < a.B) {
+      const int len = a.lens[b];
+      const int64_t slot = (int64_t)len + (a.starts ? t - a.starts[b] : 0);
+      pos = a.pos ? a.pos[t] : slot;
+      int page = -1;
+      if (len >= 0 && slot >= 0 && slot < ch.capacity)
+        page = ch.table[b * ch.table_stride + (uint32_t)slot / (uint32_t)ch.page_size];
+      row = -1;
+      if (page >= 0 && page < ch.pages)
+        row = page * ch.page_stride + (int64_t)((uint32_t)slot % (uint32_t)ch.page_size) * ch.slot_stride;
+      else if (a.status)
+        set_status(a.status, CP_EINVAL);
+    }
+    s_row[threadIdx.x] = row;
+    return pos;
+  }
+  __device__ Note note(int r, int64_t t, int i) const {
+    const Cache& ch = a.cache;
+    const int64_t row = s_row[i];
+    if (r < a.q.heads) {
+      if (row == -2) return Note{};
+      return Note{(const T*)a.q.in + t * a.q.in_t + r * a.q.in_h, (T*)a.q.out + t * a.q.out_t + r * a.q.out_h,
+                  kThere | kTurned, 0, 1.0f, 0};
+    }
+    if (row < 0) return Note{};
+    r -= a.q.heads;
+    if (r < ch.heads)
+      return Note{(const T*)a.k + t * a.k_t + r * a.k_h, (C*)ch.k + row + r * ch.head_stride,
+                  kThere | kTurned | kCached, 0, ch.k_scale ? ch.k_scale[r] : 1.0f, 0};
+    r -= ch.heads;
+    return Note{(const T*)a.v + t * a.v_t + r * a.v_h, (C*)ch.v + row + r * ch.head_stride,
+                kThere | kCached, 0, ch.v_scale ? ch.v_scale[r] : 1.0f, 0};
+  }
+};
+
 template <typename T, typename C, int V, bool SCALED>
-__global__ void __launch_bounds__(kThreads, 2) k_cache_append(AppendArgs a, Tiling tl, int vecs) {
-  extern __shared__ __align__(16) uint64_t s_turns[];
-  __shared__ int64_t s_row[2][kGroup], s_pos[2][kGroup];  // a group's rows of the cache (-1: none) and positions
-  __shared__ int s_seq[2][kGroup];
-  const Cache& ch = a.cache;
-  float2* s_cs = (float2*)(s_turns + tl.half);
-  speeds(a.rope, s_turns);
+__global__ void __launch_bounds__(kThreads, kBlocks) k_cache_append(AppendArgs a, Tiling tl) {
+  __shared__ int64_t s_row[kChunk];
   if (a.new_lens)
     for (int64_t b = (int64_t)blockIdx.x * kThreads + threadIdx.x; b < a.B; b += (int64_t)gridDim.x * kThreads) {
       const int64_t n = (int64_t)a.lens[b] + (a.starts ? a.starts[b + 1] - a.starts[b] : 1);
-      a.new_lens[b] = (int32_t)min(n, (int64_t)ch.capacity);
+      a.new_lens[b] = (int32_t)min(n, (int64_t)a.cache.capacity);
     }
-  const int vec = threadIdx.x % tl.nvt, lane = threadIdx.x / tl.nvt % tl.lanes;
-  const int mine = threadIdx.x / tl.nvt / tl.lanes;
-  const int wlane = threadIdx.x % 32;
-  int flip = 0;
-  for (int64_t g = (int64_t)blockIdx.x * tl.group; g < a.T; g += (int64_t)gridDim.x * tl.group, flip ^= 1) {
-    // where the group's tokens go, a warp a token
-    for (int i = threadIdx.x / 32; i < tl.group && g + i < a.T; i += kThreads / 32) {
-      const int64_t t = g + i;
-      const int b = a.starts ? sequence_of(a.starts, a.B, t, wlane) : (int)t;
-      if (wlane == 0) {
-        int64_t row = -1, pos = 0;
-        if (b < a.B) {
-          const int len = a.lens[b];
-          const int64_t slot = (int64_t)len + (a.starts ? t - a.starts[b] : 0);
-          int page = -1;
-          if (len >= 0 && slot >= 0 && slot < ch.capacity) page = ch.table[b * ch.table_stride + (uint32_t)slot / (uint32_t)ch.page_size];
-          if (page >= 0 && page < ch.pages)
-            row = page * ch.page_stride + (int64_t)((uint32_t)slot % (uint32_t)ch.page_size) * ch.slot_stride;
-          else if (a.status)
-            set_status(a.status, CP_EINVAL);
-          pos = a.pos ? a.pos[t] : slot;
-        }
-        s_row[flip][i] = row;
-        s_pos[flip][i] = pos;
-        s_seq[flip][i] = b;
-      }
-    }
-    __syncthreads();
-    float2* cs = s_cs + flip * tl.group * tl.half;
-    for (int i = threadIdx.x; i < tl.group * tl.half; i += kThreads) {
-      if (g + i / tl.half >= a.T) break;
-      rope_unit(s_turns[i % tl.half], s_pos[flip][i / tl.half], a.rope, &cs[i].x, &cs[i].y);
-    }
-    __syncthreads();
-    const int64_t t = g + mine;
-    if (mine >= tl.group || t >= a.T || s_seq[flip][mine] >= a.B) continue;
-    const int64_t row = s_row[flip][mine];
-    if (a.q.heads)
-      turn_rows<T, T, V, false, kRows>(tl, a.rope, cs + mine * tl.half, vec, lane, a.q.heads,
-                                [&](int r, const T** in, T** out, float*) {
-                                  *in = (const T*)a.q.in + t * a.q.in_t + r * a.q.in_h;
-                                  *out = (T*)a.q.out + t * a.q.out_t + r * a.q.out_h;
-                                });
-    if (row < 0) continue;
-    turn_rows<T, C, V, SCALED, 1>(tl, a.rope, cs + mine * tl.half, vec, lane, ch.heads,
-                               [&](int r, const T** in, C** out, float* scale) {
-                                 *in = (const T*)a.k + t * a.k_t + r * a.k_h;
-                                 *out = (C*)ch.k + row + r * ch.head_stride;
-                                 if (SCALED && ch.k_scale) *scale = ch.k_scale[r];
-                               });
-    // values as they are
-    for (int r = lane; r < ch.heads; r += tl.lanes) {
-      const float scale = SCALED && ch.v_scale ? ch.v_scale[r] : 1.0f;
-      for (int i = vec; i < vecs; i += tl.nvt) {
-        const Pack<T, V> p = load<T, V>((const T*)a.v + t * a.v_t + r * a.v_h, i * V);
-        float x[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) x[j] = SCALED ? __fdiv_rn(p[j], scale) : p[j];
-        store<C, V>((C*)ch.v + row + r * ch.head_stride, i * V, x);
-      }
-    }
-  }
+  AppendJob<T, C> job{a, a.q.heads + 2 * a.cache.heads, s_row};
+  run_rows<T, C, V, SCALED>(job, a.rope, tl, a.cache.D, a.T);
 }
 
 // Whether every row of a tensor starts on a multiple of V elements.
@@ -315,44 +499,64 @@ static bool fits(const RowSet& r, int V, size_t e) {
   return fits(r.in, s, 3, V, e) && fits(r.out, s + 3, 3, V, e);
 }
 
-// Threads to places, rows and tokens.  `rows` of a token run on as many lanes as
-// leave each thread kRows of them, fewer tokens than blocks can be had are taken
-// one at a time.
-static Tiling tiling(int half, int D, int V, int rows, int64_t tokens, int sms) {
+static Divisor divisor(int d) {
+  if (d < 1) d = 1;
+  uint32_t l = 0;
+  while (((int64_t)1 << l) < d) ++l;
+  return Divisor{(uint32_t)d, (uint32_t)((((uint64_t)1 << (31 + l)) + d - 1) / d), l};
+}
+static Tiling tiling(int half, int D, int V, int rows) {
   Tiling t;
   t.half = half;
-  t.nv = half / V + (D - 2 * half) / V;
-  t.nvt = t.nv < kThreads ? t.nv : kThreads;
-  const int most = kThreads / t.nvt;
-  const bool few = tokens < 4 * sms;
-  t.lanes = few ? rows : (rows + kRows - 1) / kRows;
-  if (t.lanes > most) t.lanes = most;
-  if (t.lanes < 1) t.lanes = 1;
-  t.group = few ? 1 : most / t.lanes;
-  if (t.group > kGroup) t.group = kGroup;
-  // the angles of two groups within 32 KB
-  while (t.group > 1 && 16 * t.group * half > 32 * 1024) --t.group;
+  t.places = half / V + (D - 2 * half + 2 * V - 1) / (2 * V);
+  t.wide = (t.places + 1) / 2 < kThreads ? (t.places + 1) / 2 : kThreads;
+  t.parts = (t.places + 2 * t.wide - 1) / (2 * t.wide);
+  t.lanes = kThreads / t.wide;
+  rows *= t.parts;
+  t.stage = kItems * t.lanes < kThreads ? kItems * t.lanes : kThreads;  // a thread notes one row
+  // angles of two stages within 40 KB, if a stage has to be shorter for it: heads
+  // of few rows and tokens of wide rotations
+  if (half > 0) {
+    const int64_t most = ((40 * 1024 / (8 * half) - 2) / 2) * (int64_t)rows;
+    if (t.stage > most) t.stage = most < 1 ? 1 : (int)most;
+  }
+  t.held = (2 * t.stage + rows - 1) / rows + 1;
+  t.rows_of = divisor(rows);
+  t.half_of = divisor(half);
   return t;
 }
-static size_t smem_of(const Tiling& t) { return (size_t)t.half * (8 + 2 * 8 * (size_t)t.group); }
-static unsigned grid_of(const Tiling& t, int64_t tokens, int sms) {
-  int64_t g = (tokens + t.group - 1) / t.group, most = 2 * (int64_t)sms;
-  if (g > most) g = most;
-  return (unsigned)(g < 1 ? 1 : g);
+static size_t smem_of(const Tiling& t, int bytes) {
+  return (bytes >= 4 ? 8 * kItems * kThreads * (size_t)bytes : 0) + 3 * (size_t)t.stage * sizeof(Note) +
+         (size_t)t.half * (8 + 8 * (size_t)t.held);
+}
+static unsigned grid_of(int64_t tokens, int sms) {
+  const int64_t most = kBlocks * (int64_t)sms;
+  return (unsigned)(tokens < 1 ? 1 : tokens < most ? tokens : most);
 }
 
 template <typename T, int V>
 static int rotary(const RotaryArgs& a, int rows, cudaStream_t s) {
+  static std::atomic<uint64_t> allowed{0};
   DeviceInfo di;
   CP_TRY_STATUS(device_info(&di));
-  const Tiling t = tiling(a.rope.half, a.D, V, rows, a.B * a.T, di.sm_count);
-  CP_TRY_STATUS(allow_smem((const void*)k_rotary<T, V>, smem_of(t), "rotary: shared memory"));
-  k_rotary<T, V><<<grid_of(t, a.B * a.T, di.sm_count), kThreads, smem_of(t), s>>>(a, t, rows);
+  const unsigned grid = grid_of(a.B * a.T, di.sm_count);
+  const Tiling t = tiling(a.rope.half, a.D, V, rows);
+  const size_t smem = smem_of(t, V * sizeof(T));
+  CP_TRY_STATUS(allow_smem_once((const void*)k_rotary<T, V>, kMostSmem, "rotary: shared memory", &allowed));
+  k_rotary<T, V><<<grid, kThreads, smem, s>>>(a, t, rows);
   return launch_status("rotary");
 }
 
 int launch_rotary(const RotaryArgs& args, int dtype, cudaStream_t s) {
   RotaryArgs a = args;
+  // a batch whose entries follow one another like tokens is one long entry
+  bool one = a.pos_stride == a.T;
+  for (int i = 0; i < a.n; ++i)
+    one = one && (!a.set[i].heads || (a.set[i].in_b == a.T * a.set[i].in_t && a.set[i].out_b == a.T * a.set[i].out_t));
+  if (one) {
+    a.T *= a.B;
+    a.B = 1;
+  }
   int rows = 0, n = 0;
   for (int i = 0; i < args.n; ++i)
     if (args.set[i].heads) {
@@ -379,13 +583,14 @@ int launch_rotary(const RotaryArgs& args, int dtype, cudaStream_t s) {
 
 template <typename T, typename C, int V, bool SCALED>
 static int append(const AppendArgs& a, cudaStream_t s) {
+  static std::atomic<uint64_t> allowed{0};
   DeviceInfo di;
   CP_TRY_STATUS(device_info(&di));
-  const int rows = a.q.heads > a.cache.heads ? a.q.heads : a.cache.heads;
-  const Tiling t = tiling(a.rope.half, a.cache.D, V, rows, a.T, di.sm_count);
+  const unsigned grid = grid_of(a.T, di.sm_count);
+  const Tiling t = tiling(a.rope.half, a.cache.D, V, a.q.heads + 2 * a.cache.heads);
   auto kernel = k_cache_append<T, C, V, SCALED>;
-  CP_TRY_STATUS(allow_smem((const void*)kernel, smem_of(t), "cache append: shared memory"));
-  kernel<<<grid_of(t, a.T, di.sm_count), kThreads, smem_of(t), s>>>(a, t, a.cache.D / V);
+  CP_TRY_STATUS(allow_smem_once((const void*)kernel, kMostSmem, "cache append: shared memory", &allowed));
+  kernel<<<grid, kThreads, smem_of(t, V * sizeof(T)), s>>>(a, t);
   return launch_status("cache append");
 }
 template <typename T, typename C, int V>
