@@ -434,7 +434,10 @@ int coverprune_rotary(const cp_rows* rows, int n, int dtype, int64_t B, int64_t 
  * elements from k (and its value equally from v); D contiguous elements.
  *   dtype       CP_BF16, CP_F32 or CP_E4M3
  *   k, v        device, 16-byte aligned; the strides and D are multiples of 16
- *               bytes, D <= 256; strides of both are the same
+ *               bytes, D <= 256; strides of both are the same and not negative.
+ *               Attention needs the pages to span at most 2^32 times the largest
+ *               power of two that divides the page and slot strides (64 GB at
+ *               least).
  *   pages       pages k and v hold (a table entry outside 0..pages - 1 is a bad
  *               page: see below)
  *   k_scale, v_scale  device float32 [heads] or NULL (1): the value of a

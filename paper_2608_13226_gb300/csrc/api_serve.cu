@@ -41,7 +41,7 @@ static int cache_of(const cp_cache* c, bool with_memory, Cache* out) {
   if (!c || c->struct_size != sizeof(cp_cache)) return CP_EINVAL;
   if (c->dtype != CP_F32 && c->dtype != CP_BF16 && c->dtype != CP_E4M3) return CP_EINVAL;
   if (c->heads < 1 || c->heads > 65536 || c->D < 1 || c->page_size < 1 || c->pages < 0 ||
-      c->table_width < 0)
+      c->table_width < 0 || c->page_stride < 0 || c->slot_stride < 0 || c->head_stride < 0)
     return CP_EINVAL;
   const int64_t e = (int64_t)size_of(c->dtype);
   if (c->page_size > kMaxSize || c->table_width > kMaxSize || c->pages > kMaxSize)

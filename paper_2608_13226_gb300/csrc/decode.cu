@@ -31,6 +31,11 @@ constexpr int kThreads = 32 * kWarps;
 constexpr int kUnit = 64;   // keys of a unit
 constexpr int kChunk = 64;  // keys whose marks a warp looks at together
 constexpr int kQueue = 128;
+// A running maximum follows the scores only when one is more than kSlack above it
+// (in units of log 2): weights up to 2^8 are as good as those up to 1, and most
+// tiles then need no maximum over their keys.
+constexpr float kSlack = 8.0f;
+constexpr float kLowest = -1e38f;  // a maximum before any score: finite, so that differences are
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -59,19 +64,31 @@ struct Shape {
   static_assert(kWarps * QT * DP * 4 <= ring, "the merge reuses the ring");
 };
 
-// What the blocks leave for the join: the part that begins in block i (a query
-// tile's first units) and over how many blocks it goes on.
+// What the blocks leave for the join: the block that a query tile of sequence b
+// begins in and over how many it goes on (0: it is whole, or there is none).
 struct Begin {
-  int b, col, blocks, pad;
+  int block, blocks, b, col;
 };
 
-// Where a chunk of a row lies: rows that are read together fall on other banks.
+// Rows of the cache in 32 bits: row r of page p starts (p * page + r * slot) << shift
+// bytes into K and V.
+struct Rows {
+  uint32_t page, slot;
+  uint32_t scale;  // 1 << shift
+  uint32_t mul, div_shift;  // key / page_size = key * mul >> 31 >> div_shift
+};
+
+// Where a chunk of a row lies, chunk c at c ^ swizzle(r): rows that are read
+// together fall on other banks.  Bits of r only, so that swizzle(r ^ s) is
+// swizzle(r) ^ swizzle(s).
 template <int CT, int CPR>
-__device__ __forceinline__ int swizzle(int r, int c) {
-  if (CT == CP_F32) return c ^ ((r & 1) << 2);
-  return CPR >= 8 ? c ^ (r & 7) : c ^ ((r >> 1) & 3);
+__host__ __device__ constexpr int swizzle(int r) {
+  return CT == CP_F32 ? (r & 1) << 2 : CPR >= 8 ? r & 7 : (r >> 1) & 3;
 }
 
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
   const int n = there ? 16 : 0;  // 0: nothing is read, zeros are written
   asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n)
@@ -106,11 +123,12 @@ __device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// Two 8-bit elements as two float16 (exact), from the low or the high half.
-__device__ __forceinline__ uint32_t e4m3_f16x2(uint32_t x) {
-  uint32_t y;
-  asm("{\n\t.reg .b16 l;\n\tcvt.u16.u32 l, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(y) : "r"(x));
-  return y;
+// Four 8-bit elements as two pairs of float16 (exact).
+__device__ __forceinline__ void e4m3_f16x2(uint32_t x, uint32_t* lo, uint32_t* hi) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+      : "=r"(*lo), "=r"(*hi)
+      : "r"(x));
 }
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -207,11 +225,18 @@ struct Math {
   float m[NT][2], l[NT][2];
   float sc[NT][2];  // score = sc * product, in units of log 2
   int g, t;
+  uint32_t k_at, v_at;  // this lane's rows in a tile's K and V, first chunk: chunk c is ^ 16 c
 
   __device__ __forceinline__ void start(const DecodeArgs& a, int b, int hk, int h0, int nq, char*,
                                         int, int lane) {
     g = lane / 4;
     t = lane % 4;
+    {
+      const int r = lane % 16, key = CT == CP_BF16 ? lane % 8 + lane / 16 * 8 : r;
+      const int kc = lane / 16, vc = CT == CP_BF16 ? lane / 8 % 2 : kc;
+      k_at = r * S::row + 16 * (kc ^ swizzle<CT, S::cpr>(r));
+      v_at = key * S::row + 16 * (vc ^ swizzle<CT, S::cpr>(key));
+    }
     const int D = a.cache.D;
     const float scale = a.scale * (a.cache.k_scale ? a.cache.k_scale[hk] : 1.0f) * kLog2e;
 #pragma unroll
@@ -259,7 +284,7 @@ struct Math {
           const int ex = (int)__shfl_sync(~0u, back, 4 * (2 * t + i));
           sc[n][i] = ldexpf(ldexpf(scale, ex / 2), ex - ex / 2);
         }
-        m[n][i] = -INFINITY;
+        m[n][i] = kLowest;
         l[n][i] = 0.0f;
       }
 #pragma unroll
@@ -269,16 +294,15 @@ struct Math {
     }
   }
 
-  __device__ __forceinline__ void tile(uint32_t at, uint32_t valid, char*, int, int lane) {
+  __device__ __forceinline__ void tile(uint32_t at, uint32_t valid, char*, int, int) {
     float s[NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
-    const int r = lane % 16, half = lane / 16;
     if (CT == CP_BF16) {
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         uint32_t x[4];
-        ldmatrix4(x, at + r * S::row + 16 * swizzle<CT, S::cpr>(r, 2 * k + half));
+        ldmatrix4(x, (at + k_at) ^ (32 * k));
 #pragma unroll
         for (int n = 0; n < NT; ++n) mma_bf16_16816(s[n], x[0], x[1], x[2], x[3], q[n][k][0], q[n][k][1]);
       }
@@ -286,61 +310,73 @@ struct Math {
 #pragma unroll
       for (int k = 0; k < KS; k += 2) {
         uint32_t x[4];
-        ldmatrix4(x, at + r * S::row + 16 * swizzle<CT, S::cpr>(r, k + half));
+        ldmatrix4(x, (at + k_at) ^ (16 * k));
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const uint32_t u = x[2 * j], w = x[2 * j + 1];
-          const uint32_t a0 = e4m3_f16x2(u), a1 = e4m3_f16x2(w), a2 = e4m3_f16x2(u >> 16), a3 = e4m3_f16x2(w >> 16);
+          uint32_t a0, a1, a2, a3;
+          e4m3_f16x2(x[2 * j], &a0, &a2);
+          e4m3_f16x2(x[2 * j + 1], &a1, &a3);
 #pragma unroll
           for (int n = 0; n < NT; ++n) mma_f16_16816(s[n], a0, a1, a2, a3, q[n][k + j][0], q[n][k + j][1]);
         }
       }
     }
-    const bool v0 = valid >> g & 1, v1 = valid >> (g + 8) & 1;
+    const bool full = valid == (1u << S::tk) - 1;
+    if (!full) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)  // scores are multiplied by sc, of either sign, next
+          if (!(valid >> (g + 8 * (i / 2)) & 1)) s[n][i] = __int_as_float(0x7fffffff);
+    }
+    bool above = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)  // fmaxf passes over the NaN of a key that is not there
+        above |= fmaxf(s[n][i] * sc[n][i], s[n][i + 2] * sc[n][i]) > m[n][i] + kSlack;
+    if (__any_sync(~0u, above)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float top = fmaxf(fmaxf(s[n][i] * sc[n][i], s[n][i + 2] * sc[n][i]), m[n][i]);
+#pragma unroll
+          for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+          const float f = exp2_fast(m[n][i] - top);
+          m[n][i] = top;
+          l[n][i] *= f;
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            o[n][k][i] *= f;
+            o[n][k][i + 2] *= f;
+          }
+        }
+    }
     uint32_t p[NT][2];
-    bool moved = false;
-    float f[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       float x[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = (i < 2 ? v0 : v1) ? s[n][i] * sc[n][i & 1] : -INFINITY;
+      for (int i = 0; i < 4; ++i) x[i] = exp2_fast(fmaf(s[n][i], sc[n][i & 1], -m[n][i & 1]));
+      if (!full) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        float top = fmaxf(x[i], x[i + 2]);
-#pragma unroll
-        for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-        top = fmaxf(top, m[n][i]);
-        const float base = top == -INFINITY ? 0.0f : top;
-        f[n][i] = exp2_fast(m[n][i] - base);
-        moved |= top != m[n][i];
-        m[n][i] = top;
-        x[i] = v0 ? exp2_fast(fmaf(s[n][i], sc[n][i], -base)) : 0.0f;
-        x[i + 2] = v1 ? exp2_fast(fmaf(s[n][i + 2], sc[n][i], -base)) : 0.0f;
-        l[n][i] = l[n][i] * f[n][i] + (x[i] + x[i + 2]);
+        for (int i = 0; i < 4; ++i)
+          if (!(valid >> (g + 8 * (i / 2)) & 1)) x[i] = 0.0f;
       }
+      l[n][0] += x[0] + x[2];
+      l[n][1] += x[1] + x[3];
       // 8 (11) bits of each weight go on: under 2^-8 (2^-11) of the output, which
       // is rounded to bfloat16 itself; the sum l has all 24
-      const uint32_t lo = CT == CP_BF16 ? pack_bf16(x[0], x[1]) : pack_f16(x[0], x[1]);
-      const uint32_t hi = CT == CP_BF16 ? pack_bf16(x[2], x[3]) : pack_f16(x[2], x[3]);
-      p[n][0] = movmatrix_trans(lo);
-      p[n][1] = movmatrix_trans(hi);
-    }
-    if (__any_sync(~0u, moved)) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int k = 0; k < KS; ++k)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[n][k][i] *= f[n][i & 1];
+      p[n][0] = movmatrix_trans(CT == CP_BF16 ? pack_bf16(x[0], x[1]) : pack_f16(x[0], x[1]));
+      p[n][1] = movmatrix_trans(CT == CP_BF16 ? pack_bf16(x[2], x[3]) : pack_f16(x[2], x[3]));
     }
     at += S::tk * S::row;
     if (CT == CP_BF16) {
-      const int key = lane % 8 + (lane / 16) * 8, c = lane / 8 % 2;
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         uint32_t x[4];
-        ldmatrix4_trans(x, at + key * S::row + 16 * swizzle<CT, S::cpr>(key, 2 * k + c));
+        ldmatrix4_trans(x, (at + v_at) ^ (32 * k));
 #pragma unroll
         for (int n = 0; n < NT; ++n) mma_bf16_16816(o[n][k], x[0], x[1], x[2], x[3], p[n][0], p[n][1]);
       }
@@ -348,12 +384,13 @@ struct Math {
 #pragma unroll
       for (int k = 0; k < KS; k += 2) {
         uint32_t x[4];
-        ldmatrix4_trans(x, at + r * S::row + 16 * swizzle<CT, S::cpr>(r, k + half));
+        ldmatrix4_trans(x, (at + v_at) ^ (16 * k));
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           // bytes: key 2 t's components 2 g, 2 g + 1, then key 2 t + 1's
-          const uint32_t u = __byte_perm(x[2 * j], 0, 0x3120), w = __byte_perm(x[2 * j + 1], 0, 0x3120);
-          const uint32_t a0 = e4m3_f16x2(u), a1 = e4m3_f16x2(u >> 16), a2 = e4m3_f16x2(w), a3 = e4m3_f16x2(w >> 16);
+          uint32_t a0, a1, a2, a3;
+          e4m3_f16x2(__byte_perm(x[2 * j], 0, 0x3120), &a0, &a1);
+          e4m3_f16x2(__byte_perm(x[2 * j + 1], 0, 0x3120), &a2, &a3);
 #pragma unroll
           for (int n = 0; n < NT; ++n) mma_f16_16816(o[n][k + j], a0, a1, a2, a3, p[n][0], p[n][1]);
         }
@@ -411,7 +448,7 @@ struct Math<CP_F32, DP, QT> {
     sc = a.scale * (a.cache.k_scale ? a.cache.k_scale[hk] : 1.0f) * kLog2e;
 #pragma unroll
     for (int n = 0; n < QT; ++n) {
-      m[n] = -INFINITY;
+      m[n] = kLowest;
       l[n] = 0.0f;
 #pragma unroll
       for (int i = 0; i < V; ++i) o[n][i] = 0.0f;
@@ -437,7 +474,7 @@ struct Math<CP_F32, DP, QT> {
       float4 k;
       asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
                    : "=f"(k.x), "=f"(k.y), "=f"(k.z), "=f"(k.w)
-                   : "r"(at + r * S::row + 16 * swizzle<CP_F32, S::cpr>(r, c)));
+                   : "r"(at + r * S::row + 16 * (c ^ swizzle<CP_F32, S::cpr>(r))));
 #pragma unroll
       for (int n = 0; n < QT; ++n) {
         const float4 x = *(const float4*)(sq + n * DP + 4 * c);
@@ -445,21 +482,30 @@ struct Math<CP_F32, DP, QT> {
       }
     }
     const bool there = valid >> r & 1;
+    bool above = false;
 #pragma unroll
     for (int n = 0; n < QT; ++n) {
       s[n] += __shfl_xor_sync(~0u, s[n], 1);
       s[n] += __shfl_xor_sync(~0u, s[n], 2);
-      const float x = there ? s[n] * sc : -INFINITY;
-      float top = x;
+      above |= there && s[n] * sc > m[n] + kSlack;
+    }
+    if (__any_sync(~0u, above)) {
 #pragma unroll
-      for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-      top = fmaxf(top, m[n]);
-      const float base = top == -INFINITY ? 0.0f : top;
-      const float f = exp2f(m[n] - base), p = there ? exp2f(fmaf(s[n], sc, -base)) : 0.0f;
-      m[n] = top;
-      l[n] = l[n] * f + p;
+      for (int n = 0; n < QT; ++n) {
+        float top = there ? fmaxf(s[n] * sc, m[n]) : m[n];
 #pragma unroll
-      for (int i = 0; i < V; ++i) o[n][i] *= f;
+        for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+        const float f = exp2f(m[n] - top);
+        m[n] = top;
+        l[n] *= f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[n][i] *= f;
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < QT; ++n) {
+      const float p = there ? exp2f(fmaf(s[n], sc, -m[n])) : 0.0f;
+      l[n] += p;
       if (sub == 0) sp[r * QT + n] = p;
     }
     __syncwarp();
@@ -470,13 +516,13 @@ struct Math<CP_F32, DP, QT> {
       if (V == 2) {
         asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];"
                      : "=f"(v[0]), "=f"(v[V > 1 ? 1 : 0])
-                     : "r"(at + k * S::row + 16 * swizzle<CP_F32, S::cpr>(k, lane / 2) + 8 * (lane % 2)));
+                     : "r"(at + k * S::row + 16 * (lane / 2 ^ swizzle<CP_F32, S::cpr>(k)) + 8 * (lane % 2)));
       } else {
 #pragma unroll
         for (int j = 0; j < V / 4; ++j)
           asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
                        : "=f"(v[4 * j]), "=f"(v[4 * j + 1]), "=f"(v[4 * j + 2]), "=f"(v[4 * j + 3])
-                       : "r"(at + k * S::row + 16 * swizzle<CP_F32, S::cpr>(k, 32 * j + lane)));
+                       : "r"(at + k * S::row + 16 * (32 * j + lane ^ swizzle<CP_F32, S::cpr>(k))));
       }
 #pragma unroll
       for (int n = 0; n < QT; ++n) {
@@ -508,11 +554,11 @@ struct Math<CP_F32, DP, QT> {
 };
 
 template <int CT, int DP, int QT>
-__global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, int unit, int tiles, float* parts,
-                                                     Begin* begins) {
+__global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, int unit, int tiles, float* parts,
+                                                     Begin* begins, int by_column) {
   using S = Shape<CT, DP, QT>;
   using Row = typename Type<CT>::Row;
-  extern __shared__ __align__(128) char smem[];
+  extern __shared__ __align__(1024) char smem[];  // addresses of rows are put together by exclusive or
   __shared__ int s_queue[kWarps][kQueue];
   __shared__ uint32_t s_valid[kWarps][S::stages];
   __shared__ float s_m[kWarps][QT], s_l[kWarps][QT], s_f[kWarps][QT], s_top[QT], s_sum[QT];
@@ -523,13 +569,14 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, int unit, int
   const int chunks = ch.D * S::e / 16;  // of a row that is there
 
   // this block's units of the line
-  int64_t total = 0;
-  for (int b = lane; b < a.B; b += 32) total += units_of(a, b, unit);
+  const int64_t mine = lane < a.B ? units_of(a, lane, unit) : 0;
+  int64_t total = mine;
+  for (int b = 32 + lane; b < a.B; b += 32) total += units_of(a, b, unit);
 #pragma unroll
   for (int d = 16; d; d /= 2) total += __shfl_xor_sync(~0u, total, d);
   total *= cols;
   const int64_t blocks = min((int64_t)gridDim.x, total);  // each of these has a unit at least
-  if (begins && threadIdx.x == 0) begins[blockIdx.x] = Begin{0, 0, 0, 0};
+  if (begins && !by_column && threadIdx.x == 0) begins[blockIdx.x] = Begin{0, 0, 0, 0};
   if (blockIdx.x >= blocks) return;
   int64_t u = total * blockIdx.x / blocks;
   const int64_t end = total * (blockIdx.x + 1) / blocks;
@@ -537,7 +584,7 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, int unit, int
   int b = 0;
   int64_t before = 0;
   for (int b0 = 0;; b0 += 32) {
-    const int64_t own = b0 + lane < a.B ? (int64_t)units_of(a, b0 + lane, unit) * cols : 0;
+    const int64_t own = (b0 == 0 ? mine : b0 + lane < a.B ? units_of(a, b0 + lane, unit) : 0) * cols;
     int64_t upto = own;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
@@ -579,37 +626,55 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, int unit, int
       if (chunks < S::cpr)  // components beyond the head's: the products run over zeros
         for (int i = lane; i < S::stages * S::tk * (S::cpr - chunks); i += 32) {
           const int c = chunks + i % (S::cpr - chunks), r = i / (S::cpr - chunks);
-          const uint32_t at = ring + r / S::tk * S::tile + r % S::tk * S::row + 16 * swizzle<CT, S::cpr>(r % S::tk, c);
+          const uint32_t at = ring + r / S::tk * S::tile + r % S::tk * S::row + 16 * (c ^ swizzle<CT, S::cpr>(r % S::tk));
           asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
         }
 
       keys.start(lo, hi, warp);
-      int key, n_next = keys.take(&key), page = -1, issued = 0;
+      int key, n_next = keys.take(&key), page = -1, slot_of = 0, issued = 0;
       auto look = [&] {
-        page = key >= 0 ? table[(uint32_t)key / (uint32_t)ch.page_size] : -1;
+        const int p = (int)((uint64_t)(uint32_t)key * rows.mul >> 31 >> rows.div_shift);
+        page = key >= 0 ? table[p] : -1;
+        slot_of = key - p * ch.page_size;
       };
       auto issue = [&] {
         if (n_next > 0) {
           const int slot = issued % S::stages;
-          const uint32_t to = ring + slot * S::tile;
           bool ok = key >= 0;
           if (ok && (page < 0 || page >= ch.pages)) {
             if (a.status) set_status(a.status, CP_EINVAL);
             ok = false;
           }
-          const int64_t mine = ok ? page * ch.page_stride + (int64_t)((uint32_t)key % (uint32_t)ch.page_size) * ch.slot_stride : 0;
+          const uint32_t mine = ok ? (uint32_t)page * rows.page + (uint32_t)slot_of * rows.slot : 0;
           const uint32_t valid = __ballot_sync(~0u, ok);
           if (lane == 0) s_valid[warp][slot] = valid;
+          // 32 chunks at a time: some rows side by side, or a part of one
+          constexpr int side = S::cpr >= 32 ? 1 : 32 / S::cpr;
+          const int c = lane % S::cpr, r0 = lane / S::cpr;
+          const uint32_t to = ring + slot * S::tile + r0 * S::row + 16 * (c ^ swizzle<CT, S::cpr>(r0));
+          auto each = [&](auto copy) {
 #pragma unroll
-          for (int i = 0; i < S::tk * S::cpr / 32; ++i) {
-            const int x = 32 * i + lane, r = x / S::cpr, c = x % S::cpr;
-            const int64_t off = __shfl_sync(~0u, mine, r) * S::e + 16 * c;
-            const bool there = valid >> r & 1;
-            if (c < chunks) {
-              const uint32_t at = to + r * S::row + 16 * swizzle<CT, S::cpr>(r, c);
-              copy16(at, kp + (there ? off : 0), there);
-              copy16(at + S::tk * S::row, vp + (there ? off : 0), there);
+            for (int i = 0; i < S::tk * S::cpr / 32; ++i) {
+              constexpr int turns = S::cpr > 32 ? S::cpr / 32 : 1;  // copies of a row
+              const int r = i / turns * side, more = i % turns * 512;
+              const uint64_t off = (uint64_t)__shfl_sync(~0u, mine, r + r0) * rows.scale + (16 * c + more);
+              const uint32_t at = (to ^ (16 * swizzle<CT, S::cpr>(r))) + r * S::row + more;
+              copy(at, off, r + r0, c + more / 16);
             }
+          };
+          if (valid == (1u << S::tk) - 1 && chunks == S::cpr) {
+            each([&](uint32_t at, uint64_t off, int, int) {
+              copy16(at, kp + off);
+              copy16(at + S::tk * S::row, vp + off);
+            });
+          } else {
+            each([&](uint32_t at, uint64_t off, int r, int c) {
+              const bool there = valid >> r & 1;
+              if (c < chunks) {
+                copy16(at, kp + (there ? off : 0), there);
+                copy16(at + S::tk * S::row, vp + (there ? off : 0), there);
+              }
+            });
           }
           ++issued;
           n_next = keys.take(&key);
@@ -636,11 +701,10 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, int unit, int
       // the warps' results by a common maximum
       if (threadIdx.x < QT) {
         const int n = threadIdx.x;
-        float top = -INFINITY, sum = 0.0f;
+        float top = kLowest, sum = 0.0f;
         for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_m[w][n]);
-        const float base = top == -INFINITY ? 0.0f : top;
         for (int w = 0; w < kWarps; ++w) {
-          const float f = exp2f(s_m[w][n] - base);
+          const float f = exp2f(s_m[w][n] - top);
           s_f[w][n] = f;
           sum += s_l[w][n] * f;
         }
@@ -674,12 +738,13 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, int unit, int
           a.lse[(int64_t)b * a.Hq + h0 + n] = s_sum[n] == 0.0f ? -INFINITY : (s_top[n] + log2f(s_sum[n])) * kLn2;
         }
       }
-      if (!whole && k0 == 0 && threadIdx.x == 0) {
+      if (begins && k0 == 0 && (by_column || !whole) && threadIdx.x == 0) {
         // the block that has the query tile's last unit: unit x is in the largest
         // block i with i * total / blocks <= x
         const int64_t last = u + nu - 1;
         const int at = (int)(((last + 1) * blocks - 1) / total);
-        begins[blockIdx.x] = Begin{b, col, at - (int)blockIdx.x + 1, 0};
+        begins[by_column ? b * cols + col : (int)blockIdx.x] =
+            Begin{(int)blockIdx.x, whole ? 0 : at - (int)blockIdx.x + 1, b, col};
       }
       u += k1 - k0;
       __syncthreads();  // the ring and the sums are free
@@ -688,58 +753,85 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, int unit, int
   }
 }
 
-// Adds the parts of the query tiles that several blocks shared, a block for 4
-// queries of the tile that begins in block blockIdx.x: part 1 of that block, then
-// part 0 of the following ones, weighed by a common maximum.
-constexpr int kJoinThreads = 256, kJoinQueries = 4;
+// Adds the parts of the query tiles that several blocks shared: part 1 of the block
+// that the tile begins in, then part 0 of the following ones, weighed by a common
+// maximum.  A block takes `side` queries of one tile, several warps each where
+// there are many parts; a lane has DP / 32 components.
+constexpr int kJoinWarps = 8;
 template <int CT, int DP, int QT>
-__global__ void __launch_bounds__(kJoinThreads) k_decode_join(DecodeArgs a, int tiles, const float* parts,
-                                                              const Begin* begins) {
+__global__ void __launch_bounds__(32 * kJoinWarps) k_decode_join(DecodeArgs a, int tiles, int side, const float* parts,
+                                                                 const Begin* begins) {
   using S = Shape<CT, DP, QT>;
   using Row = typename Type<CT>::Row;
-  constexpr int kCols = DP / 4, kGroups = kJoinThreads / kCols;  // float4 columns, parts at a time
-  __shared__ float4 s_o[kGroups][kCols];
+  constexpr int V = DP / 32;
+  __shared__ float s_o[kJoinWarps][DP];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const Begin x = begins[blockIdx.x];
   if (x.blocks == 0) return;
   const int G = a.Hq / a.cache.heads, hk = x.col / tiles, h0 = hk * G + x.col % tiles * QT;
   const int nq = min(QT, G - x.col % tiles * QT);
-  const float vs = a.cache.v_scale ? a.cache.v_scale[hk] : 1.0f;
-  const int lane = threadIdx.x % 32;
-  auto part = [&](int i) { return parts + (2 * ((int64_t)blockIdx.x + i) + (i == 0)) * S::part; };
-  for (int n = blockIdx.y * kJoinQueries; n < min(nq, (int)(blockIdx.y + 1) * kJoinQueries); ++n) {
-    float top = -INFINITY;
-    for (int i = lane; i < x.blocks; i += 32) top = fmaxf(top, part(i)[n]);
-#pragma unroll
-    for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-    const float base = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f;
-    for (int i = lane; i < x.blocks; i += 32) sum += part(i)[QT + n] * exp2f(part(i)[n] - base);
-    sum = warp_sum(sum);  // the same in every warp
-    float4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    const int col = threadIdx.x % kCols, group = threadIdx.x / kCols;
-#pragma unroll 4
-    for (int i = group; i < x.blocks; i += kGroups) {
-      const float* p = part(i);
-      const float f = exp2f(p[n] - base);
-      const float4 y = *(const float4*)(p + 2 * QT + n * DP + 4 * col);
-      o.x = fmaf(f, y.x, o.x);
-      o.y = fmaf(f, y.y, o.y);
-      o.z = fmaf(f, y.z, o.z);
-      o.w = fmaf(f, y.w, o.w);
-    }
-    s_o[group][col] = o;
-    __syncthreads();
-    if (threadIdx.x < DP && threadIdx.x < a.cache.D) {
-      float y = 0.0f;
-      for (int i = 0; i < kGroups; ++i) y += ((const float*)s_o[i])[threadIdx.x];
-      ((Row*)a.out)[x.b * a.o_b + (int64_t)(h0 + n) * a.o_h + threadIdx.x] =
-          from_f32<Row>(sum == 0.0f ? 0.0f : y * (vs / sum));
-    }
-    if (threadIdx.x == 0 && a.lse)
-      a.lse[(int64_t)x.b * a.Hq + h0 + n] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
-    __syncthreads();
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int warps = kJoinWarps / side, n = min((int)blockIdx.y * side + warp / warps, nq - 1), own = warp % warps;
+  auto part = [&](int i) { return parts + (2 * ((int64_t)x.block + i) + (i == 0)) * S::part; };
+  float top = kLowest, m0 = kLowest, l0 = 0.0f;  // the first 32 parts' are kept
+  if (lane < x.blocks) {
+    m0 = part(lane)[n];
+    l0 = part(lane)[QT + n];
   }
+  top = m0;
+  for (int i = 32 + lane; i < x.blocks; i += 32) top = fmaxf(top, part(i)[n]);
+#pragma unroll
+  for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+  float sum = 0.0f, o[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) o[j] = 0.0f;
+  for (int i0 = 0; i0 < x.blocks; i0 += 32) {
+    float m = m0, l = l0;
+    if (i0 > 0) {
+      const bool there = i0 + lane < x.blocks;
+      m = there ? part(i0 + lane)[n] : kLowest;
+      l = there ? part(i0 + lane)[QT + n] : 0.0f;
+    }
+    const float f = exp2f(m - top);
+    sum += l * f;
+    const int here = min(32, x.blocks - i0);
+#pragma unroll 4
+    for (int i = own; i < here; i += warps) {
+      const float w = __shfl_sync(~0u, f, i);
+      const float* p = part(i0 + i) + 2 * QT + n * DP + V * lane;
+      if constexpr (V == 2) {
+        const float2 y = *reinterpret_cast<const float2*>(p);
+        o[0] = fmaf(w, y.x, o[0]);
+        o[1] = fmaf(w, y.y, o[1]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < V; j += 4) {
+          const float4 y = *reinterpret_cast<const float4*>(p + j);
+          o[j] = fmaf(w, y.x, o[j]);
+          o[j + 1] = fmaf(w, y.y, o[j + 1]);
+          o[j + 2] = fmaf(w, y.z, o[j + 2]);
+          o[j + 3] = fmaf(w, y.w, o[j + 3]);
+        }
+      }
+    }
+  }
+  sum = warp_sum(sum);  // the same in every warp of a query
+  if (warps > 1) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) s_o[warp][V * lane + j] = o[j];
+    __syncthreads();
+    if (own != 0) return;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      for (int w = 1; w < warps; ++w) o[j] += s_o[warp + w][V * lane + j];
+  }
+  if ((int)blockIdx.y * side + warp / warps >= nq) return;
+  const float by = sum == 0.0f ? 0.0f : (a.cache.v_scale ? a.cache.v_scale[hk] : 1.0f) / sum;
+  Row* out = (Row*)a.out + x.b * a.o_b + (int64_t)(h0 + n) * a.o_h;
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+    if (V * lane + j < a.cache.D) out[V * lane + j] = from_f32<Row>(sum == 0.0f ? 0.0f : o[j] * by);
+  if (lane == 0 && a.lse) a.lse[(int64_t)x.b * a.Hq + h0 + n] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
 // Query heads a pass takes and the width a head is laid out for.
@@ -759,8 +851,6 @@ size_t decode_ws_bytes(int64_t B, int64_t Hq, int64_t heads, int64_t D, int cach
 template <int CT, int DP, int QT>
 static int launch(const DecodeArgs& a, cudaStream_t s) {
   using S = Shape<CT, DP, QT>;
-  DeviceInfo di;
-  CP_TRY_STATUS(device_info(&di));
   const int G = a.Hq / a.cache.heads, tiles = (G + QT - 1) / QT;
   // Sequences of at most 4 units are not cut: the join would cost more.
   const bool cut = a.cache.capacity > 4 * kUnit;
@@ -768,27 +858,50 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   const int64_t line = (int64_t)a.B * a.cache.heads * tiles *
                        (a.cache.capacity < 1 ? 1 : ((int64_t)a.cache.capacity + unit - 1) / unit);
   if (line > (int64_t)1 << 52) return CP_EUNSUPPORTED;  // units times blocks stay within 64 bits
+
+  // rows of the cache in units that fit 32 bits
+  const Cache& ch = a.cache;
+  const uint64_t page = (uint64_t)ch.page_stride * S::e, slot = (uint64_t)ch.slot_stride * S::e;
+  int shift = 4;
+  while (shift < 31 && (page | slot) != 0 && ((page | slot) >> shift & 1) == 0) ++shift;
+  const uint64_t far = (uint64_t)(ch.pages > 0 ? ch.pages - 1 : 0) * (page >> shift) +
+                       (uint64_t)(ch.page_size - 1) * (slot >> shift);
+  if (far > 0xFFFFFFFFu) return CP_EUNSUPPORTED;
+  Rows rows{(uint32_t)(page >> shift), (uint32_t)(slot >> shift), (uint32_t)1 << shift, 0, 0};
+  while (((int64_t)1 << rows.div_shift) < ch.page_size) ++rows.div_shift;
+  rows.mul = (uint32_t)((((uint64_t)1 << (31 + rows.div_shift)) + ch.page_size - 1) / ch.page_size);
+
+  DeviceInfo di;
+  CP_TRY_STATUS(device_info(&di));
   int64_t grid = (int64_t)di.sm_count * S::per_sm;
   if (grid > kMaxBlocks) grid = kMaxBlocks;
   if (grid > line) grid = line;
+  const int64_t columns = (int64_t)a.B * ch.heads * tiles;
+  const bool by_column = columns <= grid;
   Begin* begins = (Begin*)a.ws;
   float* parts = (float*)((char*)a.ws + kMaxBlocks * sizeof(Begin));
   static std::atomic<uint64_t> allowed{0};
   CP_TRY_STATUS(allow_smem_once((const void*)k_decode<CT, DP, QT>, S::smem, "decode: shared memory", &allowed));
-  k_decode<CT, DP, QT><<<(unsigned)grid, kThreads, S::smem, s>>>(a, unit, tiles, parts, cut ? begins : nullptr);
+  k_decode<CT, DP, QT><<<(unsigned)grid, kThreads, S::smem, s>>>(a, rows, unit, tiles, parts, cut ? begins : nullptr,
+                                                                 by_column);
   CP_TRY_STATUS(launch_status("decode"));
   if (!cut) return CP_OK;
+  // about so many parts a query tile, and the join's queries side by side for it
+  const int64_t share = grid / columns + 1;
+  const int queries = G < QT ? G : QT;
+  int side = share <= 4 ? 8 : share <= 12 ? 2 : 1;
+  while (side > 1 && side / 2 >= queries) side /= 2;
   // its blocks wait on the device for the parts, not for a launch after them
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)grid, (unsigned)((G < QT ? G : QT) + kJoinQueries - 1) / kJoinQueries);
-  cfg.blockDim = dim3(kJoinThreads);
+  cfg.gridDim = dim3((unsigned)(by_column ? columns : grid), (unsigned)(queries + side - 1) / side);
+  cfg.blockDim = dim3(32 * kJoinWarps);
   cfg.stream = s;
   cudaLaunchAttribute early{};
   early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   early.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &early;
   cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_decode_join<CT, DP, QT>, a, tiles, (const float*)parts,
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_decode_join<CT, DP, QT>, a, tiles, side, (const float*)parts,
                                            (const Begin*)begins);
   note_launch();
   return cuda_status(e, "decode: join");

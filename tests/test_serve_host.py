@@ -175,6 +175,9 @@ def test_decode_refuses(lib):
     for b in (dict(dt=2), dict(B=-1), dict(Hq=27), dict(Hq=-4), dict(scale=float("nan")), dict(window=-1), dict(q=0),
               dict(q=FAKE + 1), dict(out=0), dict(out=FAKE + 1), dict(lens=0), dict(lse=FAKE + 2), dict(status=FAKE + 1)):
         assert _decode(lib, **b) == cp.CP_EINVAL, b
+    # pages spread over more than 2^32 of the largest unit their strides share (16 bytes)
+    assert _decode(lib, cache(pages=0x7FFFFFFF, page_stride=16 * 512 + 8)) == cp.CP_EUNSUPPORTED
+    assert _decode(lib, cache(slot_stride=-512), B=0) == cp.CP_EINVAL
     for b in (dict(ws=0), dict(ws=FAKE + 128), dict(ws_bytes=16)):
         assert _decode(lib, **b) == cp.CP_EWORKSPACE, b
 
