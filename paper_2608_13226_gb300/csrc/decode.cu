@@ -26,6 +26,11 @@
 
 namespace cp {
 
+#ifndef BUDGET
+#define BUDGET 70
+#define LEAST 3
+#define PER 3
+#endif
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kUnit = 64;   // keys of a unit
@@ -54,14 +59,15 @@ struct Shape {
   static constexpr int cpr = row / 16;                // 16-byte chunks of it
   static constexpr int tile = 2 * tk * row;           // K and V of a tile
   // ring: as many tiles as keep two blocks on an SM, 3 at least
-  static constexpr int fit = 100 * 1024 / (kWarps * tile);
-  static constexpr int stages = fit < 3 ? 3 : fit > 8 ? 8 : fit;
+  static constexpr int fit = BUDGET * 1024 / (kWarps * tile);
+  static constexpr int stages = fit < LEAST ? LEAST : fit > 8 ? 8 : fit;
   static constexpr int ring = kWarps * stages * tile;
   static constexpr int extra = CT == CP_F32 ? (QT * DP + kWarps * tk * QT) * 4 : 0;
   static constexpr int smem = ring + extra;
-  static constexpr int per_sm = smem <= 110 * 1024 ? 2 : 1;
+  static constexpr int per_sm = smem <= 72 * 1024 ? PER : smem <= 110 * 1024 ? 2 : 1;
   static constexpr int part = QT * (DP + 2);  // floats of a partial result
-  static_assert(kWarps * QT * DP * 4 <= ring, "the merge reuses the ring");
+  static constexpr int pitch = DP + 4;        // floats of a query in the merge: the lanes' banks differ
+  static_assert(kWarps * QT * pitch * 4 <= ring, "the merge reuses the ring");
 };
 
 // What the blocks leave for the join: the block that a query tile of sequence b
@@ -144,6 +150,11 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t y;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
   return y;
+}
+
+// a / b of non-negative numbers, mostly small ones.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
 
 // Keys of sequence b: [first, len).
@@ -243,14 +254,24 @@ struct Math {
     for (int n = 0; n < NT; ++n) {
       const int row = 8 * n + g;
       const uint16_t* src = (const uint16_t*)a.q + b * a.q_b + (int64_t)(h0 + row) * a.q_h;
-      auto at = [&](int d) -> uint32_t { return row < nq && d < D ? src[d] : 0; };
+      // components of a place: bf16 2 t, 2 t + 1 and the same + 8; 8 bits 4 t .. 4 t + 3, as its
+      // keys come.  A head is even, so a pair is there or not as one.
+      const bool row_there = row < nq;
+      const bool pairs = (((uint64_t)a.q | (uint64_t)(2 * a.q_b) | (uint64_t)(2 * a.q_h)) & 3) == 0;
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        // bf16: components 2 t, 2 t + 1 and the same + 8; 8 bits: 4 t .. 4 t + 3, as its keys come
-        const int d0 = 16 * s + (CT == CP_E4M3 ? 4 * t : 2 * t), d1 = d0 + (CT == CP_E4M3 ? 2 : 8);
-        q[n][s][0] = at(d0) | at(d0 + 1) << 16;
-        q[n][s][1] = at(d1) | at(d1 + 1) << 16;
-      }
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int d = 16 * s + (CT == CP_E4M3 ? 4 * t + 2 * i : 2 * t + 8 * i);
+          uint32_t x = 0;
+          if (row_there && d < D) {
+            if (pairs)
+              x = *(const uint32_t*)(src + d);
+            else
+              x = src[d] | (uint32_t)src[d + 1] << 16;
+          }
+          q[n][s][i] = x;
+        }
       float back = 1.0f;
       if (CT == CP_E4M3) {
         // keys enter as float16, exactly, and so do queries once their largest
@@ -422,7 +443,7 @@ struct Math {
         for (int i = 0; i < 4; ++i) {
           const int query = 8 * n + 2 * t + (i & 1);
           const int d = 16 * k + (CT == CP_E4M3 ? 2 * g + i / 2 : g + 8 * (i / 2));
-          buf[query * DP + d] = o[n][k][i] * f[query];
+          buf[query * S::pitch + d] = o[n][k][i] * f[query];
         }
   }
 };
@@ -549,7 +570,7 @@ struct Math<CP_F32, DP, QT> {
 #pragma unroll
     for (int n = 0; n < QT; ++n)
 #pragma unroll
-      for (int i = 0; i < V; ++i) buf[n * DP + component(i, threadIdx.x % 32)] = o[n][i] * f[n];
+      for (int i = 0; i < V; ++i) buf[n * S::pitch + component(i, threadIdx.x % 32)] = o[n][i] * f[n];
   }
 };
 
@@ -562,7 +583,9 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
   __shared__ int s_queue[kWarps][kQueue];
   __shared__ uint32_t s_valid[kWarps][S::stages];
   __shared__ float s_m[kWarps][QT], s_l[kWarps][QT], s_f[kWarps][QT], s_top[QT], s_sum[QT];
+  // the join may come to the SMs now and wait there; what ran before this is waited for
   asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const Cache& ch = a.cache;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int G = a.Hq / ch.heads, cols = ch.heads * tiles;
@@ -578,8 +601,10 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
   const int64_t blocks = min((int64_t)gridDim.x, total);  // each of these has a unit at least
   if (begins && !by_column && threadIdx.x == 0) begins[blockIdx.x] = Begin{0, 0, 0, 0};
   if (blockIdx.x >= blocks) return;
-  int64_t u = total * blockIdx.x / blocks;
-  const int64_t end = total * (blockIdx.x + 1) / blocks;
+  // the first `longer` of them one more than the others
+  const int64_t share = quotient(total, blocks), longer = total - share * blocks;
+  int64_t u = share * blockIdx.x + min((int64_t)blockIdx.x, longer);
+  const int64_t end = u + share + (blockIdx.x < longer);
   // the sequence they start in
   int b = 0;
   int64_t before = 0;
@@ -615,7 +640,7 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
     keys.keep = a.keep ? a.keep + (int64_t)b * a.keep_stride : nullptr;
     for (; u < end && u < before + (int64_t)nu * cols;) {
       // the segment: units [k0, k1) of sequence b, query tile `col`
-      const int col = (int)((u - before) / nu), k0 = (int)((u - before) % nu);
+      const int col = (int)quotient(u - before, nu), k0 = (int)(u - before - (int64_t)col * nu);
       const int k1 = (int)min((int64_t)nu, k0 + (end - u));
       const int hk = col / tiles, h0 = hk * G + col % tiles * QT;
       const int nq = min(QT, G - col % tiles * QT);
@@ -713,7 +738,7 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
       }
       __syncthreads();
       float* buf = (float*)smem;
-      math.put(buf + warp * QT * DP, s_f[warp]);
+      math.put(buf + warp * QT * S::pitch, s_f[warp]);
       __syncthreads();
       const bool whole = k0 == 0 && k1 == nu;
       const float vs = ch.v_scale ? ch.v_scale[hk] : 1.0f;
@@ -722,7 +747,7 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
         const int n = i / DP, d = i % DP;
         float x = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) x += buf[w * QT * DP + i];
+        for (int w = 0; w < kWarps; ++w) x += buf[(w * QT + n) * S::pitch + d];
         if (!whole)
           part[2 * QT + i] = x;
         else if (d < ch.D)
@@ -739,10 +764,9 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
         }
       }
       if (begins && k0 == 0 && (by_column || !whole) && threadIdx.x == 0) {
-        // the block that has the query tile's last unit: unit x is in the largest
-        // block i with i * total / blocks <= x
-        const int64_t last = u + nu - 1;
-        const int at = (int)(((last + 1) * blocks - 1) / total);
+        // the block that has the query tile's last unit
+        const int64_t last = u + nu - 1, split = longer * (share + 1);
+        const int at = (int)(last < split ? quotient(last, share + 1) : longer + quotient(last - split, share));
         begins[by_column ? b * cols + col : (int)blockIdx.x] =
             Begin{(int)blockIdx.x, whole ? 0 : at - (int)blockIdx.x + 1, b, col};
       }
@@ -758,14 +782,33 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
 // maximum.  A block takes `side` queries of one tile, several warps each where
 // there are many parts; a lane has DP / 32 components.
 constexpr int kJoinWarps = 8;
+template <int V>
+__device__ __forceinline__ void load_part(const float* p, float (&x)[V]) {
+  if constexpr (V == 2) {
+    const float2 y = *reinterpret_cast<const float2*>(p);
+    x[0] = y.x;
+    x[1] = y.y;
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; j += 4) {
+      const float4 y = *reinterpret_cast<const float4*>(p + j);
+      x[j] = y.x;
+      x[j + 1] = y.y;
+      x[j + 2] = y.z;
+      x[j + 3] = y.w;
+    }
+  }
+}
 template <int CT, int DP, int QT>
 __global__ void __launch_bounds__(32 * kJoinWarps) k_decode_join(DecodeArgs a, int tiles, int side, const float* parts,
                                                                  const Begin* begins) {
   using S = Shape<CT, DP, QT>;
   using Row = typename Type<CT>::Row;
   constexpr int V = DP / 32;
+  constexpr int kFirst = 4;  // parts that a warp loads before it knows their weights
   __shared__ float s_o[kJoinWarps][DP];
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
   const Begin x = begins[blockIdx.x];
   if (x.blocks == 0) return;
   const int G = a.Hq / a.cache.heads, hk = x.col / tiles, h0 = hk * G + x.col % tiles * QT;
@@ -773,46 +816,45 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_decode_join(DecodeArgs a, i
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int warps = kJoinWarps / side, n = min((int)blockIdx.y * side + warp / warps, nq - 1), own = warp % warps;
   auto part = [&](int i) { return parts + (2 * ((int64_t)x.block + i) + (i == 0)) * S::part; };
-  float top = kLowest, m0 = kLowest, l0 = 0.0f;  // the first 32 parts' are kept
+  float m0 = kLowest, l0 = 0.0f;  // the first 32 parts' maxima and sums are kept
   if (lane < x.blocks) {
     m0 = part(lane)[n];
     l0 = part(lane)[QT + n];
   }
-  top = m0;
+  float y[kFirst][V];
+#pragma unroll
+  for (int k = 0; k < kFirst; ++k)
+    if (own + k * warps < min(32, x.blocks)) load_part<V>(part(own + k * warps) + 2 * QT + n * DP + V * lane, y[k]);
+  float top = m0;
   for (int i = 32 + lane; i < x.blocks; i += 32) top = fmaxf(top, part(i)[n]);
 #pragma unroll
   for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-  float sum = 0.0f, o[V];
+  float f = exp2f(m0 - top), sum = l0 * f, o[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) o[j] = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kFirst; ++k) {
+    const int i = own + k * warps;
+    const float w = __shfl_sync(~0u, f, i % 32);
+    if (i < min(32, x.blocks)) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) o[j] = fmaf(w, y[k][j], o[j]);
+    }
+  }
   for (int i0 = 0; i0 < x.blocks; i0 += 32) {
-    float m = m0, l = l0;
     if (i0 > 0) {
       const bool there = i0 + lane < x.blocks;
-      m = there ? part(i0 + lane)[n] : kLowest;
-      l = there ? part(i0 + lane)[QT + n] : 0.0f;
+      f = there ? exp2f(part(i0 + lane)[n] - top) : 0.0f;
+      sum += there ? part(i0 + lane)[QT + n] * f : 0.0f;
     }
-    const float f = exp2f(m - top);
-    sum += l * f;
     const int here = min(32, x.blocks - i0);
 #pragma unroll 4
-    for (int i = own; i < here; i += warps) {
+    for (int i = own + (i0 == 0 ? kFirst * warps : 0); i < here; i += warps) {
       const float w = __shfl_sync(~0u, f, i);
-      const float* p = part(i0 + i) + 2 * QT + n * DP + V * lane;
-      if constexpr (V == 2) {
-        const float2 y = *reinterpret_cast<const float2*>(p);
-        o[0] = fmaf(w, y.x, o[0]);
-        o[1] = fmaf(w, y.y, o[1]);
-      } else {
+      float z[V];
+      load_part<V>(part(i0 + i) + 2 * QT + n * DP + V * lane, z);
 #pragma unroll
-        for (int j = 0; j < V; j += 4) {
-          const float4 y = *reinterpret_cast<const float4*>(p + j);
-          o[j] = fmaf(w, y.x, o[j]);
-          o[j + 1] = fmaf(w, y.y, o[j + 1]);
-          o[j + 2] = fmaf(w, y.z, o[j + 2]);
-          o[j + 3] = fmaf(w, y.w, o[j + 3]);
-        }
-      }
+      for (int j = 0; j < V; ++j) o[j] = fmaf(w, z[j], o[j]);
     }
   }
   sum = warp_sum(sum);  // the same in every warp of a query
@@ -882,25 +924,31 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   float* parts = (float*)((char*)a.ws + kMaxBlocks * sizeof(Begin));
   static std::atomic<uint64_t> allowed{0};
   CP_TRY_STATUS(allow_smem_once((const void*)k_decode<CT, DP, QT>, S::smem, "decode: shared memory", &allowed));
-  k_decode<CT, DP, QT><<<(unsigned)grid, kThreads, S::smem, s>>>(a, rows, unit, tiles, parts, cut ? begins : nullptr,
-                                                                 by_column);
-  CP_TRY_STATUS(launch_status("decode"));
+  // Both launches may begin before what precedes them has ended: their blocks then
+  // wait on the device, and not for a launch after it.
+  cudaLaunchAttribute early{};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = S::smem;
+  cfg.stream = s;
+  cfg.attrs = &early;
+  cfg.numAttrs = 1;
+  note_launch();
+  CP_TRY_STATUS(cuda_status(cudaLaunchKernelEx(&cfg, k_decode<CT, DP, QT>, a, rows, unit, tiles, parts,
+                                               cut ? begins : (Begin*)nullptr, (int)by_column),
+                            "decode"));
   if (!cut) return CP_OK;
   // about so many parts a query tile, and the join's queries side by side for it
   const int64_t share = grid / columns + 1;
   const int queries = G < QT ? G : QT;
   int side = share <= 4 ? 8 : share <= 12 ? 2 : 1;
   while (side > 1 && side / 2 >= queries) side /= 2;
-  // its blocks wait on the device for the parts, not for a launch after them
-  cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(by_column ? columns : grid), (unsigned)(queries + side - 1) / side);
   cfg.blockDim = dim3(32 * kJoinWarps);
-  cfg.stream = s;
-  cudaLaunchAttribute early{};
-  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  early.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &early;
-  cfg.numAttrs = 1;
+  cfg.dynamicSmemBytes = 0;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, k_decode_join<CT, DP, QT>, a, tiles, side, (const float*)parts,
                                            (const Begin*)begins);
   note_launch();
