@@ -8,8 +8,8 @@ fails with an error.
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
 import os
-import struct
 import threading
 from dataclasses import dataclass, fields
 
@@ -433,69 +433,33 @@ def coverprune_gather(feats, pos, frame, kept, *, status=None, out=None):
 # cache of keys and values, and one token's attention over it.
 # ---------------------------------------------------------------------------
 # These calls come once a layer and token, so the host's part of them counts:
-# the C structs are packed into bytes in one go, and a tensor is asked for
-# each of its properties once.
-_CACHE_TYPES = {torch.float32: CP_F32, torch.bfloat16: CP_BF16, torch.float8_e4m3fn: CP_E4M3}
-_pack_rows = struct.Struct("@PPq3q3q").pack      # cp_rows
-_pack_rope = struct.Struct("@Piif4x").pack       # cp_rope
-_pack_cache = struct.Struct("@IiPPqqqqqqqPPPqq").pack  # cp_cache
-_pack_pair = struct.Struct("@qq").pack
-_CACHE_BYTES = C.sizeof(_Cache)
+# a module of C++ (csrc/torch_binding.cpp) checks the tensors, allocates the
+# results and calls the library.  It raises ValueError or TypeError for what it
+# refuses and returns a status other than CP_OK as a number.
+_T = None
 
 
-def _raw_stream(t) -> int:
-    """The current stream of the tensor's device."""
-    return torch.cuda.current_stream(t.device).cuda_stream
+def _torch_lib():
+    global _T
+    if _T is None:
+        _lib()
+        with _lock:
+            path = _build.TORCH_LIB
+            if not os.path.exists(path):
+                raise RuntimeError(
+                    f"CoverPrune module for PyTorch not found at {path}; build it with "
+                    "paper_2608_13226_gb300.build.build()")
+            spec = importlib.util.spec_from_file_location("coverprune_torch", path)
+            module = importlib.util.module_from_spec(spec)
+            spec.loader.exec_module(module)
+            _T = module
+    return _T
 
 
-if hasattr(torch._C, "_cuda_getCurrentRawStream"):  # the same without a Stream object (2 us)
-    def _raw_stream(t) -> int:  # noqa: F811
-        return torch._C._cuda_getCurrentRawStream(t.get_device())
-
-
-def _on_gpu(name, t, dtype, shape=None, dense=True):
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor")
-    if t.dtype is not dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
-    if dense and not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
-
-
-def _optional(name, t, dtype, shape=None):
-    return None if t is None else _on_gpu(name, t, dtype, shape)
-
-
-def _rows_of(name, t, dims):
-    """Shape and strides of a tensor of head rows; only its last dimension has to be dense."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) != dims:
-        raise ValueError(f"{name} must have {dims} dimensions, got {len(shape)}")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor")
-    if stride[-1] != 1 and shape[-1] > 1:
-        raise ValueError(f"{name} must be dense in its last dimension")
-    return shape, stride
-
-
-def _result_like(name, t, shape, dtype, dims):
-    """Strides of a result given by the caller."""
-    got, stride = _rows_of(name, t, dims)
-    if got != shape or t.dtype is not dtype:
-        raise ValueError(f"{name} must be {tuple(shape)} of {dtype}")
-    return stride
-
-
-def _rope(inv_freq, D, layout, scale):
-    if layout not in ROPE_LAYOUTS:
-        raise ValueError(f"layout must be one of {tuple(ROPE_LAYOUTS)}, got {layout!r}")
-    at, n = _on_gpu("inv_freq", inv_freq, torch.float64), inv_freq.shape
-    if len(n) != 1 or 2 * n[0] > D:
-        raise ValueError(f"inv_freq must hold one frequency for each rotated pair, at most {D // 2}")
-    return _pack_rope(at, 2 * n[0], ROPE_LAYOUTS[layout], scale)
+def _layout(name):
+    if name not in ROPE_LAYOUTS:
+        raise ValueError(f"layout must be one of {tuple(ROPE_LAYOUTS)}, got {name!r}")
+    return ROPE_LAYOUTS[name]
 
 
 def coverprune_rotary_frequencies(rot: int, base: float = 10000.0, *, stretch: str = "none",
@@ -522,70 +486,10 @@ def coverprune_rotary(x, pos, inv_freq, *, layout: str = "half", scale: float = 
     turns; out then is a list too.  Any strides with a dense last dimension;
     out may be x.  inverse=True gives the gradient with respect to x from the
     one with respect to the result."""
-    many = isinstance(x, (list, tuple))
-    xs = x if many else (x,)
-    if not 1 <= len(xs) <= 4:
-        raise ValueError("x must be a tensor or a list of one to four")
-    first = xs[0]
-    dims, dtype = first.dim(), first.dtype
-    if dims != 3 and dims != 4:
-        raise ValueError("x must be [T, heads, D] or [B, T, heads, D]")
-    if out is None:
-        outs = [torch.empty_like(t) for t in xs]
-    else:
-        outs = list(out) if many else [out]
-        if len(outs) != len(xs):
-            raise ValueError("out must match x")
-    dt, shape, rows = _dtype(first), first.shape, b""
-    lead, D = shape[:-2], shape[-1]
-    for t, o in zip(xs, outs):
-        shape, stride = _rows_of("x", t, dims)
-        if t is not first and (shape[:-2] != lead or shape[-1] != D or t.dtype is not dtype):
-            raise ValueError("tensors turned together must share tokens, width and dtype")
-        to = stride if o is t else _result_like("out", o, shape, dtype, dims)
-        if dims == 3:
-            rows += _pack_rows(t.data_ptr(), o.data_ptr(), shape[1], 0, stride[0], stride[1], 0,
-                               to[0], to[1])
-        else:
-            rows += _pack_rows(t.data_ptr(), o.data_ptr(), shape[2], stride[0], stride[1],
-                               stride[2], to[0], to[1], to[2])
-    B, T = (1, lead[0]) if dims == 3 else lead
-    at = _on_gpu("pos", pos, torch.int64)
-    if pos.shape == lead:
-        pos_stride = T
-    elif pos.dim() == 1 and pos.shape[0] == T:
-        pos_stride = 0
-    else:
-        raise ValueError(f"pos must be [{T}] or {tuple(lead)}, got {tuple(pos.shape)}")
-    st = _lib().coverprune_rotary(rows, len(xs), dt, B, T, D, at, pos_stride,
-                                  _rope(inv_freq, D, layout, scale), 1 if inverse else 0,
-                                  _raw_stream(first))
-    if st:
-        _check(st, "coverprune_rotary")
-    return outs if many else outs[0]
-
-
-def _cache(k_cache, v_cache, table, k_scale, v_scale):
-    """cp_cache as bytes, and the cache's heads, width and keys a sequence."""
-    shape, stride = _rows_of("k_cache", k_cache, 4)
-    dtype = k_cache.dtype
-    if dtype not in _CACHE_TYPES:
-        raise TypeError(f"the cache must be float32, bfloat16 or float8_e4m3fn, got {dtype}")
-    if v_cache.shape != shape or v_cache.stride() != stride or v_cache.dtype is not dtype \
-            or not v_cache.is_cuda:
-        raise ValueError("k_cache and v_cache must share shape, strides and dtype")
-    pages, page_size, heads, D = shape
-    ks = _optional("k_scale", k_scale, torch.float32, (heads,))
-    vs = _optional("v_scale", v_scale, torch.float32, (heads,))
-    at, of = _on_gpu("table", table, torch.int32, dense=False), table.shape
-    if len(of) != 2 or (of[1] > 1 and table.stride(1) != 1):
-        raise ValueError("table must be [B, width], dense in its last dimension")
-    # strides of dimensions of one do not matter, whatever the tensor says
-    c = _pack_cache(_CACHE_BYTES, _CACHE_TYPES[dtype], k_cache.data_ptr(), v_cache.data_ptr(),
-                    pages, page_size, heads, D, stride[0] if pages > 1 else 0,
-                    stride[1] if page_size > 1 else 0, stride[2] if heads > 1 else 0, ks or 0,
-                    vs or 0, at, of[1], table.stride(0))
-    return c, heads, D, of[1] * page_size
+    r = (_T or _torch_lib()).rotary(x, pos, inv_freq, _layout(layout), scale, inverse, out)
+    if type(r) is int:
+        raise CoverPruneError(r, "coverprune_rotary")
+    return r
 
 
 def coverprune_cache_append(k, v, k_cache, v_cache, table, lens, *, starts=None, pos=None,
@@ -598,36 +502,12 @@ def coverprune_cache_append(k, v, k_cache, v_cache, table, lens, *, starts=None,
     sequence's (default: one row a sequence), lens int32 [B] how many keys each
     holds already.  q [T, Hq, D] is turned in the same launch.  Returns
     {"lens": int32 [B] after the call, "q": the turned queries or None}."""
-    cache, heads, D, _ = _cache(k_cache, v_cache, table, k_scale, v_scale)
-    shape, ks = _rows_of("k", k, 3)
-    of, vs = _rows_of("v", v, 3)
-    T, B, dtype = shape[0], table.shape[0], k.dtype
-    if shape[1] != heads or shape[2] != D or of != shape or v.dtype is not dtype:
-        raise ValueError(f"k and v must be [T, {heads}, {D}] of one dtype")
-    before = _on_gpu("lens", lens, torch.int32, (B,))
-    if starts is None and T != B:
-        raise ValueError(f"without starts there is one row a sequence: {T} rows, {B} sequences")
-    rope = None if inv_freq is None else _rope(inv_freq, D, layout, scale)
-    if new_lens is None:
-        new_lens = torch.empty_like(lens)
-    rows = None
-    if q is not None:
-        of, st = _rows_of("q", q, 3)
-        if of[0] != T or of[2] != D or q.dtype is not dtype:
-            raise ValueError(f"q must be [{T}, heads, {D}] of k's dtype")
-        if q_out is None:
-            q_out = torch.empty_like(q)
-        to = st if q_out is q else _result_like("q_out", q_out, of, dtype, 3)
-        rows = _pack_rows(q.data_ptr(), q_out.data_ptr(), of[1], 0, st[0], st[1], 0, to[0], to[1])
-    st = _lib().coverprune_cache_append(
-        cache, k.data_ptr(), _pack_pair(ks[0], ks[1]), v.data_ptr(), _pack_pair(vs[0], vs[1]),
-        _dtype(k), T, _optional("starts", starts, torch.int32, (B + 1,)), before, B,
-        _optional("pos", pos, torch.int64, (T,)), rope, rows,
-        _on_gpu("new_lens", new_lens, torch.int32, (B,)), _optional("status", status, torch.int32),
-        _raw_stream(k))
-    if st:
-        _check(st, "coverprune_cache_append")
-    return {"lens": new_lens, "q": q_out}
+    r = (_T or _torch_lib()).cache_append(k, v, k_cache, v_cache, table, lens, starts, pos,
+                                          inv_freq, _layout(layout), scale, q, k_scale, v_scale,
+                                          new_lens, q_out, status)
+    if type(r) is int:
+        raise CoverPruneError(r, "coverprune_cache_append")
+    return {"lens": r[0], "q": r[1]}
 
 
 def coverprune_decode_attention(q, k_cache, v_cache, table, lens, *, scale=None, window: int = 0,
@@ -638,39 +518,11 @@ def coverprune_decode_attention(q, k_cache, v_cache, table, lens, *, scale=None,
     only; keep bool [B, >= keys]: the keys marked only.  scale defaults to
     1 / sqrt(D).  Returns {"out": [B, Hq, D], "lse": float32 [B, Hq] or None,
     "ws": the workspace, to pass to the next call}."""
-    cache, heads, D, keys = _cache(k_cache, v_cache, table, k_scale, v_scale)
-    shape, qs = _rows_of("q", q, 3)
-    B, Hq, dtype = shape[0], shape[1], q.dtype
-    if shape[2] != D or table.shape[0] != B:
-        raise ValueError(f"q must be [{table.shape[0]}, heads, {D}], got {tuple(shape)}")
-    n = _on_gpu("lens", lens, torch.int32, (B,))
-    marks, marks_stride = None, 0
-    if keep is not None:
-        marks, of = _on_gpu("keep", keep, torch.bool, dense=False), keep.shape
-        if len(of) != 2 or of[0] != B or of[1] < keys or (of[1] > 1 and keep.stride(1) != 1):
-            raise ValueError(f"keep must be [{B}, at least {keys}], dense in its last dimension")
-        marks_stride = keep.stride(0)
-    dt = _dtype(q)
-    if out is None:
-        out = torch.empty(shape, dtype=dtype, device=q.device)
-        to = (Hq * D, D)
-    else:
-        to = _result_like("out", out, shape, dtype, 3)
-    lse_out = torch.empty((B, Hq), dtype=torch.float32, device=q.device) if lse else None
-    lib = _lib()
-    if ws is None:
-        size = C.c_size_t()
-        _check(lib.coverprune_decode_workspace_size(B, Hq, cache, C.byref(size)),
-               "coverprune_decode_workspace_size")
-        ws = torch.empty(max(size.value, 256), dtype=torch.uint8, device=q.device)
-    st = lib.coverprune_decode_attention(
-        q.data_ptr(), _pack_pair(qs[0], qs[1]), dt, B, Hq, cache, n, marks, marks_stride,
-        D ** -0.5 if scale is None else scale, window, out.data_ptr(), _pack_pair(to[0], to[1]),
-        None if lse_out is None else lse_out.data_ptr(), ws.data_ptr(), ws.numel(),
-        _optional("status", status, torch.int32), _raw_stream(q))
-    if st:
-        _check(st, "coverprune_decode_attention")
-    return {"out": out, "lse": lse_out, "ws": ws}
+    r = (_T or _torch_lib()).decode_attention(q, k_cache, v_cache, table, lens, scale, window,
+                                              keep, k_scale, v_scale, lse, out, ws, status)
+    if type(r) is int:
+        raise CoverPruneError(r, "coverprune_decode_attention")
+    return {"out": r[0], "lse": r[1], "ws": r[2]}
 
 
 def coverprune_barrier_selftest(n_blocks: int, expected: int, timeout_ms: float, ws) -> int:

@@ -26,11 +26,6 @@
 
 namespace cp {
 
-#ifndef BUDGET
-#define BUDGET 70
-#define LEAST 3
-#define PER 3
-#endif
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kUnit = 64;   // keys of a unit
@@ -58,13 +53,15 @@ struct Shape {
   static constexpr int row = DP * e;                  // bytes of a row in shared memory
   static constexpr int cpr = row / 16;                // 16-byte chunks of it
   static constexpr int tile = 2 * tk * row;           // K and V of a tile
-  // ring: as many tiles as keep two blocks on an SM, 3 at least
-  static constexpr int fit = BUDGET * 1024 / (kWarps * tile);
-  static constexpr int stages = fit < LEAST ? LEAST : fit > 8 ? 8 : fit;
+  // Ring: as many tiles as keep two blocks on an SM, 3 at least.  Three blocks of
+  // shorter rings leave the join no room beside them and wait longer: 128 ragged
+  // 8-bit sequences 101 us with two, 115 with three; four 125.
+  static constexpr int fit = 100 * 1024 / (kWarps * tile);
+  static constexpr int stages = fit < 3 ? 3 : fit > 8 ? 8 : fit;
   static constexpr int ring = kWarps * stages * tile;
   static constexpr int extra = CT == CP_F32 ? (QT * DP + kWarps * tk * QT) * 4 : 0;
   static constexpr int smem = ring + extra;
-  static constexpr int per_sm = smem <= 72 * 1024 ? PER : smem <= 110 * 1024 ? 2 : 1;
+  static constexpr int per_sm = smem <= 110 * 1024 ? 2 : 1;
   static constexpr int part = QT * (DP + 2);  // floats of a partial result
   static constexpr int pitch = DP + 4;        // floats of a query in the merge: the lanes' banks differ
   static_assert(kWarps * QT * pitch * 4 <= ring, "the merge reuses the ring");
