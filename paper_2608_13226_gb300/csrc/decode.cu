@@ -30,6 +30,7 @@ constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kUnit = 64;   // keys of a unit
 constexpr int kChunk = 64;  // keys whose marks a warp looks at together
+constexpr int kMarks = 4;   // of them under way, so that few marks in a chunk hold nothing up
 constexpr int kQueue = 128;
 // A running maximum follows the scores only when one is more than kSlack above it
 // (in units of log 2): weights up to 2^8 are as good as those up to 1, and most
@@ -63,6 +64,9 @@ struct Shape {
   static constexpr int smem = ring + extra;
   static constexpr int per_sm = smem <= 110 * 1024 ? 2 : 1;
   static constexpr int part = QT * (DP + 2);  // floats of a partial result
+  // What beginning and merging a segment costs, in units of 64 keys: about 3 us, in
+  // which a block takes 72 KB.
+  static constexpr int setup = 72 * 1024 / (2 * kUnit * row) < 1 ? 1 : 72 * 1024 / (2 * kUnit * row);
   static constexpr int pitch = DP + 4;        // floats of a query in the merge: the lanes' banks differ
   static_assert(kWarps * QT * pitch * 4 <= ring, "the merge reuses the ring");
 };
@@ -138,6 +142,8 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// 2^e for -126 <= e <= 127.
+__device__ __forceinline__ float power(int e) { return __int_as_float((e + 127) << 23); }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t y;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
@@ -174,7 +180,7 @@ struct Keys {
   const uint8_t* keep;  // the sequence's marks, or null
   int* queue;           // marked keys that are still to be taken
   int head, count;
-  uint32_t mark[2][2];  // of the next two chunks
+  uint32_t mark[kMarks][2];  // of the next chunks
 
   __device__ void load(int i, int at) {
     mark[i][0] = at + lane < hi ? keep[at + lane] : 0;
@@ -185,8 +191,8 @@ struct Keys {
     head = count = 0;
     next = lo + warp * (keep ? kChunk : TK);
     if (keep) {
-      load(0, next);
-      load(1, next + kWarps * kChunk);
+#pragma unroll
+      for (int i = 0; i < kMarks; ++i) load(i, next + i * kWarps * kChunk);
     }
   }
   // How many keys the next tile has (0: no more); this lane's, or -1.
@@ -205,10 +211,13 @@ struct Keys {
           queue[(head + count + __popc(all & ((1u << lane) - 1))) % kQueue] = next + 32 * h + lane;
         count += __popc(all);
       }
-      mark[0][0] = mark[1][0];
-      mark[0][1] = mark[1][1];
+#pragma unroll
+      for (int i = 0; i + 1 < kMarks; ++i) {
+        mark[i][0] = mark[i + 1][0];
+        mark[i][1] = mark[i + 1][1];
+      }
+      load(kMarks - 1, next + kMarks * kWarps * kChunk);
       next += kWarps * kChunk;
-      load(1, next + kWarps * kChunk);
     }
     __syncwarp();
     const int n = min(count, TK);
@@ -269,11 +278,12 @@ struct Math {
           }
           q[n][s][i] = x;
         }
-      float back = 1.0f;
+      int ex = 0;
       if (CT == CP_E4M3) {
         // keys enter as float16, exactly, and so do queries once their largest
         // component is brought to [2^8, 2^9) by a power of two (bf16 has fewer bits;
-        // what lies 2^22 below the largest component loses some)
+        // what lies 2^22 below the largest component loses some; below 2^-92 the
+        // largest itself does, and every score is as good as 0)
         float top = 0.0f;
 #pragma unroll
         for (int s = 0; s < KS; ++s)
@@ -283,25 +293,19 @@ struct Math {
                                    fabsf(__uint_as_float(q[n][s][i] & 0xFFFF0000u))));
         top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
         top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-        int ex = 0;
-        if (top > 0.0f && top < INFINITY) ex = ilogbf(top) - 8;
-        const float f1 = ldexpf(1.0f, -ex / 2), f2 = ldexpf(1.0f, -(ex - ex / 2));
+        ex = min(max((int)(__float_as_uint(top) >> 23) - 127 - 8, -100), 100);
+        const float f = power(-ex);
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
           for (int i = 0; i < 2; ++i)
-            q[n][s][i] = pack_f16(__uint_as_float(q[n][s][i] << 16) * f1 * f2,
-                                  __uint_as_float(q[n][s][i] & 0xFFFF0000u) * f1 * f2);
-        back = (float)ex;
+            q[n][s][i] = pack_f16(__uint_as_float(q[n][s][i] << 16) * f, __uint_as_float(q[n][s][i] & 0xFFFF0000u) * f);
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         // the two queries whose scores this lane has
         sc[n][i] = scale;
-        if (CT == CP_E4M3) {
-          const int ex = (int)__shfl_sync(~0u, back, 4 * (2 * t + i));
-          sc[n][i] = ldexpf(ldexpf(scale, ex / 2), ex - ex / 2);
-        }
+        if (CT == CP_E4M3) sc[n][i] *= power(__shfl_sync(~0u, ex, 4 * (2 * t + i)));
         m[n][i] = kLowest;
         l[n][i] = 0.0f;
       }
@@ -591,10 +595,15 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
   // this block's units of the line
   const int64_t mine = lane < a.B ? units_of(a, lane, unit) : 0;
   int64_t total = mine;
+#pragma unroll 4
   for (int b = 32 + lane; b < a.B; b += 32) total += units_of(a, b, unit);
 #pragma unroll
   for (int d = 16; d; d /= 2) total += __shfl_xor_sync(~0u, total, d);
   total *= cols;
+  // Where blocks have many units, a query tile counts for `setup` more, so that one
+  // with several short ones does not end last.
+  const int setup = total >= 8 * (int64_t)gridDim.x ? S::setup : 0;
+  total += (int64_t)setup * a.B * cols;
   const int64_t blocks = min((int64_t)gridDim.x, total);  // each of these has a unit at least
   if (begins && !by_column && threadIdx.x == 0) begins[blockIdx.x] = Begin{0, 0, 0, 0};
   if (blockIdx.x >= blocks) return;
@@ -605,8 +614,10 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
   // the sequence they start in
   int b = 0;
   int64_t before = 0;
+#pragma unroll 1
   for (int b0 = 0;; b0 += 32) {
-    const int64_t own = (b0 == 0 ? mine : b0 + lane < a.B ? units_of(a, b0 + lane, unit) : 0) * cols;
+    const int64_t units = b0 == 0 ? mine : b0 + lane < a.B ? units_of(a, b0 + lane, unit) : 0;
+    const int64_t own = b0 + lane < a.B ? (units + setup) * cols : 0;
     int64_t upto = own;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
@@ -635,10 +646,14 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
     const int nu = max(1, (int)(((int64_t)(len - first) + unit - 1) / unit));
     const int32_t* table = ch.table + (int64_t)b * ch.table_stride;
     keys.keep = a.keep ? a.keep + (int64_t)b * a.keep_stride : nullptr;
-    for (; u < end && u < before + (int64_t)nu * cols;) {
-      // the segment: units [k0, k1) of sequence b, query tile `col`
-      const int col = (int)quotient(u - before, nu), k0 = (int)(u - before - (int64_t)col * nu);
-      const int k1 = (int)min((int64_t)nu, k0 + (end - u));
+    const int long_nu = nu + setup;
+    for (; u < end && u < before + (int64_t)long_nu * cols;) {
+      // the segment: units [k0, k1) of sequence b, query tile `col`, on the line after its setup
+      const int col = (int)quotient(u - before, long_nu);
+      const int64_t at = before + (int64_t)col * long_nu + setup;  // its unit 0
+      const int k0 = (int)max(u - at, (int64_t)0), k1 = (int)min((int64_t)nu, end - at);
+      u = min(end, at + nu);
+      if (k1 <= 0) continue;  // the block ends before unit 0
       const int hk = col / tiles, h0 = hk * G + col % tiles * QT;
       const int nq = min(QT, G - col % tiles * QT);
       const int lo = first + k0 * unit, hi = (int)min((int64_t)len, first + (int64_t)k1 * unit);
@@ -762,15 +777,14 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
       }
       if (begins && k0 == 0 && (by_column || !whole) && threadIdx.x == 0) {
         // the block that has the query tile's last unit
-        const int64_t last = u + nu - 1, split = longer * (share + 1);
-        const int at = (int)(last < split ? quotient(last, share + 1) : longer + quotient(last - split, share));
+        const int64_t last = at + nu - 1, split = longer * (share + 1);
+        const int to = (int)(last < split ? quotient(last, share + 1) : longer + quotient(last - split, share));
         begins[by_column ? b * cols + col : (int)blockIdx.x] =
-            Begin{(int)blockIdx.x, whole ? 0 : at - (int)blockIdx.x + 1, b, col};
+            Begin{(int)blockIdx.x, whole ? 0 : to - (int)blockIdx.x + 1, b, col};
       }
-      u += k1 - k0;
       __syncthreads();  // the ring and the sums are free
     }
-    before += (int64_t)nu * cols;
+    before += (int64_t)long_nu * cols;
   }
 }
 
