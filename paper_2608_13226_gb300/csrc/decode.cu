@@ -47,8 +47,8 @@ template <> struct Type<CP_E4M3> { static constexpr int e = 1, tk = 16; using Ro
 template <> struct Type<CP_F32> { static constexpr int e = 4, tk = 8; using Row = float; };
 
 // Shape of one variant: CT cache type, DP head width it is laid out for, QT query
-// heads a pass.
-template <int CT, int DP, int QT>
+// heads a pass, SHORT whether each warp has sequences of its own (k_decode_short).
+template <int CT, int DP, int QT, bool SHORT = false>
 struct Shape {
   static constexpr int e = Type<CT>::e, tk = Type<CT>::tk;
   static constexpr int row = DP * e;                  // bytes of a row in shared memory
@@ -57,18 +57,23 @@ struct Shape {
   // Ring: as many tiles as keep two blocks on an SM, 3 at least.  Three blocks of
   // shorter rings leave the join no room beside them and wait longer: 128 ragged
   // 8-bit sequences 101 us with two, 115 with three; four 125.
-  static constexpr int fit = 100 * 1024 / (kWarps * tile);
-  static constexpr int stages = fit < 3 ? 3 : fit > 8 ? 8 : fit;
+  // Short sequences: three blocks, as registers allow, as there is more to begin
+  // than to copy.
+  static constexpr int fit = (SHORT ? 64 : 100) * 1024 / (kWarps * tile);
+  static constexpr int least = SHORT ? 2 : 3;
+  static constexpr int stages = fit < least ? least : fit > 8 ? 8 : fit;
   static constexpr int ring = kWarps * stages * tile;
-  static constexpr int extra = CT == CP_F32 ? (QT * DP + kWarps * tk * QT) * 4 : 0;
+  // float32 queries, the block's or each warp's, and each warp's weights of a tile
+  static constexpr int queries = SHORT ? kWarps : 1;
+  static constexpr int extra = CT == CP_F32 ? (queries * QT * DP + kWarps * tk * QT) * 4 : 0;
   static constexpr int smem = ring + extra;
-  static constexpr int per_sm = smem <= 110 * 1024 ? 2 : 1;
+  static constexpr int per_sm = SHORT && smem <= 70 * 1024 ? 3 : smem <= 110 * 1024 ? 2 : 1;
   static constexpr int part = QT * (DP + 2);  // floats of a partial result
   // What beginning and merging a segment costs, in units of 64 keys: about 3 us, in
   // which a block takes 72 KB.
   static constexpr int setup = 72 * 1024 / (2 * kUnit * row) < 1 ? 1 : 72 * 1024 / (2 * kUnit * row);
   static constexpr int pitch = DP + 4;        // floats of a query in the merge: the lanes' banks differ
-  static_assert(kWarps * QT * pitch * 4 <= ring, "the merge reuses the ring");
+  static_assert(SHORT || kWarps * QT * pitch * 4 <= ring, "the merge reuses the ring");
 };
 
 // What the blocks leave for the join: the block that a query tile of sequence b
@@ -173,8 +178,9 @@ __device__ __forceinline__ int units_of(const DecodeArgs& a, int b, int unit) {
 }
 
 // The keys that a warp takes from its part [lo, hi) of a segment, a tile at a
-// time: every kWarps-th run of `tk` keys, or of the marked ones among them.
-template <int TK>
+// time: every SIDE-th run of `tk` keys, or of the marked ones among them (SIDE warps
+// share a segment).
+template <int TK, int SIDE>
 struct Keys {
   int next, hi, lane;
   const uint8_t* keep;  // the sequence's marks, or null
@@ -192,7 +198,7 @@ struct Keys {
     next = lo + warp * (keep ? kChunk : TK);
     if (keep) {
 #pragma unroll
-      for (int i = 0; i < kMarks; ++i) load(i, next + i * kWarps * kChunk);
+      for (int i = 0; i < kMarks; ++i) load(i, next + i * SIDE * kChunk);
     }
   }
   // How many keys the next tile has (0: no more); this lane's, or -1.
@@ -200,7 +206,7 @@ struct Keys {
     if (!keep) {
       const int n = min(max(hi - next, 0), TK);
       *key = lane < n ? next + lane : -1;
-      next += kWarps * TK;
+      next += SIDE * TK;
       return n;
     }
     while (count < TK && next < hi) {
@@ -216,8 +222,8 @@ struct Keys {
         mark[i][0] = mark[i + 1][0];
         mark[i][1] = mark[i + 1][1];
       }
-      load(kMarks - 1, next + kMarks * kWarps * kChunk);
-      next += kWarps * kChunk;
+      load(kMarks - 1, next + kMarks * SIDE * kChunk);
+      next += SIDE * kChunk;
     }
     __syncwarp();
     const int n = min(count, TK);
@@ -233,9 +239,9 @@ struct Keys {
 // Lane (g, t) = (lane / 4, lane % 4) has the scores of keys g and g + 8 and
 // queries 2 t, 2 t + 1 of each group of 8, and the same queries' outputs at
 // components 16 i + g, + 8 (8-bit caches: 16 i + 2 g, + 1).
-template <int CT, int DP, int QT>
+template <int CT, int DP, int QT, bool SHORT>
 struct Math {
-  using S = Shape<CT, DP, QT>;
+  using S = Shape<CT, DP, QT, SHORT>;
   static constexpr int NT = QT / 8, KS = DP / 16;
   uint32_t q[NT][KS][2];
   float o[NT][KS][4];
@@ -420,6 +426,27 @@ struct Math {
     }
   }
 
+  // The outputs over their sums, for a warp that has all keys: out(query, component,
+  // value), and lse(query, value).
+  template <typename Out, typename Lse>
+  __device__ __forceinline__ void write(float vs, Out out, Lse lse) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int d = 4; d < 32; d *= 2) l[n][i] += __shfl_xor_sync(~0u, l[n][i], d);
+        const int query = 8 * n + 2 * t + i;
+        const float by = vs / l[n][i];
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          out(query, 16 * k + (CT == CP_E4M3 ? 2 * g : g), l[n][i] == 0.0f ? 0.0f : o[n][k][i] * by);
+          out(query, 16 * k + (CT == CP_E4M3 ? 2 * g + 1 : g + 8), l[n][i] == 0.0f ? 0.0f : o[n][k][i + 2] * by);
+        }
+        if (g == 0) lse(query, l[n][i] == 0.0f ? -INFINITY : (m[n][i] + log2f(l[n][i])) * kLn2);
+      }
+  }
+
   // This warp's maximum and sum of each query.
   __device__ __forceinline__ void finish(float* sm, float* sl) {
 #pragma unroll
@@ -451,9 +478,9 @@ struct Math {
 
 // The same in float32 on the FMA units: 4 lanes a key for the scores, then the
 // components spread over the lanes.
-template <int DP, int QT>
-struct Math<CP_F32, DP, QT> {
-  using S = Shape<CP_F32, DP, QT>;
+template <int DP, int QT, bool SHORT>
+struct Math<CP_F32, DP, QT, SHORT> {
+  using S = Shape<CP_F32, DP, QT, SHORT>;
   static constexpr int V = DP / 32;  // components of a lane
   float o[QT][V];
   float m[QT], l[QT];
@@ -461,12 +488,15 @@ struct Math<CP_F32, DP, QT> {
 
   __device__ __forceinline__ void start(const DecodeArgs& a, int b, int hk, int h0, int nq, char* extra,
                                         int warp, int lane) {
-    float* sq = (float*)extra;  // the block's queries; each warp fills a part
-    for (int i = warp * 32 + lane; i < QT * DP; i += kThreads) {
+    float* sq = queries(extra, warp);  // the block's, of which each warp fills a part, or the warp's
+    for (int i = SHORT ? lane : warp * 32 + lane; i < QT * DP; i += SHORT ? 32 : kThreads) {
       const int n = i / DP, d = i % DP;
       sq[i] = n < nq && d < a.cache.D ? ((const float*)a.q)[b * a.q_b + (int64_t)(h0 + n) * a.q_h + d] : 0.0f;
     }
-    __syncthreads();
+    if (SHORT)
+      __syncwarp();
+    else
+      __syncthreads();
     sc = a.scale * (a.cache.k_scale ? a.cache.k_scale[hk] : 1.0f) * kLog2e;
 #pragma unroll
     for (int n = 0; n < QT; ++n) {
@@ -477,6 +507,7 @@ struct Math<CP_F32, DP, QT> {
     }
   }
 
+  __device__ static float* queries(char* extra, int warp) { return (float*)extra + (SHORT ? warp * QT * DP : 0); }
   // Component of this lane's i-th: consecutive float4 (float2 for heads of 64).
   __device__ static int component(int i, int lane) {
     return V == 2 ? 2 * lane + i : 128 * (i / 4) + 4 * lane + i % 4;
@@ -484,8 +515,8 @@ struct Math<CP_F32, DP, QT> {
 
   __device__ __forceinline__ void tile(uint32_t at, uint32_t valid, char* extra, int warp,
                                        int lane) {
-    const float* sq = (const float*)extra;
-    float* sp = (float*)extra + QT * DP + warp * S::tk * QT;
+    const float* sq = queries(extra, warp);
+    float* sp = (float*)extra + S::queries * QT * DP + warp * S::tk * QT;
     const int r = lane / 4, sub = lane % 4;
     float s[QT];
 #pragma unroll
@@ -556,6 +587,18 @@ struct Math<CP_F32, DP, QT> {
     __syncwarp();
   }
 
+  template <typename Out, typename Lse>
+  __device__ __forceinline__ void write(float vs, Out out, Lse lse) {
+#pragma unroll
+    for (int n = 0; n < QT; ++n) {
+#pragma unroll
+      for (int d = 4; d < 32; d *= 2) l[n] += __shfl_xor_sync(~0u, l[n], d);
+      const float by = vs / l[n];
+#pragma unroll
+      for (int i = 0; i < V; ++i) out(n, component(i, threadIdx.x % 32), l[n] == 0.0f ? 0.0f : o[n][i] * by);
+      if (threadIdx.x % 32 == 0) lse(n, l[n] == 0.0f ? -INFINITY : (m[n] + log2f(l[n])) * kLn2);
+    }
+  }
   __device__ __forceinline__ void finish(float* sm, float* sl) {
 #pragma unroll
     for (int n = 0; n < QT; ++n) {
@@ -575,6 +618,90 @@ struct Math<CP_F32, DP, QT> {
   }
 };
 
+// A warp's keys [lo, hi) of sequence b for the queries from h0 on: their tiles through
+// its ring into `math`.
+template <int CT, int DP, int QT, bool SHORT, typename K>
+__device__ __forceinline__ void math_of_keys(const DecodeArgs& a, const Rows& rows, K& keys, const int32_t* table, int lo,
+                                             int hi, int hk, int b, int h0, int nq, int warp, int lane, uint32_t ring,
+                                             uint32_t* s_valid, char* extra, Math<CT, DP, QT, SHORT>& math) {
+  using S = Shape<CT, DP, QT, SHORT>;
+  const Cache& ch = a.cache;
+  const int chunks = ch.D * S::e / 16;  // of a row that is there
+  const char* kp = (const char*)ch.k + (int64_t)hk * ch.head_stride * S::e;
+  const char* vp = (const char*)ch.v + (int64_t)hk * ch.head_stride * S::e;
+  if (chunks < S::cpr)  // components beyond the head's: the products run over zeros
+    for (int i = lane; i < S::stages * S::tk * (S::cpr - chunks); i += 32) {
+      const int c = chunks + i % (S::cpr - chunks), r = i / (S::cpr - chunks);
+      const uint32_t at = ring + r / S::tk * S::tile + r % S::tk * S::row + 16 * (c ^ swizzle<CT, S::cpr>(r % S::tk));
+      asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
+    }
+
+  keys.start(lo, hi, SHORT ? 0 : warp);
+  int key, n_next = keys.take(&key), page = -1, slot_of = 0, issued = 0;
+  auto look = [&] {
+    const int p = (int)((uint64_t)(uint32_t)key * rows.mul >> 31 >> rows.div_shift);
+    page = key >= 0 ? table[p] : -1;
+    slot_of = key - p * ch.page_size;
+  };
+  auto issue = [&] {
+    if (n_next > 0) {
+      const int slot = issued % S::stages;
+      bool ok = key >= 0;
+      if (ok && (page < 0 || page >= ch.pages)) {
+        if (a.status) set_status(a.status, CP_EINVAL);
+        ok = false;
+      }
+      const uint32_t mine = ok ? (uint32_t)page * rows.page + (uint32_t)slot_of * rows.slot : 0;
+      const uint32_t valid = __ballot_sync(~0u, ok);
+      if (lane == 0) s_valid[slot] = valid;
+      // 32 chunks at a time: some rows side by side, or a part of one
+      constexpr int side = S::cpr >= 32 ? 1 : 32 / S::cpr;
+      const int c = lane % S::cpr, r0 = lane / S::cpr;
+      const uint32_t to = ring + slot * S::tile + r0 * S::row + 16 * (c ^ swizzle<CT, S::cpr>(r0));
+      auto each = [&](auto copy) {
+#pragma unroll
+        for (int i = 0; i < S::tk * S::cpr / 32; ++i) {
+          constexpr int turns = S::cpr > 32 ? S::cpr / 32 : 1;  // copies of a row
+          const int r = i / turns * side, more = i % turns * 512;
+          const uint64_t off = (uint64_t)__shfl_sync(~0u, mine, r + r0) * rows.scale + (16 * c + more);
+          const uint32_t at = (to ^ (16 * swizzle<CT, S::cpr>(r))) + r * S::row + more;
+          copy(at, off, r + r0, c + more / 16);
+        }
+      };
+      if (valid == (1u << S::tk) - 1 && chunks == S::cpr) {
+        each([&](uint32_t at, uint64_t off, int, int) {
+          copy16(at, kp + off);
+          copy16(at + S::tk * S::row, vp + off);
+        });
+      } else {
+        each([&](uint32_t at, uint64_t off, int r, int c) {
+          const bool there = valid >> r & 1;
+          if (c < chunks) {
+            copy16(at, kp + (there ? off : 0), there);
+            copy16(at + S::tk * S::row, vp + (there ? off : 0), there);
+          }
+        });
+      }
+      ++issued;
+      n_next = keys.take(&key);
+      look();
+    }
+    copy_commit();
+  };
+  look();
+  __syncwarp();
+#pragma unroll 1
+  for (int i = 0; i < S::stages - 1; ++i) issue();
+  math.start(a, b, hk, h0, nq, extra, warp, lane);
+  for (int i = 0; i < issued; ++i) {
+    copy_wait<S::stages - 2>();
+    __syncwarp();  // tile i is there for every lane, and tile i - 1 done with
+    issue();
+    const int slot = i % S::stages;
+    math.tile(ring + slot * S::tile, s_valid[slot], extra, warp, lane);
+  }
+}
+
 template <int CT, int DP, int QT>
 __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, int unit, int tiles, float* parts,
                                                      Begin* begins, int by_column) {
@@ -590,7 +717,6 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
   const Cache& ch = a.cache;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int G = a.Hq / ch.heads, cols = ch.heads * tiles;
-  const int chunks = ch.D * S::e / 16;  // of a row that is there
 
   // this block's units of the line
   const int64_t mine = lane < a.B ? units_of(a, lane, unit) : 0;
@@ -636,7 +762,7 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
 
   const uint32_t ring = smem_addr(smem) + warp * S::stages * S::tile;
   char* extra = smem + S::ring;
-  Keys<S::tk> keys;
+  Keys<S::tk, kWarps> keys;
   keys.lane = lane;
   keys.queue = s_queue[warp];
 
@@ -657,81 +783,9 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
       const int hk = col / tiles, h0 = hk * G + col % tiles * QT;
       const int nq = min(QT, G - col % tiles * QT);
       const int lo = first + k0 * unit, hi = (int)min((int64_t)len, first + (int64_t)k1 * unit);
-      const char* kp = (const char*)ch.k + (int64_t)hk * ch.head_stride * S::e;
-      const char* vp = (const char*)ch.v + (int64_t)hk * ch.head_stride * S::e;
-
-      if (chunks < S::cpr)  // components beyond the head's: the products run over zeros
-        for (int i = lane; i < S::stages * S::tk * (S::cpr - chunks); i += 32) {
-          const int c = chunks + i % (S::cpr - chunks), r = i / (S::cpr - chunks);
-          const uint32_t at = ring + r / S::tk * S::tile + r % S::tk * S::row + 16 * (c ^ swizzle<CT, S::cpr>(r % S::tk));
-          asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
-        }
-
-      keys.start(lo, hi, warp);
-      int key, n_next = keys.take(&key), page = -1, slot_of = 0, issued = 0;
-      auto look = [&] {
-        const int p = (int)((uint64_t)(uint32_t)key * rows.mul >> 31 >> rows.div_shift);
-        page = key >= 0 ? table[p] : -1;
-        slot_of = key - p * ch.page_size;
-      };
-      auto issue = [&] {
-        if (n_next > 0) {
-          const int slot = issued % S::stages;
-          bool ok = key >= 0;
-          if (ok && (page < 0 || page >= ch.pages)) {
-            if (a.status) set_status(a.status, CP_EINVAL);
-            ok = false;
-          }
-          const uint32_t mine = ok ? (uint32_t)page * rows.page + (uint32_t)slot_of * rows.slot : 0;
-          const uint32_t valid = __ballot_sync(~0u, ok);
-          if (lane == 0) s_valid[warp][slot] = valid;
-          // 32 chunks at a time: some rows side by side, or a part of one
-          constexpr int side = S::cpr >= 32 ? 1 : 32 / S::cpr;
-          const int c = lane % S::cpr, r0 = lane / S::cpr;
-          const uint32_t to = ring + slot * S::tile + r0 * S::row + 16 * (c ^ swizzle<CT, S::cpr>(r0));
-          auto each = [&](auto copy) {
-#pragma unroll
-            for (int i = 0; i < S::tk * S::cpr / 32; ++i) {
-              constexpr int turns = S::cpr > 32 ? S::cpr / 32 : 1;  // copies of a row
-              const int r = i / turns * side, more = i % turns * 512;
-              const uint64_t off = (uint64_t)__shfl_sync(~0u, mine, r + r0) * rows.scale + (16 * c + more);
-              const uint32_t at = (to ^ (16 * swizzle<CT, S::cpr>(r))) + r * S::row + more;
-              copy(at, off, r + r0, c + more / 16);
-            }
-          };
-          if (valid == (1u << S::tk) - 1 && chunks == S::cpr) {
-            each([&](uint32_t at, uint64_t off, int, int) {
-              copy16(at, kp + off);
-              copy16(at + S::tk * S::row, vp + off);
-            });
-          } else {
-            each([&](uint32_t at, uint64_t off, int r, int c) {
-              const bool there = valid >> r & 1;
-              if (c < chunks) {
-                copy16(at, kp + (there ? off : 0), there);
-                copy16(at + S::tk * S::row, vp + (there ? off : 0), there);
-              }
-            });
-          }
-          ++issued;
-          n_next = keys.take(&key);
-          look();
-        }
-        copy_commit();
-      };
-      look();
-      __syncwarp();
-#pragma unroll 1
-      for (int i = 0; i < S::stages - 1; ++i) issue();
-      Math<CT, DP, QT> math;
-      math.start(a, b, hk, h0, nq, extra, warp, lane);
-      for (int i = 0; i < issued; ++i) {
-        copy_wait<S::stages - 2>();
-        __syncwarp();  // tile i is there for every lane, and tile i - 1 done with
-        issue();
-        const int slot = i % S::stages;
-        math.tile(ring + slot * S::tile, s_valid[warp][slot], extra, warp, lane);
-      }
+      Math<CT, DP, QT, false> math;
+      math_of_keys<CT, DP, QT, false>(a, rows, keys, table, lo, hi, hk, b, h0, nq, warp, lane, ring, s_valid[warp], extra,
+                                      math);
       math.finish(s_m[warp], s_l[warp]);
       copy_wait<0>();
       __syncthreads();
@@ -785,6 +839,48 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
       __syncthreads();  // the ring and the sums are free
     }
     before += (int64_t)long_nu * cols;
+  }
+}
+
+// Sequences of up to 4 units and more query tiles than blocks: a warp takes a tile
+// alone, and then another, so that one's beginning (table, keys, queries: three trips
+// to memory) runs beside the others' and nothing is merged.
+template <int CT, int DP, int QT>
+__global__ void __launch_bounds__(kThreads) k_decode_short(DecodeArgs a, Rows rows, int tiles, int64_t columns) {
+  using S = Shape<CT, DP, QT, true>;
+  using Row = typename Type<CT>::Row;
+  extern __shared__ __align__(1024) char smem[];
+  __shared__ int s_queue[kWarps][kQueue];
+  __shared__ uint32_t s_valid[kWarps][S::stages];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
+  const Cache& ch = a.cache;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int G = a.Hq / ch.heads, cols = ch.heads * tiles;
+  const uint32_t ring = smem_addr(smem) + warp * S::stages * S::tile;
+  Keys<S::tk, 1> keys;
+  keys.lane = lane;
+  keys.queue = s_queue[warp];
+  for (int64_t c = (int64_t)blockIdx.x * kWarps + warp; c < columns; c += (int64_t)gridDim.x * kWarps) {
+    const int b = (int)quotient(c, cols), col = (int)(c - (int64_t)b * cols);
+    const int hk = col / tiles, h0 = hk * G + col % tiles * QT;
+    const int nq = min(QT, G - col % tiles * QT);
+    int first, len;
+    keys_of(a, b, &first, &len);
+    keys.keep = a.keep ? a.keep + (int64_t)b * a.keep_stride : nullptr;
+    Math<CT, DP, QT, true> math;
+    math_of_keys<CT, DP, QT, true>(a, rows, keys, ch.table + (int64_t)b * ch.table_stride, first, len, hk, b, h0, nq, warp,
+                                   lane, ring, s_valid[warp], smem + S::ring, math);
+    copy_wait<0>();
+    math.write(
+        ch.v_scale ? ch.v_scale[hk] : 1.0f,
+        [&](int n, int d, float x) {
+          if (n < nq && d < ch.D) ((Row*)a.out)[b * a.o_b + (int64_t)(h0 + n) * a.o_h + d] = from_f32<Row>(x);
+        },
+        [&](int n, float x) {
+          if (n < nq && a.lse) a.lse[(int64_t)b * a.Hq + h0 + n] = x;
+        });
+    __syncwarp();  // the ring is free
   }
 }
 
@@ -906,10 +1002,10 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   using S = Shape<CT, DP, QT>;
   const int G = a.Hq / a.cache.heads, tiles = (G + QT - 1) / QT;
   // Sequences of at most 4 units are not cut: the join would cost more.
-  const bool cut = a.cache.capacity > 4 * kUnit;
+  const int64_t most = a.window > 0 && a.window < a.cache.capacity ? a.window : a.cache.capacity;  // keys of one
+  const bool cut = most > 4 * kUnit;
   const int unit = cut ? kUnit : 4 * kUnit;
-  const int64_t line = (int64_t)a.B * a.cache.heads * tiles *
-                       (a.cache.capacity < 1 ? 1 : ((int64_t)a.cache.capacity + unit - 1) / unit);
+  const int64_t line = (int64_t)a.B * a.cache.heads * tiles * (most < 1 ? 1 : (most + unit - 1) / unit);
   if (line > (int64_t)1 << 52) return CP_EUNSUPPORTED;  // units times blocks stay within 64 bits
 
   // rows of the cache in units that fit 32 bits
@@ -928,6 +1024,7 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   CP_TRY_STATUS(device_info(&di));
   int64_t grid = (int64_t)di.sm_count * S::per_sm;
   if (grid > kMaxBlocks) grid = kMaxBlocks;
+  const int64_t all = grid;
   if (grid > line) grid = line;
   const int64_t columns = (int64_t)a.B * ch.heads * tiles;
   const bool by_column = columns <= grid;
@@ -947,6 +1044,17 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   cfg.stream = s;
   cfg.attrs = &early;
   cfg.numAttrs = 1;
+  if (!cut && columns > all) {
+    using Short = Shape<CT, DP, QT, true>;
+    static std::atomic<uint64_t> short_allowed{0};
+    CP_TRY_STATUS(allow_smem_once((const void*)k_decode_short<CT, DP, QT>, Short::smem, "decode: shared memory",
+                                  &short_allowed));
+    const int64_t room = (int64_t)di.sm_count * Short::per_sm, wanted = (columns + kWarps - 1) / kWarps;
+    cfg.gridDim = dim3((unsigned)(wanted < room ? wanted : room));
+    cfg.dynamicSmemBytes = Short::smem;
+    note_launch();
+    return cuda_status(cudaLaunchKernelEx(&cfg, k_decode_short<CT, DP, QT>, a, rows, tiles, columns), "decode: short");
+  }
   note_launch();
   CP_TRY_STATUS(cuda_status(cudaLaunchKernelEx(&cfg, k_decode<CT, DP, QT>, a, rows, unit, tiles, parts,
                                                cut ? begins : (Begin*)nullptr, (int)by_column),

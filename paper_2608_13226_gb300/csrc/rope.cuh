@@ -19,13 +19,30 @@ __device__ __forceinline__ uint64_t rope_turns(double inv_freq) {
   return __double2ull_rz(t * 18446744073709551616.0);
 }
 
+// (cos, sin) of the angle, times the scale.  The turn's fraction is cut to 32 bits
+// (1.5e-9 rad), its nearest quarter taken off as an integer, and the rest, within
+// pi / 4, goes into the series of sine and cosine up to x^9 / 9! and x^10 / 10!
+// (what is left out is under 2e-9): about 6e-8 of error from roundings, in a third
+// of the instructions of a call that reduces its argument itself.
 __device__ __forceinline__ void rope_unit(uint64_t turns, int64_t pos, const Rope& r, float* c,
                                           float* s) {
-  const int64_t a = (int64_t)(turns * (uint64_t)pos);
-  float sn, cs;
-  sincospif(__ll2float_rn(a) * 0x1p-63f, &sn, &cs);  // 2 a / 2^64 half turns, in [-1, 1]
-  *c = cs * r.scale;
-  *s = (r.back ? -sn : sn) * r.scale;
+  const uint32_t a = (uint32_t)((turns * (uint64_t)pos) >> 32);
+  const uint32_t quarter = (a + 0x20000000u) >> 30;
+  const float x = (float)(int32_t)(a - (quarter << 30)) * (float)(1.57079632679489661923 / 1073741824.0);
+  const float y = x * x;
+  float sn = fmaf(y, 1.0f / 362880.0f, -1.0f / 5040.0f);
+  sn = fmaf(y, sn, 1.0f / 120.0f);
+  sn = fmaf(y, sn, -1.0f / 6.0f);
+  sn = fmaf(x * y, sn, x);
+  float cs = fmaf(y, -1.0f / 3628800.0f, 1.0f / 40320.0f);
+  cs = fmaf(y, cs, -1.0f / 720.0f);
+  cs = fmaf(y, cs, 1.0f / 24.0f);
+  cs = fmaf(y, cs, -0.5f);
+  cs = fmaf(y, cs, 1.0f);
+  const bool odd = quarter & 1;
+  const float u = odd ? sn : cs, v = odd ? cs : sn;
+  *c = ((quarter + 1) & 2 ? -u : u) * r.scale;
+  *s = ((quarter & 2) != 0) != (r.back != 0) ? -v * r.scale : v * r.scale;
 }
 
 template <typename T> __device__ __forceinline__ T from_f32(float x);
