@@ -842,8 +842,7 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
   }
 }
 
-// Sequences of up to 4 units and more query tiles than blocks: a warp takes a tile
-// alone, and then another, so that one's beginning (table, keys, queries: three trips
+// Many short sequences: a warp takes a query tile alone, and then another, so that one's beginning (table, keys, queries: three trips
 // to memory) runs beside the others' and nothing is merged.
 template <int CT, int DP, int QT>
 __global__ void __launch_bounds__(kThreads) k_decode_short(DecodeArgs a, Rows rows, int tiles, int64_t columns) {
@@ -1044,7 +1043,13 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   cfg.stream = s;
   cfg.attrs = &early;
   cfg.numAttrs = 1;
-  if (!cut && columns > all) {
+  // Many short sequences: a warp a query tile, up to 64 keys for every third of the
+  // blocks' number that there are tiles, and 64 more.  us with blocks / with warps,
+  // 7 queries a head of 128: 320 tiles of up to 300 keys 17 / 16, of 500 18 / 26; 640
+  // of 300 26 / 17, of 500 38 / 38, of 1000 62 / 69; 1600 of 300 46 / 28, of 500 79 /
+  // 65, of 1000 138 / 122; 8 bits: 640 of 500 30 / 27, of 1000 45 / 50; 1600 of 1000
+  // 97 / 67.  Longer ones have not been measured.
+  if (columns > all && most <= 16 * kUnit && most * all <= kUnit * (3 * columns + all)) {
     using Short = Shape<CT, DP, QT, true>;
     static std::atomic<uint64_t> short_allowed{0};
     CP_TRY_STATUS(allow_smem_once((const void*)k_decode_short<CT, DP, QT>, Short::smem, "decode: shared memory",

@@ -379,6 +379,16 @@ def test_decode_lengths(cdt, scales):
 
 
 @pytest.mark.parametrize("cdt,scales", TYPES)
+@pytest.mark.parametrize("Hq,H,D,page", [(14, 2, 128, 16), (2, 2, 64, 7), (12, 1, 80, 100), (4, 1, 256, 1), (20, 1, 96, 64)])
+def test_decode_many_short(Hq, H, D, page, cdt, scales):
+    """More query tiles than blocks: whole, with marks, a window that makes long ones short."""
+    lens = [0, 1, 2, 15, 16, 17, 31, 100, 7, 0] * 40
+    check_decode(D, lens, page, Hq, H, D, cdt, scales=scales, junk=math.nan)
+    check_decode(D + 1, [3 * n for n in lens], page, Hq, H, D, cdt, scales=scales, keep=0.4, junk=math.nan, heads_first=True)
+    check_decode(D + 2, [7 * n for n in lens], page, Hq, H, D, cdt, scales=scales, window=33, junk=math.nan, q_view=True)
+
+
+@pytest.mark.parametrize("cdt,scales", TYPES)
 def test_decode_sharp_and_scaled(cdt, scales):
     """Scores in the hundreds (one key takes all), all alike, and a negative scale."""
     check_decode(1, [400, 1], 16, 8, 2, 64, cdt, scales=scales, sharp=300.0)
