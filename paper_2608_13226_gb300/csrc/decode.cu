@@ -711,9 +711,7 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
   __shared__ int s_queue[kWarps][kQueue];
   __shared__ uint32_t s_valid[kWarps][S::stages];
   __shared__ float s_m[kWarps][QT], s_l[kWarps][QT], s_f[kWarps][QT], s_top[QT], s_sum[QT];
-  // the join may come to the SMs now and wait there; what ran before this is waited for
-  asm volatile("griddepcontrol.launch_dependents;");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  wait_for_stream();
   const Cache& ch = a.cache;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int G = a.Hq / ch.heads, cols = ch.heads * tiles;
@@ -851,8 +849,7 @@ __global__ void __launch_bounds__(kThreads) k_decode_short(DecodeArgs a, Rows ro
   extern __shared__ __align__(1024) char smem[];
   __shared__ int s_queue[kWarps][kQueue];
   __shared__ uint32_t s_valid[kWarps][S::stages];
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;");
+  wait_for_stream();
   const Cache& ch = a.cache;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int G = a.Hq / ch.heads, cols = ch.heads * tiles;
@@ -913,8 +910,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_decode_join(DecodeArgs a, i
   constexpr int V = DP / 32;
   constexpr int kFirst = 4;  // parts that a warp loads before it knows their weights
   __shared__ float s_o[kJoinWarps][DP];
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;");
+  // What follows comes to the SMs once the parts are there: while they are being
+  // made, its blocks would be in their way (one scene 7.7 us a call, else 8.7).
+  wait_for_stream(false);
   const Begin x = begins[blockIdx.x];
   if (x.blocks == 0) return;
   const int G = a.Hq / a.cache.heads, hk = x.col / tiles, h0 = hk * G + x.col % tiles * QT;
@@ -1031,18 +1029,6 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   float* parts = (float*)((char*)a.ws + kMaxBlocks * sizeof(Begin));
   static std::atomic<uint64_t> allowed{0};
   CP_TRY_STATUS(allow_smem_once((const void*)k_decode<CT, DP, QT>, S::smem, "decode: shared memory", &allowed));
-  // Both launches may begin before what precedes them has ended: their blocks then
-  // wait on the device, and not for a launch after it.
-  cudaLaunchAttribute early{};
-  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  early.val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)grid);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = S::smem;
-  cfg.stream = s;
-  cfg.attrs = &early;
-  cfg.numAttrs = 1;
   // Many short sequences: a warp a query tile, up to 64 keys for every third of the
   // blocks' number that there are tiles, and 64 more.  us with blocks / with warps,
   // 7 queries a head of 128: 320 tiles of up to 300 keys 17 / 16, of 500 18 / 26; 640
@@ -1055,14 +1041,12 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
     CP_TRY_STATUS(allow_smem_once((const void*)k_decode_short<CT, DP, QT>, Short::smem, "decode: shared memory",
                                   &short_allowed));
     const int64_t room = (int64_t)di.sm_count * Short::per_sm, wanted = (columns + kWarps - 1) / kWarps;
-    cfg.gridDim = dim3((unsigned)(wanted < room ? wanted : room));
-    cfg.dynamicSmemBytes = Short::smem;
-    note_launch();
-    return cuda_status(cudaLaunchKernelEx(&cfg, k_decode_short<CT, DP, QT>, a, rows, tiles, columns), "decode: short");
+    return cuda_status(launch_early(k_decode_short<CT, DP, QT>, dim3((unsigned)(wanted < room ? wanted : room)), kThreads,
+                                    Short::smem, s, a, rows, tiles, columns),
+                       "decode: short");
   }
-  note_launch();
-  CP_TRY_STATUS(cuda_status(cudaLaunchKernelEx(&cfg, k_decode<CT, DP, QT>, a, rows, unit, tiles, parts,
-                                               cut ? begins : (Begin*)nullptr, (int)by_column),
+  CP_TRY_STATUS(cuda_status(launch_early(k_decode<CT, DP, QT>, dim3((unsigned)grid), kThreads, S::smem, s, a, rows, unit,
+                                         tiles, parts, cut ? begins : nullptr, (int)by_column),
                             "decode"));
   if (!cut) return CP_OK;
   // about so many parts a query tile, and the join's queries side by side for it
@@ -1070,13 +1054,9 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   const int queries = G < QT ? G : QT;
   int side = share <= 4 ? 8 : share <= 12 ? 2 : 1;
   while (side > 1 && side / 2 >= queries) side /= 2;
-  cfg.gridDim = dim3((unsigned)(by_column ? columns : grid), (unsigned)(queries + side - 1) / side);
-  cfg.blockDim = dim3(32 * kJoinWarps);
-  cfg.dynamicSmemBytes = 0;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_decode_join<CT, DP, QT>, a, tiles, side, (const float*)parts,
-                                           (const Begin*)begins);
-  note_launch();
-  return cuda_status(e, "decode: join");
+  const dim3 joins((unsigned)(by_column ? columns : grid), (unsigned)(queries + side - 1) / side);
+  return cuda_status(launch_early(k_decode_join<CT, DP, QT>, joins, 32 * kJoinWarps, 0, s, a, tiles, side, parts, begins),
+                     "decode: join");
 }
 
 template <int CT, int DP>

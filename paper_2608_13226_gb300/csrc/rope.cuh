@@ -9,6 +9,15 @@
 
 namespace cp {
 
+// What ran before on the stream has ended and is seen from here on; what comes after
+// may begin to wait likewise (launch_early), at once or from then on.  Every thread
+// of the grid calls it before it reads or writes memory.
+__device__ __forceinline__ void wait_for_stream(bool at_once = true) {
+  if (at_once) asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (!at_once) asm volatile("griddepcontrol.launch_dependents;");
+}
+
 // A pair's speed as the fraction of a turn that one position takes, in units
 // of 2^-64 turns.  Whole turns drop out, and so they do of position * speed in
 // 64-bit integers: the angle of any position is off by no more than the speed's

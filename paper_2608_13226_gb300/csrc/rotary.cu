@@ -411,6 +411,7 @@ struct RotaryJob {
 
 template <typename T, int V>
 __global__ void __launch_bounds__(kThreads, kBlocks) k_rotary(RotaryArgs a, Tiling tl, int rows) {
+  wait_for_stream();
   RotaryJob<T> job{a, rows};
   run_rows<T, T, V, false>(job, a.rope, tl, a.D, a.B * a.T);
 }
@@ -478,6 +479,7 @@ struct AppendJob {
 template <typename T, typename C, int V, bool SCALED>
 __global__ void __launch_bounds__(kThreads, kBlocks) k_cache_append(AppendArgs a, Tiling tl) {
   __shared__ int64_t s_row[kChunk];
+  wait_for_stream();
   if (a.new_lens)
     for (int64_t b = (int64_t)blockIdx.x * kThreads + threadIdx.x; b < a.B; b += (int64_t)gridDim.x * kThreads) {
       const int64_t n = (int64_t)a.lens[b] + (a.starts ? a.starts[b + 1] - a.starts[b] : 1);
@@ -543,8 +545,7 @@ static int rotary(const RotaryArgs& a, int rows, cudaStream_t s) {
   const Tiling t = tiling(a.rope.half, a.D, V, rows);
   const size_t smem = smem_of(t, V * sizeof(T));
   CP_TRY_STATUS(allow_smem_once((const void*)k_rotary<T, V>, kMostSmem, "rotary: shared memory", &allowed));
-  k_rotary<T, V><<<grid, kThreads, smem, s>>>(a, t, rows);
-  return launch_status("rotary");
+  return cuda_status(launch_early(k_rotary<T, V>, dim3(grid), kThreads, smem, s, a, t, rows), "rotary");
 }
 
 int launch_rotary(const RotaryArgs& args, int dtype, cudaStream_t s) {
@@ -590,8 +591,7 @@ static int append(const AppendArgs& a, cudaStream_t s) {
   const Tiling t = tiling(a.rope.half, a.cache.D, V, a.q.heads + 2 * a.cache.heads);
   auto kernel = k_cache_append<T, C, V, SCALED>;
   CP_TRY_STATUS(allow_smem_once((const void*)kernel, kMostSmem, "cache append: shared memory", &allowed));
-  kernel<<<grid, kThreads, smem_of(t, V * sizeof(T)), s>>>(a, t);
-  return launch_status("cache append");
+  return cuda_status(launch_early(kernel, dim3(grid), kThreads, smem_of(t, V * sizeof(T)), s, a, t), "cache append");
 }
 template <typename T, typename C, int V>
 static int append_scaled(const AppendArgs& a, cudaStream_t s) {

@@ -76,6 +76,26 @@ struct DecodeArgs {
   void* ws;
   int32_t* status;
 };
+// A launch that may begin before what precedes it on the stream has ended: its
+// blocks come to the SMs and wait there (wait_for_stream, first of all), so that its
+// latency is spent beside the other's last blocks.
+template <typename... Params, typename... Args>
+cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t s,
+                         Args... args) {
+  cudaLaunchAttribute early{};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = &early;
+  cfg.numAttrs = 1;
+  note_launch();
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
+
 size_t decode_ws_bytes(int64_t B, int64_t Hq, int64_t heads, int64_t D, int cache_dtype);
 int launch_decode(const DecodeArgs& a, int cache_dtype, cudaStream_t s);
 
