@@ -193,7 +193,7 @@ int coverprune_decode_workspace_size(int64_t B, int64_t Hq, const cp_cache* cach
   if (!bytes) return CP_EINVAL;
   Cache c;
   CP_TRY_STATUS(check_decode(B, Hq, cache, false, &c));
-  *bytes = decode_ws_bytes(B, Hq, c.heads, c.D, cache->dtype);
+  *bytes = decode_ws_bytes(Hq, c.heads, c.D, cache->dtype);
   return CP_OK;
 }
 
@@ -213,7 +213,7 @@ int coverprune_decode_attention(const void* q, const int64_t* q_stride, int dtyp
       !aligned(status, 4))
     return CP_EINVAL;
   if (!ws || !aligned(ws, 256) ||
-      ws_bytes < decode_ws_bytes(B, Hq, a.cache.heads, a.cache.D, cache->dtype))
+      ws_bytes < decode_ws_bytes(Hq, a.cache.heads, a.cache.D, cache->dtype))
     return CP_EWORKSPACE;
   a.q = q;
   a.q_b = q_stride[0];

@@ -96,7 +96,24 @@ cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, int threads, size
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
 }
 
-size_t decode_ws_bytes(int64_t B, int64_t Hq, int64_t heads, int64_t D, int cache_dtype);
+size_t decode_ws_bytes(int64_t Hq, int64_t heads, int64_t D, int cache_dtype);
 int launch_decode(const DecodeArgs& a, int cache_dtype, cudaStream_t s);
+int launch_decode_bf16(const DecodeArgs& a, cudaStream_t s);
+int launch_decode_e4m3(const DecodeArgs& a, cudaStream_t s);
+int launch_decode_f32(const DecodeArgs& a, cudaStream_t s);
+
+// Query heads that one pass of the attention takes for groups of G, the width that a
+// head is laid out for, and the most blocks of a launch: what the workspace goes by.
+inline int decode_pass(int cache_dtype, int64_t G) {
+  if (cache_dtype == CP_F32) return G <= 4 ? 4 : 8;
+  return G <= 8 ? 8 : 16;
+}
+inline int decode_width(int64_t D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
+constexpr int kDecodeBlocks = 1024;
+// What the blocks leave for the join: the block that a query tile of sequence b
+// begins in and over how many it goes on (0: it is whole, or there is none).
+struct Begin {
+  int block, blocks, b, col;
+};
 
 }  // namespace cp

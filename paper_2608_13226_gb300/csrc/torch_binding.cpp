@@ -13,7 +13,9 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/utils/object_ptr.h>
 
+#include <cmath>
 #include <string>
 
 #include "coverprune.h"
@@ -75,9 +77,15 @@ struct Call {
     return t;
   }
   const Tensor& result(const char* name, PyObject* o, const Tensor& like) {
-    const Tensor& t = rows(name, o, (int)like.dim());
+    const Tensor& t = written(name, rows(name, o, (int)like.dim()));
     if (t.sizes() != like.sizes() || t.scalar_type() != like.scalar_type())
       bad_value(std::string(name) + " must be " + text(like.sizes()) + " of " + c10::toString(like.scalar_type()));
+    return t;
+  }
+  // What is written must not share elements (an expanded tensor does).
+  static const Tensor& written(const char* name, const Tensor& t) {
+    for (int64_t i = 0; i < t.dim(); ++i)
+      if (t.size(i) > 1 && t.stride(i) == 0) bad_value(std::string(name) + " is written and must not be expanded");
     return t;
   }
   cp_stream_t stream() const { return (cp_stream_t)c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream(); }
@@ -193,9 +201,11 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   if (!counted(n_args, 7)) return nullptr;
   return entry([&]() -> PyObject* {
     const bool many = PyList_Check(a[0]) || PyTuple_Check(a[0]);
-    const Py_ssize_t n = many ? PySequence_Fast_GET_SIZE(a[0]) : 1;
+    // tuples of our own: a list may change while other threads run
+    const THPObjectPtr x_list(many ? PySequence_Tuple(a[0]) : nullptr);
+    const Py_ssize_t n = many ? PyTuple_GET_SIZE(x_list.get()) : 1;
     if (n < 1 || n > 4) bad_value("x must be a tensor or a list of one to four");
-    PyObject* const* xs = many ? PySequence_Fast_ITEMS(a[0]) : a;
+    PyObject* const* xs = many ? PySequence_Fast_ITEMS(x_list.get()) : a;
     Call c;
     if (!THPVariable_Check(xs[0])) bad_type("x must be a tensor");
     const int dims = (int)THPVariable_Unpack(xs[0]).dim();
@@ -219,8 +229,9 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     const cp_rope rope = rope_of(c, a[2], D, (int)integer(a[3]), (float)real(a[4]));
     const int inverse = (int)integer(a[5]);
     const bool given = a[6] != Py_None, given_many = PyList_Check(a[6]) || PyTuple_Check(a[6]);
-    if (given && (given_many != many || (many && PySequence_Fast_GET_SIZE(a[6]) != n))) bad_value("out must match x");
-    PyObject* const* outs = given_many ? PySequence_Fast_ITEMS(a[6]) : a + 6;
+    const THPObjectPtr out_list(given_many ? PySequence_Tuple(a[6]) : nullptr);
+    if (given && (given_many != many || (many && PyTuple_GET_SIZE(out_list.get()) != n))) bad_value("out must match x");
+    PyObject* const* outs = given_many ? PySequence_Fast_ITEMS(out_list.get()) : a + 6;
 
     c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.device);
     cp_rows rows[4];
@@ -249,6 +260,7 @@ PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return entry([&]() -> PyObject* {
     Call c;
     const cp_cache cache = cache_of(c, a[2], a[3], a[4], a[12], a[13]);
+    Call::written("k_cache", THPVariable_Unpack(a[2]));
     const Tensor& k = c.rows("k", a[0], 3);
     const Tensor& v = c.rows("v", a[1], 3);
     const int64_t T = k.size(0), B = THPVariable_Unpack(a[4]).size(0);

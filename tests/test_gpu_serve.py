@@ -476,6 +476,12 @@ def test_decode_refuses_on_gpu():
         with pytest.raises(cp.CoverPruneError) as e:
             cp.coverprune_decode_attention(**{**ok, **bad})
         assert e.value.status == st
+    wide_pool = pool(g, 1, 16, 2, 64, BF16).expand(4, 16, 2, 64)
+    with pytest.raises(ValueError):
+        cp.coverprune_decode_attention(**ok, out=q[:1].expand(3, 4, 64))
+    with pytest.raises(ValueError):
+        cp.coverprune_cache_append(q[:, :2], q[:, :2], wide_pool, wide_pool, table, lens)
+    cp.coverprune_decode_attention(**{**ok, "k_cache": wide_pool, "v_cache": wide_pool})  # only read
     k = randn(g, 3, 2, 64, dtype=BF16)
     for bad in (dict(v=k[:2]), dict(lens=lens[:2]), dict(k=k[:2], v=k[:2]), dict(q=q[:2]), dict(q=q.float()),
                 dict(starts=torch.zeros(3, dtype=torch.int32, device="cuda")), dict(new_lens=lens[:2])):
