@@ -58,7 +58,7 @@ def _torch_flags():
             *(f"-I{i}" for i in inc)]
     # torch's own libraries are loaded by the import of torch that comes first
     link = ["-L" + BUILD, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN", "-L" + os.path.join(at, "lib"),
-            "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
+            "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
     return comp, link
 
 

@@ -7,8 +7,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
-#include <ATen/ops/empty.h>
-#include <ATen/ops/empty_like.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -87,6 +86,17 @@ struct Call {
     for (int64_t i = 0; i < t.dim(); ++i)
       if (t.size(i) > 1 && t.stride(i) == 0) bad_value(std::string(name) + " is written and must not be expanded");
     return t;
+  }
+  // A new tensor, dense; allocated straight from CUDA's allocator, past the dispatch
+  // of torch.empty (1 us a tensor).
+  Tensor made(at::IntArrayRef sizes, at::ScalarType type) const {
+    return Tensor(at::detail::empty_cuda(sizes, type, c10::Device(c10::kCUDA, (c10::DeviceIndex)device), std::nullopt));
+  }
+  // One like `t`, in the order of its strides where they leave no gaps.
+  Tensor like(const Tensor& t) const {
+    if (t.is_contiguous() || !t.is_non_overlapping_and_dense()) return made(t.sizes(), t.scalar_type());
+    return Tensor(at::detail::empty_strided_cuda(t.sizes(), t.strides(), t.scalar_type(),
+                                                 c10::Device(c10::kCUDA, (c10::DeviceIndex)device)));
   }
   cp_stream_t stream() const { return (cp_stream_t)c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream(); }
 };
@@ -238,7 +248,7 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     Tensor made[4];
     for (Py_ssize_t i = 0; i < n; ++i) {
       const Tensor& x = THPVariable_Unpack(xs[i]);
-      if (!given) made[i] = at::empty_like(x);
+      if (!given) made[i] = c.like(x);
       rows[i] = rows_of(x, given ? c.result("out", outs[i], x) : made[i]);
     }
     const int st = launch([&] {
@@ -285,11 +295,11 @@ PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 
     c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.device);
     Tensor lens_out, q_out;
-    if (!given_lens) lens_out = at::empty_like(lens);
+    if (!given_lens) lens_out = c.like(lens);
     cp_rows rows{};
     if (queries) {
       const Tensor& q = THPVariable_Unpack(a[11]);
-      if (a[15] == Py_None) q_out = at::empty_like(q);
+      if (a[15] == Py_None) q_out = c.like(q);
       rows = rows_of(q, a[15] == Py_None ? q_out : c.result("q_out", a[15], q));
     }
     const int64_t ks[2] = {k.stride(0), k.stride(1)}, vs[2] = {v.stride(0), v.stride(1)};
@@ -342,12 +352,12 @@ PyObject* decode_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
       size_t bytes = 0;
       const int st = coverprune_decode_workspace_size(B, Hq, &cache, &bytes);
       if (st != CP_OK) return PyLong_FromLong(st);
-      ws = at::empty({(int64_t)bytes}, q.options().dtype(at::kByte));
+      ws = c.made({(int64_t)bytes}, at::kByte);
     }
     const Tensor& work = a[12] == Py_None ? ws : c.tensor("ws", a[12]);
-    if (a[11] == Py_None) out = at::empty(q.sizes(), q.options());
+    if (a[11] == Py_None) out = c.made(q.sizes(), q.scalar_type());
     const Tensor& to = a[11] == Py_None ? out : c.result("out", a[11], q);
-    if (with_lse) lse = at::empty({B, Hq}, q.options().dtype(at::kFloat));
+    if (with_lse) lse = c.made({B, Hq}, at::kFloat);
     const int64_t qs[2] = {q.stride(0), q.stride(1)}, os[2] = {to.stride(0), to.stride(1)};
     const int st = launch([&] {
       return coverprune_decode_attention(q.data_ptr(), qs, dtype, B, Hq, &cache, (const int32_t*)lens.data_ptr(), keep,
