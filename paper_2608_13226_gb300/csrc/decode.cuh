@@ -32,6 +32,7 @@ constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kUnit = 64;   // keys of a unit
 constexpr int kChunk = 64;  // keys whose marks a warp looks at together
+constexpr int kMaxCluster = 16;
 constexpr int kMarks = 4;   // of them under way, so that few marks in a chunk hold nothing up
 constexpr int kQueue = 128;
 // A running maximum follows the scores only when one is more than kSlack above it
@@ -75,7 +76,7 @@ struct Shape {
   // which a block takes 72 KB.
   static constexpr int setup = 72 * 1024 / (2 * kUnit * row) < 1 ? 1 : 72 * 1024 / (2 * kUnit * row);
   static constexpr int pitch = DP + 4;        // floats of a query in the merge: the lanes' banks differ
-  static_assert(SHORT || kWarps * QT * pitch * 4 <= ring, "the merge reuses the ring");
+  static_assert(SHORT || (kWarps * pitch + DP) * QT * 4 <= ring, "the merge reuses the ring");
 };
 
 // Rows of the cache in 32 bits: row r of page p starts (p * page + r * slot) << shift
@@ -710,6 +711,29 @@ __device__ __forceinline__ void math_of_keys(const DecodeArgs& a, const Rows& ro
   }
 }
 
+// Query n's maximum and sum of all warps, and what each warp's output is to be
+// multiplied by.
+template <int QT>
+__device__ __forceinline__ void merge_sums(const float (&s_m)[kWarps][QT], const float (&s_l)[kWarps][QT],
+                                           float (&s_f)[kWarps][QT], int n, float* top_of, float* sum_of) {
+  float top = kLowest, sum = 0.0f;
+  for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_m[w][n]);
+  for (int w = 0; w < kWarps; ++w) {
+    const float f = exp2f(s_m[w][n] - top);
+    s_f[w][n] = f;
+    sum += s_l[w][n] * f;
+  }
+  *top_of = top;
+  *sum_of = sum;
+}
+
+// A float of another block of the cluster, at the place of this block's *p.
+__device__ __forceinline__ float remote(const float* p, int rank) {
+  float x;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(map_rank(smem_addr(p), (uint32_t)rank)) : "memory");
+  return x;
+}
+
 template <int CT, int DP, int QT>
 __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, int unit, int tiles, float* parts,
                                                      Begin* begins, int by_column) {
@@ -796,18 +820,7 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
       copy_wait<0>();
       __syncthreads();
       // the warps' results by a common maximum
-      if (threadIdx.x < QT) {
-        const int n = threadIdx.x;
-        float top = kLowest, sum = 0.0f;
-        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_m[w][n]);
-        for (int w = 0; w < kWarps; ++w) {
-          const float f = exp2f(s_m[w][n] - top);
-          s_f[w][n] = f;
-          sum += s_l[w][n] * f;
-        }
-        s_top[n] = top;
-        s_sum[n] = sum;
-      }
+      if (threadIdx.x < QT) merge_sums<QT>(s_m, s_l, s_f, threadIdx.x, &s_top[threadIdx.x], &s_sum[threadIdx.x]);
       __syncthreads();
       float* buf = (float*)smem;
       math.put(buf + warp * QT * S::pitch, s_f[warp]);
@@ -846,6 +859,86 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
     }
     before += (int64_t)long_nu * cols;
   }
+}
+
+// Few query tiles of a few units a block: a cluster of blocks shares each, and adds its
+// parts from one another's shared memory, an element a thread, so that no launch has
+// to follow.
+template <int CT, int DP, int QT>
+__global__ void __launch_bounds__(kThreads) k_decode_cluster(DecodeArgs a, Rows rows, int tiles, int size) {
+  using S = Shape<CT, DP, QT>;
+  using Row = typename Type<CT>::Row;
+  extern __shared__ __align__(1024) char smem[];
+  __shared__ int s_queue[kWarps][kQueue];
+  __shared__ uint32_t s_valid[kWarps][S::stages];
+  __shared__ float s_m[kWarps][QT], s_l[kWarps][QT], s_f[kWarps][QT];
+  __shared__ float s_top[QT], s_sum[QT];          // this block's, for the others
+  __shared__ float s_w[QT][kMaxCluster], s_all[QT];  // the blocks' weights and the whole sum
+  wait_for_stream();
+  const Cache& ch = a.cache;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int G = a.Hq / ch.heads, cols = ch.heads * tiles;
+  const int rank = (int)cluster_ctarank(), column = blockIdx.x / size;
+  const int b = column / cols, col = column - b * cols;
+  const int hk = col / tiles, h0 = hk * G + col % tiles * QT;
+  const int nq = min(QT, G - col % tiles * QT);
+  int first, len;
+  keys_of(a, b, &first, &len);
+  // this block's tiles of the keys
+  const int n = (len - first + S::tk - 1) / S::tk;
+  const int lo = first + (int)((int64_t)n * rank / size) * S::tk;
+  const int hi = min(len, first + (int)((int64_t)n * (rank + 1) / size) * S::tk);
+  Keys<S::tk, kWarps> keys;
+  keys.lane = lane;
+  keys.queue = s_queue[warp];
+  keys.keep = a.keep ? a.keep + (int64_t)b * a.keep_stride : nullptr;
+  Math<CT, DP, QT, false> math;
+  math_of_keys<CT, DP, QT, false>(a, rows, keys, ch.table + (int64_t)b * ch.table_stride, lo, hi, hk, b, h0, nq, warp, lane,
+                                  smem_addr(smem) + warp * S::stages * S::tile, s_valid[warp], smem + S::ring, math);
+  math.finish(s_m[warp], s_l[warp]);
+  copy_wait<0>();
+  __syncthreads();
+  if (threadIdx.x < QT) merge_sums<QT>(s_m, s_l, s_f, threadIdx.x, &s_top[threadIdx.x], &s_sum[threadIdx.x]);
+  __syncthreads();
+  float* buf = (float*)smem;
+  math.put(buf + warp * QT * S::pitch, s_f[warp]);
+  __syncthreads();
+  float* mine = buf + kWarps * QT * S::pitch;  // [nq][DP]
+  for (int i = threadIdx.x; i < nq * DP; i += kThreads) {
+    float x = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) x += buf[(w * QT + i / DP) * S::pitch + i % DP];
+    mine[i] = x;
+  }
+  __syncwarp();
+  hw_cluster_sync();
+  // every block weighs the parts, and adds its share of the elements
+  for (int q = warp; q < nq; q += kWarps) {
+    const float m = lane < size ? remote(&s_top[q], lane) : kLowest, l = lane < size ? remote(&s_sum[q], lane) : 0.0f;
+    float top = m;
+#pragma unroll
+    for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+    const float f = exp2f(m - top), sum = warp_sum(l * f);
+    if (lane < size) s_w[q][lane] = f;
+    if (lane == 0) {
+      s_all[q] = sum;
+      if (rank == 0 && a.lse)
+        a.lse[(int64_t)b * a.Hq + h0 + q] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
+    }
+  }
+  __syncthreads();
+  const float vs = ch.v_scale ? ch.v_scale[hk] : 1.0f;
+  for (int i = rank * kThreads + threadIdx.x; i < nq * DP; i += size * kThreads) {
+    const int q = i / DP, d = i % DP;
+    float x = 0.0f;
+#pragma unroll 4
+    for (int r = 0; r < size; ++r) x = fmaf(s_w[q][r], remote(&mine[i], r), x);
+    if (d < ch.D)
+      ((Row*)a.out)[b * a.o_b + (int64_t)(h0 + q) * a.o_h + d] =
+          from_f32<Row>(s_all[q] == 0.0f ? 0.0f : x * (vs / s_all[q]));
+  }
+  __syncwarp();
+  hw_cluster_sync();  // no block's memory goes while it is read
 }
 
 // Many short sequences: a warp takes a query tile alone, and then another, so that one's beginning (table, keys, queries: three trips
@@ -988,6 +1081,49 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_decode_join(DecodeArgs a, i
   if (lane == 0 && a.lse) a.lse[(int64_t)x.b * a.Hq + h0 + n] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
+// The largest clusters of which `columns` run at the same time, 2 to kMaxCluster blocks
+// (1: there are none): at most `all` blocks, and no more clusters than the device
+// holds, which is asked once a device and size.
+template <int CT, int DP, int QT>
+static int cluster_size(int64_t columns, int64_t all, int* size) {
+  using S = Shape<CT, DP, QT>;
+  static std::atomic<uint64_t> allowed{0};
+  static std::atomic<int> held[64][5];  // a device's clusters of 2^i blocks, and one more (0: not asked yet)
+  *size = 1;
+  if (columns * 2 > all) return CP_OK;
+  const void* kernel = (const void*)k_decode_cluster<CT, DP, QT>;
+  int dev = 0;
+  CP_TRY_STATUS(cuda_status(cudaGetDevice(&dev), "decode: device"));
+  if (!(allowed.load(std::memory_order_acquire) >> (dev & 63) & 1))
+    CP_TRY_STATUS(cuda_status(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1),
+                              "decode: cluster"));
+  CP_TRY_STATUS(allow_smem_once(kernel, S::smem, "decode: shared memory", &allowed));
+  int most = kMaxCluster, i = 4;
+  for (; most > 1; most /= 2, --i) {
+    if (columns * most > all) continue;
+    int n = held[dev & 63][i].load(std::memory_order_relaxed) - 1;
+    if (n < 0) {
+      cudaLaunchAttribute with{};
+      with.id = cudaLaunchAttributeClusterDimension;
+      with.val.clusterDim = {(unsigned)most, 1, 1};
+      cudaLaunchConfig_t cfg{};
+      cfg.gridDim = dim3((unsigned)most);
+      cfg.blockDim = dim3(kThreads);
+      cfg.dynamicSmemBytes = S::smem;
+      cfg.attrs = &with;
+      cfg.numAttrs = 1;
+      if (cudaOccupancyMaxActiveClusters(&n, k_decode_cluster<CT, DP, QT>, &cfg) != cudaSuccess) {
+        (void)cudaGetLastError();  // a size that the device does not take
+        n = 0;
+      }
+      held[dev & 63][i].store(n + 1, std::memory_order_relaxed);
+    }
+    if (columns <= n) break;
+  }
+  *size = most;
+  return CP_OK;
+}
+
 template <int CT, int DP, int QT>
 static int launch(const DecodeArgs& a, cudaStream_t s) {
   using S = Shape<CT, DP, QT>;
@@ -1039,6 +1175,21 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
                                     Short::smem, s, a, rows, tiles, columns),
                        "decode: short");
   }
+  // Few query tiles: a cluster each, if all run at once.  That saves 4 us of joining,
+  // and costs what the blocks that get no tile would have done (at most 8 units' time
+  // a block) and, where sequences differ in length more than the table's width
+  // tells, the longest one's time: at most 16 units a block, of marked keys thrice
+  // that.  us as one line / with clusters, 7 queries a head of 128: 4 tiles of 500 keys
+  // 8.2 / 6.7, of 1500 8.2 / 7.2, of 8000 16.1 / 11.3, of 16000 16.2 / 17.3; 64 of 1500
+  // 15.4 / 11.3, of 4000 29.9 / 26.2, of 8000 with 15% marked 19.8 / 16.2; 128 of 1229
+  // to 1741 24.1 / 22.8.
+  const int64_t n64 = (most + kUnit - 1) / kUnit;
+  int size = 0;
+  if (cut) CP_TRY_STATUS((cluster_size<CT, DP, QT>(columns, all, &size)));
+  if (size > 1 && n64 <= (a.keep ? 48 : 16) * size && n64 * (all - columns * size) <= 8 * size * all)
+    return cuda_status(launch_early_cluster(k_decode_cluster<CT, DP, QT>, dim3((unsigned)(columns * size)), kThreads, S::smem,
+                                            s, size, a, rows, tiles, size),
+                       "decode: cluster");
   CP_TRY_STATUS(cuda_status(launch_early(k_decode<CT, DP, QT>, dim3((unsigned)grid), kThreads, S::smem, s, a, rows, unit,
                                          tiles, parts, cut ? begins : nullptr, (int)by_column),
                             "decode"));

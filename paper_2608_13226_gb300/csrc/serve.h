@@ -80,20 +80,27 @@ struct DecodeArgs {
 // blocks come to the SMs and wait there (wait_for_stream, first of all), so that its
 // latency is spent beside the other's last blocks.
 template <typename... Params, typename... Args>
-cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t s,
-                         Args... args) {
-  cudaLaunchAttribute early{};
-  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  early.val.programmaticStreamSerializationAllowed = 1;
+cudaError_t launch_early_cluster(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t s,
+                                 int cluster, Args... args) {
+  cudaLaunchAttribute with[2] = {};
+  with[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  with[0].val.programmaticStreamSerializationAllowed = 1;
+  with[1].id = cudaLaunchAttributeClusterDimension;
+  with[1].val.clusterDim = {(unsigned)cluster, 1, 1};
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
   cfg.blockDim = dim3((unsigned)threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
-  cfg.attrs = &early;
-  cfg.numAttrs = 1;
+  cfg.attrs = with;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   note_launch();
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
+template <typename... Params, typename... Args>
+cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t s,
+                         Args... args) {
+  return launch_early_cluster(kernel, grid, threads, smem, s, 1, args...);
 }
 
 size_t decode_ws_bytes(int64_t Hq, int64_t heads, int64_t D, int cache_dtype);

@@ -389,6 +389,17 @@ def test_decode_many_short(Hq, H, D, page, cdt, scales):
 
 
 @pytest.mark.parametrize("cdt,scales", TYPES)
+@pytest.mark.parametrize("Hq,H,D,page", [(14, 2, 128, 16), (1, 1, 64, 7), (12, 1, 256, 100), (24, 2, 80, 1), (4, 4, 16, 64)])
+def test_decode_few_long(Hq, H, D, page, cdt, scales):
+    """Few query tiles, which clusters of blocks share, at lengths that leave some of them
+    nothing: whole, with marks and a window."""
+    for lens in ([257], [1000, 0, 3], [300, 2000, 1, 17, 999]):
+        check_decode(D, lens, page, Hq, H, D, cdt, scales=scales, junk=math.nan)
+        check_decode(D + 1, lens, page, Hq, H, D, cdt, scales=scales, keep=0.3, junk=math.nan, heads_first=True)
+        check_decode(D + 2, lens, page, Hq, H, D, cdt, scales=scales, window=290, junk=math.nan, q_view=True)
+
+
+@pytest.mark.parametrize("cdt,scales", TYPES)
 def test_decode_sharp_and_scaled(cdt, scales):
     """Scores in the hundreds (one key takes all), all alike, and a negative scale."""
     check_decode(1, [400, 1], 16, 8, 2, 64, cdt, scales=scales, sharp=300.0)
