@@ -400,6 +400,27 @@ def test_decode_few_long(Hq, H, D, page, cdt, scales):
 
 
 @pytest.mark.parametrize("cdt,scales", TYPES)
+@pytest.mark.parametrize("Hq,H,D", [(14, 2, 128), (3, 3, 64), (12, 1, 256), (40, 2, 80)])
+@pytest.mark.parametrize("most", [1, 7, 8, 9, 16, 17, 32, 33, 64])
+def test_decode_few_tiny(most, Hq, H, D, cdt, scales):
+    """Few query tiles of hardly any keys, on both sides of a tile and of two."""
+    lens = [most, 0, max(most - 1, 1), 1, most]
+    check_decode(most, lens, 1, Hq, H, D, cdt, scales=scales, junk=math.nan)
+    check_decode(most + 1, [3 * n for n in lens], 7, Hq, H, D, cdt, scales=scales, window=most, keep=0.6, junk=math.inf,
+                 heads_first=True, q_view=True)
+
+
+@pytest.mark.parametrize("cdt", [BF16, F32, E4M3])
+def test_decode_empty_table(cdt):
+    g = gen(3)
+    kc, vc = pool(g, 4, 16, 2, 64, cdt), pool(g, 4, 16, 2, 64, cdt)
+    q = randn(g, 3, 4, 64, dtype=F32 if cdt == F32 else BF16)
+    table = torch.empty(3, 0, dtype=torch.int32, device="cuda")
+    r = cp.coverprune_decode_attention(q, kc, vc, table, torch.tensor([0, 5, 100], dtype=torch.int32, device="cuda"), lse=True)
+    assert bool((r["out"] == 0).all()) and bool((r["lse"] == -math.inf).all())
+
+
+@pytest.mark.parametrize("cdt,scales", TYPES)
 def test_decode_sharp_and_scaled(cdt, scales):
     """Scores in the hundreds (one key takes all), all alike, and a negative scale."""
     check_decode(1, [400, 1], 16, 8, 2, 64, cdt, scales=scales, sharp=300.0)
