@@ -28,6 +28,7 @@ constexpr int kThreads = 256;
 constexpr int kBlocks = 2;
 constexpr int kItems = 2;
 constexpr int kChunk = 256;  // tokens looked up at a time
+constexpr int64_t kTwoBlocks = 108 * 1024;  // dynamic shared memory of a block that leaves room for another
 constexpr size_t kMostSmem = 160 * 1024;  // more than any launch takes
 
 // n / d for 0 <= n < 2^31 by a product: with 2^l >= d, mul = ceil(2^(31 + l) / d)
@@ -41,11 +42,12 @@ struct Divisor {
 struct Tiling {
   int places, wide;  // of V pairs (and then of 2 V components that pass) in a row; threads for them, two each
   int parts;         // of a row: places / (2 wide), rounded up
-  Divisor rows_of, half_of;  // by the parts of a token's rows, by half
+  Divisor rows_of;   // by the parts of a token's rows
   int lanes;         // rows side by side: wide * lanes threads at most
   int stage;         // parts of rows of a stage
   int held;          // tokens whose angles are held: those of two stages
   int half;
+  int pairs, side;   // threads for the angles of a token, tokens side by side
 };
 
 // V consecutive elements in as few registers as they fill.
@@ -232,6 +234,8 @@ __device__ __forceinline__ void run_rows(Job& job, const Rope& rope, const Tilin
   const int vec0 = threadIdx.x % tl.wide, lane = threadIdx.x / tl.wide;
   const int rows = job.rows * tl.parts, turned_places = tl.half / V;
   const bool works = lane < tl.lanes;
+  // The pair whose angles a thread computes, and the first token (-1: none).
+  const int p0 = threadIdx.x % tl.pairs, tok0 = threadIdx.x / tl.pairs < tl.side ? threadIdx.x / tl.pairs : -1;
   // The components of this lane's places in a row, two vectors each (`n` of them
   // there): of a row that turns and of one that passes whole, in the row's first
   // part.  Rows of several parts are rare and work theirs out.
@@ -295,11 +299,15 @@ __device__ __forceinline__ void run_rows(Job& job, const Rope& rope, const Tilin
       if (s >= -1 && s + 1 < stages) {
         // angles of the next stage's tokens
         const int upto = min(n, tl.rows_of.of((s + 2) * tl.stage + rows - 1));
-        for (int i = threadIdx.x; i < (upto - known) * tl.half; i += kThreads) {
-          const int k = tl.half_of.of(i), p = i - k * tl.half;
-          const int at = (known_at + k >= tl.held ? known_at + k - tl.held : known_at + k) * tl.half + p;
-          rope_unit(s_turns[p], s_pos[known + k], rope, s_cos + at, s_sin + at);
-        }
+        if (tok0 >= 0)
+          for (int p = p0; p < tl.half; p += tl.pairs) {
+            const uint64_t turns = s_turns[p];
+#pragma unroll 2  // 40.3 us as below, one at a time 41.3
+            for (int k = tok0; k < upto - known; k += tl.side) {
+              const int at = (known_at + k >= tl.held ? known_at + k - tl.held : known_at + k) * tl.half + p;
+              rope_unit(turns, s_pos[known + k], rope, s_cos + at, s_sin + at);
+            }
+          }
         known_at += upto - known;
         if (known_at >= tl.held) known_at -= tl.held;
         known = upto;
@@ -507,7 +515,8 @@ static Divisor divisor(int d) {
   while (((int64_t)1 << l) < d) ++l;
   return Divisor{(uint32_t)d, (uint32_t)((((uint64_t)1 << (31 + l)) + d - 1) / d), l};
 }
-static Tiling tiling(int half, int D, int V, int rows) {
+static size_t slots_of(int bytes) { return bytes >= 4 ? 8 * kItems * kThreads * (size_t)bytes : 0; }
+static Tiling tiling(int half, int D, int V, int rows, int bytes) {
   Tiling t;
   t.half = half;
   t.places = half / V + (D - 2 * half + 2 * V - 1) / (2 * V);
@@ -516,19 +525,20 @@ static Tiling tiling(int half, int D, int V, int rows) {
   t.lanes = kThreads / t.wide;
   rows *= t.parts;
   t.stage = kItems * t.lanes < kThreads ? kItems * t.lanes : kThreads;  // a thread notes one row
-  // angles of two stages within 40 KB, if a stage has to be shorter for it: heads
-  // of few rows and tokens of wide rotations
-  if (half > 0) {
-    const int64_t most = ((40 * 1024 / (8 * half) - 2) / 2) * (int64_t)rows;
-    if (t.stage > most) t.stage = most < 1 ? 1 : (int)most;
-  }
+  // Where angles take much room, heads of few rows and tokens of wide rotations, a
+  // stage is as short as leaves two blocks on an SM: 115,255 tokens of two heads of 128
+  // 40 us, with one block and longer ones 64.
+  const int64_t room = kTwoBlocks - (int64_t)slots_of(bytes) - 8 * half * (int64_t)4;
+  const int64_t most = room * rows / (3 * (int64_t)sizeof(Note) * rows + 16 * half);
+  if (t.stage > most) t.stage = most < 1 ? 1 : (int)most;
   t.held = (2 * t.stage + rows - 1) / rows + 1;
   t.rows_of = divisor(rows);
-  t.half_of = divisor(half);
+  t.pairs = half < 1 ? 1 : half < kThreads ? half : kThreads;
+  t.side = kThreads / t.pairs;
   return t;
 }
 static size_t smem_of(const Tiling& t, int bytes) {
-  return (bytes >= 4 ? 8 * kItems * kThreads * (size_t)bytes : 0) + 3 * (size_t)t.stage * sizeof(Note) +
+  return slots_of(bytes) + 3 * (size_t)t.stage * sizeof(Note) +
          (size_t)t.half * (8 + 8 * (size_t)t.held);
 }
 static unsigned grid_of(int64_t tokens, int sms) {
@@ -542,7 +552,7 @@ static int rotary(const RotaryArgs& a, int rows, cudaStream_t s) {
   DeviceInfo di;
   CP_TRY_STATUS(device_info(&di));
   const unsigned grid = grid_of(a.B * a.T, di.sm_count);
-  const Tiling t = tiling(a.rope.half, a.D, V, rows);
+  const Tiling t = tiling(a.rope.half, a.D, V, rows, V * sizeof(T));
   const size_t smem = smem_of(t, V * sizeof(T));
   CP_TRY_STATUS(allow_smem_once((const void*)k_rotary<T, V>, kMostSmem, "rotary: shared memory", &allowed));
   return cuda_status(launch_early(k_rotary<T, V>, dim3(grid), kThreads, smem, s, a, t, rows), "rotary");
@@ -588,7 +598,7 @@ static int append(const AppendArgs& a, cudaStream_t s) {
   DeviceInfo di;
   CP_TRY_STATUS(device_info(&di));
   const unsigned grid = grid_of(a.T, di.sm_count);
-  const Tiling t = tiling(a.rope.half, a.cache.D, V, a.q.heads + 2 * a.cache.heads);
+  const Tiling t = tiling(a.rope.half, a.cache.D, V, a.q.heads + 2 * a.cache.heads, V * sizeof(T));
   auto kernel = k_cache_append<T, C, V, SCALED>;
   CP_TRY_STATUS(allow_smem_once((const void*)kernel, kMostSmem, "cache append: shared memory", &allowed));
   return cuda_status(launch_early(kernel, dim3(grid), kThreads, smem_of(t, V * sizeof(T)), s, a, t), "cache append");

@@ -84,6 +84,20 @@ def test_rotary(B, T, H, D, rot, dtype, layout):
         assert torch.equal(y[..., rot:], x[..., rot:])
 
 
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T,H,D,rot", [(100003, 1, 128, 128), (90001, 2, 64, 64), (50000, 1, 80, 80), (100000, 3, 48, 36),
+                                       (20011, 1, 1100, 1100), (20000, 2, 256, 256)])
+def test_rotary_many_tokens_of_few_heads(T, H, D, rot, dtype, layout):
+    """Runs of tokens over many stages, whose angles outweigh their rows."""
+    g = gen(T)
+    x = randn(g, 1, T, H, D, dtype=dtype)
+    pos = torch.randint(0, 1 << 20, (1, T), generator=g, device="cuda")
+    y = cp.coverprune_rotary(x, pos, freq(rot // 2), layout=layout)
+    want, mag = turned(x, pos, freq(rot // 2), layout)
+    assert_stored(y, want, 5e-7 * mag, "rotary")
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("D,shift", [(64, 0), (64, 1), (64, 4), (80, 2), (128, 8)])
 def test_rotary_strides(D, shift, dtype):
@@ -219,6 +233,13 @@ def test_append(dtype, cdt, D, rot, layout, page, hf):
     check_append(D + page, [5, 0, 1, 63, 0], [0, 9, 40, 3, 0], page, 6, 3, D, rot, dtype, cdt, hf, True, layout, cdt == E4M3)
     check_append(D + page + 1, [1] * 9, [0, 1, 2, 15, 16, 31, 32, 99, 100], page, 4, 2, D, rot, dtype, cdt, hf, False, layout,
                  True, starts=False)
+
+
+@pytest.mark.parametrize("dtype,cdt", [(BF16, BF16), (F32, F32), (BF16, E4M3)])
+@pytest.mark.parametrize("Hq,Hk,D,rot,page,hf", [(1, 1, 128, 128, 16, False), (8, 8, 64, 64, 16, True), (3, 1, 80, 80, 7, False),
+                                                 (2, 2, 112, 48, 64, False), (5, 1, 128, 64, 100, True), (0, 2, 32, 32, 3, False)])
+def test_append_many_tokens(Hq, Hk, D, rot, page, hf, dtype, cdt):
+    check_append(D + Hq, [9000, 0, 12345, 7001, 1], [3, 0, 100, 0, 77], page, Hq, Hk, D, rot, dtype, cdt, hf, scales=cdt == E4M3)
 
 
 def test_append_many_and_padding():
