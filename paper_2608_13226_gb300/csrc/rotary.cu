@@ -5,12 +5,12 @@
 //  - a block has a run of tokens for the whole call.  The speeds' float64 arithmetic
 //    (1/64 of the float32 rate) is done once a block, and where the tokens go
 //    is looked up kChunk of them at a time, a thread each;
-//  - the rows of its tokens are one line, taken a stage of up to 2 rows a lane
-//    at a time.  Between two barriers the block notes where the rows of the
+//  - the rows of its tokens are one line, taken a stage of up to 2 (narrow ones 4)
+//    rows a lane at a time.  Between two barriers the block notes where the rows of the
 //    stage after next lie (a thread a row), computes the angles of the next
 //    stage's tokens (a thread a pair, once for all heads), starts the next
 //    stage's copies and turns this one's rows;
-//  - a lane turns two places of a row, each V pairs in two 16-byte vectors where
+//  - a lane turns two places of a row (of a narrow one a place), each V pairs in two 16-byte vectors where
 //    alignment allows.  It copies them into slots of its own, so a copy is
 //    waited for by the lane that made it and the barrier never waits for one.
 // The products are packed pairs of float32 (half the FMA instructions).
@@ -21,7 +21,7 @@
 namespace cp {
 
 constexpr int kThreads = 256;
-// Blocks of an SM and rows of a stage that a lane has at most.  39,328 tokens of
+// Blocks of an SM and rows of a stage that a lane has at most (narrow ones: twice that).  39,328 tokens of
 // 28 + 4 bf16 heads of 128, us for rotary / append: 2 and 2 101 / 112, 2 and 1
 // 105 / 130, 3 and 1 110 / 118, 4 and 1 116 / 122 (fewer bytes under way), 3 and 2
 // 112 / 132 (two blocks fit).
@@ -40,8 +40,8 @@ struct Divisor {
 
 // Sizes of a launch that the kernels share.
 struct Tiling {
-  int places, wide;  // of V pairs (and then of 2 V components that pass) in a row; threads for them, two each
-  int parts;         // of a row: places / (2 wide), rounded up
+  int places, wide;  // of V pairs (and then of 2 V components that pass) in a row; threads for them
+  int parts;         // of a row: places / what those threads take at a time, rounded up
   Divisor rows_of;   // by the parts of a token's rows
   int lanes;         // rows side by side: wide * lanes threads at most
   int stage;         // parts of rows of a stage
@@ -216,11 +216,12 @@ struct Note {
 // A block's run of tokens.  The job says how many rows a token has (`rows`) and
 // what row r of token tok is (`note`); `locate` looks up a chunk of tokens, a
 // thread each, and gives a token's position.
-template <typename T, typename C, int V, bool SCALED, typename Job>
+template <typename T, typename C, int V, int SUBS, bool SCALED, typename Job>
 __device__ __forceinline__ void run_rows(Job& job, const Rope& rope, const Tiling& tl, int D, int64_t tokens) {
   extern __shared__ __align__(16) char smem[];  // slots, notes of three stages, angles, speeds
   __shared__ int64_t s_pos[kChunk];
   constexpr int kBytes = V * (int)sizeof(T);
+  constexpr int kRows = 2 * kItems / SUBS;  // rows of a stage that a lane has at most
   constexpr bool kSlots = kBytes >= 4;  // smaller vectors are loaded when they are turned
   using Vec = Pack<T, V>;
   Vec* slots = reinterpret_cast<Vec*>(smem);
@@ -244,7 +245,7 @@ __device__ __forceinline__ void run_rows(Job& job, const Rope& rope, const Tilin
     bool turned;
   };
   auto place_of = [&](bool turns, int part, int sub) {
-    int vec = vec0 + (2 * part + sub) * tl.wide;
+    int vec = vec0 + (SUBS * part + sub) * tl.wide;
     Place p;
     p.turned = turns && vec < turned_places;
     // neighbouring lanes have neighbouring vectors, of the first and of the second
@@ -266,8 +267,8 @@ __device__ __forceinline__ void run_rows(Job& job, const Rope& rope, const Tilin
     p.n = !works || p.at0 >= D ? 0 : p.at1 < to ? 2 : 1;
     return p;
   };
-  const Place turning[2] = {place_of(true, 0, 0), place_of(true, 0, 1)};
-  const Place passing[2] = {place_of(false, 0, 0), place_of(false, 0, 1)};
+  const Place turning[2] = {place_of(true, 0, 0), place_of(true, 0, SUBS - 1)};
+  const Place passing[2] = {place_of(false, 0, 0), place_of(false, 0, SUBS - 1)};
   auto place = [&](int kind, int part, int sub) {
     if (tl.parts > 1 && part) return place_of(kind & kTurned, part, sub);
     return kind & kTurned ? turning[sub] : passing[sub];
@@ -316,15 +317,15 @@ __device__ __forceinline__ void run_rows(Job& job, const Rope& rope, const Tilin
           const Note* of = notes + (s + 1) % 3 * tl.stage;
           Vec* to = slots + (s + 1) % 2 * (kItems * 4 * kThreads) + threadIdx.x;
 #pragma unroll
-          for (int k = 0; k < kItems; ++k) {
+          for (int k = 0; k < kRows; ++k) {
             const int j = lane + k * tl.lanes;
             const int kind = j < tl.stage ? of[j].kind : 0;
             if (!kind) continue;
             const T* in = (const T*)of[j].in;
 #pragma unroll
-            for (int sub = 0; sub < 2; ++sub) {
+            for (int sub = 0; sub < SUBS; ++sub) {
               const Place p = place(kind, of[j].part, sub);
-              const uint32_t at = smem_addr(to + (2 * k + sub) * 2 * kThreads);
+              const uint32_t at = smem_addr(to + (SUBS * k + sub) * 2 * kThreads);
               if (p.n > 0) copy_ahead<kSlots ? kBytes : 4>(at, in + p.at0);
               if (p.n > 1) copy_ahead<kSlots ? kBytes : 4>(at + kThreads * kBytes, in + p.at1);
             }
@@ -337,19 +338,19 @@ __device__ __forceinline__ void run_rows(Job& job, const Rope& rope, const Tilin
         const Note* of = notes + s % 3 * tl.stage;
         const Vec* from = slots + s % 2 * (kItems * 4 * kThreads) + threadIdx.x;
 #pragma unroll
-        for (int k = 0; k < kItems; ++k) {
+        for (int k = 0; k < kRows; ++k) {
           const int j = lane + k * tl.lanes;
           const int kind = j < tl.stage ? of[j].kind : 0;
           if (!kind) continue;
           const Note x = of[j];
 #pragma unroll
-          for (int sub = 0; sub < 2; ++sub) {
+          for (int sub = 0; sub < SUBS; ++sub) {
             const Place p = place(kind, x.part, sub);
             if (p.n == 0) continue;
             Vec a{}, b{};
             if (kSlots) {
-              a = from[(2 * k + sub) * 2 * kThreads];
-              b = from[((2 * k + sub) * 2 + 1) * kThreads];
+              a = from[(SUBS * k + sub) * 2 * kThreads];
+              b = from[((SUBS * k + sub) * 2 + 1) * kThreads];
             } else {
               a = load<T, V>((const T*)x.in, p.at0);
               if (p.n > 1) b = load<T, V>((const T*)x.in, p.at1);
@@ -417,11 +418,11 @@ struct RotaryJob {
   }
 };
 
-template <typename T, int V>
+template <typename T, int V, int SUBS>
 __global__ void __launch_bounds__(kThreads, kBlocks) k_rotary(RotaryArgs a, Tiling tl, int rows) {
   wait_for_stream();
   RotaryJob<T> job{a, rows};
-  run_rows<T, T, V, false>(job, a.rope, tl, a.D, a.B * a.T);
+  run_rows<T, T, V, SUBS, false>(job, a.rope, tl, a.D, a.B * a.T);
 }
 
 // The sequence that row t belongs to: how many of starts[1..B] are <= t.
@@ -484,7 +485,7 @@ struct AppendJob {
   }
 };
 
-template <typename T, typename C, int V, bool SCALED>
+template <typename T, typename C, int V, int SUBS, bool SCALED>
 __global__ void __launch_bounds__(kThreads, kBlocks) k_cache_append(AppendArgs a, Tiling tl) {
   __shared__ int64_t s_row[kChunk];
   wait_for_stream();
@@ -494,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) k_cache_append(AppendArgs a
       a.new_lens[b] = (int32_t)min(n, (int64_t)a.cache.capacity);
     }
   AppendJob<T, C> job{a, a.q.heads + 2 * a.cache.heads, s_row};
-  run_rows<T, C, V, SCALED>(job, a.rope, tl, a.cache.D, a.T);
+  run_rows<T, C, V, SUBS, SCALED>(job, a.rope, tl, a.cache.D, a.T);
 }
 
 // Whether every row of a tensor starts on a multiple of V elements.
@@ -516,15 +517,16 @@ static Divisor divisor(int d) {
   return Divisor{(uint32_t)d, (uint32_t)((((uint64_t)1 << (31 + l)) + d - 1) / d), l};
 }
 static size_t slots_of(int bytes) { return bytes >= 4 ? 8 * kItems * kThreads * (size_t)bytes : 0; }
-static Tiling tiling(int half, int D, int V, int rows, int bytes) {
+static int places_of(int half, int D, int V) { return half / V + (D - 2 * half + 2 * V - 1) / (2 * V); }
+static Tiling tiling(int half, int D, int V, int subs, int rows, int bytes) {
   Tiling t;
   t.half = half;
-  t.places = half / V + (D - 2 * half + 2 * V - 1) / (2 * V);
-  t.wide = (t.places + 1) / 2 < kThreads ? (t.places + 1) / 2 : kThreads;
-  t.parts = (t.places + 2 * t.wide - 1) / (2 * t.wide);
+  t.places = places_of(half, D, V);
+  t.wide = (t.places + subs - 1) / subs < kThreads ? (t.places + subs - 1) / subs : kThreads;
+  t.parts = (t.places + subs * t.wide - 1) / (subs * t.wide);
   t.lanes = kThreads / t.wide;
   rows *= t.parts;
-  t.stage = kItems * t.lanes < kThreads ? kItems * t.lanes : kThreads;  // a thread notes one row
+  t.stage = 2 * kItems / subs * t.lanes < kThreads ? 2 * kItems / subs * t.lanes : kThreads;  // a thread notes one row
   // Where angles take much room, heads of few rows and tokens of wide rotations, a
   // stage is as short as leaves two blocks on an SM: 115,255 tokens of two heads of 128
   // 40 us, with one block and longer ones 64.
@@ -546,16 +548,26 @@ static unsigned grid_of(int64_t tokens, int sms) {
   return (unsigned)(tokens < 1 ? 1 : tokens < most ? tokens : most);
 }
 
-template <typename T, int V>
+// Rows of at most so many places give a lane one place of twice as many rows: the
+// lanes of a warp then read longer pieces of fewer rows, and odd numbers of places
+// leave no lane idle.  us with two places / with one, bf16: append of 32,000 tokens'
+// 8 + 2 x 8 heads of 64 (4 places) 48 / 37, 28 + 2 x 4 to 8 bits 87 / 67, 16 + 2 x 4
+// of 80 (5) 60 / 54, of 96 (6) 67 / 57, of 128 of which 64 turn (8) 72 / 65, all (8)
+// 111.2 / 110.2 (39,328 tokens of 28 + 2 x 4); of 256 (16) 29.1 / 29.5; float32 of 64
+// (8) 71.6 / 72.4.  Rotary of 16 + 4 heads of 80 (5) 48 / 44, of 128 (8) 53.8 / 55.0.
+constexpr int kNarrowRotary = 7, kNarrowAppend = 8;
+template <typename T, int V, int SUBS = 2>
 static int rotary(const RotaryArgs& a, int rows, cudaStream_t s) {
+  if constexpr (SUBS == 2 && V * sizeof(T) == 16)
+    if (places_of(a.rope.half, a.D, V) <= kNarrowRotary) return rotary<T, V, 1>(a, rows, s);
   static std::atomic<uint64_t> allowed{0};
   DeviceInfo di;
   CP_TRY_STATUS(device_info(&di));
   const unsigned grid = grid_of(a.B * a.T, di.sm_count);
-  const Tiling t = tiling(a.rope.half, a.D, V, rows, V * sizeof(T));
+  const Tiling t = tiling(a.rope.half, a.D, V, SUBS, rows, V * sizeof(T));
   const size_t smem = smem_of(t, V * sizeof(T));
-  CP_TRY_STATUS(allow_smem_once((const void*)k_rotary<T, V>, kMostSmem, "rotary: shared memory", &allowed));
-  return cuda_status(launch_early(k_rotary<T, V>, dim3(grid), kThreads, smem, s, a, t, rows), "rotary");
+  CP_TRY_STATUS(allow_smem_once((const void*)k_rotary<T, V, SUBS>, kMostSmem, "rotary: shared memory", &allowed));
+  return cuda_status(launch_early(k_rotary<T, V, SUBS>, dim3(grid), kThreads, smem, s, a, t, rows), "rotary");
 }
 
 int launch_rotary(const RotaryArgs& args, int dtype, cudaStream_t s) {
@@ -592,14 +604,16 @@ int launch_rotary(const RotaryArgs& args, int dtype, cudaStream_t s) {
   return rotary<float, 1>(a, rows, s);
 }
 
-template <typename T, typename C, int V, bool SCALED>
+template <typename T, typename C, int V, bool SCALED, int SUBS = 2>
 static int append(const AppendArgs& a, cudaStream_t s) {
+  if constexpr (SUBS == 2 && V * sizeof(T) == 16)
+    if (places_of(a.rope.half, a.cache.D, V) <= kNarrowAppend) return append<T, C, V, SCALED, 1>(a, s);
   static std::atomic<uint64_t> allowed{0};
   DeviceInfo di;
   CP_TRY_STATUS(device_info(&di));
   const unsigned grid = grid_of(a.T, di.sm_count);
-  const Tiling t = tiling(a.rope.half, a.cache.D, V, a.q.heads + 2 * a.cache.heads, V * sizeof(T));
-  auto kernel = k_cache_append<T, C, V, SCALED>;
+  const Tiling t = tiling(a.rope.half, a.cache.D, V, SUBS, a.q.heads + 2 * a.cache.heads, V * sizeof(T));
+  auto kernel = k_cache_append<T, C, V, SUBS, SCALED>;
   CP_TRY_STATUS(allow_smem_once((const void*)kernel, kMostSmem, "cache append: shared memory", &allowed));
   return cuda_status(launch_early(kernel, dim3(grid), kThreads, smem_of(t, V * sizeof(T)), s, a, t), "cache append");
 }
