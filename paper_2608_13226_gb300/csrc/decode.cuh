@@ -745,6 +745,22 @@ __device__ __forceinline__ void merge_sums(const float (&s_m)[kWarps][QT], const
   *sum_of = sum;
 }
 
+// Four components of a query added over the warps, quad i of [QT][DP / 4].
+template <int DP, int QT, int PITCH>
+__device__ __forceinline__ float4 merge_quad(const float* buf, int i) {
+  const float* at = buf + i / (DP / 4) * PITCH + 4 * (i % (DP / 4));
+  float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    const float4 y = *(const float4*)(at + w * QT * PITCH);
+    x.x += y.x;
+    x.y += y.y;
+    x.z += y.z;
+    x.w += y.w;
+  }
+  return x;
+}
+
 // A float of another block of the cluster, at the place of this block's *p.
 __device__ __forceinline__ float remote(const float* p, int rank) {
   float x;
@@ -846,16 +862,19 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
       const bool whole = k0 == 0 && k1 == nu;
       const float vs = ch.v_scale ? ch.v_scale[hk] : 1.0f;
       float* part = whole ? nullptr : parts + (2 * (int64_t)blockIdx.x + (k0 == 0)) * S::part;
-      for (int i = threadIdx.x; i < nq * DP; i += kThreads) {
-        const int n = i / DP, d = i % DP;
-        float x = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) x += buf[(w * QT + n) * S::pitch + d];
-        if (!whole)
-          part[2 * QT + i] = x;
-        else if (d < ch.D)
-          ((Row*)a.out)[b * a.o_b + (int64_t)(h0 + n) * a.o_h + d] =
-              from_f32<Row>(s_sum[n] == 0.0f ? 0.0f : x * (vs / s_sum[n]));
+      for (int i = threadIdx.x; i < nq * (DP / 4); i += kThreads) {
+        const float4 x = merge_quad<DP, QT, S::pitch>(buf, i);
+        const int n = i / (DP / 4), d = 4 * (i % (DP / 4));
+        if (!whole) {
+          *(float4*)(part + 2 * QT + 4 * i) = x;
+        } else if (d < ch.D) {
+          const float sum = s_sum[n], by = vs / sum;
+          Row* out = (Row*)a.out + b * a.o_b + (int64_t)(h0 + n) * a.o_h + d;
+          out[0] = from_f32<Row>(sum == 0.0f ? 0.0f : x.x * by);
+          out[1] = from_f32<Row>(sum == 0.0f ? 0.0f : x.y * by);
+          out[2] = from_f32<Row>(sum == 0.0f ? 0.0f : x.z * by);
+          out[3] = from_f32<Row>(sum == 0.0f ? 0.0f : x.w * by);
+        }
       }
       if (threadIdx.x < nq) {
         const int n = threadIdx.x;
@@ -922,12 +941,8 @@ __global__ void __launch_bounds__(kThreads) k_decode_cluster(DecodeArgs a, Rows 
   math.put(buf + warp * QT * S::pitch, s_f[warp]);
   __syncthreads();
   float* mine = buf + kWarps * QT * S::pitch;  // [nq][DP]
-  for (int i = threadIdx.x; i < nq * DP; i += kThreads) {
-    float x = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) x += buf[(w * QT + i / DP) * S::pitch + i % DP];
-    mine[i] = x;
-  }
+  for (int i = threadIdx.x; i < nq * (DP / 4); i += kThreads)
+    *(float4*)(mine + 4 * i) = merge_quad<DP, QT, S::pitch>(buf, i);
   __syncwarp();
   hw_cluster_sync();
   // every block weighs the parts, and adds its share of the elements
@@ -949,8 +964,12 @@ __global__ void __launch_bounds__(kThreads) k_decode_cluster(DecodeArgs a, Rows 
   for (int i = rank * kThreads + threadIdx.x; i < nq * DP; i += size * kThreads) {
     const int q = i / DP, d = i % DP;
     float x = 0.0f;
-#pragma unroll 4
-    for (int r = 0; r < size; ++r) x = fmaf(s_w[q][r], remote(&mine[i], r), x);
+    float y[kMaxCluster];
+#pragma unroll
+    for (int r = 0; r < kMaxCluster; ++r) y[r] = r < size ? remote(&mine[i], r) : 0.0f;
+#pragma unroll
+    for (int r = 0; r < kMaxCluster; ++r)
+      if (r < size) x = fmaf(s_w[q][r], y[r], x);
     if (d < ch.D)
       ((Row*)a.out)[b * a.o_b + (int64_t)(h0 + q) * a.o_h + d] =
           from_f32<Row>(s_all[q] == 0.0f ? 0.0f : x * (vs / s_all[q]));
