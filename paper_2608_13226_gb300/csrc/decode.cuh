@@ -1201,13 +1201,17 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   // 7 queries a head of 128: 320 tiles of up to 300 keys 17 / 16, of 500 18 / 26; 640
   // of 300 26 / 17, of 500 38 / 38, of 1000 62 / 69; 1600 of 300 46 / 28, of 500 79 /
   // 65, of 1000 138 / 122; 8 bits: 640 of 500 30 / 27, of 1000 45 / 50; 1600 of 1000
-  // 97 / 67.  Longer ones have not been measured.
+  // 97 / 67.  Longer ones have not been measured.  float32 computes longer on a key: up
+  // to 48 keys for every such share of tiles; 320 of 300 keys 39 / 40, 468 of up to 155
+  // 30 / 36, 640 of 64 27 / 22, of 300 68 / 80, 1600 of 150 100 / 85, of up to 300 103 /
+  // 128, 6400 (heads of 64) of 300 240 / 178, of 900 582 / 491.
   // Few tiles too, when two tiles of keys (one of float32) are all there is: one sequence
   // of 4 tiles and 16 keys 5.5 / 3.8, of 50 5.5 / 6.2; 60 of 4, 16 keys 6.5 / 4.1, 50 keys
   // 7.2 / 6.5; float32, 8 keys 8.9 / 7.4, 16 keys 9.0 / 8.6 and, for one sequence, 7.9 /
   // 8.2.
   constexpr int kFew = (CT == CP_F32 ? 1 : 2) * S::tk;
-  if (most <= kFew || (columns > all && most <= 16 * kUnit && most * all <= kUnit * (3 * columns + all))) {
+  const int64_t reach = CT == CP_F32 ? 48 * columns : kUnit * (3 * columns + all);
+  if (most <= kFew || (columns > all && most <= 16 * kUnit && most * all <= reach)) {
     using Short = Shape<CT, DP, QT, true>;
     static std::atomic<uint64_t> short_allowed{0};
     CP_TRY_STATUS(allow_smem_once((const void*)k_decode_short<CT, DP, QT>, Short::smem, "decode: shared memory",
