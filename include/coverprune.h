@@ -510,9 +510,10 @@ int coverprune_cache_append(const cp_cache* cache, const void* k, const int64_t*
  *           nothing between calls
  *   status  device int32 or NULL; set to CP_EINVAL (and otherwise not written)
  *           if a visible key lies on a bad page; such keys are left out.
- * Scores, maxima, sums and outputs are float32; with a bfloat16 (8-bit) cache
- * the weights exp(s_j - m) enter the second product as bfloat16 (float16).  The
- * same call gives the same bits.  B * heads <= 2^24; a table's row holds at most
+ * Scores, maxima, sums and outputs are float32; the weights exp(s_j - m) enter
+ * the second product as two bfloat16 terms with a bfloat16 cache (their sum off
+ * by 2^-16 at most), as one float16 with an 8-bit cache.  The same call gives
+ * the same bits.  B * heads <= 2^24; a table's row holds at most
  * 2^30 keys (everywhere).
  */
 int coverprune_decode_workspace_size(int64_t B, int64_t Hq, const cp_cache* cache, size_t* bytes);

@@ -5,23 +5,32 @@
 // Each visible key and value row is read once for up to 16 query heads, and a
 // bf16 cache gives 1 flop a byte and query head: the kernel is bound by HBM as
 // long as enough bytes are in flight (about 1 us of it, 45 KB an SM) whatever
-// the lengths.  So
-//  - the keys of all sequences and kv heads are one line of units of 64 keys,
-//    cut evenly among as many blocks as the device holds at a time: a single
-//    long sequence and a batch of ragged ones fill it alike, and no lengths have
-//    to be known on the host;
-//  - in a block every warp runs on its own: it copies tiles of 16 keys (16 rows
-//    of K and of V, wherever their pages are) into a ring in shared memory by
-//    16-byte asynchronous copies, several tiles ahead, and keeps its own running
-//    maximum, sum and output; no barrier between warps until a segment (the
-//    block's part of one sequence and kv head) ends;
-//  - a segment that is a whole sequence is written out, a part of one goes to
-//    the workspace and k_decode_join adds the parts in the order of the blocks.
+// the lengths.  In a block every warp runs on its own: it copies tiles of 16 keys
+// (16 rows of K and of V, wherever their pages are; 8 of float32) into a ring in
+// shared memory by 16-byte asynchronous copies, several tiles ahead, and keeps its
+// own running maximum, sum and output; no barrier between warps until the block's
+// part of one sequence and kv head ends, and no lengths have to be known on the
+// host.  How the keys of the B sequences and their kv heads are dealt out
+// (launch() has the rule and both sides of each of its lines):
+//  - k_decode, one line: the keys of all of them are one line of units of 64
+//    keys, cut evenly among as many blocks as the device holds at a time, so that
+//    one long sequence and a batch of ragged ones fill it alike.  What is whole in
+//    a block is written out, a part goes to the workspace, and k_decode_join adds
+//    the parts in the order of the blocks: 32 sequences of 8192 to 8704
+//    keys and 4 kv heads of 128 90 us (0.91 of the HBM's rate), one of 200,001 and 8
+//    heads 129 us (0.94).
+//  - k_decode_cluster: few sequences have a cluster of blocks each, whose parts
+//    meet in shared memory: no second launch.  One sequence of 1500 keys 6.5 us,
+//    with parts through the workspace 8.2.
+//  - k_decode, uncut: sequences of at most 256 keys, a block each.
+//  - k_decode_short: many short ones, or hardly any keys, a warp each; nothing is
+//    to be merged.
 // The products run on mma.sync with keys as rows: S^T = K Q^T (16 keys x 8
 // queries) and O^T = V^T P^T, so a group of 8 query heads wastes nothing and
-// the columns of S and O lie in the same lanes.  One tile of 16 keys costs 16
-// MMAs of a warp (head 128, 8 queries) for 8 KB: a tenth of the tensor pipe at
-// the full rate of HBM, where tcgen05's 128 rows would be 7 of 8 empty.
+// the columns of S and O lie in the same lanes.  One tile of 16 keys costs 24
+// MMAs of a warp (head 128, 8 queries; a third of them for the weights' second
+// term) for 8 KB: a sixth of the tensor pipe at the full rate of HBM, where
+// tcgen05's 128 rows would be 7 of 8 empty.
 #pragma once
 
 #include "rope.cuh"
