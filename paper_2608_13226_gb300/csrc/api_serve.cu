@@ -26,11 +26,12 @@ static int rope_of(const cp_rope* r, int64_t D, int back, Rope* out) {
   return CP_OK;
 }
 
-static int rows_of(const cp_rows& r, int dtype, RowSet* out) {
+// Rows' description; where `tokens` is false there need not be memory.
+static int rows_of(const cp_rows& r, int dtype, bool tokens, RowSet* out) {
   if (r.heads < 0 || r.heads > 65536) return CP_EINVAL;
   *out = RowSet{r.in, r.out, r.in_stride[0], r.in_stride[1], r.in_stride[2],
                 r.out_stride[0], r.out_stride[1], r.out_stride[2], (int)r.heads};
-  if (r.heads == 0) return CP_OK;
+  if (r.heads == 0 || !tokens) return CP_OK;
   if (!r.in || !r.out || !aligned(r.in, size_of(dtype)) || !aligned(r.out, size_of(dtype)))
     return CP_EINVAL;
   return CP_OK;
@@ -125,7 +126,7 @@ int coverprune_rotary(const cp_rows* rows, int n, int dtype, int64_t B, int64_t 
   CP_TRY_STATUS(rope_of(rope, D, inverse, &a.rope));
   int64_t heads = 0;
   for (int i = 0; i < n; ++i) {
-    CP_TRY_STATUS(rows_of(rows[i], dtype, &a.set[i]));
+    CP_TRY_STATUS(rows_of(rows[i], dtype, true, &a.set[i]));
     heads += rows[i].heads;
   }
   if (B == 0 || T == 0 || heads == 0) return CP_OK;
@@ -151,7 +152,7 @@ int coverprune_cache_append(const cp_cache* cache, const void* k, const int64_t*
   CP_TRY_STATUS(cache_of(cache, true, &a.cache));
   if (cache->dtype != CP_E4M3 && cache->dtype != dtype) return CP_EUNSUPPORTED;
   CP_TRY_STATUS(rope_of(rope, cache->D, 0, &a.rope));
-  if (q) CP_TRY_STATUS(rows_of(*q, dtype, &a.q));
+  if (q) CP_TRY_STATUS(rows_of(*q, dtype, T > 0, &a.q));
   if (!starts && T != B) return CP_EINVAL;
   if (B == 0) return CP_OK;  // whatever rows there are, are padding
   if (!lens || !aligned(lens, 4) || !aligned(starts, 4) || !aligned(new_lens, 4) ||

@@ -167,7 +167,7 @@ cp_cache cache_of(Call& c, PyObject* k_cache, PyObject* v_cache, PyObject* table
   x.k_scale = c.optional<const float>("k_scale", k_scale, at::kFloat, {x.heads}, false);
   x.v_scale = c.optional<const float>("v_scale", v_scale, at::kFloat, {x.heads}, false);
   x.table = (const int32_t*)t.data_ptr();
-  x.table_width = t.size(1);
+  x.table_width = t.size(0) ? t.size(1) : 0;  // nothing, at no address
   x.table_stride = t.stride(0);
   return x;
 }
@@ -250,6 +250,7 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
       const Tensor& x = THPVariable_Unpack(xs[i]);
       if (!given) made[i] = c.like(x);
       rows[i] = rows_of(x, given ? c.result("out", outs[i], x) : made[i]);
+      if (B == 0 || T == 0) rows[i].heads = 0;  // nothing, at no address
     }
     const int st = launch([&] {
       return coverprune_rotary(rows, (int)n, dtype, B, T, D, (const int64_t*)pos.data_ptr(), pos_stride, &rope, inverse,

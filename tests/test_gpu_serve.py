@@ -242,6 +242,26 @@ def test_append_many_tokens(Hq, Hk, D, rot, page, hf, dtype, cdt):
     check_append(D + Hq, [9000, 0, 12345, 7001, 1], [3, 0, 100, 0, 77], page, Hq, Hk, D, rot, dtype, cdt, hf, scales=cdt == E4M3)
 
 
+def test_no_tokens_at_all():
+    """Tensors without an element, whose address is null."""
+    f, kc, vc = freq(32), torch.zeros(4, 16, 2, 64, device="cuda"), torch.zeros(4, 16, 2, 64, device="cuda")
+    table = torch.arange(4, device="cuda").int().view(2, 2)
+    none = torch.empty(0, 2, 64, device="cuda")
+    lens = torch.tensor([3, 0], dtype=torch.int32, device="cuda")
+    for pos in (None, torch.empty(0, dtype=torch.int64, device="cuda")):
+        r = cp.coverprune_cache_append(none, none, kc, vc, table, lens, starts=torch.zeros(3, dtype=torch.int32, device="cuda"),
+                                       pos=pos, inv_freq=f, q=torch.empty(0, 6, 64, device="cuda"))
+        assert r["lens"].tolist() == [3, 0] and r["q"].shape == (0, 6, 64)
+    r = cp.coverprune_cache_append(none, none, kc, vc, table[:0], lens[:0], inv_freq=f, q=torch.empty(0, 6, 64, device="cuda"))
+    assert r["lens"].shape == (0,)
+    assert not bool(kc.any()) and not bool(vc.any())
+    for shape in ((1, 0, 2, 64), (0, 5, 2, 64), (2, 3, 0, 64)):
+        x = torch.empty(shape, device="cuda")
+        assert cp.coverprune_rotary(x, torch.zeros(shape[:2], dtype=torch.int64, device="cuda"), f).shape == shape
+    r = cp.coverprune_decode_attention(torch.empty(0, 4, 64, device="cuda"), kc, vc, table[:0], lens[:0], lse=True)
+    assert r["out"].shape == (0, 4, 64) and r["lse"].shape == (0, 4)
+
+
 def test_append_many_and_padding():
     check_append(1, [0] * 700 + [3] + [0] * 300 + [2, 1], [1] * 1003, 4, 0, 1, 64, 64, BF16, BF16, padding=3)
     check_append(2, [1] * 1500, [7] * 1500, 16, 2, 1, 64, 64, BF16, E4M3, starts=False, scales=True)
