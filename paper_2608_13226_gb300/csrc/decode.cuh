@@ -507,9 +507,17 @@ struct Math<CP_F32, DP, QT, SHORT> {
   __device__ __forceinline__ void start(const DecodeArgs& a, int b, int hk, int h0, int nq, char* extra,
                                         int warp, int lane) {
     float* sq = queries(extra, warp);  // the block's, of which each warp fills a part, or the warp's
-    for (int i = SHORT ? lane : warp * 32 + lane; i < QT * DP; i += SHORT ? 32 : kThreads) {
-      const int n = i / DP, d = i % DP;
-      sq[i] = n < nq && d < a.cache.D ? ((const float*)a.q)[b * a.q_b + (int64_t)(h0 + n) * a.q_h + d] : 0.0f;
+    const float* src = (const float*)a.q + b * a.q_b + (int64_t)h0 * a.q_h;
+    const bool quads = (((uint64_t)a.q | (uint64_t)(4 * a.q_b) | (uint64_t)(4 * a.q_h)) & 15) == 0;
+#pragma unroll 4
+    for (int i = SHORT ? lane : warp * 32 + lane; i < QT * (DP / 4); i += SHORT ? 32 : kThreads) {
+      const int n = i / (DP / 4), d = 4 * (i % (DP / 4));  // heads are a multiple of 4
+      float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (n < nq && d < a.cache.D) {
+        const float* from = src + n * a.q_h + d;
+        x = quads ? *(const float4*)from : make_float4(from[0], from[1], from[2], from[3]);
+      }
+      *(float4*)(sq + 4 * i) = x;
     }
     if (SHORT)
       __syncwarp();
