@@ -62,7 +62,11 @@ template <> struct Type<CP_F32> { static constexpr int e = 4, tk = 8; using Row 
 // heads a pass, SHORT whether each warp has sequences of its own (k_decode_short).
 template <int CT, int DP, int QT, bool SHORT = false>
 struct Shape {
-  static constexpr int e = Type<CT>::e, tk = Type<CT>::tk;
+  static constexpr int e = Type<CT>::e;
+  // Keys of a tile: 4 of float32 heads of 256, whose rings leave room for two blocks then:
+  // 102 sequences of 574 to 1149 keys and 6 query tiles 242 us, with 8 keys and one block
+  // 283; 47 of up to 125 15.0, 18.3.
+  static constexpr int tk = CT == CP_F32 && DP == 256 ? 4 : Type<CT>::tk;
   static constexpr int row = DP * e;                  // bytes of a row in shared memory
   static constexpr int cpr = row / 16;                // 16-byte chunks of it
   static constexpr int tile = 2 * tk * row;           // K and V of a tile
@@ -500,6 +504,7 @@ template <int DP, int QT, bool SHORT>
 struct Math<CP_F32, DP, QT, SHORT> {
   using S = Shape<CP_F32, DP, QT, SHORT>;
   static constexpr int V = DP / 32;  // components of a lane
+  static constexpr int L = 32 / S::tk;  // lanes of a key
   float o[QT][V];
   float m[QT], l[QT];
   float sc;
@@ -545,25 +550,25 @@ struct Math<CP_F32, DP, QT, SHORT> {
     float* sp = (float*)extra + S::queries * QT * DP + warp * S::tk * QT;
     const char* smem = extra - S::ring;
     const char* keys = smem + (at - smem_addr(smem));
-    const int r = lane / 4, sub = lane % 4;
+    const int r = lane / L, sub = lane % L;
     float s[QT];
 #pragma unroll
     for (int n = 0; n < QT; ++n) s[n] = 0.0f;
     // Chunks of the key in flight at a time: 32 sequences of 1000 to 4000 keys and 32
     // heads of 64 246 us, one by one 292.
-    constexpr int kHeld = S::cpr / 4 < 8 ? S::cpr / 4 : 8;
+    constexpr int kHeld = S::cpr / L < 8 ? S::cpr / L : 8;
 #pragma unroll
-    for (int j0 = 0; j0 < S::cpr / 4; j0 += kHeld) {
+    for (int j0 = 0; j0 < S::cpr / L; j0 += kHeld) {
       float4 k[kHeld];
 #pragma unroll
       for (int j = 0; j < kHeld; ++j)
         k[j] = *(const float4*)(keys + r * S::row +
-                                16 * ((4 * (j0 + j) + sub) ^ swizzle<CP_F32, S::cpr>(r)));
+                                16 * ((L * (j0 + j) + sub) ^ swizzle<CP_F32, S::cpr>(r)));
 #pragma unroll
       for (int j = 0; j < kHeld; ++j)
 #pragma unroll
         for (int n = 0; n < QT; ++n) {
-          const float4 x = *(const float4*)(sq + n * DP + 4 * (4 * (j0 + j) + sub));
+          const float4 x = *(const float4*)(sq + n * DP + 4 * (L * (j0 + j) + sub));
           s[n] = fmaf(x.x, k[j].x, fmaf(x.y, k[j].y, fmaf(x.z, k[j].z, fmaf(x.w, k[j].w, s[n]))));
         }
     }
@@ -571,8 +576,8 @@ struct Math<CP_F32, DP, QT, SHORT> {
     bool above = false;
 #pragma unroll
     for (int n = 0; n < QT; ++n) {
-      s[n] += __shfl_xor_sync(~0u, s[n], 1);
-      s[n] += __shfl_xor_sync(~0u, s[n], 2);
+#pragma unroll
+      for (int d = 1; d < L; d *= 2) s[n] += __shfl_xor_sync(~0u, s[n], d);
       above |= there && s[n] * sc > m[n] + kSlack;
     }
     if (__any_sync(~0u, above)) {
@@ -580,7 +585,7 @@ struct Math<CP_F32, DP, QT, SHORT> {
       for (int n = 0; n < QT; ++n) {
         float top = there ? fmaxf(s[n] * sc, m[n]) : m[n];
 #pragma unroll
-        for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+        for (int d = L; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
         const float f = exp2f(m[n] - top);
         m[n] = top;
         l[n] *= f;
@@ -636,7 +641,7 @@ struct Math<CP_F32, DP, QT, SHORT> {
 #pragma unroll
     for (int n = 0; n < QT; ++n) {
 #pragma unroll
-      for (int d = 4; d < 32; d *= 2) l[n] += __shfl_xor_sync(~0u, l[n], d);
+      for (int d = L; d < 32; d *= 2) l[n] += __shfl_xor_sync(~0u, l[n], d);
       const float by = vs / l[n];
 #pragma unroll
       for (int i = 0; i < V; ++i) out(n, component(i, threadIdx.x % 32), l[n] == 0.0f ? 0.0f : o[n][i] * by);
@@ -647,7 +652,7 @@ struct Math<CP_F32, DP, QT, SHORT> {
 #pragma unroll
     for (int n = 0; n < QT; ++n) {
 #pragma unroll
-      for (int d = 4; d < 32; d *= 2) l[n] += __shfl_xor_sync(~0u, l[n], d);
+      for (int d = L; d < 32; d *= 2) l[n] += __shfl_xor_sync(~0u, l[n], d);
       if (threadIdx.x % 32 == 0) {
         sm[n] = m[n];
         sl[n] = l[n];
@@ -1226,7 +1231,7 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   // of 4 tiles and 16 keys 5.5 / 3.8, of 50 5.5 / 6.2; 60 of 4, 16 keys 6.5 / 4.1, 50 keys
   // 7.2 / 6.5; float32, 8 keys 8.9 / 7.4, 16 keys 9.0 / 8.6 and, for one sequence, 7.9 /
   // 8.2.
-  constexpr int kFew = (CT == CP_F32 ? 1 : 2) * S::tk;
+  constexpr int kFew = CT == CP_F32 ? 8 : 32;
   const int64_t reach = CT == CP_F32 ? 48 * columns : kUnit * (3 * columns + all);
   if (most <= kFew || (columns > all && most <= 16 * kUnit && most * all <= reach)) {
     using Short = Shape<CT, DP, QT, true>;
@@ -1246,10 +1251,16 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   // 8.2 / 6.7, of 1500 8.2 / 7.2, of 8000 16.1 / 11.3, of 16000 16.2 / 17.3; 64 of 1500
   // 15.4 / 11.3, of 4000 29.9 / 26.2, of 8000 with 15% marked 19.8 / 16.2; 128 of 1229
   // to 1741 24.1 / 22.8.
+  // float32 computes longer on a unit: half of the longest one's time and a quarter of
+  // what idles; 64 tiles of 500 to 3000 keys 46 / 67 (heads of 256), 27 / 34 (128), 19 /
+  // 25 (64), of 1500 41 / 40, 23.2 / 21.4, 17.4 / 15.7; 4 of 4000 16.1 / 19.5, 12.3 / 12.6,
+  // 10.6 / 11.6, of 1500 12.0 / 11.0, 9.3 / 8.2, 8.1 / 7.4.
   const int64_t n64 = (most + kUnit - 1) / kUnit;
   int size = 0;
   if (cut) CP_TRY_STATUS((cluster_size<CT, DP, QT>(columns, all, &size)));
-  if (size > 1 && n64 <= (a.keep ? 48 : 16) * size && n64 * (all - columns * size) <= 8 * size * all)
+  const bool slow = CT == CP_F32 && !a.keep;
+  if (size > 1 && n64 <= (a.keep ? 48 : slow ? 8 : 16) * size &&
+      n64 * (all - columns * size) <= (slow ? 2 : 8) * size * all)
     return cuda_status(launch_early_cluster(k_decode_cluster<CT, DP, QT>, dim3((unsigned)(columns * size)), kThreads, S::smem,
                                             s, size, a, rows, tiles, size),
                        "decode: cluster");
