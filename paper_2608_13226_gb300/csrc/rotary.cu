@@ -233,7 +233,7 @@ __device__ __forceinline__ void run_rows(Job& job, const Rope& rope, const Tilin
 
   const int64_t first = tokens * blockIdx.x / gridDim.x, last = tokens * (blockIdx.x + 1) / gridDim.x;
   const int vec0 = threadIdx.x % tl.wide, lane = threadIdx.x / tl.wide;
-  const int rows = job.rows * tl.parts, turned_places = tl.half / V;
+  const int rows = job.rows * tl.parts, turned_places = (tl.half + V - 1) / V;
   const bool works = lane < tl.lanes;
   // The pair whose angles a thread computes, and the first token (-1: none).
   const int p0 = threadIdx.x % tl.pairs, tok0 = threadIdx.x / tl.pairs < tl.side ? threadIdx.x / tl.pairs : -1;
@@ -360,7 +360,7 @@ __device__ __forceinline__ void run_rows(Job& job, const Rope& rope, const Tilin
               float co[V], si[V];
               if (rope.interleaved) {
                 constexpr int H = V > 1 ? V / 2 : 1;  // pairs of a vector
-                const int at = x.angles + p.at0 / 2, bt = x.angles + p.at1 / 2;
+                const int at = x.angles + p.at0 / 2, bt = p.n > 1 ? x.angles + p.at1 / 2 : at;
                 load_floats<H>(s_cos + at, co);
                 load_floats<H>(s_sin + at, si);
                 load_floats<H>(s_cos + bt, co + V - H);
@@ -517,7 +517,12 @@ static Divisor divisor(int d) {
   return Divisor{(uint32_t)d, (uint32_t)((((uint64_t)1 << (31 + l)) + d - 1) / d), l};
 }
 static size_t slots_of(int bytes) { return bytes >= 4 ? 8 * kItems * kThreads * (size_t)bytes : 0; }
-static int places_of(int half, int D, int V) { return half / V + (D - 2 * half + 2 * V - 1) / (2 * V); }
+static int places_of(int half, int D, int V) { return (half + V - 1) / V + (D - 2 * half + 2 * V - 1) / (2 * V); }
+// Whether rows come in vectors of V: in the half layout a pair's second components are
+// vectors of their own, interleaved both are in one vector.
+static bool vectors(const Rope& r, int D, int V) {
+  return (r.interleaved && V > 1 ? 2 * r.half : r.half) % V == 0 && D % V == 0;
+}
 static Tiling tiling(int half, int D, int V, int subs, int rows, int bytes) {
   Tiling t;
   t.half = half;
@@ -588,7 +593,7 @@ int launch_rotary(const RotaryArgs& args, int dtype, cudaStream_t s) {
     }
   a.n = n;
   auto all = [&](int V) {
-    if (a.rope.half % V || a.D % V) return false;
+    if (!vectors(a.rope, a.D, V)) return false;
     for (int i = 0; i < n; ++i)
       if (!fits(a.set[i], V, dtype == CP_BF16 ? 2 : 4)) return false;
     return true;
@@ -626,7 +631,7 @@ static int append_wide(const AppendArgs& a, cudaStream_t s) {
   auto all = [&](int V) {
     const int64_t k[2] = {a.k_t, a.k_h}, v[2] = {a.v_t, a.v_h};
     // a cache's rows start on 16 bytes and hold a multiple of it
-    return a.rope.half % V == 0 && a.cache.D % V == 0 && fits(a.k, k, 2, V, sizeof(T)) && fits(a.v, v, 2, V, sizeof(T)) &&
+    return vectors(a.rope, a.cache.D, V) && fits(a.k, k, 2, V, sizeof(T)) && fits(a.v, v, 2, V, sizeof(T)) &&
            (a.q.heads == 0 || fits(a.q, V, sizeof(T)));
   };
   if (sizeof(T) == 2 && all(8)) return append_scaled<T, C, sizeof(T) == 2 ? 8 : 4>(a, s);

@@ -242,6 +242,19 @@ def test_append_many_tokens(Hq, Hk, D, rot, page, hf, dtype, cdt):
     check_append(D + Hq, [9000, 0, 12345, 7001, 1], [3, 0, 100, 0, 77], page, Hq, Hk, D, rot, dtype, cdt, hf, scales=cdt == E4M3)
 
 
+@pytest.mark.parametrize("dtype,cdt", [(BF16, BF16), (F32, F32), (BF16, E4M3)])
+@pytest.mark.parametrize("D,rot", [(80, 20), (80, 40), (96, 24), (96, 72), (128, 8), (16, 12)])
+def test_append_interleaved_part(D, rot, dtype, cdt):
+    """Turned parts of an odd number of vectors."""
+    check_append(D + rot, [5, 0, 40, 1], [0, 3, 9, 70], 16, 5, 2, D, rot, dtype, cdt, layout="interleaved", scales=cdt == E4M3)
+    x = randn(gen(rot), 2, 700, 3, D, dtype=dtype)
+    pos = torch.randint(0, 1 << 20, (2, 700), generator=gen(D), device="cuda")
+    y = cp.coverprune_rotary(x, pos, freq(rot // 2), layout="interleaved", inverse=True)
+    want, mag = turned(x, pos, freq(rot // 2), "interleaved", back=True)
+    assert_stored(y, want, 5e-7 * mag, "rotary")
+    assert torch.equal(y[..., rot:], x[..., rot:])
+
+
 def test_no_tokens_at_all():
     """Tensors without an element, whose address is null."""
     f, kc, vc = freq(32), torch.zeros(4, 16, 2, 64, device="cuda"), torch.zeros(4, 16, 2, 64, device="cuda")
