@@ -1227,13 +1227,17 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   // to 48 keys for every such share of tiles; 320 of 300 keys 39 / 40, 468 of up to 155
   // 30 / 36, 640 of 64 27 / 22, of 300 68 / 80, 1600 of 150 100 / 85, of up to 300 103 /
   // 128, 6400 (heads of 64) of 300 240 / 178, of 900 582 / 491.
+  // Of marked keys, which may be few, twice that (float32: five times): 10% / 50% marked,
+  // 1000 tiles of up to 1000 keys 31 / 16, 50 / 48, 8 bits 30 / 14, 45 / 35, float32 of up
+  // to 600 41 / 24, 89 / 81; beyond it what some gain others lose: 1000 of up to 2000 37 /
+  // 31, 76 / 90, float32 of up to 1000 50 / 34, 122 / 129.
   // Few tiles too, when two tiles of keys (one of float32) are all there is: one sequence
   // of 4 tiles and 16 keys 5.5 / 3.8, of 50 5.5 / 6.2; 60 of 4, 16 keys 6.5 / 4.1, 50 keys
   // 7.2 / 6.5; float32, 8 keys 8.9 / 7.4, 16 keys 9.0 / 8.6 and, for one sequence, 7.9 /
   // 8.2.
   constexpr int kFew = CT == CP_F32 ? 8 : 32;
-  const int64_t reach = CT == CP_F32 ? 48 * columns : kUnit * (3 * columns + all);
-  if (most <= kFew || (columns > all && most <= 16 * kUnit && most * all <= reach)) {
+  const int64_t reach = CT == CP_F32 ? (a.keep ? 240 : 48) * columns : (a.keep ? 2 : 1) * kUnit * (3 * columns + all);
+  if (most <= kFew || (columns > all && most <= (a.keep ? 32 : 16) * kUnit && most * all <= reach)) {
     using Short = Shape<CT, DP, QT, true>;
     static std::atomic<uint64_t> short_allowed{0};
     CP_TRY_STATUS(allow_smem_once((const void*)k_decode_short<CT, DP, QT>, Short::smem, "decode: shared memory",

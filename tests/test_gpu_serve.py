@@ -443,6 +443,15 @@ def test_decode_many_short(Hq, H, D, page, cdt, scales):
 
 
 @pytest.mark.parametrize("cdt,scales", TYPES)
+@pytest.mark.parametrize("Hq,H,D,page,keep", [(14, 2, 128, 16, 0.1), (8, 8, 64, 1, 0.5), (6, 2, 256, 100, 0.02)])
+def test_decode_many_marked(Hq, H, D, page, keep, cdt, scales):
+    """Many sequences of some hundred keys of which few are marked, and some none."""
+    lens = [0, 1, 200, 517, 64, 333, 1000, 90] * (50 if H == 2 else 13)
+    check_decode(D, lens, page, Hq, H, D, cdt, scales=scales, keep=keep, junk=math.nan, heads_first=True)
+    check_decode(D + 1, lens, page, Hq, H, D, cdt, scales=scales, keep=keep, window=400, junk=math.nan)
+
+
+@pytest.mark.parametrize("cdt,scales", TYPES)
 @pytest.mark.parametrize("Hq,H,D,page", [(14, 2, 128, 16), (1, 1, 64, 7), (12, 1, 256, 100), (24, 2, 80, 1), (4, 4, 16, 64)])
 def test_decode_few_long(Hq, H, D, page, cdt, scales):
     """Few query tiles, which clusters of blocks share, at lengths that leave some of them
