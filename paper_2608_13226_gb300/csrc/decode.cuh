@@ -1224,7 +1224,7 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   // of 300 26 / 17, of 500 38 / 38, of 1000 62 / 69; 1600 of 300 46 / 28, of 500 79 /
   // 65, of 1000 138 / 122; 8 bits: 640 of 500 30 / 27, of 1000 45 / 50; 1600 of 1000
   // 97 / 67.  Longer ones have not been measured.  float32 computes longer on a key: up
-  // to 48 keys for every such share of tiles; 320 of 300 keys 39 / 40, 468 of up to 155
+  // to 48 keys for every blocks' number that there are tiles; 320 of 300 keys 39 / 40, 468 of up to 155
   // 30 / 36, 640 of 64 27 / 22, of 300 68 / 80, 1600 of 150 100 / 85, of up to 300 103 /
   // 128, 6400 (heads of 64) of 300 240 / 178, of 900 582 / 491.
   // Of marked keys, which may be few, twice that (float32: five times): 10% / 50% marked,
