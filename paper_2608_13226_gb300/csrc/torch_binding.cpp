@@ -356,6 +356,7 @@ PyObject* decode_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
       ws = c.made({(int64_t)bytes}, at::kByte);
     }
     const Tensor& work = a[12] == Py_None ? ws : c.tensor("ws", a[12]);
+    if (!work.is_contiguous()) bad_value("ws must be contiguous");  // all its bytes are written to, in a row
     if (a[11] == Py_None) out = c.made(q.sizes(), q.scalar_type());
     const Tensor& to = a[11] == Py_None ? out : c.result("out", a[11], q);
     if (with_lse) lse = c.made({B, Hq}, at::kFloat);
