@@ -406,13 +406,22 @@ struct Math {
       l[n][1] += x[1] + x[3];
       // A weight goes on in 11 bits beside an 8-bit cache, float16's.  bfloat16's 8 would
       // add as much error as the output's own rounding (0.0024 of its norm against
-      // 0.0017), so what they leave goes on as well, in a second product.
+      // 0.0017), so what they leave goes on as well, in a second product.  The first term
+      // is the largest bfloat16 below the weight: what it leaves is above 0 then, never 0
+      // or less, and an infinite value stays that infinity in both products (but for weights
+      // below 2^-100, whose second term may be none).
       if (CT == CP_BF16) {
-        const uint32_t lo = pack_bf16(x[0], x[1]), hi = pack_bf16(x[2], x[3]);
-        p[n][0] = movmatrix_trans(lo);
-        p[n][1] = movmatrix_trans(hi);
-        rest[n][0] = movmatrix_trans(pack_bf16(x[0] - __uint_as_float(lo << 16), x[1] - __uint_as_float(lo & 0xFFFF0000u)));
-        rest[n][1] = movmatrix_trans(pack_bf16(x[2] - __uint_as_float(hi << 16), x[3] - __uint_as_float(hi & 0xFFFF0000u)));
+        uint32_t below[4];
+        float left[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          below[i] = (uint32_t)max(__float_as_int(x[i]) - 1, 0);  // 0 stays 0
+          left[i] = x[i] - __uint_as_float(below[i] & 0xFFFF0000u);
+        }
+        p[n][0] = movmatrix_trans(__byte_perm(below[0], below[1], 0x7632));
+        p[n][1] = movmatrix_trans(__byte_perm(below[2], below[3], 0x7632));
+        rest[n][0] = movmatrix_trans(pack_bf16(left[0], left[1]));
+        rest[n][1] = movmatrix_trans(pack_bf16(left[2], left[3]));
       } else {
         p[n][0] = movmatrix_trans(pack_f16(x[0], x[1]));
         p[n][1] = movmatrix_trans(pack_f16(x[2], x[3]));

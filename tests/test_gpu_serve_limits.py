@@ -1,13 +1,19 @@
 """The decoding model's operators at the edges of what they take: arguments that
 are refused, values at the ends of a type, and the bounds that the header states."""
+import math
+
 import pytest
 import torch
 
 import paper_2608_13226_gb300 as cp
+from test_gpu_serve import ULP, attention, gen, pool, randn
 
 pytestmark = pytest.mark.gpu
 E4M3 = torch.float8_e4m3fn
 BF16, F32 = torch.bfloat16, torch.float32
+# lengths that are dealt out in each way: a warp a query tile (few keys; many
+# sequences), a block each, a cluster each, one line
+LENGTHS = {"tiny": [5, 9, 1], "warps": [300, 41] * 200, "blocks": [200, 130, 256], "clusters": [1500, 3], "line": [700] * 200}
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -31,3 +37,31 @@ def test_workspace_that_is_not_dense_is_refused():
             cp.coverprune_decode_attention(q, kc, vc, table, lens, ws=bad)
     assert not bool(room.any())
     cp.coverprune_decode_attention(q, kc, vc, table, lens, ws=room.view(2, n)[0])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("lens", LENGTHS.values(), ids=list(LENGTHS))
+def test_infinite_values(lens, dtype):
+    """An infinite visible value makes its component infinite, two of both signs NaN, and no
+    other component notices."""
+    g, B, H, G, D, page = gen(len(lens)), len(lens), 2, 3, 64, 16
+    W = -(-max(lens) // page)
+    kc, vc = pool(g, B * W, page, H, D, dtype), pool(g, B * W, page, H, D, dtype)
+    table = torch.randperm(B * W, generator=g, device="cuda").int().view(B, W)
+    n = torch.tensor(lens, device="cuda")
+    # a key of each sequence, another one, and what they hold in components 5, 9 and 40
+    one = (torch.rand(B, generator=g, device="cuda") * n).long()
+    other = (one + 1 + (torch.rand(B, generator=g, device="cuda") * (n - 1)).long()) % n
+    seq = torch.arange(B, device="cuda")
+    for key, at, x in ((one, 5, math.inf), (other, 9, -math.inf), (one, 40, math.inf), (other, 40, -math.inf)):
+        some = n > 1 if at == 40 else n > 0
+        vc[table.long()[seq, key // page][some], (key % page)[some], 1, at] = x
+    q, lens = randn(g, B, G * H, D, dtype=dtype), n.int()
+    got = cp.coverprune_decode_attention(q, kc, vc, table, lens)["out"].double()
+    want, _, dout, _ = attention(q, kc, vc, table, lens, None, None, 0, None, D ** -0.5)
+    assert bool((want[:, G:, 5] == math.inf).all()) and bool((want[:, G:, 9] == -math.inf).all())
+    assert bool(want[n > 1][:, G:, 40].isnan().all()) and bool(want[:, :G].isfinite().all())
+    assert torch.equal(got.isnan(), want.isnan())
+    assert torch.equal(got.isinf() * got.sign(), want.isinf() * want.sign())
+    fine = want.isfinite()
+    assert bool(((got - want).abs() <= ULP[dtype] * (want.abs() + dout) + dout)[fine].all())
