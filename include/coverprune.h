@@ -512,7 +512,8 @@ int coverprune_cache_append(const cp_cache* cache, const void* k, const int64_t*
  *           if a visible key lies on a bad page; such keys are left out.
  * Scores, maxima, sums and outputs are float32; the weights exp(s_j - m) enter
  * the second product as two bfloat16 terms with a bfloat16 cache (their sum off
- * by 2^-16 at most), as one float16 with an 8-bit cache.  An infinite visible value
+ * by 2^-16 at most), as one float16 with an 8-bit cache (off by 2^-11 of itself
+ * or 2^-32 of the largest weight).  An infinite visible value
  * makes its component that infinity (both signs or a NaN: NaN), unless its
  * weight is below 2^-100 of the largest: float32's 0 times infinity, NaN, may
  * come of that.  The same call gives the same bits.  B * heads <= 2^24; a table's row holds at most

@@ -65,3 +65,33 @@ def test_infinite_values(lens, dtype):
     assert torch.equal(got.isinf() * got.sign(), want.isinf() * want.sign())
     fine = want.isfinite()
     assert bool(((got - want).abs() <= ULP[dtype] * (want.abs() + dout) + dout)[fine].all())
+
+
+@pytest.mark.parametrize("apart", [4.0, 11.0, 15.0, 17.35, 20.0])
+@pytest.mark.parametrize("cdt,n", [(E4M3, 30), (E4M3, 250), (E4M3, 5000), (E4M3, 200001), (BF16, 200001), (F32, 200001)])
+def test_many_weak_keys_beside_a_strong_one(cdt, n, apart):
+    """What n equal keys weigh together beside one that is `apart` (natural units) above each."""
+    D, page, dt = 64, 64, F32 if cdt == F32 else BF16
+    W = -(-n // page)
+    kc, vc = torch.zeros(2, W, page, 1, D, device="cuda")
+    strong = n // 3
+    kc[strong // page, strong % page, 0, 0] = 1.0     # a score of 1 times the scale, where the others have 0
+    vc[..., 0], vc[..., 1] = 1.0, 1.0
+    vc[strong // page, strong % page, 0, 1] = 0.0     # component 0 is 1 whatever the weights, 1 is the weak keys' share
+    q = torch.zeros(1, 1, D, dtype=dt, device="cuda")
+    q[..., 0] = 1.0
+    table = torch.arange(W, device="cuda").int()[None]
+    r = cp.coverprune_decode_attention(q, kc.to(cdt), vc.to(cdt), table, torch.tensor([n], dtype=torch.int32, device="cuda"),
+                                       scale=apart, lse=True)
+    each = math.exp(-apart)
+    total = 1 + (n - 1) * each
+    share = (n - 1) * each / total
+    # a weight is off by 2^-11 of itself and 2^-(25 + 7) of the largest (8 bits), 2^-16 (bfloat16); scores below 32 in float32,
+    # in units of log 2, give 2^-18 at most, sums of n terms n 2^-24 at most (but for very few warps they are far shorter)
+    part = {E4M3: 2.0 ** -11, BF16: 2.0 ** -16, F32: 0.0}[cdt] + 2.0 ** -17 + min(n, 4096) * 2.0 ** -24
+    floor = 2.0 ** -32 * n / total if cdt == E4M3 else 0.0
+    got, want = r["out"][0, 0].double().tolist(), [1.0, share]
+    for i in range(2):
+        off = part * want[i] + floor
+        assert abs(got[i] - want[i]) <= off + ULP[dt] * (want[i] + off), (i, got[i], want[i])
+    assert abs(float(r["lse"]) - (apart + math.log(total))) <= part + 2.0 ** -22 * 32
