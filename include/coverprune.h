@@ -498,6 +498,8 @@ int coverprune_cache_append(const cp_cache* cache, const void* k, const int64_t*
  * over the visible keys j: j < lens[b], j >= lens[b] - window (window > 0), and
  * keep[b * keep_stride + j] != 0 (keep not NULL).  With none visible out is 0
  * and lse -infinity.  Rows that are not visible are not read, whatever they hold.
+ * <q, k_j> and s_j / ln 2 have to stay within float32's range; a key whose score is
+ * -infinity weighs nothing.
  *   q       [B, Hq, D] of `dtype`, q_stride HOST {batch, head} in elements.
  *           bfloat16 goes with a bfloat16 or 8-bit cache, float32 with a float32 one.
  *   lens    device int32 [B]; negative is 0, more than the table's row

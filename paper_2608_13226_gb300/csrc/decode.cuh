@@ -54,7 +54,9 @@ constexpr int kQueue = 128;
 // 54.2 and 55.0 us, with 7 53.9; 128 ragged ones 94.9 and 97.2, with 7 94.9.
 template <int CT> struct Maximum { static constexpr float slack = 8.0f, under = 0.0f; };
 template <> struct Maximum<CP_E4M3> { static constexpr float slack = 15.0f, under = 7.0f; };
-constexpr float kLowest = -1e38f;  // a maximum before any score: finite, so that differences are
+// A maximum before any score: finite, so that differences of two are, and below no
+// finite score (of weight 1 beside it).
+constexpr float kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 

@@ -95,3 +95,37 @@ def test_many_weak_keys_beside_a_strong_one(cdt, n, apart):
         off = part * want[i] + floor
         assert abs(got[i] - want[i]) <= off + ULP[dt] * (want[i] + off), (i, got[i], want[i])
     assert abs(float(r["lse"]) - (apart + math.log(total))) <= part + 2.0 ** -22 * 32
+
+
+@pytest.mark.parametrize("cdt", [BF16, F32, E4M3])
+@pytest.mark.parametrize("lens", LENGTHS.values(), ids=list(LENGTHS))
+def test_scores_near_the_lowest_number(lens, cdt):
+    """Keys that all score about -1.3e38, or -2.2e38: they are visible, alike ones weigh the
+    same, and one that is above the others takes all."""
+    g, dt, B, H, G, D, page = gen(len(lens)), F32 if cdt == F32 else BF16, len(lens), 2, 3, 64, 16
+    W = -(-max(lens) // page)
+    vc = pool(g, B * W, page, H, D, cdt)
+    k = torch.zeros(B * W, page, H, D, device="cuda")
+    q = torch.zeros(B, G * H, D, device="cuda", dtype=dt)
+    unit = 2.0 ** 63
+    q[..., 0] = unit
+    k[..., 0] = -16.0  # kv head 0: all alike; 1: the first key above the rest
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    table = torch.arange(B * W, device="cuda").int().view(B, W)
+    k[:, :, 1, 0] = -28.0
+    k[table[:, 0].long(), 0, 1, 0] = -16.0
+    factor = 2.0 ** 60 if cdt != E4M3 else 1.0  # 8 bits take it as their scale
+    ks = torch.full((H,), 2.0 ** 60, device="cuda") if cdt == E4M3 else None
+    vs = torch.full((H,), 0.02, device="cuda") if cdt == E4M3 else None
+    r = cp.coverprune_decode_attention(q, (k * factor).to(cdt), vc, table, n, scale=0.75, k_scale=ks, v_scale=vs, lse=True)
+    score = -16.0 * 2.0 ** 123 * 0.75
+    assert -1.4e38 < score < -1.2e38 and -28.0 * 2.0 ** 123 * 0.75 / math.log(2) > -3.4028e38
+    v = vc.float().double() * (0.02 if cdt == E4M3 else 1.0)
+    # weights of exactly 1, sums of n terms in float32, one product and quotient, 1 / 0.02 of 8 bits rounded once
+    for b in range(0, B, max(1, B // 7)):
+        m = lens[b]
+        rows = v[table[b].long()].reshape(-1, H, D)[:m]
+        for h, want, mag in ((0, rows[:, 0].mean(0), rows[:, 0].abs().mean(0)), (1, rows[0, 1], rows[0, 1].abs())):
+            got, extra = r["out"][b, h * G:(h + 1) * G].double(), (m + 8) * 2.0 ** -24 * mag
+            assert bool(((got - want).abs() <= ULP[dt] * (want.abs() + extra) + extra).all()), (b, h)
+    assert bool(((r["lse"].double() - score).abs() <= 2.0 ** -22 * abs(score)).all())
