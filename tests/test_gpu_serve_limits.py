@@ -129,3 +129,34 @@ def test_scores_near_the_lowest_number(lens, cdt):
             got, extra = r["out"][b, h * G:(h + 1) * G].double(), (m + 8) * 2.0 ** -24 * mag
             assert bool(((got - want).abs() <= ULP[dt] * (want.abs() + extra) + extra).all()), (b, h)
     assert bool(((r["lse"].double() - score).abs() <= 2.0 ** -22 * abs(score)).all())
+
+
+@pytest.mark.parametrize("lens", LENGTHS.values(), ids=list(LENGTHS))
+def test_bf16_weights_have_two_terms(lens):
+    """Few keys that count and values of one sign, so that errors of weights do not average
+    out: the output is one of the bfloat16 between the exact one less and plus 2^-16 of it.
+    The same computed with weights of a single term is not, so the bound would notice it."""
+    g, B, D, page = gen(len(lens)), len(lens), 64, 16
+    W = -(-max(lens) // page)
+    table = torch.arange(B * W, device="cuda").int().view(B, W)
+    k = torch.zeros(B * W, page, 1, D, dtype=BF16, device="cuda")
+    k[..., 0] = -300.0
+    v = (1 + torch.rand(B * W, page, 1, D, generator=g, device="cuda")).bfloat16()
+    q = torch.zeros(B, 1, D, dtype=BF16, device="cuda")
+    q[..., 0] = 1.0
+    want, single = torch.zeros(B, D, dtype=torch.float64, device="cuda"), torch.zeros(B, D, dtype=torch.float64, device="cuda")
+    for b, n in enumerate(lens):
+        at = torch.randperm(n, generator=g, device="cuda")[:5]
+        page_of = table[b].long()[at // page]
+        score = (-3 * torch.rand(len(at), generator=g, device="cuda")).bfloat16()
+        k[page_of, at % page, 0, 0] = score
+        w = (score.double() - score.double().max()).exp()
+        x = v[page_of, at % page, 0].double()
+        want[b], single[b] = w @ x / w.sum(), w.bfloat16().double() @ x / w.sum()
+    # a score is one product, scaled in float32 (below 8: 2^-21), exp2 within 2^-22, a few sums and a quotient; the rest weigh e^-297
+    off = 2.0 ** -16 + 2.0 ** -19
+    low, high = (want * (1 - off)).bfloat16(), (want * (1 + off)).bfloat16()
+    got = cp.coverprune_decode_attention(q, k, v, table, torch.tensor(lens, dtype=torch.int32, device="cuda"), scale=1.0)["out"][:, 0]
+    assert bool(((low <= got) & (got <= high)).all())
+    other = single.bfloat16()
+    assert bool(((other < low) | (other > high)).any())
