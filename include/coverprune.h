@@ -353,8 +353,8 @@ int coverprune_gather(const void* feats, int dtype, const float* pos, const int3
  *   (a, b) -> scale * (a cos - b sin, b cos + a sin)
  * Components from rot on pass through unchanged.
  *   inv_freq  device, [rot / 2] float64, radians a position (finite).  The
- *             angle is reduced by whole turns in 64-bit fixed point, so it is
- *             as good at position 2^40 as at 1.
+ *             angle is reduced by whole turns in 64-bit fixed point: it is off
+ *             by 2^-64 turns a position (4e-7 at 2^40), besides 6e-8.
  *   rot       even, 0..D (0: nothing is turned and inv_freq is not read)
  *   layout    CP_ROPE_HALF: pair i is components i and i + rot / 2;
  *             CP_ROPE_INTERLEAVED: components 2 i and 2 i + 1

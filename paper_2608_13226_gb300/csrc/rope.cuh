@@ -20,12 +20,20 @@ __device__ __forceinline__ void wait_for_stream(bool at_once = true) {
 
 // A pair's speed as the fraction of a turn that one position takes, in units
 // of 2^-64 turns.  Whole turns drop out, and so they do of position * speed in
-// 64-bit integers: the angle of any position is off by no more than the speed's
-// own rounding (float64: 2^-54 of the turns made).
+// 64-bit integers: the angle of a position is off by 2^-64 turns for each of it.
+// The float64's significand times 2^128 / (2 pi), cut to the units below a turn: integers, as a
+// float64 product's two roundings would make 9e-5 rad at position 2^40.  (Three float64
+// operations that keep what they round off would do as well, 0.1 us later: 1/64 of the
+// float32 rate.)  Speeds of 2^53 and more, which are whole radians, count as 0.
 __device__ __forceinline__ uint64_t rope_turns(double inv_freq) {
-  double t = inv_freq * 0.15915494309189533577;  // 1 / (2 pi)
-  t -= floor(t);
-  return __double2ull_rz(t * 18446744073709551616.0);
+  constexpr uint64_t high = 0x28BE60DB9391054Aull, low = 0x7F09D5F47D4D3770ull;
+  const uint64_t bits = (uint64_t)__double_as_longlong(inv_freq);
+  const int s = (int)(bits >> 52 & 2047) - 1011;  // inv_freq = m 2^(s - 64)
+  if (s > 64 || s < -63) return 0;
+  const uint64_t m = (bits & (((uint64_t)1 << 52) - 1)) | (uint64_t)1 << 52;
+  const unsigned __int128 p = (unsigned __int128)m * high + __umul64hi(m, low);  // m 2^64 / (2 pi)
+  const uint64_t u = (uint64_t)(p >> (64 - s));
+  return bits >> 63 ? 0 - u : u;
 }
 
 // (cos, sin) of the angle, times the scale.  The turn's fraction is cut to 32 bits

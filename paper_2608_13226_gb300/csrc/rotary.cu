@@ -2,9 +2,9 @@
 //
 // Both read every row once and write it once, a few operations an element: HBM
 // bounds them, if about 50 KB an SM of it are on their way all the time.  So
-//  - a block has a run of tokens for the whole call.  The speeds' float64 arithmetic
-//    (1/64 of the float32 rate) is done once a block, and where the tokens go
-//    is looked up kChunk of them at a time, a thread each;
+//  - a block has a run of tokens for the whole call.  The speeds become fractions of a turn
+//    once a block, and where the tokens go is looked up kChunk of them at a time, a
+//    thread each;
 //  - the rows of its tokens are one line, taken a stage of up to 2 (narrow ones 4)
 //    rows a lane at a time.  Between two barriers the block notes where the rows of the
 //    stage after next lie (a thread a row), computes the angles of the next
