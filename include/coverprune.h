@@ -465,8 +465,8 @@ typedef struct {
  *             HOST arrays {token, head} in elements.  A float32 cache takes
  *             float32 rows, a bfloat16 one bfloat16 rows, an 8-bit one either.
  *   starts    device int32 [B + 1]: sequence b's new tokens are rows
- *             starts[b]..starts[b + 1] - 1, ascending from 0 on; rows from starts[B] on are
- *             padding and left alone.  NULL: T == B, one token a sequence.
+ *             starts[b]..starts[b + 1] - 1, ascending; rows before starts[0] and from
+ *             starts[B] on are padding and left alone.  NULL: T == B, one token a sequence.
  *   lens      device int32 [B]: keys that each sequence holds before the call;
  *             token i of sequence b becomes key lens[b] + i
  *   pos       device int64 [T]: positions of the rotation (a kept token's index

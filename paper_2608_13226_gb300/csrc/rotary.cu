@@ -450,9 +450,10 @@ struct AppendJob {
     const Cache& ch = a.cache;
     const int b = a.starts ? sequence_of(a.starts, a.B, t) : (int)t;
     int64_t row = -2, pos = 0;
-    if (b < a.B) {
+    const int64_t i = a.starts && b < a.B ? t - a.starts[b] : 0;  // below 0: before the first sequence's rows
+    if (b < a.B && i >= 0) {
       const int len = a.lens[b];
-      const int64_t slot = (int64_t)len + (a.starts ? t - a.starts[b] : 0);
+      const int64_t slot = (int64_t)len + i;
       pos = a.pos ? a.pos[t] : slot;
       int page = -1;
       if (len >= 0 && slot >= 0 && slot < ch.capacity)

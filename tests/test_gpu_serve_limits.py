@@ -181,3 +181,27 @@ def test_rotary_angles_at_far_positions():
             t = Decimal(p) * Decimal(s) / turn
             a = float((t - t.to_integral_value()) * turn)
             assert abs(y[i, 0, j] - math.cos(a)) <= off and abs(y[i, 0, j + 32] - math.sin(a)) <= off, (p, s)
+
+
+@pytest.mark.parametrize("cdt", [BF16, F32, E4M3])
+def test_rows_before_the_first_sequence_are_padding(cdt):
+    """A part of a longer batch: its starts begin above 0, and what lies before is left alone."""
+    g, dt, page, H, D = gen(5), F32 if cdt == F32 else BF16, 4, 2, 64
+    kc, vc = pool(g, 9, page, H, D, cdt), pool(g, 9, page, H, D, cdt)
+    k0, v0 = kc.clone(), vc.clone()
+    table = torch.randperm(9, generator=g, device="cuda").int().view(3, 3)
+    k, v, q = (randn(g, 15, h, D, dtype=dt) for h in (H, H, 6))
+    lens = torch.tensor([5, 0, 2], dtype=torch.int32, device="cuda")
+    starts = torch.tensor([3, 8, 8, 12], dtype=torch.int32, device="cuda")
+    status, q_out = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.full_like(q, 7.0)
+    r = cp.coverprune_cache_append(k, v, kc, vc, table, lens, starts=starts, q=q, q_out=q_out, status=status)
+    assert r["lens"].tolist() == [10, 0, 6] and int(status) == 0
+    rows = {(0, 5 + i): 3 + i for i in range(5)} | {(2, 2 + i): 8 + i for i in range(4)}
+    for (b, j), t in rows.items():
+        at = (int(table[b, j // page]), j % page)
+        for c, c0, x in ((kc, k0, k), (vc, v0, v)):
+            assert torch.equal(c[at].view(torch.uint8), x[t].to(cdt).view(torch.uint8))
+            c0.view(torch.uint8)[at] = c[at].view(torch.uint8)
+    for c, c0 in ((kc, k0), (vc, v0)):
+        assert torch.equal(c.view(torch.uint8), c0.view(torch.uint8))
+    assert torch.equal(q_out[3:12], q[3:12]) and bool((q_out[:3] == 7).all()) and bool((q_out[12:] == 7).all())
