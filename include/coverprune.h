@@ -475,7 +475,8 @@ typedef struct {
  *   q         NULL, or the queries: B = 1 and T rows as in coverprune_rotary
  *             (the batch strides are not read)
  *   new_lens  device int32 [B] or NULL: lens[b] plus its new tokens, at most what
- *             the table's row holds; must not overlap lens
+ *             the table's row holds; a negative lens[b] stays as it is, as none of its
+ *             tokens is stored; must not overlap lens
  *   status    device int32 or NULL; set to CP_EINVAL (and otherwise not
  *             written) if a token's key lies beyond the table's row or on a bad
  *             page, or lens[b] is negative; that token's key and value are

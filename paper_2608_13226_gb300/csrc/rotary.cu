@@ -492,8 +492,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks) k_cache_append(AppendArgs a
   wait_for_stream();
   if (a.new_lens)
     for (int64_t b = (int64_t)blockIdx.x * kThreads + threadIdx.x; b < a.B; b += (int64_t)gridDim.x * kThreads) {
-      const int64_t n = (int64_t)a.lens[b] + (a.starts ? a.starts[b + 1] - a.starts[b] : 1);
-      a.new_lens[b] = (int32_t)min(n, (int64_t)a.cache.capacity);
+      const int len = a.lens[b];
+      const int64_t n = (int64_t)len + (a.starts ? (int64_t)a.starts[b + 1] - a.starts[b] : 1);
+      a.new_lens[b] = len < 0 ? len : (int32_t)min(n, (int64_t)a.cache.capacity);
     }
   AppendJob<T, C> job{a, a.q.heads + 2 * a.cache.heads, s_row};
   run_rows<T, C, V, SUBS, SCALED>(job, a.rope, tl, a.cache.D, a.T);

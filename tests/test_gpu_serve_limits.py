@@ -205,3 +205,20 @@ def test_rows_before_the_first_sequence_are_padding(cdt):
     for c, c0 in ((kc, k0), (vc, v0)):
         assert torch.equal(c.view(torch.uint8), c0.view(torch.uint8))
     assert torch.equal(q_out[3:12], q[3:12]) and bool((q_out[:3] == 7).all()) and bool((q_out[12:] == 7).all())
+
+
+def test_a_negative_length_stays_negative():
+    """Its tokens are skipped, so the sequence must not come to hold keys that were never written."""
+    g, page, H, D = gen(6), 4, 2, 64
+    kc, vc = pool(g, 6, page, H, D, BF16), pool(g, 6, page, H, D, BF16)
+    k0 = kc.clone()
+    table = torch.arange(6, device="cuda").int().view(3, 2)
+    k = randn(g, 12, H, D, dtype=BF16)
+    lens = torch.tensor([-2, 1, -1], dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, 6, 7, 12], dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    r = cp.coverprune_cache_append(k, k, kc, vc, table, lens, starts=starts, status=status)
+    assert int(status) == cp.CP_EINVAL and r["lens"].tolist() == [-2, 2, -1]
+    assert torch.equal(kc[2, 1], k[6]) and torch.equal(kc[[0, 1, 4, 5]], k0[[0, 1, 4, 5]])
+    out = cp.coverprune_decode_attention(randn(g, 3, 4, D, dtype=BF16), kc, vc, table, r["lens"])["out"]
+    assert bool((out[[0, 2]] == 0).all()) and bool((out[1] != 0).any())
