@@ -476,7 +476,7 @@ typedef struct {
  *             (the batch strides are not read)
  *   new_lens  device int32 [B] or NULL: lens[b] plus its new tokens, at most what
  *             the table's row holds; a negative lens[b] stays as it is, as none of its
- *             tokens is stored; must not overlap lens
+ *             tokens is stored; must not overlap lens or starts
  *   status    device int32 or NULL; set to CP_EINVAL (and otherwise not
  *             written) if a token's key lies beyond the table's row or on a bad
  *             page, or lens[b] is negative; that token's key and value are

@@ -8,6 +8,9 @@
 using namespace cp;
 
 static bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
+static bool overlap(const int32_t* p, int64_t n, const int32_t* q, int64_t m) {
+  return p && q && (uintptr_t)p < (uintptr_t)(q + m) && (uintptr_t)q < (uintptr_t)(p + n);
+}
 static size_t size_of(int dtype) { return dtype == CP_F32 ? 4 : dtype == CP_BF16 ? 2 : 1; }
 
 // Room for a call's element offsets (a stride times a size) in 64 bits.
@@ -158,7 +161,8 @@ int coverprune_cache_append(const cp_cache* cache, const void* k, const int64_t*
   if (!lens || !aligned(lens, 4) || !aligned(starts, 4) || !aligned(new_lens, 4) ||
       !aligned(status, 4) || !aligned(pos, 8))
     return CP_EINVAL;
-  if (new_lens == lens) return CP_EINVAL;
+  // blocks read the lengths and starts while others write
+  if (overlap(new_lens, B, lens, B) || overlap(new_lens, B, starts, B + 1)) return CP_EINVAL;
   if (T > 0 && (!k || !v || !k_stride || !v_stride || !aligned(k, size_of(dtype)) ||
                 !aligned(v, size_of(dtype))))
     return CP_EINVAL;
