@@ -66,6 +66,12 @@ struct Call {
   T* optional(const char* name, PyObject* o, at::ScalarType type, at::IntArrayRef shape = {}, bool any = true) {
     return o == Py_None ? nullptr : (T*)dense(name, o, type, shape, any).data_ptr();
   }
+  // The status word; a tensor without one would pass for none given.
+  int32_t* word(const char* name, PyObject* o) {
+    int32_t* p = optional<int32_t>(name, o, at::kInt);
+    if (o != Py_None && !p) bad_value(std::string(name) + " must have an element");
+    return p;
+  }
   // Rows of heads: only the last dimension has to be dense.
   const Tensor& rows(const char* name, PyObject* o, int dims) {
     if (!THPVariable_Check(o)) bad_type(std::string(name) + " must be a tensor");
@@ -291,7 +297,7 @@ PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
       if (q.size(0) != T || q.size(2) != cache.D || q.scalar_type() != k.scalar_type())
         bad_value("q must be [" + std::to_string(T) + ", heads, " + std::to_string(cache.D) + "] of k's dtype");
     }
-    int32_t* status = c.optional<int32_t>("status", a[16], at::kInt);
+    int32_t* status = c.word("status", a[16]);
     int32_t* given_lens = c.optional<int32_t>("new_lens", a[14], at::kInt, {B}, false);
 
     c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.device);
@@ -344,7 +350,7 @@ PyObject* decode_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     }
     const float scale = a[5] == Py_None ? (float)(1.0 / std::sqrt((double)(cache.D > 0 ? cache.D : 1))) : (float)real(a[5]);
     const int64_t window = integer(a[6]);
-    int32_t* status = c.optional<int32_t>("status", a[13], at::kInt);
+    int32_t* status = c.word("status", a[13]);
     const bool with_lse = PyObject_IsTrue(a[10]) == 1;
 
     c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.device);

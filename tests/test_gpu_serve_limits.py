@@ -222,3 +222,14 @@ def test_a_negative_length_stays_negative():
     assert torch.equal(kc[2, 1], k[6]) and torch.equal(kc[[0, 1, 4, 5]], k0[[0, 1, 4, 5]])
     out = cp.coverprune_decode_attention(randn(g, 3, 4, D, dtype=BF16), kc, vc, table, r["lens"])["out"]
     assert bool((out[[0, 2]] == 0).all()) and bool((out[1] != 0).any())
+
+
+def test_status_without_an_element_is_refused():
+    """Errors would go nowhere, though the caller asked for them."""
+    kc, vc = torch.zeros(2, 4, 16, 2, 64, dtype=BF16, device="cuda")
+    table, lens = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    q, none = torch.zeros(1, 2, 64, dtype=BF16, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        cp.coverprune_decode_attention(q, kc, vc, table, lens, status=none)
+    with pytest.raises(ValueError):
+        cp.coverprune_cache_append(q, q, kc, vc, table, lens, status=none)
