@@ -478,6 +478,29 @@ def coverprune_rotary_frequencies(rot: int, base: float = 10000.0, *, stretch: s
     return f.to(device)
 
 
+class _Rotary(torch.autograd.Function):
+    """The rotation of tensors of which one at least requires a gradient: its gradient is the
+    turn back (the rotation is linear)."""
+
+    @staticmethod
+    def forward(ctx, pos, inv_freq, layout, scale, inverse, *xs):
+        ctx.save_for_backward(pos, inv_freq)
+        ctx.how = layout, scale, inverse
+        ys = coverprune_rotary(xs, pos, inv_freq, layout=layout, scale=scale, inverse=inverse)
+        ctx.mark_non_differentiable(*(y for y, need in zip(ys, ctx.needs_input_grad[5:]) if not need))
+        return tuple(ys)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        pos, inv_freq = ctx.saved_tensors
+        layout, scale, inverse = ctx.how
+        need = ctx.needs_input_grad[5:]
+        # a gradient may be expanded along its last dimension (that of a sum is)
+        rows = [g if g.stride(-1) == 1 else g.contiguous() for g, n in zip(grads, need) if n]
+        back = iter(coverprune_rotary(rows, pos, inv_freq, layout=layout, scale=scale, inverse=not inverse))
+        return (None,) * 5 + tuple(next(back) if n else None for n in need)
+
+
 def coverprune_rotary(x, pos, inv_freq, *, layout: str = "half", scale: float = 1.0,
                       inverse: bool = False, out=None):
     """x turned to its positions: [T, heads, D] with pos int64 [T], or
@@ -485,8 +508,13 @@ def coverprune_rotary(x, pos, inv_freq, *, layout: str = "half", scale: float = 
     four tensors of the same tokens (queries and keys, say), which one launch
     turns; out then is a list too.  Any strides with a dense last dimension;
     out may be x.  inverse=True gives the gradient with respect to x from the
-    one with respect to the result."""
+    one with respect to the result; autograd does so by itself where x requires
+    a gradient (and out is not given)."""
     r = (_T or _torch_lib()).rotary(x, pos, inv_freq, _layout(layout), scale, inverse, out)
+    if r is None:
+        many = isinstance(x, (list, tuple))
+        ys = _Rotary.apply(pos, inv_freq, layout, scale, inverse, *(x if many else (x,)))
+        return list(ys) if many else ys[0]
     if type(r) is int:
         raise CoverPruneError(r, "coverprune_rotary")
     return r
@@ -500,7 +528,8 @@ def coverprune_cache_append(k, v, k_cache, v_cache, table, lens, *, starts=None,
     keys turned to pos [T] (int64; default: their place in the sequence) where
     inv_freq is given.  starts int32 [B + 1] says which rows are which
     sequence's (default: one row a sequence), lens int32 [B] how many keys each
-    holds already.  q [T, Hq, D] is turned in the same launch.  Returns
+    holds already.  q [T, Hq, D] is turned in the same launch.  No gradient: a
+    tensor that requires one is refused while autograd records.  Returns
     {"lens": int32 [B] after the call, "q": the turned queries or None}."""
     r = (_T or _torch_lib()).cache_append(k, v, k_cache, v_cache, table, lens, starts, pos,
                                           inv_freq, _layout(layout), scale, q, k_scale, v_scale,
@@ -516,7 +545,7 @@ def coverprune_decode_attention(q, k_cache, v_cache, table, lens, *, scale=None,
     """Attention of one query a sequence, q [B, Hq, D], over a paged cache of
     which sequence b holds lens[b] keys.  window > 0: the last ``window`` keys
     only; keep bool [B, >= keys]: the keys marked only.  scale defaults to
-    1 / sqrt(D).  Returns {"out": [B, Hq, D], "lse": float32 [B, Hq] or None,
+    1 / sqrt(D).  No gradient, as coverprune_cache_append.  Returns {"out": [B, Hq, D], "lse": float32 [B, Hq] or None,
     "ws": the workspace, to pass to the next call}."""
     r = (_T or _torch_lib()).decode_attention(q, k_cache, v_cache, table, lens, scale, window,
                                               keep, k_scale, v_scale, lse, out, ws, status)

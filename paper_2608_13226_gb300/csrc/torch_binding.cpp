@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -36,9 +37,12 @@ std::string text(at::IntArrayRef s) {
   return x + (s.size() == 1 ? ",)" : ")");
 }
 
-// Every tensor of a call is on one device: the first one's.
+// Every tensor of a call is on one device: the first one's.  None may require a gradient
+// where autograd records, as the results carry no history, but those read while
+// `differentiable` is set: `history` tells whether one did.
 struct Call {
   int device = -1;
+  bool differentiable = false, history = false;
 
   const Tensor& tensor(const char* name, PyObject* o) {
     if (!THPVariable_Check(o)) bad_type(std::string(name) + " must be a tensor");
@@ -47,6 +51,11 @@ struct Call {
     const int at = (int)t.get_device();
     if (device < 0) device = at;
     if (at != device) bad_value(std::string(name) + " is on another device than the tensors before it");
+    if (t.requires_grad() && at::GradMode::is_enabled()) {
+      if (!differentiable)
+        bad_value(std::string(name) + " requires a gradient, which this call does not give: detach it or call under torch.no_grad()");
+      history = true;
+    }
     return t;
   }
   // A dense tensor of a type (and, where it is given, a shape).
@@ -212,7 +221,8 @@ bool counted(Py_ssize_t n, Py_ssize_t want) {
   return false;
 }
 
-// (x or a sequence of them, pos, inv_freq, layout, scale, inverse, out or None)
+// (x or a sequence of them, pos, inv_freq, layout, scale, inverse, out or None); None comes
+// back, and nothing is done, where an x requires a gradient
 PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   if (!counted(n_args, 7)) return nullptr;
   return entry([&]() -> PyObject* {
@@ -223,6 +233,7 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     if (n < 1 || n > 4) bad_value("x must be a tensor or a list of one to four");
     PyObject* const* xs = many ? PySequence_Fast_ITEMS(x_list.get()) : a;
     Call c;
+    c.differentiable = true;
     if (!THPVariable_Check(xs[0])) bad_type("x must be a tensor");
     const int dims = (int)THPVariable_Unpack(xs[0]).dim();
     if (dims != 3 && dims != 4) bad_value("x must be [T, heads, D] or [B, T, heads, D]");
@@ -235,6 +246,7 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
           x.scalar_type() != first.scalar_type())
         bad_value("tensors turned together must share tokens, width and dtype");
     }
+    c.differentiable = false;
     const Tensor& pos = c.dense("pos", a[1], at::kLong);
     int64_t pos_stride = 0;
     if (dims == 4 && pos.dim() == 2 && pos.size(0) == B && pos.size(1) == T)
@@ -248,6 +260,10 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     const THPObjectPtr out_list(given_many ? PySequence_Tuple(a[6]) : nullptr);
     if (given && (given_many != many || (many && PyTuple_GET_SIZE(out_list.get()) != n))) bad_value("out must match x");
     PyObject* const* outs = given_many ? PySequence_Fast_ITEMS(out_list.get()) : a + 6;
+    if (c.history) {
+      if (given) bad_value("out cannot be given where x requires a gradient");
+      return own(Py_None);
+    }
 
     c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.device);
     cp_rows rows[4];

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2608_13226_gb300 as cp
-from test_gpu_serve import ULP, attention, gen, pool, randn
+from test_gpu_serve import ULP, assert_stored, attention, freq, gen, pool, randn, turned
 
 pytestmark = pytest.mark.gpu
 E4M3 = torch.float8_e4m3fn
@@ -233,3 +233,74 @@ def test_status_without_an_element_is_refused():
         cp.coverprune_decode_attention(q, kc, vc, table, lens, status=none)
     with pytest.raises(ValueError):
         cp.coverprune_cache_append(q, q, kc, vc, table, lens, status=none)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_rotary_is_part_of_autograd(dtype, layout, inverse):
+    """The gradient through a call against autograd of the formula in 64 bits; of two tensors
+    of which one wants it; of an expanded gradient; and the gradient's own."""
+    g, f = gen(8), freq(24)
+    x, other = randn(g, 2, 33, 5, 64, dtype=dtype).requires_grad_(), randn(g, 2, 33, 2, 64, dtype=dtype)
+    pos = torch.randint(0, 1 << 20, (2, 33), generator=g, device="cuda")
+    up = randn(g, 2, 33, 5, 64, dtype=dtype).requires_grad_()
+    kw = dict(layout=layout, scale=1.25, inverse=inverse)
+    y, z = cp.coverprune_rotary([x, other], pos, f, **kw)
+    assert y.requires_grad and not z.requires_grad
+    with torch.no_grad():
+        assert torch.equal(y, cp.coverprune_rotary(x, pos, f, **kw)) and torch.equal(z, cp.coverprune_rotary(other, pos, f, **kw))
+    got, = torch.autograd.grad(y, x, up, create_graph=True)
+    wide = x.detach().double().requires_grad_()
+    want, = torch.autograd.grad(turned(wide, pos, f, layout, 1.25, inverse)[0], wide, up.detach().double())
+    mag = turned(up.detach(), pos, f, layout, 1.25)[1]
+    assert got.dtype == dtype
+    assert_stored(got.detach(), want, 5e-7 * mag, "gradient")
+    # the gradient is linear in `up`, by the turn that the call itself makes
+    w = randn(g, 2, 33, 5, 64, dtype=dtype)
+    assert torch.equal(torch.autograd.grad(got, up, w)[0], cp.coverprune_rotary(w, pos, f, **kw))
+    cp.coverprune_rotary(x, pos, f, **kw).sum().backward()
+    assert torch.equal(x.grad, cp.coverprune_rotary(torch.ones_like(w), pos, f, layout=layout, scale=1.25, inverse=not inverse))
+    with torch.no_grad():
+        assert not cp.coverprune_rotary(x, pos, f, **kw).requires_grad
+
+
+def test_rotary_gradient_by_differences():
+    """Through autograd, of a function that is not linear: (R x)^2 / 2 summed with weights."""
+    g, f, pos = gen(9), freq(32), torch.arange(40, device="cuda") * 5
+    x, d, w = (randn(g, 40, 3, 64) for _ in range(3))
+    value = lambda t: (w.double() * cp.coverprune_rotary(t, pos, f, scale=0.75).double() ** 2).sum() / 2
+    x.requires_grad_()
+    grad, = torch.autograd.grad(value(x), x)
+    h = 2.0 ** -6
+    with torch.no_grad():
+        num = (value(x + h * d) - value(x - h * d)) / (2 * h)
+        got = (grad.double() * d.double()).sum()
+    # the function is quadratic: only roundings differ, 2^-22 of each of n terms of up to 5^3, signs as they fall, over h
+    assert abs(num - got) <= 5 * math.sqrt(x.numel()) * 125 * 2.0 ** -22 / h
+
+
+def test_what_gives_no_gradient_refuses_to_drop_one():
+    g, D, H = gen(10), 64, 2
+    kc, vc = pool(g, 4, 16, H, D, F32), pool(g, 4, 16, H, D, F32)
+    table, lens = torch.arange(4, device="cuda").int().view(2, 2), torch.tensor([3, 5], dtype=torch.int32, device="cuda")
+    k, q, f, pos = randn(g, 2, H, D), randn(g, 2, 4, D), freq(32), torch.tensor([3, 5], device="cuda")
+    append = dict(k=k, v=k, k_cache=kc, v_cache=vc, table=table, lens=lens, inv_freq=f, q=q)
+    attend = dict(q=q, k_cache=kc, v_cache=vc, table=table, lens=lens)
+    keep = kc.clone()
+    for call, args, names in ((cp.coverprune_cache_append, append, ("k", "v", "q", "k_cache", "inv_freq")),
+                              (cp.coverprune_decode_attention, attend, ("q", "k_cache", "v_cache"))):
+        for name in names:
+            bad = {**args, name: args[name].detach().requires_grad_()}
+            with pytest.raises(ValueError, match="gradient"):
+                call(**bad)
+            if name != "k_cache":
+                with torch.no_grad():
+                    call(**bad)
+                    kc.copy_(keep)
+    wanting = q.detach().clone().requires_grad_()
+    for kw in (dict(x=wanting, out=torch.empty_like(q)), dict(x=q, out=wanting), dict(x=wanting, out=wanting)):
+        with pytest.raises(ValueError, match="gradient"):
+            cp.coverprune_rotary(kw.pop("x"), pos, f, **kw)
+    with pytest.raises(ValueError, match="gradient"):
+        cp.coverprune_rotary(q, pos, f.clone().requires_grad_())
