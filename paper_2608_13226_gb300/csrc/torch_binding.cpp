@@ -187,6 +187,14 @@ cp_cache cache_of(Call& c, PyObject* k_cache, PyObject* v_cache, PyObject* table
   return x;
 }
 
+// Autograd learns that a tensor of the caller's was written, and so notices where it had
+// saved it.
+void changed(PyObject* o) {
+  if (o == Py_None) return;
+  const Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // The call itself, with other threads let run: a full queue makes it wait.
 template <typename F>
 int launch(F f) {
@@ -279,6 +287,7 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                                c.stream());
     });
     if (st != CP_OK) return PyLong_FromLong(st);
+    for (Py_ssize_t i = 0; given && i < n; ++i) changed(outs[i]);
     if (!many) return given ? own(a[6]) : THPVariable_Wrap(made[0]);
     PyObject* list = PyList_New(n);
     for (Py_ssize_t i = 0; list && i < n; ++i) PyList_SET_ITEM(list, i, given ? own(outs[i]) : THPVariable_Wrap(made[i]));
@@ -333,6 +342,8 @@ PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                                      c.stream());
     });
     if (st != CP_OK) return PyLong_FromLong(st);
+    for (const int i : {2, 3, 14, 16}) changed(a[i]);  // the caches, new_lens, status
+    if (queries) changed(a[15]);
     PyObject* first = given_lens ? own(a[14]) : THPVariable_Wrap(lens_out);
     PyObject* second = !queries || a[15] != Py_None ? own(a[15]) : THPVariable_Wrap(q_out);
     PyObject* both = first && second ? PyTuple_Pack(2, first, second) : nullptr;
@@ -390,6 +401,7 @@ PyObject* decode_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                                          (size_t)work.numel() * work.element_size(), status, c.stream());
     });
     if (st != CP_OK) return PyLong_FromLong(st);
+    for (const int i : {11, 12, 13}) changed(a[i]);  // out, ws, status
     PyObject* x = a[11] == Py_None ? THPVariable_Wrap(out) : own(a[11]);
     PyObject* y = with_lse ? THPVariable_Wrap(lse) : own(Py_None);
     PyObject* z = a[12] == Py_None ? THPVariable_Wrap(ws) : own(a[12]);

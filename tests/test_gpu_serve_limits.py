@@ -304,3 +304,32 @@ def test_what_gives_no_gradient_refuses_to_drop_one():
             cp.coverprune_rotary(kw.pop("x"), pos, f, **kw)
     with pytest.raises(ValueError, match="gradient"):
         cp.coverprune_rotary(q, pos, f.clone().requires_grad_())
+
+
+def test_autograd_notices_what_is_written():
+    """A tensor that autograd saved and a call then overwrote must not enter a gradient."""
+    g, D, H = gen(11), 64, 2
+    kc, vc = pool(g, 4, 16, H, D, F32), pool(g, 4, 16, H, D, F32)
+    table, lens = torch.arange(4, device="cuda").int().view(2, 2), torch.tensor([3, 5], dtype=torch.int32, device="cuda")
+    k, q, f, pos = randn(g, 2, H, D), randn(g, 2, 4, D), freq(32), torch.tensor([3, 5], device="cuda")
+    q_out, out = torch.zeros_like(q), torch.zeros_like(q)
+    new_lens, status = torch.zeros_like(lens), torch.zeros(1, dtype=torch.int32, device="cuda")
+    one = torch.ones((), device="cuda", requires_grad=True)
+    append = lambda: cp.coverprune_cache_append(k, k, kc, vc, table, lens, inv_freq=f, q=q, q_out=q_out, new_lens=new_lens, status=status)
+    attend = lambda: cp.coverprune_decode_attention(q, kc, vc, table, lens, out=out, status=status)
+    turn = lambda: cp.coverprune_rotary(q, pos, f, out=q)
+    turns = lambda: cp.coverprune_rotary([q, k], pos, f, out=[q, k])
+    for call, written, read in ((append, (kc, vc, q_out, new_lens, status), (k, q, lens, table)), (attend, (out, status), (q, kc, vc)),
+                                (turn, (q,), (k,)), (turns, (q, k), (out,))):
+        before = {id(t): t._version for t in (*written, *read)}
+        call()
+        assert all(t._version > before[id(t)] for t in written) and all(t._version == before[id(t)] for t in read)
+        for t in (t for t in written if t.is_floating_point()):
+            product = (one * t).sum()
+            call()
+            with pytest.raises(RuntimeError, match="inplace"):
+                product.backward()
+    with torch.inference_mode():
+        kc, vc, out = kc.clone(), vc.clone(), out.clone()
+        append(), attend()
+    append(), attend()  # tensors made in inference mode have no versions
