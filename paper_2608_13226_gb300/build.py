@@ -16,6 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(BUILD, "libcoverprune.so")
 TORCH_LIB = os.path.join(BUILD, "coverprune_torch.so")
+TORCH_MARK = os.path.join(BUILD, "coverprune_torch.txt")  # what TORCH_LIB was compiled against
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
@@ -43,7 +44,21 @@ def up_to_date() -> bool:
     if not os.path.exists(LIB) or not os.path.exists(TORCH_LIB):
         return False
     t = min(os.path.getmtime(LIB), os.path.getmtime(TORCH_LIB))
-    return all(os.path.getmtime(p) <= t for p in _deps())
+    return all(os.path.getmtime(p) <= t for p in _deps()) and _compiled_against() == _torch_id()
+
+
+def _torch_id() -> str:
+    """The interpreter and torch whose headers and layout a module depends on."""
+    import torch
+    return f"{torch.__version__} {os.path.dirname(torch.__file__)} {sys.implementation.cache_tag}"
+
+
+def _compiled_against():
+    try:
+        with open(TORCH_MARK) as f:
+            return f.read()
+    except OSError:
+        return None
 
 
 def _torch_flags():
@@ -101,6 +116,8 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
         if r.returncode != 0:
             raise RuntimeError(f"link failed:\n{r.stdout}")
         os.replace(tmp, out)
+    with open(TORCH_MARK, "w") as f:
+        f.write(_torch_id())
     return LIB
 
 
