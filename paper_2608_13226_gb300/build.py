@@ -1,7 +1,8 @@
 """Build of libcoverprune.so: every CUDA source compiled for sm_103a (in
 parallel, one nvcc per translation unit) and linked in-tree into
 paper_2608_13226_gb300/_build/, with coverprune_torch beside it, the module that
-takes tensors to the decoding model's calls.  No CMake, no setuptools."""
+takes tensors to the decoding model's calls.  No CMake, no setuptools.  Run as a
+file with --library it builds the library alone, without Python's or torch's headers."""
 from __future__ import annotations
 
 import glob
@@ -35,16 +36,22 @@ def _sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.cu")))
 
 
-def _deps():
-    return _sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + \
-        glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cpp")) + glob.glob(os.path.join(INCLUDE, "*.h")) + [__file__]
+def _newer(out, deps) -> bool:
+    return os.path.exists(out) and all(os.path.getmtime(p) <= os.path.getmtime(out) for p in deps)
+
+
+def library_up_to_date() -> bool:
+    heads = [glob.glob(os.path.join(d, e)) for d, e in ((CSRC, "*.cuh"), (CSRC, "*.h"), (INCLUDE, "*.h"))]
+    return _newer(LIB, _sources() + sum(heads, []) + [__file__])
+
+
+def module_up_to_date() -> bool:
+    deps = glob.glob(os.path.join(CSRC, "*.cpp")) + glob.glob(os.path.join(INCLUDE, "*.h")) + [__file__]
+    return _newer(TORCH_LIB, deps) and _compiled_against() == _torch_id()
 
 
 def up_to_date() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(TORCH_LIB):
-        return False
-    t = min(os.path.getmtime(LIB), os.path.getmtime(TORCH_LIB))
-    return all(os.path.getmtime(p) <= t for p in _deps()) and _compiled_against() == _torch_id()
+    return library_up_to_date() and module_up_to_date()
 
 
 def _torch_id() -> str:
@@ -77,29 +84,13 @@ def _torch_flags():
     return comp, link
 
 
-def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
-    """Compile and link; returns the library path."""
-    if not force and up_to_date():
-        return LIB
-    os.makedirs(BUILD, exist_ok=True)
-    cc = nvcc()
-    procs = []
-    objs = []
-    for src in _sources():
-        obj = os.path.join(BUILD, os.path.basename(src)[:-3] + ".o")
-        objs.append(obj)
-        cmd = [cc, *ARCH, *NVCC_FLAGS, *extra_flags, "-c", src, "-o", obj]
-        procs.append((src, cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE,
-                                                 stderr=subprocess.STDOUT, text=True)))
-    comp, torch_link = _torch_flags()
-    cxx = shutil.which("g++") or "c++"
-    src = os.path.join(CSRC, "torch_binding.cpp")
-    torch_obj = os.path.join(BUILD, "torch_binding.o")
-    cmd = [cxx, *comp, "-c", src, "-o", torch_obj]
-    procs.append((src, cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT,
-                                             text=True)))
+def _start(cmd):
+    return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
+
+def _finish(procs, verbose):
     failed = []
-    for src, cmd, p in procs:
+    for src, p in procs:
         out, _ = p.communicate()
         if verbose and out:
             sys.stdout.write(out)
@@ -108,14 +99,52 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
     if failed:
         msg = "\n".join(f"--- {s}\n{o}" for s, o in failed)
         raise RuntimeError(f"compilation failed:\n{msg}")
-    for out, link in ((LIB, [cc, *ARCH, "-shared", "-o", None, *objs]),
-                      (TORCH_LIB, [cxx, "-shared", "-o", None, torch_obj, *torch_link])):
-        tmp = out + f".tmp{os.getpid()}"
-        link[link.index(None)] = tmp
-        r = subprocess.run(link, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-        if r.returncode != 0:
-            raise RuntimeError(f"link failed:\n{r.stdout}")
-        os.replace(tmp, out)
+
+
+def _link(out, cmd):
+    """Links to a file of this process's own and moves it to its place."""
+    tmp = out + f".tmp{os.getpid()}"
+    r = subprocess.run([*cmd, "-o", tmp], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"link failed:\n{r.stdout}")
+    os.replace(tmp, out)
+
+
+def _build_library(verbose, extra_flags):
+    cc = nvcc()
+    objs, procs = [], []
+    for src in _sources():
+        objs.append(os.path.join(BUILD, os.path.basename(src)[:-3] + ".o"))
+        procs.append((src, _start([cc, *ARCH, *NVCC_FLAGS, *extra_flags, "-c", src, "-o", objs[-1]])))
+    _finish(procs, verbose)
+    _link(LIB, [cc, *ARCH, "-shared", *objs])
+
+
+def build(force: bool = False, verbose: bool = False, extra_flags=(), module: bool = True) -> str:
+    """Compile and link; returns the library path.  The library needs nvcc alone; module=False
+    leaves out the module for PyTorch, which needs Python's and torch's headers."""
+    os.makedirs(BUILD, exist_ok=True)
+    library = force or not library_up_to_date()
+    if not module:
+        if library:
+            _build_library(verbose, extra_flags)
+        return LIB
+    if not library and not force and module_up_to_date():
+        return LIB
+    # the module compiles beside the library; whatever fails of it, the library is there
+    src, obj, failed = os.path.join(CSRC, "torch_binding.cpp"), os.path.join(BUILD, "torch_binding.o"), None
+    cxx = shutil.which("g++") or "c++"
+    try:
+        comp, link = _torch_flags()
+        proc = (src, _start([cxx, *comp, "-c", src, "-o", obj]))
+    except Exception as e:
+        failed = e
+    if library:
+        _build_library(verbose, extra_flags)
+    if failed:
+        raise RuntimeError(f"the module for PyTorch cannot be compiled: {failed}") from failed
+    _finish([proc], verbose)
+    _link(TORCH_LIB, [cxx, "-shared", obj, *link])
     with open(TORCH_MARK, "w") as f:
         f.write(_torch_id())
     return LIB
@@ -123,4 +152,4 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
 
 if __name__ == "__main__":
     print(build(force="--force" in sys.argv, verbose="-v" in sys.argv,
-                extra_flags=["-Xptxas", "-v"] if "--ptxas" in sys.argv else []))
+                extra_flags=["-Xptxas", "-v"] if "--ptxas" in sys.argv else [], module="--library" not in sys.argv))
