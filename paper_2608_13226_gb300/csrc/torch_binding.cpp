@@ -378,7 +378,8 @@ PyObject* decode_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     const float scale = a[5] == Py_None ? (float)(1.0 / std::sqrt((double)(cache.D > 0 ? cache.D : 1))) : (float)real(a[5]);
     const int64_t window = integer(a[6]);
     int32_t* status = c.word("status", a[13]);
-    const bool with_lse = PyObject_IsTrue(a[10]) == 1;
+    const int with_lse = PyObject_IsTrue(a[10]);
+    if (with_lse < 0) throw python_error();
 
     c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.device);
     Tensor out, lse, ws;

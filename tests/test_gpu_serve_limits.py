@@ -333,3 +333,15 @@ def test_autograd_notices_what_is_written():
         kc, vc, out = kc.clone(), vc.clone(), out.clone()
         append(), attend()
     append(), attend()  # tensors made in inference mode have no versions
+
+
+def test_lse_that_is_neither_true_nor_false():
+    """What its truth raises comes through."""
+    class Unclear:
+        def __bool__(self):
+            raise KeyError("unclear")
+
+    kc, vc = torch.zeros(2, 4, 16, 2, 64, dtype=BF16, device="cuda")
+    table, lens = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    with pytest.raises(KeyError):
+        cp.coverprune_decode_attention(torch.zeros(1, 2, 64, dtype=BF16, device="cuda"), kc, vc, table, lens, lse=Unclear())
