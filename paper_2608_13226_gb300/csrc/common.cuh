@@ -12,8 +12,6 @@ namespace cp {
 // ---------------------------------------------------------------------------
 // Element loads: features are bf16 or fp32; every product and sum is fp32.
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ float to_f32(float x) { return x; }
-__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 
 // 16 bytes of features as fp32 values: 4 for fp32, 8 for bf16.
 template <typename T> struct Vec16;

@@ -70,6 +70,5 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(flo
 template <> __device__ __forceinline__ __nv_fp8_e4m3 from_f32<__nv_fp8_e4m3>(float x) {
   return __nv_fp8_e4m3(x);  // to nearest even, saturating
 }
-__device__ __forceinline__ float to_f32(__nv_fp8_e4m3 x) { return (float)x; }
 
 }  // namespace cp
