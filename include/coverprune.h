@@ -443,7 +443,8 @@ int coverprune_rotary(const cp_rows* rows, int n, int dtype, int64_t B, int64_t 
  *   k_scale, v_scale  device float32 [heads] or NULL (1): the value of a
  *               stored element is scale * element (any dtype)
  *   table       device int32 [B, table_width], rows table_stride apart; entries
- *               beyond a sequence's length are not read
+ *               beyond a sequence's length are not read.  Attention is planned by
+ *               what a row holds: one far wider than the sequences costs some us
  */
 typedef struct {
   uint32_t struct_size; /* = sizeof(cp_cache) */

@@ -64,6 +64,8 @@ class _CallStats(C.Structure):
                 ("cost_bytes_read", C.c_uint64)]
 
 
+# The decoding calls' structs, for callers through ctypes; the module of C++ that the
+# functions below go through makes its own.
 class _Rope(C.Structure):
     _fields_ = [("inv_freq", C.c_void_p), ("rot", C.c_int32), ("layout", C.c_int32),
                 ("scale", C.c_float)]

@@ -2,8 +2,8 @@
 // for every query head, where a group of query heads shares a kv head's keys
 // and values.
 //
-// Each visible key and value row is read once for up to 16 query heads, and a
-// bf16 cache gives 1 flop a byte and query head: the kernel is bound by HBM as
+// Each visible key and value row is read once for up to 16 query heads (of a float32
+// cache 8), and a bf16 cache gives 1 flop a byte and query head: the kernel is bound by HBM as
 // long as enough bytes are in flight (about 1 us of it, 45 KB an SM) whatever
 // the lengths.  In a block every warp runs on its own: it copies tiles of 16 keys
 // (16 rows of K and of V, wherever their pages are; 8 of float32) into a ring in
@@ -20,8 +20,8 @@
 //    keys and 4 kv heads of 128 90 us (0.91 of the HBM's rate), one of 200,001 and 8
 //    heads 129 us (0.94).
 //  - k_decode_cluster: few sequences have a cluster of blocks each, whose parts
-//    meet in shared memory: no second launch.  One sequence of 1500 keys 6.5 us,
-//    with parts through the workspace 8.2.
+//    meet in shared memory: no second launch.  One sequence of 1500 keys 6.7 us,
+//    with parts through the workspace 7.7.
 //  - k_decode, uncut: sequences of at most 256 keys, a block each.
 //  - k_decode_short: many short ones, or hardly any keys, a warp each; nothing is
 //    to be merged.
@@ -91,6 +91,9 @@ struct Shape {
   static constexpr int queries = SHORT ? kWarps : 1;
   static constexpr int extra = CT == CP_F32 ? (queries * QT * DP + kWarps * tk * QT) * 4 : 0;
   static constexpr int smem = ring + extra;
+  // (Registers allow them but for some spills, 4 to 84 bytes a thread: 16 queries and heads of
+  // 256 (255 registers), an 8-bit cache's 8 queries and heads of 64, float32's of 4 queries and
+  // heads of 128 and 256 and, for short sequences, of 8 and 128.)
   static constexpr int per_sm = SHORT && smem <= 70 * 1024 ? 3 : smem <= 110 * 1024 ? 2 : 1;
   static constexpr int part = QT * (DP + 2);  // floats of a partial result
   // What beginning and merging a segment costs, in units of 64 keys: about 3 us, in
@@ -1204,6 +1207,10 @@ template <int CT, int DP, int QT>
 static int launch(const DecodeArgs& a, cudaStream_t s) {
   using S = Shape<CT, DP, QT>;
   const int G = a.Hq / a.cache.heads, tiles = (G + QT - 1) / QT;
+  // What a table's row or the window holds stands for the longest sequence, which only the
+  // device knows: a row far wider than that goes as one line.  Exact rows / rows of 32,768
+  // keys, us: one sequence of 1500 keys 6.7 / 8.2, 32 of 1229 to 1741 22.9 / 23.7, 160 of
+  // 100 to 300 23.4 / 25.6, 16 of 8192 to 8704 with 15% marked 16.3 / 19.4.
   // Sequences of at most 4 units are not cut: the join would cost more.
   const int64_t most = a.window > 0 && a.window < a.cache.capacity ? a.window : a.cache.capacity;  // keys of one
   const bool cut = most > 4 * kUnit;
@@ -1269,7 +1276,7 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   // a block) and, where sequences differ in length more than the table's width
   // tells, the longest one's time: at most 16 units a block, of marked keys thrice
   // that.  us as one line / with clusters, 7 queries a head of 128: 4 tiles of 500 keys
-  // 8.2 / 6.7, of 1500 8.2 / 7.2, of 8000 16.1 / 11.3, of 16000 16.2 / 17.3; 64 of 1500
+  // 7.5 / 6.0, of 1500 7.7 / 6.7, of 8000 15.2 / 11.1, of 16000 16.2 / 17.3; 64 of 1500
   // 15.4 / 11.3, of 4000 29.9 / 26.2, of 8000 with 15% marked 19.8 / 16.2; 128 of 1229
   // to 1741 24.1 / 22.8.
   // float32 computes longer on a unit: half of the longest one's time and a quarter of

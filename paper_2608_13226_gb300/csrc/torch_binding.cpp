@@ -1,6 +1,6 @@
 // The decoding model's calls for PyTorch: tensors in, tensors out.  These come
 // once a layer and token, so their host time counts; marshalling them from
-// Python through ctypes took 10 to 20 us a call, this takes 5.  Checks of
+// Python through ctypes took 18 to 28 us a call, this takes 5 to 7.  Checks of
 // arguments and allocation of results only: the work is behind the C ABI
 // (include/coverprune.h), whose entry points are called here.
 #define PY_SSIZE_T_CLEAN
