@@ -74,9 +74,9 @@ typedef enum {
   CP_EDEVICE = 6       /* a device-side consistency check failed (see coverprune_check) */
 } cp_status;
 
-/* CP_E4M3 (8 bits: 4 of exponent, 3 of fraction, largest value 448) is a type
- * of caches only. */
-typedef enum { CP_F32 = 0, CP_BF16 = 1, CP_E4M3 = 2 } cp_dtype;
+/* CP_E4M3 (8 bits: 4 of exponent, 3 of fraction, largest value 448) and CP_I4
+ * (4 bits: see cp_cache) are types of caches only. */
+typedef enum { CP_F32 = 0, CP_BF16 = 1, CP_E4M3 = 2, CP_I4 = 4 } cp_dtype;
 
 /* Which entry point a workspace is sized for. */
 typedef enum {
@@ -432,9 +432,10 @@ int coverprune_rotary(const cp_rows* rows, int n, int dtype, int64_t B, int64_t 
  * of page table[b * table_stride + j / page_size], at
  *   page * page_stride + row * slot_stride + head * head_stride
  * elements from k (and its value equally from v); D contiguous elements.
- *   dtype       CP_BF16, CP_F32 or CP_E4M3
+ *   dtype       CP_BF16, CP_F32, CP_E4M3 or CP_I4
  *   k, v        device, 16-byte aligned; the strides and D are multiples of 16
  *               bytes, D <= 256; strides of both are the same and not negative.
+ *               An element of CP_I4 is half a byte (so 16 bytes are 32 of them).
  *               Attention needs the pages to span at most 2^32 times the largest
  *               power of two that divides the page and slot strides (64 GB at
  *               least).
@@ -445,9 +446,19 @@ int coverprune_rotary(const cp_rows* rows, int n, int dtype, int64_t B, int64_t 
  *   table       device int32 [B, table_width], rows table_stride apart; entries
  *               beyond a sequence's length are not read.  Attention is planned by
  *               what a row holds: one far wider than the sequences costs some us
+ * CP_I4: component d of a row is n * s, n a whole number from -7 to 7 held as n + 8
+ * in half d % 2 (0: the low one) of byte d / 2, and s the e4m3 value of byte d / 16
+ * of the row's scales, D / 16 bytes rounded up to a multiple of 4 (the last ones are
+ * written as 0 and not used).  The scales of row r of page p and head h are at
+ *   p * block_page_stride + r * block_slot_stride + h * block_head_stride
+ * bytes from k_block (and v's equally from v_block).
+ *   k_block, v_block  device, 4-byte aligned; the strides are multiples of 4 (8 or
+ *               16, with such an alignment, are faster for heads above 64 or 128
+ *               components) and not negative; pages span at most 2^32 times 4 bytes.
+ *               Not read for other types.
  */
 typedef struct {
-  uint32_t struct_size; /* = sizeof(cp_cache) */
+  uint32_t struct_size; /* = sizeof(cp_cache), or without k_block and what follows it where dtype is not CP_I4 */
   int32_t dtype;
   void* k;
   void* v;
@@ -457,6 +468,9 @@ typedef struct {
   const float* v_scale;
   const int32_t* table;
   int64_t table_width, table_stride;
+  void* k_block;
+  void* v_block;
+  int64_t block_page_stride, block_slot_stride, block_head_stride; /* bytes */
 } cp_cache;
 
 /*
@@ -464,7 +478,7 @@ typedef struct {
  * rotated on the way, and optionally the queries of the same tokens rotated.
  *   k, v      [T, heads, D] of `dtype` (CP_F32 or CP_BF16); k_stride, v_stride
  *             HOST arrays {token, head} in elements.  A float32 cache takes
- *             float32 rows, a bfloat16 one bfloat16 rows, an 8-bit one either.
+ *             float32 rows, a bfloat16 one bfloat16 rows, an 8- or 4-bit one either.
  *   starts    device int32 [B + 1]: sequence b's new tokens are rows
  *             starts[b]..starts[b + 1] - 1, ascending; rows before starts[0] and from
  *             starts[B] on are padding and left alone.  NULL: T == B, one token a sequence.
@@ -484,13 +498,65 @@ typedef struct {
  *             skipped.
  * Rotation in float32, one rounding; an 8-bit cache holds
  * round(x / scale) to nearest even, saturated at +-448 (infinities too; NaN
- * stays NaN).  Two tokens on one row of the cache are the caller's mistake.
+ * stays NaN).  A 4-bit one takes for 16 components the scale
+ *   s = round(min(max |x| / (7 scale), 448)) to e4m3, to nearest even,
+ * and for each n = round(x / (s scale)) to nearest even, at most 7 either way, in
+ * float32 (s = 0: 0; an infinity is 7; a NaN makes s and so its 16 components NaN).
+ * Two tokens on one row of the cache are the caller's mistake.
  */
 int coverprune_cache_append(const cp_cache* cache, const void* k, const int64_t* k_stride,
                             const void* v, const int64_t* v_stride, int dtype, int64_t T,
                             const int32_t* starts, const int32_t* lens, int64_t B,
                             const int64_t* pos, const cp_rope* rope, const cp_rows* q,
                             int32_t* new_lens, int32_t* status, cp_stream_t stream);
+
+/*
+ * coverprune_cache_read -- rows of the cache as its readers see them: the mirror of
+ * coverprune_cache_append, for what takes keys and values as dense tensors (a
+ * prompt's own attention on what the cache holds; a cache of another type).
+ *   T, starts, lens, B, status  as there: row t of sequence b's rows is key
+ *             lens[b] + (t - starts[b])
+ *   k, v      [T, heads, D] of `dtype`, written; strides HOST {token, head} in elements,
+ *             pointers aligned to an element.  A float32 cache gives CP_F32, a bfloat16
+ *             one CP_BF16, an 8- or 4-bit one either.
+ * An element times its scales in float32 (a 4-bit one n * s, which is exact, times the
+ * head's), rounded once.  A row whose key lies beyond the table's row or on a bad page
+ * becomes 0 and sets the status; padding rows are left as they are.  k and v must not
+ * overlap each other or the cache.
+ */
+int coverprune_cache_read(const cp_cache* cache, int64_t T, const int32_t* starts,
+                          const int32_t* lens, int64_t B, void* k, const int64_t* k_stride,
+                          void* v, const int64_t* v_stride, int dtype, int32_t* status,
+                          cp_stream_t stream);
+
+/*
+ * coverprune_cache_evict -- cuts every sequence to at most `left` keys: its first
+ * `first` ones, its last `recent` ones and the heaviest of those between, the earlier of
+ * equal ones.  Their rows move up, in their order, to keys 0..; the cache is changed in
+ * place, every other row stays as it is.
+ *   lens      device int32 [B]; negative is 0, more than the table's row holds is
+ *             what it holds.  A sequence of at most `left` keys keeps them all.
+ *   weight    device float32, weight[b * weight_stride + j] of key j (of
+ *             coverprune_decode_attention_weigh, say); read for the keys between
+ *             only.  A NaN counts as less than any number, -0 as 0.
+ *   left      >= 0;  first, recent >= 0 with first + recent <= left
+ *   new_lens  device int32 [B] or NULL: the keys left; a negative lens[b] stays
+ *   new_weight  device float32 or NULL, row b at b * new_weight_stride: the weights of the keys
+ *             left, then 0 up to new_weight_width entries
+ *   kept      device int32 [B, left]: the index that each key left had, -1 after the
+ *             last
+ *   status    device int32 or NULL; set to CP_EINVAL (and otherwise not written)
+ *             if a key that is left lies, or would come to lie, on a bad page: it is not
+ *             moved (its new place keeps what it held).
+ * new_lens, new_weight and kept must not overlap lens, weight or one another.  Sequences
+ * that share pages are the caller's mistake.  weight_stride and new_weight_stride in elements,
+ * not negative.  B <= 2^24, B * left < 2^31 * 16.
+ */
+int coverprune_cache_evict(const cp_cache* cache, const int32_t* lens, int64_t B,
+                           const float* weight, int64_t weight_stride, int64_t left,
+                           int64_t first, int64_t recent, int32_t* new_lens, float* new_weight,
+                           int64_t new_weight_stride, int64_t new_weight_width, int32_t* kept,
+                           int32_t* status, cp_stream_t stream);
 
 /*
  * coverprune_decode_attention -- attention of one query a sequence over the
@@ -503,7 +569,7 @@ int coverprune_cache_append(const cp_cache* cache, const void* k, const int64_t*
  * <q, k_j> and s_j / ln 2 have to stay within float32's range; a key whose score is
  * -infinity weighs nothing.
  *   q       [B, Hq, D] of `dtype`, q_stride HOST {batch, head} in elements.
- *           bfloat16 goes with a bfloat16 or 8-bit cache, float32 with a float32 one.
+ *           bfloat16 goes with a bfloat16, 8- or 4-bit cache, float32 with a float32 one.
  *   lens    device int32 [B]; negative is 0, more than the table's row
  *           holds is what it holds
  *   keep    device uint8 or NULL, a byte a key
@@ -516,7 +582,7 @@ int coverprune_cache_append(const cp_cache* cache, const void* k, const int64_t*
  *           if a visible key lies on a bad page; such keys are left out.
  * Scores, maxima, sums and outputs are float32; the weights exp(s_j - m) enter
  * the second product as two bfloat16 terms with a bfloat16 cache (their sum off
- * by 2^-16 at most), as one float16 with an 8-bit cache (off by 2^-11 of itself
+ * by 2^-16 at most), as one float16 with an 8- or 4-bit cache (off by 2^-11 of itself
  * or 2^-32 of the largest weight).  An infinite visible value
  * makes its component that infinity (both signs or a NaN: NaN), unless its
  * weight is below 2^-100 of the largest: float32's 0 times infinity, NaN, may
@@ -529,6 +595,25 @@ int coverprune_decode_attention(const void* q, const int64_t* q_stride, int dtyp
                                 const uint8_t* keep, int64_t keep_stride, float scale,
                                 int64_t window, void* out, const int64_t* out_stride, float* lse,
                                 void* ws, size_t ws_bytes, int32_t* status, cp_stream_t stream);
+
+/*
+ * coverprune_decode_attention_weigh -- the same, with what weight each key got added up:
+ *   weight[b * weight_stride + j] += sum over the query heads h of exp(s_hj - lse_h)
+ * for every visible key j (in float32, the heads in a fixed order); others are not
+ * touched.  A NaN among a query head's visible scores makes its weights NaN.
+ *   weight    device float32, rows of B sequences weight_stride >= 0 elements apart, which
+ *             must not overlap; each holds the keys that the table's row does
+ *   ws        coverprune_decode_weigh_workspace_size bytes: the attention's, and a float for
+ *             every query head and key that the table's row holds (B * Hq * keys)
+ */
+int coverprune_decode_weigh_workspace_size(int64_t B, int64_t Hq, const cp_cache* cache,
+                                           size_t* bytes);
+int coverprune_decode_attention_weigh(const void* q, const int64_t* q_stride, int dtype, int64_t B,
+                                      int64_t Hq, const cp_cache* cache, const int32_t* lens,
+                                      const uint8_t* keep, int64_t keep_stride, float scale,
+                                      int64_t window, void* out, const int64_t* out_stride,
+                                      float* lse, float* weight, int64_t weight_stride, void* ws,
+                                      size_t ws_bytes, int32_t* status, cp_stream_t stream);
 
 /*
  * coverprune_barrier_selftest -- exercises the device-side wait limit

@@ -18,7 +18,7 @@ import torch
 from . import build as _build
 
 CP_OK, CP_EINVAL, CP_EWORKSPACE, CP_ECUDA, CP_ETIMEOUT, CP_EUNSUPPORTED, CP_EDEVICE = range(7)
-CP_F32, CP_BF16, CP_E4M3 = 0, 1, 2
+CP_F32, CP_BF16, CP_E4M3, CP_I4 = 0, 1, 2, 4
 CP_OP_COST, CP_OP_SELECT, CP_OP_LITE, CP_OP_KNN = 0, 1, 2, 3
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 STRETCHES = {"none": 0, "linear": 1, "base": 2, "turns": 3, "index": 4}
@@ -31,7 +31,9 @@ EXPORTS = ("cp_default_params", "coverprune_budget", "coverprune_workspace_size"
            "coverprune_knn_noalloc",
            "coverprune_gather", "coverprune_rotary_frequencies", "coverprune_rotary",
            "coverprune_cache_append", "coverprune_decode_workspace_size",
-           "coverprune_decode_attention", "coverprune_barrier_selftest", "coverprune_profile_enable",
+           "coverprune_decode_attention", "coverprune_decode_weigh_workspace_size",
+           "coverprune_decode_attention_weigh", "coverprune_cache_read", "coverprune_cache_evict",
+           "coverprune_barrier_selftest", "coverprune_profile_enable",
            "coverprune_profile_read", "coverprune_last_error", "coverprune_call_stats",
            "coverprune_version")
 STAGES = ("prep", "gram", "cost", "capacity", "sgs", "lite_order", "lite_proto", "output",
@@ -82,7 +84,9 @@ class _Cache(C.Structure):
                 ("heads", C.c_int64), ("D", C.c_int64), ("page_stride", C.c_int64),
                 ("slot_stride", C.c_int64), ("head_stride", C.c_int64), ("k_scale", C.c_void_p),
                 ("v_scale", C.c_void_p), ("table", C.c_void_p), ("table_width", C.c_int64),
-                ("table_stride", C.c_int64)]
+                ("table_stride", C.c_int64), ("k_block", C.c_void_p), ("v_block", C.c_void_p),
+                ("block_page_stride", C.c_int64), ("block_slot_stride", C.c_int64),
+                ("block_head_stride", C.c_int64)]
 
 
 @dataclass
@@ -171,6 +175,11 @@ def _lib():
         lib.coverprune_decode_workspace_size.argtypes = [I64, I64, P, C.POINTER(C.c_size_t)]
         lib.coverprune_decode_attention.argtypes = [P, P, I32, I64, I64, P, P, P, I64, C.c_float,
                                                     I64, P, P, P, P, SZ, P, P]
+        lib.coverprune_decode_weigh_workspace_size.argtypes = lib.coverprune_decode_workspace_size.argtypes
+        lib.coverprune_decode_attention_weigh.argtypes = [P, P, I32, I64, I64, P, P, P, I64, C.c_float,
+                                                          I64, P, P, P, P, I64, P, SZ, P, P]
+        lib.coverprune_cache_read.argtypes = [P, I64, P, P, I64, P, P, P, P, I32, P, P]
+        lib.coverprune_cache_evict.argtypes = [P, P, I64, P, I64, I64, I64, I64, P, P, I64, I64, P, P, P]
         lib.coverprune_barrier_selftest.argtypes = [C.c_int32, C.c_int32, C.c_float, P, SZ, P]
         lib.coverprune_call_stats.argtypes = [P, P, C.POINTER(_CallStats)]
         lib.coverprune_last_error.argtypes = []
@@ -525,32 +534,76 @@ def coverprune_rotary(x, pos, inv_freq, *, layout: str = "half", scale: float = 
 def coverprune_cache_append(k, v, k_cache, v_cache, table, lens, *, starts=None, pos=None,
                             inv_freq=None, layout: str = "half", scale: float = 1.0, q=None,
                             k_scale=None, v_scale=None, new_lens=None, q_out=None,
-                            status=None) -> dict:
+                            status=None, k_block=None, v_block=None) -> dict:
     """Appends k, v [T, heads, D] to a paged cache [pages, page_size, heads, D],
     keys turned to pos [T] (int64; default: their place in the sequence) where
     inv_freq is given.  starts int32 [B + 1] says which rows are which
     sequence's (default: one row a sequence), lens int32 [B] how many keys each
-    holds already.  q [T, Hq, D] is turned in the same launch.  No gradient: a
+    holds already.  q [T, Hq, D] is turned in the same launch.  A cache of uint8
+    [pages, page_size, heads, D / 2] holds 4 bits a component, with the scales of
+    16 components each in k_block and v_block, float8_e4m3fn [pages, page_size,
+    heads, D / 16 rounded up to 4] (D a multiple of 32).  No gradient: a
     tensor that requires one is refused while autograd records.  Returns
     {"lens": int32 [B] after the call, "q": the turned queries or None}."""
     r = (_T or _torch_lib()).cache_append(k, v, k_cache, v_cache, table, lens, starts, pos,
                                           inv_freq, _layout(layout), scale, q, k_scale, v_scale,
-                                          new_lens, q_out, status)
+                                          new_lens, q_out, status, k_block, v_block)
     if type(r) is int:
         raise CoverPruneError(r, "coverprune_cache_append")
     return {"lens": r[0], "q": r[1]}
 
 
+def coverprune_cache_read(k_cache, v_cache, table, lens, *, starts=None, tokens=None, k_scale=None,
+                          v_scale=None, k_block=None, v_block=None, dtype=None, k_out=None,
+                          v_out=None, status=None):
+    """(k, v) [tokens, heads, D]: cached rows as attention sees them, the mirror of
+    coverprune_cache_append: row t of sequence b's rows (by starts, default one a
+    sequence) is its key lens[b] + (t - starts[b]).  With starts, tokens says how many rows there are.
+    dtype: bfloat16 or float32 for caches of 8 and 4 bits (default bfloat16), the
+    cache's own otherwise.  Keys that are not there become 0 and set the
+    status; rows outside starts are not written.  No gradient."""
+    if dtype not in (None, torch.bfloat16, torch.float32):
+        raise TypeError(f"dtype must be bfloat16 or float32, got {dtype}")
+    r = (_T or _torch_lib()).cache_read(k_cache, v_cache, table, lens, starts, tokens, k_scale,
+                                        v_scale, k_block, v_block,
+                                        None if dtype is None else dtype == torch.float32, k_out,
+                                        v_out, status)
+    if type(r) is int:
+        raise CoverPruneError(r, "coverprune_cache_read")
+    return r
+
+
+def coverprune_cache_evict(k_cache, v_cache, table, lens, weight, left: int, *, first: int = 0,
+                           recent: int = 0, k_block=None, v_block=None, new_lens=None,
+                           new_weight=None, kept=None, status=None) -> dict:
+    """Cuts each sequence of a paged cache to at most ``left`` keys: its first
+    ``first``, its last ``recent`` and the heaviest between by weight float32 [B, >= keys]
+    (the earlier of equal ones).  Their rows move up in their order, in place.
+    Scores of later tokens are as before, as keys carry their position; append with
+    pos then.  No gradient.  Returns {"lens": int32 [B] keys left, "weight": their weights, 0 behind
+    them, "kept": int32 [B, left] the indices that they had, -1 behind them}."""
+    r = (_T or _torch_lib()).cache_evict(k_cache, v_cache, table, lens, weight, left, first, recent,
+                                         k_block, v_block, new_lens, new_weight, kept, status)
+    if type(r) is int:
+        raise CoverPruneError(r, "coverprune_cache_evict")
+    return {"lens": r[0], "weight": r[1], "kept": r[2]}
+
+
 def coverprune_decode_attention(q, k_cache, v_cache, table, lens, *, scale=None, window: int = 0,
                                 keep=None, k_scale=None, v_scale=None, lse: bool = False,
-                                out=None, ws=None, status=None) -> dict:
+                                out=None, ws=None, status=None, k_block=None, v_block=None,
+                                weight=None) -> dict:
     """Attention of one query a sequence, q [B, Hq, D], over a paged cache of
     which sequence b holds lens[b] keys.  window > 0: the last ``window`` keys
     only; keep bool [B, >= keys]: the keys marked only.  scale defaults to
-    1 / sqrt(D).  No gradient, as coverprune_cache_append.  Returns {"out": [B, Hq, D], "lse": float32 [B, Hq] or None,
+    1 / sqrt(D).  A cache of uint8 holds 4 bits, as coverprune_cache_append writes them.
+    weight float32 [B, >= keys]: what weight each key got from all query heads together is
+    added to it (this takes a larger workspace).  No gradient, as coverprune_cache_append.
+    Returns {"out": [B, Hq, D], "lse": float32 [B, Hq] or None,
     "ws": the workspace, to pass to the next call}."""
     r = (_T or _torch_lib()).decode_attention(q, k_cache, v_cache, table, lens, scale, window,
-                                              keep, k_scale, v_scale, lse, out, ws, status)
+                                              keep, k_scale, v_scale, lse, out, ws, status,
+                                              k_block, v_block, weight)
     if type(r) is int:
         raise CoverPruneError(r, "coverprune_decode_attention")
     return {"out": r[0], "lse": r[1], "ws": r[2]}

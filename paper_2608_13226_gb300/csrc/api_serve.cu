@@ -2,14 +2,15 @@
 // (rotary positions, cache append, attention over the cache): argument
 // validation and launches.
 #include <math.h>
+#include <stddef.h>
 
 #include "serve.h"
 
 using namespace cp;
 
 static bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
-static bool overlap(const int32_t* p, int64_t n, const int32_t* q, int64_t m) {
-  return p && q && (uintptr_t)p < (uintptr_t)(q + m) && (uintptr_t)q < (uintptr_t)(p + n);
+static bool overlap(const void* p, int64_t n, const void* q, int64_t m) {  // of n and m 4-byte words
+  return p && q && (uintptr_t)p < (uintptr_t)q + 4 * (uintptr_t)m && (uintptr_t)q < (uintptr_t)p + 4 * (uintptr_t)n;
 }
 static size_t size_of(int dtype) { return dtype == CP_F32 ? 4 : dtype == CP_BF16 ? 2 : 1; }
 
@@ -42,17 +43,23 @@ static int rows_of(const cp_rows& r, int dtype, bool tokens, RowSet* out) {
 
 // A cache's description; the table is wanted by the calls that go through it.
 static int cache_of(const cp_cache* c, bool with_memory, Cache* out) {
-  if (!c || c->struct_size != sizeof(cp_cache)) return CP_EINVAL;
-  if (c->dtype != CP_F32 && c->dtype != CP_BF16 && c->dtype != CP_E4M3) return CP_EINVAL;
+  // (what was compiled before there were 4-bit caches has no fields for them)
+  if (!c || (c->struct_size != sizeof(cp_cache) &&
+             (c->struct_size != offsetof(cp_cache, k_block) || c->dtype == CP_I4)))
+    return CP_EINVAL;
+  if (c->dtype != CP_F32 && c->dtype != CP_BF16 && c->dtype != CP_E4M3 && c->dtype != CP_I4) return CP_EINVAL;
   if (c->heads < 1 || c->heads > 65536 || c->D < 1 || c->page_size < 1 || c->pages < 0 ||
       c->table_width < 0 || c->page_stride < 0 || c->slot_stride < 0 || c->head_stride < 0)
     return CP_EINVAL;
-  const int64_t e = (int64_t)size_of(c->dtype);
+  const auto unaligned = [&](int64_t n) { return (c->dtype == CP_I4 ? n : n * (int64_t)size_of(c->dtype) * 2) % 32 != 0; };
   if (c->page_size > kMaxSize || c->table_width > kMaxSize || c->pages > kMaxSize)
     return CP_EINVAL;
   if (c->table_width * c->page_size > kMaxKeys) return CP_EUNSUPPORTED;
-  if (c->D > 256 || c->D * e % 16 != 0) return CP_EUNSUPPORTED;
-  if (c->page_stride * e % 16 != 0 || c->slot_stride * e % 16 != 0 || c->head_stride * e % 16 != 0)
+  if (c->D > 256 || unaligned(c->D)) return CP_EUNSUPPORTED;
+  if (unaligned(c->page_stride) || unaligned(c->slot_stride) || unaligned(c->head_stride)) return CP_EINVAL;
+  const bool fours = c->dtype == CP_I4;
+  if (fours && (c->block_page_stride < 0 || c->block_slot_stride < 0 || c->block_head_stride < 0 ||
+                c->block_page_stride % 4 != 0 || c->block_slot_stride % 4 != 0 || c->block_head_stride % 4 != 0))
     return CP_EINVAL;
   *out = Cache{};
   out->k = c->k;
@@ -69,7 +76,16 @@ static int cache_of(const cp_cache* c, bool with_memory, Cache* out) {
   out->capacity = (int32_t)(c->table_width * c->page_size);
   out->heads = (int)c->heads;
   out->D = (int)c->D;
+  if (fours) {
+    out->k_block = (uint8_t*)c->k_block;
+    out->v_block = (uint8_t*)c->v_block;
+    out->block_page = c->block_page_stride;
+    out->block_slot = c->block_slot_stride;
+    out->block_head = c->block_head_stride;
+  }
   if (!with_memory) return CP_OK;
+  if (fours && (!aligned(c->k_block, 4) || !aligned(c->v_block, 4) || (c->pages > 0 && (!c->k_block || !c->v_block))))
+    return CP_EINVAL;
   if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_scale, 4) ||
       !aligned(c->v_scale, 4) || !aligned(c->table, 4))
     return CP_EINVAL;
@@ -153,7 +169,7 @@ int coverprune_cache_append(const cp_cache* cache, const void* k, const int64_t*
   if (T < 0 || B < 0 || T > kMaxSize || B > (1 << 24)) return CP_EINVAL;
   AppendArgs a{};
   CP_TRY_STATUS(cache_of(cache, true, &a.cache));
-  if (cache->dtype != CP_E4M3 && cache->dtype != dtype) return CP_EUNSUPPORTED;
+  if (cache->dtype != CP_E4M3 && cache->dtype != CP_I4 && cache->dtype != dtype) return CP_EUNSUPPORTED;
   CP_TRY_STATUS(rope_of(rope, cache->D, 0, &a.rope));
   if (q) CP_TRY_STATUS(rows_of(*q, dtype, T > 0, &a.q));
   if (!starts && T != B) return CP_EINVAL;
@@ -186,6 +202,20 @@ int coverprune_cache_append(const cp_cache* cache, const void* k, const int64_t*
   return launch_cache_append(a, dtype, cache->dtype, (cudaStream_t)stream);
 }
 
+// Where the parts of the attention's workspace begin: its own, and with weights the lse and the scores.
+struct Room {
+  size_t decode, lse, scores, all;
+};
+static Room room_of(int64_t B, int64_t Hq, const Cache& c, int cache_dtype) {
+  const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  Room r;
+  r.decode = decode_ws_bytes(Hq, c.heads, c.D, cache_dtype);
+  r.lse = up(r.decode);
+  r.scores = r.lse + up(4 * (size_t)B * (size_t)Hq);
+  r.all = r.scores + 4 * (size_t)B * (size_t)Hq * (size_t)c.capacity;
+  return r;
+}
+
 static int check_decode(int64_t B, int64_t Hq, const cp_cache* cache, bool with_memory, Cache* c) {
   CP_TRY_STATUS(cache_of(cache, with_memory, c));
   if (B < 0 || Hq < 0 || Hq > 65536 || Hq % cache->heads != 0) return CP_EINVAL;
@@ -202,24 +232,27 @@ int coverprune_decode_workspace_size(int64_t B, int64_t Hq, const cp_cache* cach
   return CP_OK;
 }
 
-int coverprune_decode_attention(const void* q, const int64_t* q_stride, int dtype, int64_t B,
-                                int64_t Hq, const cp_cache* cache, const int32_t* lens,
-                                const uint8_t* keep, int64_t keep_stride, float scale,
-                                int64_t window, void* out, const int64_t* out_stride, float* lse,
-                                void* ws, size_t ws_bytes, int32_t* status, cp_stream_t stream) {
+// The attention's arguments; `weights`: its scores are left behind for them, in the workspace's rest.
+static int attend(const void* q, const int64_t* q_stride, int dtype, int64_t B, int64_t Hq,
+                  const cp_cache* cache, const int32_t* lens, const uint8_t* keep,
+                  int64_t keep_stride, float scale, int64_t window, void* out,
+                  const int64_t* out_stride, float* lse, bool weights, float* weight,
+                  int64_t weight_stride, void* ws, size_t ws_bytes, int32_t* status,
+                  cp_stream_t stream) {
   if (dtype != CP_F32 && dtype != CP_BF16) return CP_EINVAL;
   DecodeArgs a{};
   CP_TRY_STATUS(check_decode(B, Hq, cache, true, &a.cache));
   if ((dtype == CP_F32) != (cache->dtype == CP_F32)) return CP_EUNSUPPORTED;
-  if (!isfinite(scale) || window < 0) return CP_EINVAL;
+  if (!isfinite(scale) || window < 0 || weight_stride < 0) return CP_EINVAL;
   if (B == 0 || Hq == 0) return CP_OK;
   if (!q || !q_stride || !out || !out_stride || !lens || !aligned(q, size_of(dtype)) ||
       !aligned(out, size_of(dtype)) || !aligned(lens, 4) || !aligned(lse, 4) ||
       !aligned(status, 4))
     return CP_EINVAL;
-  if (!ws || !aligned(ws, 256) ||
-      ws_bytes < decode_ws_bytes(Hq, a.cache.heads, a.cache.D, cache->dtype))
-    return CP_EWORKSPACE;
+  if (weights && ((!weight && a.cache.capacity > 0) || !aligned(weight, 4) || (B > 1 && weight_stride < a.cache.capacity)))
+    return CP_EINVAL;
+  const Room room = room_of(B, Hq, a.cache, cache->dtype);
+  if (!ws || !aligned(ws, 256) || ws_bytes < (weights ? room.all : room.decode)) return CP_EWORKSPACE;
   a.q = q;
   a.q_b = q_stride[0];
   a.q_h = q_stride[1];
@@ -237,7 +270,110 @@ int coverprune_decode_attention(const void* q, const int64_t* q_stride, int dtyp
   a.ws = ws;
   a.status = status;
   Stage st(CP_STAGE_ATTEND, (cudaStream_t)stream);
-  return launch_decode(a, cache->dtype, (cudaStream_t)stream);
+  if (!weights) return launch_decode(a, cache->dtype, (cudaStream_t)stream);
+  if (!lse) a.lse = (float*)((char*)ws + room.lse);
+  a.scores = (float*)((char*)ws + room.scores);
+  CP_TRY_STATUS(launch_decode_scores(a, cache->dtype, (cudaStream_t)stream));
+  return launch_weigh(a, weight, weight_stride, (cudaStream_t)stream);
+}
+
+int coverprune_decode_attention(const void* q, const int64_t* q_stride, int dtype, int64_t B,
+                                int64_t Hq, const cp_cache* cache, const int32_t* lens,
+                                const uint8_t* keep, int64_t keep_stride, float scale,
+                                int64_t window, void* out, const int64_t* out_stride, float* lse,
+                                void* ws, size_t ws_bytes, int32_t* status, cp_stream_t stream) {
+  return attend(q, q_stride, dtype, B, Hq, cache, lens, keep, keep_stride, scale, window, out, out_stride, lse,
+                false, nullptr, 0, ws, ws_bytes, status, stream);
+}
+
+int coverprune_decode_weigh_workspace_size(int64_t B, int64_t Hq, const cp_cache* cache,
+                                           size_t* bytes) {
+  if (!bytes) return CP_EINVAL;
+  Cache c;
+  CP_TRY_STATUS(check_decode(B, Hq, cache, false, &c));
+  *bytes = room_of(B, Hq, c, cache->dtype).all;
+  return CP_OK;
+}
+
+int coverprune_decode_attention_weigh(const void* q, const int64_t* q_stride, int dtype, int64_t B,
+                                      int64_t Hq, const cp_cache* cache, const int32_t* lens,
+                                      const uint8_t* keep, int64_t keep_stride, float scale,
+                                      int64_t window, void* out, const int64_t* out_stride,
+                                      float* lse, float* weight, int64_t weight_stride, void* ws,
+                                      size_t ws_bytes, int32_t* status, cp_stream_t stream) {
+  return attend(q, q_stride, dtype, B, Hq, cache, lens, keep, keep_stride, scale, window, out, out_stride, lse,
+                true, weight, weight_stride, ws, ws_bytes, status, stream);
+}
+
+int coverprune_cache_read(const cp_cache* cache, int64_t T, const int32_t* starts,
+                          const int32_t* lens, int64_t B, void* k, const int64_t* k_stride,
+                          void* v, const int64_t* v_stride, int dtype, int32_t* status,
+                          cp_stream_t stream) {
+  if (dtype != CP_F32 && dtype != CP_BF16) return CP_EINVAL;
+  if (T < 0 || B < 0 || T > kMaxSize || B > (1 << 24)) return CP_EINVAL;
+  ReadArgs a{};
+  CP_TRY_STATUS(cache_of(cache, true, &a.cache));
+  if (cache->dtype != CP_E4M3 && cache->dtype != CP_I4 && cache->dtype != dtype) return CP_EUNSUPPORTED;
+  if (!starts && T != B) return CP_EINVAL;
+  if (B == 0 || T == 0) return CP_OK;
+  if (!lens || !aligned(lens, 4) || !aligned(starts, 4) || !aligned(status, 4) || !k || !v || !k_stride ||
+      !v_stride || !aligned(k, size_of(dtype)) || !aligned(v, size_of(dtype)))
+    return CP_EINVAL;
+  a.k = k;
+  a.v = v;
+  a.k_t = k_stride[0];
+  a.k_h = k_stride[1];
+  a.v_t = v_stride[0];
+  a.v_h = v_stride[1];
+  a.T = T;
+  a.starts = starts;
+  a.lens = lens;
+  a.B = (int)B;
+  a.status = status;
+  Stage st(CP_STAGE_CACHE, (cudaStream_t)stream);
+  return launch_cache_read(a, dtype, cache->dtype, (cudaStream_t)stream);
+}
+
+int coverprune_cache_evict(const cp_cache* cache, const int32_t* lens, int64_t B,
+                           const float* weight, int64_t weight_stride, int64_t left,
+                           int64_t first, int64_t recent, int32_t* new_lens, float* new_weight,
+                           int64_t new_weight_stride, int64_t new_weight_width, int32_t* kept,
+                           int32_t* status, cp_stream_t stream) {
+  EvictArgs a{};
+  CP_TRY_STATUS(cache_of(cache, true, &a.cache));
+  if (B < 0 || B > (1 << 24) || left < 0 || first < 0 || recent < 0 || first > left || recent > left - first ||
+      weight_stride < 0 || new_weight_stride < 0 || new_weight_width < 0 || new_weight_width > kMaxSize)
+    return CP_EINVAL;
+  if (left > kMaxKeys || left * B > kMaxSize * 16) return CP_EUNSUPPORTED;
+  if (B == 0) return CP_OK;
+  if (!lens || !aligned(lens, 4) || !aligned(weight, 4) || !aligned(new_lens, 4) || !aligned(new_weight, 4) ||
+      !aligned(kept, 4) || !aligned(status, 4) || (left > 0 && !kept) || (a.cache.capacity > 0 && !weight))
+    return CP_EINVAL;
+  if (new_weight && B > 1 && new_weight_stride < new_weight_width) return CP_EINVAL;
+  // what a block writes others still read
+  const int64_t w = (B - 1) * weight_stride + a.cache.capacity, nw = (B - 1) * new_weight_stride + new_weight_width;
+  const struct { const void* p; int64_t n; } in[2] = {{lens, B}, {weight, w}}, out[3] = {{new_lens, B}, {new_weight, nw}, {kept, left * B}};
+  for (int i = 0; i < 3; ++i) {
+    for (const auto& x : in)
+      if (overlap(out[i].p, out[i].n, x.p, x.n)) return CP_EINVAL;
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return CP_EINVAL;
+  }
+  a.lens = lens;
+  a.B = (int)B;
+  a.weight = weight;
+  a.weight_stride = weight_stride;
+  a.left = (int)left;
+  a.first = (int)first;
+  a.recent = (int)recent;
+  a.new_lens = new_lens;
+  a.new_weight = new_weight;
+  a.new_weight_stride = new_weight_stride;
+  a.new_weight_width = new_weight_width;
+  a.kept = kept;
+  a.status = status;
+  Stage st(CP_STAGE_CACHE, (cudaStream_t)stream);
+  return launch_cache_evict(a, cache->dtype, (cudaStream_t)stream);
 }
 
 }  // extern "C"

@@ -14,7 +14,15 @@ size_t decode_ws_bytes(int64_t Hq, int64_t heads, int64_t D, int cache_dtype) {
 int launch_decode(const DecodeArgs& a, int cache_dtype, cudaStream_t s) {
   if (cache_dtype == CP_F32) return launch_decode_f32(a, s);
   if (cache_dtype == CP_BF16) return launch_decode_bf16(a, s);
+  if (cache_dtype == CP_I4) return launch_decode_i4(a, s);
   return launch_decode_e4m3(a, s);
+}
+
+int launch_decode_scores(const DecodeArgs& a, int cache_dtype, cudaStream_t s) {
+  if (cache_dtype == CP_F32) return launch_decode_f32_scores(a, s);
+  if (cache_dtype == CP_BF16) return launch_decode_bf16_scores(a, s);
+  if (cache_dtype == CP_I4) return launch_decode_i4_scores(a, s);
+  return launch_decode_e4m3_scores(a, s);
 }
 
 }  // namespace cp

@@ -54,30 +54,34 @@ constexpr int kQueue = 128;
 // 54.2 and 55.0 us, with 7 53.9; 128 ragged ones 94.9 and 97.2, with 7 94.9.
 template <int CT> struct Maximum { static constexpr float slack = 8.0f, under = 0.0f; };
 template <> struct Maximum<CP_E4M3> { static constexpr float slack = 15.0f, under = 7.0f; };
+template <> struct Maximum<CP_I4> : Maximum<CP_E4M3> {};
 // A maximum before any score: finite, so that differences of two are, and below no
 // finite score (of weight 1 beside it).
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-// What a cache's type changes: bytes an element, keys a tile.
+// What a cache's type changes: keys a tile (a lane has a key's page and row, so 32 at
+// most), the type of queries and outputs.
 template <int CT> struct Type;
-template <> struct Type<CP_BF16> { static constexpr int e = 2, tk = 16; using Row = __nv_bfloat16; };
-template <> struct Type<CP_E4M3> { static constexpr int e = 1, tk = 16; using Row = __nv_bfloat16; };
-template <> struct Type<CP_F32> { static constexpr int e = 4, tk = 8; using Row = float; };
+template <> struct Type<CP_BF16> { static constexpr int tk = 16; using Row = __nv_bfloat16; };
+template <> struct Type<CP_E4M3> { static constexpr int tk = 16; using Row = __nv_bfloat16; };
+template <> struct Type<CP_I4> { static constexpr int tk = 32; using Row = __nv_bfloat16; };
+template <> struct Type<CP_F32> { static constexpr int tk = 8; using Row = float; };
 
 // Shape of one variant: CT cache type, DP head width it is laid out for, QT query
 // heads a pass, SHORT whether each warp has sequences of its own (k_decode_short).
 template <int CT, int DP, int QT, bool SHORT = false>
 struct Shape {
-  static constexpr int e = Type<CT>::e;
   // Keys of a tile: 4 of float32 heads of 256, whose rings leave room for two blocks then:
   // 102 sequences of 574 to 1149 keys and 6 query tiles 242 us, with 8 keys and one block
   // 283; 47 of up to 125 15.0, 18.3.
   static constexpr int tk = CT == CP_F32 && DP == 256 ? 4 : Type<CT>::tk;
-  static constexpr int row = DP * e;                  // bytes of a row in shared memory
+  static constexpr uint32_t all = tk == 32 ? ~0u : (1u << tk % 32) - 1;  // every key of a tile
+  static constexpr int row = (int)cache_bytes(CT, DP);  // bytes of a row in shared memory
   static constexpr int cpr = row / 16;                // 16-byte chunks of it
-  static constexpr int tile = 2 * tk * row;           // K and V of a tile
+  static constexpr int sb = CT == CP_I4 ? DP / 16 : 0;  // bytes of its scales
+  static constexpr int tile = 2 * tk * (row + sb);    // K and V of a tile, and their scales
   // Ring: as many tiles as keep two blocks on an SM, 3 at least.  Three blocks of
   // shorter rings leave the join no room beside them and wait longer: 128 ragged
   // 8-bit sequences 101 us with two, 115 with three; four 125.
@@ -105,10 +109,14 @@ struct Shape {
 
 // Rows of the cache in 32 bits: row r of page p starts (p * page + r * slot) << shift
 // bytes into K and V.
+// Its scales start (p * block_page + r * block_slot) * 4 bytes into theirs, and are copied
+// `piece` bytes at a time.
 struct Rows {
   uint32_t page, slot;
   uint32_t scale;  // 1 << shift
   uint32_t mul, div_shift;  // key / page_size = key * mul >> 31 >> div_shift
+  uint32_t block_page, block_slot;
+  int piece;
 };
 
 // Where a chunk of a row lies, chunk c at c ^ swizzle(r): rows that are read
@@ -116,7 +124,7 @@ struct Rows {
 // swizzle(r) ^ swizzle(s).
 template <int CT, int CPR>
 __host__ __device__ constexpr int swizzle(int r) {
-  return CT == CP_F32 ? (r & 1) << 2 : CPR >= 8 ? r & 7 : (r >> 1) & 3;
+  return CT == CP_F32 ? (r & 1) << 2 : CPR >= 8 ? r & 7 : CPR == 4 ? (r >> 1) & 3 : (r >> 2) & 1;
 }
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
@@ -126,6 +134,12 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
   const int n = there ? 16 : 0;  // 0: nothing is read, zeros are written
   asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n)
                : "memory");
+}
+// 4, 8 or 16 bytes, or as many zeros.
+template <int BYTES>
+__device__ __forceinline__ void copy_few(uint32_t dst, const void* src, bool there) {
+  const int n = there ? BYTES : 0;
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(n) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copy_wait() {
@@ -162,6 +176,56 @@ __device__ __forceinline__ void e4m3_f16x2(uint32_t x, uint32_t* lo, uint32_t* h
       "cvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
       : "=r"(*lo), "=r"(*hi)
       : "r"(x));
+}
+// Four bits of each half of x, as 2 x 2 of them come: numbers n + 8 in bits 0-3 (LOW) or
+// 4-7 of a half become n in float16.  1024 and the bits are a float16 as they are
+// (with bits 4-7 1024 and 16 times the number); what is taken off again is exact.
+template <bool LOW>
+__device__ __forceinline__ uint32_t i4_f16x2(uint32_t x) {
+  uint32_t y;
+  if (LOW) {
+    asm("{\n\t.reg .b32 a;\n\tlop3.b32 a, %1, 0x000F000F, 0x64006400, 0xEA;\n\tadd.rn.f16x2 %0, a, %2;\n\t}"
+        : "=r"(y)
+        : "r"(x), "r"(0xE408E408u));  // -1032
+  } else {
+    asm("{\n\t.reg .b32 a;\n\tlop3.b32 a, %1, 0x00F000F0, 0x64006400, 0xEA;\n\tfma.rn.f16x2 %0, a, %2, %3;\n\t}"
+        : "=r"(y)
+        : "r"(x), "r"(0x2C002C00u), "r"(0xD480D480u));  // 1 / 16, -72
+  }
+  return y;
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t y;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
+  return y;
+}
+// Bytes of a and b picked by `sel`, as two 8-bit elements, in float16 (exact).
+__device__ __forceinline__ uint32_t scales_f16x2(uint32_t a, uint32_t b, uint32_t sel) {
+  uint32_t y;
+  asm("{\n\t.reg .b32 p;\n\t.reg .b16 l, h;\n\tprmt.b32 p, %1, %2, %3;\n\tmov.b32 {l, h}, p;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %0, l;\n\t}"
+      : "=r"(y)
+      : "r"(a), "r"(b), "r"(sel));
+  return y;
+}
+__device__ __forceinline__ uint32_t load_shared(uint32_t at) {
+  uint32_t y;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(y) : "r"(at) : "memory");
+  return y;
+}
+// N words of a 4-bit row's scales.
+template <int N>
+__device__ __forceinline__ void load_words(uint32_t (&w)[N], uint32_t at) {
+  if constexpr (N == 1) {
+    w[0] = load_shared(at);
+  } else if constexpr (N == 2) {
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at) : "memory");
+  } else {
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                 : "r"(at)
+                 : "memory");
+  }
 }
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -256,20 +320,49 @@ struct Keys {
   }
 };
 
+// Where the scores of a segment's tiles go, for those who add the weights up by them:
+// `to` is key 0's and query h0's, pitch floats a key; `keys` the tile's, -1 for none.
+struct NoScores {
+  static constexpr bool on = false;
+};
+struct Scores {
+  static constexpr bool on = true;
+  float* to;
+  int64_t pitch;
+  int nq;
+  const int* keys;
+  __device__ __forceinline__ void put(int row, uint32_t valid, int query, float s) const {
+    const int key = keys[row];  // one on a bad page weighs nothing
+    if (key >= 0 && query < nq) to[key * pitch + query] = valid >> row & 1 ? s : -INFINITY;
+  }
+};
+
 // A warp's running softmax and output of one segment on the tensor cores.
-// Lane (g, t) = (lane / 4, lane % 4) has the scores of keys g and g + 8 and
+// Lane (g, t) = (lane / 4, lane % 4) has the scores of keys g and g + 8 (of a tile's every 16) and
 // queries 2 t, 2 t + 1 of each group of 8, and the same queries' outputs at
-// components 16 i + g, + 8 (8-bit caches: 16 i + 2 g, + 1).
+// components 16 i + g, + 8 (8-bit caches: 16 i + 2 g, + 1; 4-bit ones: as component() says).
+// A 4-bit element enters as n s, which float16 holds exactly (5 bits times 4), its scale's byte
+// turned into float16 as well.
 template <int CT, int DP, int QT, bool SHORT>
 struct Math {
   using S = Shape<CT, DP, QT, SHORT>;
   static constexpr int NT = QT / 8, KS = DP / 16;
+  static constexpr int H = S::tk / 16;       // groups of 16 keys in a tile
+  static constexpr int SW = DP < 64 ? 1 : DP / 64;  // words of a 4-bit row's scales
   uint32_t q[NT][KS][2];
   float o[NT][KS][4];
   float m[NT][2], l[NT][2];
   float sc[NT][2];  // score = sc * product, in units of log 2
   int g, t;
   uint32_t k_at, v_at;  // this lane's rows in a tile's K and V, first chunk: chunk c is ^ 16 c
+  int half_word;        // the word of a 4-bit row's scales whose upper half is padding; -1: none
+
+  // The component of o[n][k]'s row g (half 0) or g + 8 (half 1).
+  __device__ __forceinline__ int component(int k, int half) const {
+    if (CT == CP_BF16) return 16 * k + g + 8 * half;
+    if (CT == CP_E4M3) return 16 * k + 2 * g + half;
+    return 32 * (k / 2) + 4 * g + 2 * (k % 2) + half;
+  }
 
   __device__ __forceinline__ void start(const DecodeArgs& a, int b, int hk, int h0, int nq, char*,
                                         int, int lane) {
@@ -282,6 +375,7 @@ struct Math {
       v_at = key * S::row + 16 * (vc ^ swizzle<CT, S::cpr>(key));
     }
     const int D = a.cache.D;
+    half_word = D % 64 != 0 ? D / 64 : -1;  // whose padding might be a NaN
     const float scale = a.scale * (a.cache.k_scale ? a.cache.k_scale[hk] : 1.0f) * kLog2e;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -295,7 +389,9 @@ struct Math {
       for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int d = 16 * s + (CT == CP_E4M3 ? 4 * t + 2 * i : 2 * t + 8 * i);
+          // (4 bits: pairs 4 t .. 4 t + 3 of 32 components, put in order below)
+          const int d = CT == CP_I4 ? 32 * (s / 2) + 8 * t + 4 * (s % 2) + 2 * i
+                                    : 16 * s + (CT == CP_E4M3 ? 4 * t + 2 * i : 2 * t + 8 * i);
           uint32_t x = 0;
           if (row_there && d < D) {
             if (pairs)
@@ -305,8 +401,20 @@ struct Math {
           }
           q[n][s][i] = x;
         }
+      if (CT == CP_I4) {
+        // a word of a row has components 0 to 7 in its eight places; two at a time come out
+        // of it, four places apart
+#pragma unroll
+        for (int s = 0; s < KS; s += 2) {
+          const uint32_t w0 = q[n][s][0], w1 = q[n][s][1], w2 = q[n][s + 1][0], w3 = q[n][s + 1][1];
+          q[n][s][0] = __byte_perm(w0, w2, 0x5410);
+          q[n][s][1] = __byte_perm(w0, w2, 0x7632);
+          q[n][s + 1][0] = __byte_perm(w1, w3, 0x5410);
+          q[n][s + 1][1] = __byte_perm(w1, w3, 0x7632);
+        }
+      }
       int ex = 0;
-      if (CT == CP_E4M3) {
+      if (CT != CP_BF16) {
         // keys enter as float16, exactly, and so do queries once their largest
         // component is brought to [2^8, 2^9) by a power of two (bf16 has fewer bits;
         // what lies 2^22 below the largest component loses some; below 2^-92 the
@@ -332,7 +440,7 @@ struct Math {
       for (int i = 0; i < 2; ++i) {
         // the two queries whose scores this lane has
         sc[n][i] = scale;
-        if (CT == CP_E4M3) sc[n][i] *= power(__shfl_sync(~0u, ex, 4 * (2 * t + i)));
+        if (CT != CP_BF16) sc[n][i] *= power(__shfl_sync(~0u, ex, 4 * (2 * t + i)));
         m[n][i] = kLowest;
         l[n][i] = 0.0f;
       }
@@ -343,19 +451,22 @@ struct Math {
     }
   }
 
-  __device__ __forceinline__ void tile(uint32_t at, uint32_t valid, char*, int, int) {
-    float s[NT][4];
+  template <typename Score>
+  __device__ __forceinline__ void tile(uint32_t at, uint32_t valid, char*, int, int, const Score& scores) {
+    float s[H][NT][4];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s[h][n][0] = s[h][n][1] = s[h][n][2] = s[h][n][3] = 0.0f;
     if (CT == CP_BF16) {
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         uint32_t x[4];
         ldmatrix4(x, (at + k_at) ^ (32 * k));
 #pragma unroll
-        for (int n = 0; n < NT; ++n) mma_bf16_16816(s[n], x[0], x[1], x[2], x[3], q[n][k][0], q[n][k][1]);
+        for (int n = 0; n < NT; ++n) mma_bf16_16816(s[0][n], x[0], x[1], x[2], x[3], q[n][k][0], q[n][k][1]);
       }
-    } else {
+    } else if (CT == CP_E4M3) {
 #pragma unroll
       for (int k = 0; k < KS; k += 2) {
         uint32_t x[4];
@@ -366,30 +477,79 @@ struct Math {
           e4m3_f16x2(x[2 * j], &a0, &a2);
           e4m3_f16x2(x[2 * j + 1], &a1, &a3);
 #pragma unroll
-          for (int n = 0; n < NT; ++n) mma_f16_16816(s[n], a0, a1, a2, a3, q[n][k + j][0], q[n][k + j][1]);
+          for (int n = 0; n < NT; ++n) mma_f16_16816(s[0][n], a0, a1, a2, a3, q[n][k + j][0], q[n][k + j][1]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        // scales of keys g and g + 8; a lane's word of chunk c is of components 32 c + 8 t to + 7, one scale
+        uint32_t lo[SW], hi[SW];
+        load_words<SW>(lo, at + 2 * S::tk * S::row + (16 * h + g) * S::sb);
+        load_words<SW>(hi, at + 2 * S::tk * S::row + (16 * h + g + 8) * S::sb);
+#pragma unroll
+        for (int w = 0; w < SW; ++w) {
+          lo[w] &= w == half_word ? 0xFFFFu : ~0u;
+          hi[w] &= w == half_word ? 0xFFFFu : ~0u;
+        }
+#pragma unroll
+        for (int c = 0; c < DP / 32; c += 2) {
+          uint32_t x[4];
+          ldmatrix4(x, (at + 16 * h * S::row + k_at) ^ (16 * c));
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t sel = (2 * j + t / 2) * 0x11;
+            const uint32_t s0 = scales_f16x2(lo[c / 2], 0, sel), s1 = scales_f16x2(hi[c / 2], 0, sel);
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+              const uint32_t w0 = x[2 * j] >> 8 * m, w1 = x[2 * j + 1] >> 8 * m;
+              const uint32_t a0 = mul_f16x2(i4_f16x2<true>(w0), s0), a1 = mul_f16x2(i4_f16x2<true>(w1), s1);
+              const uint32_t a2 = mul_f16x2(i4_f16x2<false>(w0), s0), a3 = mul_f16x2(i4_f16x2<false>(w1), s1);
+#pragma unroll
+              for (int n = 0; n < NT; ++n)
+                mma_f16_16816(s[h][n], a0, a1, a2, a3, q[n][2 * (c + j) + m][0], q[n][2 * (c + j) + m][1]);
+            }
+          }
         }
       }
     }
-    const bool full = valid == (1u << S::tk) - 1;
+    if constexpr (Score::on) {
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            scores.put(16 * h + g + 8 * (i / 2), valid, 8 * n + 2 * t + (i & 1), s[h][n][i] * sc[n][i & 1]);
+    }
+    const bool full = valid == S::all;
     if (!full) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int h = 0; h < H; ++h)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)  // scores are multiplied by sc, of either sign, next
-          if (!(valid >> (g + 8 * (i / 2)) & 1)) s[n][i] = __int_as_float(0x7fffffff);
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)  // scores are multiplied by sc, of either sign, next
+            if (!(valid >> (16 * h + g + 8 * (i / 2)) & 1)) s[h][n][i] = __int_as_float(0x7fffffff);
     }
+    // the largest of this lane's scores of a query; fmaxf passes over the NaN of a key that is not there
+    auto most = [&](int n, int i) {
+      float x = fmaxf(s[0][n][i] * sc[n][i], s[0][n][i + 2] * sc[n][i]);
+#pragma unroll
+      for (int h = 1; h < H; ++h) x = fmaxf(x, fmaxf(s[h][n][i] * sc[n][i], s[h][n][i + 2] * sc[n][i]));
+      return x;
+    };
     bool above = false;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)  // fmaxf passes over the NaN of a key that is not there
-        above |= fmaxf(s[n][i] * sc[n][i], s[n][i + 2] * sc[n][i]) > m[n][i] + Maximum<CT>::slack;
+      for (int i = 0; i < 2; ++i) above |= most(n, i) > m[n][i] + Maximum<CT>::slack;
     if (__any_sync(~0u, above)) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          float top = fmaxf(fmaxf(s[n][i] * sc[n][i], s[n][i + 2] * sc[n][i]) - Maximum<CT>::under, m[n][i]);
+          float top = fmaxf(most(n, i) - Maximum<CT>::under, m[n][i]);
 #pragma unroll
           for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
           const float f = exp2_fast(m[n][i] - top);
@@ -402,42 +562,45 @@ struct Math {
           }
         }
     }
-    uint32_t p[NT][2], rest[NT][2];
+    uint32_t p[H][NT][2], rest[NT][2];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      float x[4];
+    for (int h = 0; h < H; ++h)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = exp2_fast(fmaf(s[n][i], sc[n][i & 1], -m[n][i & 1]));
-      if (!full) {
+      for (int n = 0; n < NT; ++n) {
+        float x[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (!(valid >> (g + 8 * (i / 2)) & 1)) x[i] = 0.0f;
-      }
-      l[n][0] += x[0] + x[2];
-      l[n][1] += x[1] + x[3];
-      // A weight goes on in 11 bits beside an 8-bit cache, float16's (see Maximum).  bfloat16's 8 would
-      // add as much error as the output's own rounding (0.0024 of its norm against
-      // 0.0017), so what they leave goes on as well, in a second product.  The first term
-      // is the largest bfloat16 below the weight: what it leaves is above 0 then, never 0
-      // or less, and an infinite value stays that infinity in both products (but for weights
-      // below 2^-100, whose second term may be none).
-      if (CT == CP_BF16) {
-        uint32_t below[4];
-        float left[4];
+        for (int i = 0; i < 4; ++i) x[i] = exp2_fast(fmaf(s[h][n][i], sc[n][i & 1], -m[n][i & 1]));
+        if (!full) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          below[i] = (uint32_t)max(__float_as_int(x[i]) - 1, 0);  // 0 stays 0
-          left[i] = x[i] - __uint_as_float(below[i] & 0xFFFF0000u);
+          for (int i = 0; i < 4; ++i)
+            if (!(valid >> (16 * h + g + 8 * (i / 2)) & 1)) x[i] = 0.0f;
         }
-        p[n][0] = movmatrix_trans(__byte_perm(below[0], below[1], 0x7632));
-        p[n][1] = movmatrix_trans(__byte_perm(below[2], below[3], 0x7632));
-        rest[n][0] = movmatrix_trans(pack_bf16(left[0], left[1]));
-        rest[n][1] = movmatrix_trans(pack_bf16(left[2], left[3]));
-      } else {
-        p[n][0] = movmatrix_trans(pack_f16(x[0], x[1]));
-        p[n][1] = movmatrix_trans(pack_f16(x[2], x[3]));
+        l[n][0] += x[0] + x[2];
+        l[n][1] += x[1] + x[3];
+        // A weight goes on in 11 bits beside an 8- or 4-bit cache, float16's (see Maximum).  bfloat16's 8 would
+        // add as much error as the output's own rounding (0.0024 of its norm against
+        // 0.0017), so what they leave goes on as well, in a second product.  The first term
+        // is the largest bfloat16 below the weight: what it leaves is above 0 then, never 0
+        // or less, and an infinite value stays that infinity in both products (but for weights
+        // below 2^-100, whose second term may be none).
+        if (CT == CP_BF16) {
+          uint32_t below[4];
+          float left[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            below[i] = (uint32_t)max(__float_as_int(x[i]) - 1, 0);  // 0 stays 0
+            left[i] = x[i] - __uint_as_float(below[i] & 0xFFFF0000u);
+          }
+          p[h][n][0] = movmatrix_trans(__byte_perm(below[0], below[1], 0x7632));
+          p[h][n][1] = movmatrix_trans(__byte_perm(below[2], below[3], 0x7632));
+          rest[n][0] = movmatrix_trans(pack_bf16(left[0], left[1]));
+          rest[n][1] = movmatrix_trans(pack_bf16(left[2], left[3]));
+        } else {
+          p[h][n][0] = movmatrix_trans(pack_f16(x[0], x[1]));
+          p[h][n][1] = movmatrix_trans(pack_f16(x[2], x[3]));
+        }
       }
-    }
+    const uint32_t blocks = at + (2 * S::row + S::sb) * S::tk;  // V's scales
     at += S::tk * S::row;
     if (CT == CP_BF16) {
 #pragma unroll
@@ -446,11 +609,11 @@ struct Math {
         ldmatrix4_trans(x, (at + v_at) ^ (32 * k));
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          mma_bf16_16816(o[n][k], x[0], x[1], x[2], x[3], p[n][0], p[n][1]);
+          mma_bf16_16816(o[n][k], x[0], x[1], x[2], x[3], p[0][n][0], p[0][n][1]);
           mma_bf16_16816(o[n][k], x[0], x[1], x[2], x[3], rest[n][0], rest[n][1]);
         }
       }
-    } else {
+    } else if (CT == CP_E4M3) {
 #pragma unroll
       for (int k = 0; k < KS; k += 2) {
         uint32_t x[4];
@@ -462,7 +625,35 @@ struct Math {
           e4m3_f16x2(__byte_perm(x[2 * j], 0, 0x3120), &a0, &a1);
           e4m3_f16x2(__byte_perm(x[2 * j + 1], 0, 0x3120), &a2, &a3);
 #pragma unroll
-          for (int n = 0; n < NT; ++n) mma_f16_16816(o[n][k + j], a0, a1, a2, a3, p[n][0], p[n][1]);
+          for (int n = 0; n < NT; ++n) mma_f16_16816(o[n][k + j], a0, a1, a2, a3, p[0][n][0], p[0][n][1]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        // scales of keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+        uint32_t ks[4][SW];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_words<SW>(ks[i], blocks + (16 * h + 2 * t + i % 2 + 8 * (i / 2)) * S::sb);
+#pragma unroll
+        for (int c = 0; c < DP / 32; c += 2) {
+          uint32_t x[4];
+          ldmatrix4_trans(x, (at + 16 * h * S::row + v_at) ^ (16 * c));
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            // halves: key 2 t's components 4 g to 4 g + 3, key 2 t + 1's; one scale a key
+            const uint32_t sel = 0x40 + (2 * j + g / 4) * 0x11;
+            const uint32_t s0 = scales_f16x2(ks[0][c / 2], ks[1][c / 2], sel);
+            const uint32_t s1 = scales_f16x2(ks[2][c / 2], ks[3][c / 2], sel);
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+              const uint32_t w0 = x[2 * j] >> 8 * m, w1 = x[2 * j + 1] >> 8 * m;
+              const uint32_t a0 = mul_f16x2(i4_f16x2<true>(w0), s0), a1 = mul_f16x2(i4_f16x2<false>(w0), s0);
+              const uint32_t a2 = mul_f16x2(i4_f16x2<true>(w1), s1), a3 = mul_f16x2(i4_f16x2<false>(w1), s1);
+#pragma unroll
+              for (int n = 0; n < NT; ++n) mma_f16_16816(o[n][2 * (c + j) + m], a0, a1, a2, a3, p[h][n][0], p[h][n][1]);
+            }
+          }
         }
       }
     }
@@ -482,8 +673,8 @@ struct Math {
         const float by = vs / l[n][i];
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-          out(query, 16 * k + (CT == CP_E4M3 ? 2 * g : g), l[n][i] == 0.0f ? 0.0f : o[n][k][i] * by);
-          out(query, 16 * k + (CT == CP_E4M3 ? 2 * g + 1 : g + 8), l[n][i] == 0.0f ? 0.0f : o[n][k][i + 2] * by);
+          out(query, component(k, 0), l[n][i] == 0.0f ? 0.0f : o[n][k][i] * by);
+          out(query, component(k, 1), l[n][i] == 0.0f ? 0.0f : o[n][k][i + 2] * by);
         }
         if (g == 0) lse(query, l[n][i] == 0.0f ? -INFINITY : (m[n][i] + log2f(l[n][i])) * kLn2);
       }
@@ -512,8 +703,7 @@ struct Math {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int query = 8 * n + 2 * t + (i & 1);
-          const int d = 16 * k + (CT == CP_E4M3 ? 2 * g + i / 2 : g + 8 * (i / 2));
-          buf[query * S::pitch + d] = o[n][k][i] * f[query];
+          buf[query * S::pitch + component(k, i / 2)] = o[n][k][i] * f[query];
         }
   }
 };
@@ -564,8 +754,9 @@ struct Math<CP_F32, DP, QT, SHORT> {
     return V == 2 ? 2 * lane + i : 128 * (i / 4) + 4 * lane + i % 4;
   }
 
-  __device__ __forceinline__ void tile(uint32_t at, uint32_t valid, char* extra, int warp,
-                                       int lane) {
+  template <typename Score>
+  __device__ __forceinline__ void tile(uint32_t at, uint32_t valid, char* extra, int warp, int lane,
+                                       const Score& scores) {
     const float* sq = queries(extra, warp);
     float* sp = (float*)extra + S::queries * QT * DP + warp * S::tk * QT;
     const char* smem = extra - S::ring;
@@ -598,6 +789,8 @@ struct Math<CP_F32, DP, QT, SHORT> {
     for (int n = 0; n < QT; ++n) {
 #pragma unroll
       for (int d = 1; d < L; d *= 2) s[n] += __shfl_xor_sync(~0u, s[n], d);
+      if constexpr (Score::on)
+        if (sub == n % L) scores.put(r, valid, n, s[n] * sc);
       above |= there && s[n] * sc > m[n] + Maximum<CP_F32>::slack;
     }
     if (__any_sync(~0u, above)) {
@@ -689,15 +882,15 @@ struct Math<CP_F32, DP, QT, SHORT> {
 
 // A warp's keys [lo, hi) of sequence b for the queries from h0 on: their tiles through
 // its ring into `math`.
-template <int CT, int DP, int QT, bool SHORT, typename K>
+template <int CT, int DP, int QT, bool SHORT, bool SCORES, typename K>
 __device__ __forceinline__ void math_of_keys(const DecodeArgs& a, const Rows& rows, K& keys, const int32_t* table, int lo,
                                              int hi, int hk, int b, int h0, int nq, int warp, int lane, uint32_t ring,
-                                             uint32_t* s_valid, char* extra, Math<CT, DP, QT, SHORT>& math) {
+                                             uint32_t* s_valid, int* s_keys, char* extra, Math<CT, DP, QT, SHORT>& math) {
   using S = Shape<CT, DP, QT, SHORT>;
   const Cache& ch = a.cache;
-  const int chunks = ch.D * S::e / 16;  // of a row that is there
-  const char* kp = (const char*)ch.k + (int64_t)hk * ch.head_stride * S::e;
-  const char* vp = (const char*)ch.v + (int64_t)hk * ch.head_stride * S::e;
+  const int chunks = (int)cache_bytes(CT, ch.D) / 16;  // of a row that is there
+  const char* kp = (const char*)ch.k + cache_bytes(CT, (int64_t)hk * ch.head_stride);
+  const char* vp = (const char*)ch.v + cache_bytes(CT, (int64_t)hk * ch.head_stride);
   if (chunks < S::cpr)  // components beyond the head's: the products run over zeros
     for (int i = lane; i < S::stages * S::tk * (S::cpr - chunks); i += 32) {
       const int c = chunks + i % (S::cpr - chunks), r = i / (S::cpr - chunks);
@@ -723,6 +916,25 @@ __device__ __forceinline__ void math_of_keys(const DecodeArgs& a, const Rows& ro
       const uint32_t mine = ok ? (uint32_t)page * rows.page + (uint32_t)slot_of * rows.slot : 0;
       const uint32_t valid = __ballot_sync(~0u, ok);
       if (lane == 0) s_valid[slot] = valid;
+      if (SCORES && lane < S::tk) s_keys[slot * S::tk + lane] = key;
+      if constexpr (CT == CP_I4) {  // a lane copies the scales of its own key
+        const uint64_t off = ok ? (uint64_t)((uint32_t)page * rows.block_page + (uint32_t)slot_of * rows.block_slot) * 4 : 0;
+        const uint8_t* kb = ch.k_block + (int64_t)hk * ch.block_head + off;
+        const uint8_t* vb = ch.v_block + (int64_t)hk * ch.block_head + off;
+        const uint32_t at = ring + slot * S::tile + 2 * S::tk * S::row + lane * S::sb;
+        if (S::sb >= 8 && rows.piece == S::sb) {
+          copy_few<(S::sb >= 8 ? S::sb : 4)>(at, kb, ok);
+          copy_few<(S::sb >= 8 ? S::sb : 4)>(at + S::tk * S::sb, vb, ok);
+        } else {
+          const int there = block_bytes(ch.D);
+#pragma unroll
+          for (int i = 0; i < S::sb; i += 4) {  // what lies beyond the row's becomes 0
+            const bool real = ok && i < there;
+            copy_few<4>(at + i, kb + (real ? i : 0), real);
+            copy_few<4>(at + S::tk * S::sb + i, vb + (real ? i : 0), real);
+          }
+        }
+      }
       // 32 chunks at a time: some rows side by side, or a part of one
       constexpr int side = S::cpr >= 32 ? 1 : 32 / S::cpr;
       const int c = lane % S::cpr, r0 = lane / S::cpr;
@@ -737,7 +949,7 @@ __device__ __forceinline__ void math_of_keys(const DecodeArgs& a, const Rows& ro
           copy(at, off, r + r0, c + more / 16);
         }
       };
-      if (valid == (1u << S::tk) - 1 && chunks == S::cpr) {
+      if (valid == S::all && chunks == S::cpr) {
         each([&](uint32_t at, uint64_t off, int, int) {
           copy16(at, kp + off);
           copy16(at + S::tk * S::row, vp + off);
@@ -767,7 +979,11 @@ __device__ __forceinline__ void math_of_keys(const DecodeArgs& a, const Rows& ro
     __syncwarp();  // tile i is there for every lane, and tile i - 1 done with
     issue();
     const int slot = i % S::stages;
-    math.tile(ring + slot * S::tile, s_valid[slot], extra, warp, lane);
+    if constexpr (SCORES)
+      math.tile(ring + slot * S::tile, s_valid[slot], extra, warp, lane,
+                Scores{a.scores + (int64_t)b * ch.capacity * a.Hq + h0, a.Hq, nq, s_keys + slot * S::tk});
+    else
+      math.tile(ring + slot * S::tile, s_valid[slot], extra, warp, lane, NoScores{});
   }
 }
 
@@ -810,7 +1026,7 @@ __device__ __forceinline__ float remote(const float* p, int rank) {
   return x;
 }
 
-template <int CT, int DP, int QT>
+template <int CT, int DP, int QT, bool SCORES>
 __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, int unit, int tiles, float* parts,
                                                      Begin* begins, int by_column) {
   using S = Shape<CT, DP, QT>;
@@ -818,6 +1034,7 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
   extern __shared__ __align__(1024) char smem[];  // addresses of rows are put together by exclusive or
   __shared__ int s_queue[kWarps][kQueue];
   __shared__ uint32_t s_valid[kWarps][S::stages];
+  __shared__ int s_keys[kWarps][SCORES ? S::stages * S::tk : 1];
   __shared__ float s_m[kWarps][QT], s_l[kWarps][QT], s_f[kWarps][QT], s_top[QT], s_sum[QT];
   wait_for_stream();
   const Cache& ch = a.cache;
@@ -890,8 +1107,8 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
       const int nq = min(QT, G - col % tiles * QT);
       const int lo = first + k0 * unit, hi = (int)min((int64_t)len, first + (int64_t)k1 * unit);
       Math<CT, DP, QT, false> math;
-      math_of_keys<CT, DP, QT, false>(a, rows, keys, table, lo, hi, hk, b, h0, nq, warp, lane, ring, s_valid[warp], extra,
-                                      math);
+      math_of_keys<CT, DP, QT, false, SCORES>(a, rows, keys, table, lo, hi, hk, b, h0, nq, warp, lane, ring, s_valid[warp],
+                                              s_keys[warp], extra, math);
       math.finish(s_m[warp], s_l[warp]);
       copy_wait<0>();
       __syncthreads();
@@ -943,13 +1160,14 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
 // Few query tiles of a few units a block: a cluster of blocks shares each, and adds its
 // parts from one another's shared memory, an element a thread, so that no launch has
 // to follow.
-template <int CT, int DP, int QT>
+template <int CT, int DP, int QT, bool SCORES>
 __global__ void __launch_bounds__(kThreads) k_decode_cluster(DecodeArgs a, Rows rows, int tiles, int size) {
   using S = Shape<CT, DP, QT>;
   using Row = typename Type<CT>::Row;
   extern __shared__ __align__(1024) char smem[];
   __shared__ int s_queue[kWarps][kQueue];
   __shared__ uint32_t s_valid[kWarps][S::stages];
+  __shared__ int s_keys[kWarps][SCORES ? S::stages * S::tk : 1];
   __shared__ float s_m[kWarps][QT], s_l[kWarps][QT], s_f[kWarps][QT];
   __shared__ float s_top[QT], s_sum[QT];          // this block's, for the others
   __shared__ float s_w[QT][kMaxCluster], s_all[QT];  // the blocks' weights and the whole sum
@@ -972,8 +1190,9 @@ __global__ void __launch_bounds__(kThreads) k_decode_cluster(DecodeArgs a, Rows 
   keys.queue = s_queue[warp];
   keys.keep = a.keep ? a.keep + (int64_t)b * a.keep_stride : nullptr;
   Math<CT, DP, QT, false> math;
-  math_of_keys<CT, DP, QT, false>(a, rows, keys, ch.table + (int64_t)b * ch.table_stride, lo, hi, hk, b, h0, nq, warp, lane,
-                                  smem_addr(smem) + warp * S::stages * S::tile, s_valid[warp], smem + S::ring, math);
+  math_of_keys<CT, DP, QT, false, SCORES>(a, rows, keys, ch.table + (int64_t)b * ch.table_stride, lo, hi, hk, b, h0, nq, warp,
+                                          lane, smem_addr(smem) + warp * S::stages * S::tile, s_valid[warp], s_keys[warp],
+                                          smem + S::ring, math);
   math.finish(s_m[warp], s_l[warp]);
   copy_wait<0>();
   __syncthreads();
@@ -1022,13 +1241,14 @@ __global__ void __launch_bounds__(kThreads) k_decode_cluster(DecodeArgs a, Rows 
 
 // Many short sequences: a warp takes a query tile alone, and then another, so that one's beginning (table, keys, queries: three trips
 // to memory) runs beside the others' and nothing is merged.
-template <int CT, int DP, int QT>
+template <int CT, int DP, int QT, bool SCORES>
 __global__ void __launch_bounds__(kThreads) k_decode_short(DecodeArgs a, Rows rows, int tiles, int64_t columns) {
   using S = Shape<CT, DP, QT, true>;
   using Row = typename Type<CT>::Row;
   extern __shared__ __align__(1024) char smem[];
   __shared__ int s_queue[kWarps][kQueue];
   __shared__ uint32_t s_valid[kWarps][S::stages];
+  __shared__ int s_keys[kWarps][SCORES ? S::stages * S::tk : 1];
   wait_for_stream();
   const Cache& ch = a.cache;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -1045,8 +1265,8 @@ __global__ void __launch_bounds__(kThreads) k_decode_short(DecodeArgs a, Rows ro
     keys_of(a, b, &first, &len);
     keys.keep = a.keep ? a.keep + (int64_t)b * a.keep_stride : nullptr;
     Math<CT, DP, QT, true> math;
-    math_of_keys<CT, DP, QT, true>(a, rows, keys, ch.table + (int64_t)b * ch.table_stride, first, len, hk, b, h0, nq, warp,
-                                   lane, ring, s_valid[warp], smem + S::ring, math);
+    math_of_keys<CT, DP, QT, true, SCORES>(a, rows, keys, ch.table + (int64_t)b * ch.table_stride, first, len, hk, b, h0, nq,
+                                           warp, lane, ring, s_valid[warp], s_keys[warp], smem + S::ring, math);
     copy_wait<0>();
     math.write(
         ch.v_scale ? ch.v_scale[hk] : 1.0f,
@@ -1082,7 +1302,7 @@ __device__ __forceinline__ void load_part(const float* p, float (&x)[V]) {
     }
   }
 }
-template <int CT, int DP, int QT>
+template <int CT, int DP, int QT, bool SCORES>
 __global__ void __launch_bounds__(32 * kJoinWarps) k_decode_join(DecodeArgs a, int tiles, int side, const float* parts,
                                                                  const Begin* begins) {
   using S = Shape<CT, DP, QT>;
@@ -1163,14 +1383,14 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_decode_join(DecodeArgs a, i
 // The largest clusters of which `columns` run at the same time, 2 to kMaxCluster blocks
 // (1: there are none): at most `all` blocks, and no more clusters than the device
 // holds, which is asked once a device and size.
-template <int CT, int DP, int QT>
+template <int CT, int DP, int QT, bool SCORES>
 static int cluster_size(int64_t columns, int64_t all, int* size) {
   using S = Shape<CT, DP, QT>;
   static std::atomic<uint64_t> allowed{0};
   static std::atomic<int> held[64][5];  // a device's clusters of 2^i blocks, and one more (0: not asked yet)
   *size = 1;
   if (columns * 2 > all) return CP_OK;
-  const void* kernel = (const void*)k_decode_cluster<CT, DP, QT>;
+  const void* kernel = (const void*)k_decode_cluster<CT, DP, QT, SCORES>;
   int dev = 0;
   CP_TRY_STATUS(cuda_status(cudaGetDevice(&dev), "decode: device"));
   if (!(allowed.load(std::memory_order_acquire) >> (dev & 63) & 1))
@@ -1191,7 +1411,7 @@ static int cluster_size(int64_t columns, int64_t all, int* size) {
       cfg.dynamicSmemBytes = S::smem;
       cfg.attrs = &with;
       cfg.numAttrs = 1;
-      if (cudaOccupancyMaxActiveClusters(&n, k_decode_cluster<CT, DP, QT>, &cfg) != cudaSuccess) {
+      if (cudaOccupancyMaxActiveClusters(&n, k_decode_cluster<CT, DP, QT, SCORES>, &cfg) != cudaSuccess) {
         (void)cudaGetLastError();  // a size that the device does not take
         n = 0;
       }
@@ -1203,7 +1423,7 @@ static int cluster_size(int64_t columns, int64_t all, int* size) {
   return CP_OK;
 }
 
-template <int CT, int DP, int QT>
+template <int CT, int DP, int QT, bool SCORES>
 static int launch(const DecodeArgs& a, cudaStream_t s) {
   using S = Shape<CT, DP, QT>;
   const int G = a.Hq / a.cache.heads, tiles = (G + QT - 1) / QT;
@@ -1220,13 +1440,24 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
 
   // rows of the cache in units that fit 32 bits
   const Cache& ch = a.cache;
-  const uint64_t page = (uint64_t)ch.page_stride * S::e, slot = (uint64_t)ch.slot_stride * S::e;
+  const uint64_t page = (uint64_t)cache_bytes(CT, ch.page_stride), slot = (uint64_t)cache_bytes(CT, ch.slot_stride);
   int shift = 4;
   while (shift < 31 && (page | slot) != 0 && ((page | slot) >> shift & 1) == 0) ++shift;
   const uint64_t far = (uint64_t)(ch.pages > 0 ? ch.pages - 1 : 0) * (page >> shift) +
                        (uint64_t)(ch.page_size - 1) * (slot >> shift);
   if (far > 0xFFFFFFFFu) return CP_EUNSUPPORTED;
-  Rows rows{(uint32_t)(page >> shift), (uint32_t)(slot >> shift), (uint32_t)1 << shift, 0, 0};
+  Rows rows{(uint32_t)(page >> shift), (uint32_t)(slot >> shift), (uint32_t)1 << shift, 0, 0, 0, 0, 4};
+  if constexpr (CT == CP_I4) {
+    if ((uint64_t)(ch.pages > 0 ? ch.pages - 1 : 0) * (uint64_t)(ch.block_page / 4) +
+            (uint64_t)(ch.page_size - 1) * (uint64_t)(ch.block_slot / 4) > 0xFFFFFFFFu)
+      return CP_EUNSUPPORTED;
+    rows.block_page = (uint32_t)(ch.block_page / 4);
+    rows.block_slot = (uint32_t)(ch.block_slot / 4);
+    // a row's scales in one copy, where they fill the layout's and are aligned to that
+    const uint64_t any = (uint64_t)ch.k_block | (uint64_t)ch.v_block | (uint64_t)ch.block_page | (uint64_t)ch.block_slot |
+                         (uint64_t)ch.block_head;
+    if (S::sb >= 8 && block_bytes(ch.D) == S::sb && any % S::sb == 0) rows.piece = S::sb;
+  }
   while (((int64_t)1 << rows.div_shift) < ch.page_size) ++rows.div_shift;
   rows.mul = (uint32_t)((((uint64_t)1 << (31 + rows.div_shift)) + ch.page_size - 1) / ch.page_size);
 
@@ -1241,7 +1472,7 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   Begin* begins = (Begin*)a.ws;
   float* parts = (float*)((char*)a.ws + kDecodeBlocks * sizeof(Begin));
   static std::atomic<uint64_t> allowed{0};
-  CP_TRY_STATUS(allow_smem_once((const void*)k_decode<CT, DP, QT>, S::smem, "decode: shared memory", &allowed));
+  CP_TRY_STATUS(allow_smem_once((const void*)k_decode<CT, DP, QT, SCORES>, S::smem, "decode: shared memory", &allowed));
   // Many short sequences: a warp a query tile, up to 64 keys for every third of the
   // blocks' number that there are tiles, and 64 more.  us with blocks / with warps,
   // 7 queries a head of 128: 320 tiles of up to 300 keys 17 / 16, of 500 18 / 26; 640
@@ -1264,10 +1495,10 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   if (most <= kFew || (columns > all && most <= (a.keep ? 32 : 16) * kUnit && most * all <= reach)) {
     using Short = Shape<CT, DP, QT, true>;
     static std::atomic<uint64_t> short_allowed{0};
-    CP_TRY_STATUS(allow_smem_once((const void*)k_decode_short<CT, DP, QT>, Short::smem, "decode: shared memory",
+    CP_TRY_STATUS(allow_smem_once((const void*)k_decode_short<CT, DP, QT, SCORES>, Short::smem, "decode: shared memory",
                                   &short_allowed));
     const int64_t room = (int64_t)di.sm_count * Short::per_sm, wanted = (columns + kWarps - 1) / kWarps;
-    return cuda_status(launch_early(k_decode_short<CT, DP, QT>, dim3((unsigned)(wanted < room ? wanted : room)), kThreads,
+    return cuda_status(launch_early(k_decode_short<CT, DP, QT, SCORES>, dim3((unsigned)(wanted < room ? wanted : room)), kThreads,
                                     Short::smem, s, a, rows, tiles, columns),
                        "decode: short");
   }
@@ -1285,14 +1516,14 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   // 10.6 / 11.6, of 1500 12.0 / 11.0, 9.3 / 8.2, 8.1 / 7.4.
   const int64_t n64 = (most + kUnit - 1) / kUnit;
   int size = 0;
-  if (cut) CP_TRY_STATUS((cluster_size<CT, DP, QT>(columns, all, &size)));
+  if (cut) CP_TRY_STATUS((cluster_size<CT, DP, QT, SCORES>(columns, all, &size)));
   const bool slow = CT == CP_F32 && !a.keep;
   if (size > 1 && n64 <= (a.keep ? 48 : slow ? 8 : 16) * size &&
       n64 * (all - columns * size) <= (slow ? 2 : 8) * size * all)
-    return cuda_status(launch_early_cluster(k_decode_cluster<CT, DP, QT>, dim3((unsigned)(columns * size)), kThreads, S::smem,
+    return cuda_status(launch_early_cluster(k_decode_cluster<CT, DP, QT, SCORES>, dim3((unsigned)(columns * size)), kThreads, S::smem,
                                             s, size, a, rows, tiles, size),
                        "decode: cluster");
-  CP_TRY_STATUS(cuda_status(launch_early(k_decode<CT, DP, QT>, dim3((unsigned)grid), kThreads, S::smem, s, a, rows, unit,
+  CP_TRY_STATUS(cuda_status(launch_early(k_decode<CT, DP, QT, SCORES>, dim3((unsigned)grid), kThreads, S::smem, s, a, rows, unit,
                                          tiles, parts, cut ? begins : nullptr, (int)by_column),
                             "decode"));
   if (!cut) return CP_OK;
@@ -1302,21 +1533,21 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   int side = share <= 4 ? 8 : share <= 12 ? 2 : 1;
   while (side > 1 && side / 2 >= queries) side /= 2;
   const dim3 joins((unsigned)(by_column ? columns : grid), (unsigned)(queries + side - 1) / side);
-  return cuda_status(launch_early(k_decode_join<CT, DP, QT>, joins, 32 * kJoinWarps, 0, s, a, tiles, side, parts, begins),
+  return cuda_status(launch_early(k_decode_join<CT, DP, QT, SCORES>, joins, 32 * kJoinWarps, 0, s, a, tiles, side, parts, begins),
                      "decode: join");
 }
 
-template <int CT, int DP>
+template <int CT, int DP, bool SCORES>
 static int launch_pass(const DecodeArgs& a, cudaStream_t s) {
   constexpr int one = CT == CP_F32 ? 4 : 8;
-  return decode_pass(CT, a.Hq / a.cache.heads) == one ? launch<CT, DP, one>(a, s) : launch<CT, DP, 2 * one>(a, s);
+  return decode_pass(CT, a.Hq / a.cache.heads) == one ? launch<CT, DP, one, SCORES>(a, s) : launch<CT, DP, 2 * one, SCORES>(a, s);
 }
-template <int CT>
+template <int CT, bool SCORES = false>
 static int launch_type(const DecodeArgs& a, cudaStream_t s) {
   switch (decode_width(a.cache.D)) {
-    case 64: return launch_pass<CT, 64>(a, s);
-    case 128: return launch_pass<CT, 128>(a, s);
-    default: return launch_pass<CT, 256>(a, s);
+    case 64: return launch_pass<CT, 64, SCORES>(a, s);
+    case 128: return launch_pass<CT, 128, SCORES>(a, s);
+    default: return launch_pass<CT, 256, SCORES>(a, s);
   }
 }
 

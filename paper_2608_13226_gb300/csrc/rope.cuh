@@ -71,4 +71,19 @@ template <> __device__ __forceinline__ __nv_fp8_e4m3 from_f32<__nv_fp8_e4m3>(flo
   return __nv_fp8_e4m3(x);  // to nearest even, saturating
 }
 
+// The sequence that row t belongs to: how many of starts[1..B] are <= t.
+__device__ __forceinline__ int sequence_of(const int32_t* starts, int B, int64_t t) {
+  int lo = 0, n = B;  // the first lo are, those from lo + n on are not
+  while (n > 0) {
+    const int h = n / 2;
+    if (starts[1 + lo + h] <= t) {
+      lo += h + 1;
+      n -= h + 1;
+    } else {
+      n = h;
+    }
+  }
+  return lo;
+}
+
 }  // namespace cp

@@ -425,21 +425,6 @@ __global__ void __launch_bounds__(kThreads, kBlocks) k_rotary(RotaryArgs a, Tili
   run_rows<T, T, V, SUBS, false>(job, a.rope, tl, a.D, a.B * a.T);
 }
 
-// The sequence that row t belongs to: how many of starts[1..B] are <= t.
-__device__ __forceinline__ int sequence_of(const int32_t* starts, int B, int64_t t) {
-  int lo = 0, n = B;  // the first lo are, those from lo + n on are not
-  while (n > 0) {
-    const int h = n / 2;
-    if (starts[1 + lo + h] <= t) {
-      lo += h + 1;
-      n -= h + 1;
-    } else {
-      n = h;
-    }
-  }
-  return lo;
-}
-
 // Rows of a token: its queries, keys and values.
 template <typename T, typename C>
 struct AppendJob {
@@ -643,6 +628,7 @@ static int append_wide(const AppendArgs& a, cudaStream_t s) {
 }
 
 int launch_cache_append(const AppendArgs& a, int dtype, int cache_dtype, cudaStream_t s) {
+  if (cache_dtype == CP_I4) return launch_append_fours(a, dtype, s);
   if (cache_dtype == CP_F32) return append_wide<float, float>(a, s);
   if (cache_dtype == CP_BF16) return append_wide<__nv_bfloat16, __nv_bfloat16>(a, s);
   if (dtype == CP_F32) return append_wide<float, __nv_fp8_e4m3>(a, s);

@@ -44,7 +44,16 @@ struct Cache {
   int32_t page_size;
   int32_t capacity;  // keys a table row holds
   int heads, D;
+  uint8_t *k_block, *v_block;  // CP_I4: the rows' scales
+  int64_t block_page, block_slot, block_head;  // bytes
 };
+
+// n elements of a cache in bytes (4 bits: n is even wherever it is asked for).
+__host__ __device__ constexpr int64_t cache_bytes(int dtype, int64_t n) {
+  return dtype == CP_F32 ? 4 * n : dtype == CP_BF16 ? 2 * n : dtype == CP_E4M3 ? n : n / 2;
+}
+// Bytes of a 4-bit row's scales.
+__host__ __device__ constexpr int block_bytes(int D) { return (D / 16 + 3) / 4 * 4; }
 
 struct AppendArgs {
   Cache cache;
@@ -59,6 +68,34 @@ struct AppendArgs {
   int32_t *new_lens, *status;
 };
 int launch_cache_append(const AppendArgs& a, int dtype, int cache_dtype, cudaStream_t s);
+
+// The append to a 4-bit cache.
+int launch_append_fours(const AppendArgs& a, int dtype, cudaStream_t s);
+
+struct ReadArgs {
+  Cache cache;
+  void *k, *v;
+  int64_t k_t, k_h, v_t, v_h;
+  int64_t T;
+  const int32_t *starts, *lens;
+  int B;
+  int32_t* status;
+};
+int launch_cache_read(const ReadArgs& a, int dtype, int cache_dtype, cudaStream_t s);
+
+struct EvictArgs {
+  Cache cache;
+  const int32_t* lens;
+  int B;
+  const float* weight;
+  int64_t weight_stride;
+  int left, first, recent;
+  int32_t* new_lens;
+  float* new_weight;
+  int64_t new_weight_stride, new_weight_width;
+  int32_t *kept, *status;
+};
+int launch_cache_evict(const EvictArgs& a, int cache_dtype, cudaStream_t s);
 
 struct DecodeArgs {
   Cache cache;
@@ -75,6 +112,7 @@ struct DecodeArgs {
   float* lse;
   void* ws;
   int32_t* status;
+  float* scores;  // [B, capacity, Hq], in units of log 2: only where weights are added up
 };
 // A launch that may begin before what precedes it on the stream has ended: its
 // blocks come to the SMs and wait there (wait_for_stream, first of all), so that its
@@ -108,6 +146,14 @@ int launch_decode(const DecodeArgs& a, int cache_dtype, cudaStream_t s);
 int launch_decode_bf16(const DecodeArgs& a, cudaStream_t s);
 int launch_decode_e4m3(const DecodeArgs& a, cudaStream_t s);
 int launch_decode_f32(const DecodeArgs& a, cudaStream_t s);
+int launch_decode_i4(const DecodeArgs& a, cudaStream_t s);
+// With the scores left in `scores`; launch_weigh then adds the weights up by them.
+int launch_decode_scores(const DecodeArgs& a, int cache_dtype, cudaStream_t s);
+int launch_decode_bf16_scores(const DecodeArgs& a, cudaStream_t s);
+int launch_decode_e4m3_scores(const DecodeArgs& a, cudaStream_t s);
+int launch_decode_f32_scores(const DecodeArgs& a, cudaStream_t s);
+int launch_decode_i4_scores(const DecodeArgs& a, cudaStream_t s);
+int launch_weigh(const DecodeArgs& a, float* weight, int64_t weight_stride, cudaStream_t s);
 
 // Query heads that one pass of the attention takes for groups of G, the width that a
 // head is laid out for, and the most blocks of a launch: what the workspace goes by.

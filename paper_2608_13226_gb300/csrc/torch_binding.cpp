@@ -153,7 +153,19 @@ cp_rows rows_of(const Tensor& in, const Tensor& out) {
   return r;
 }
 
-cp_cache cache_of(Call& c, PyObject* k_cache, PyObject* v_cache, PyObject* table, PyObject* k_scale, PyObject* v_scale) {
+// The scales of a 4-bit cache's rows; 1 for a row's components each 16, to a multiple of 4.
+const Tensor& blocks_of(Call& c, const char* name, PyObject* o, const cp_cache& x) {
+  const Tensor& t = c.rows(name, o, 4);
+  if (t.scalar_type() != at::kFloat8_e4m3fn)
+    bad_type(std::string(name) + " must be float8_e4m3fn, got " + c10::toString(t.scalar_type()));
+  const int64_t shape[4] = {x.pages, x.page_size, x.heads, (x.D / 16 + 3) / 4 * 4};
+  if (t.sizes() != at::IntArrayRef(shape, 4))
+    bad_value(std::string(name) + " must have shape " + text(at::IntArrayRef(shape, 4)) + ", got " + text(t.sizes()));
+  return t;
+}
+
+cp_cache cache_of(Call& c, PyObject* k_cache, PyObject* v_cache, PyObject* table, PyObject* k_scale, PyObject* v_scale,
+                  PyObject* k_block, PyObject* v_block) {
   const Tensor& k = c.rows("k_cache", k_cache, 4);
   const Tensor& v = c.tensor("v_cache", v_cache);
   cp_cache x{};
@@ -162,6 +174,12 @@ cp_cache cache_of(Call& c, PyObject* k_cache, PyObject* v_cache, PyObject* table
     case at::kFloat: x.dtype = CP_F32; break;
     case at::kBFloat16: x.dtype = CP_BF16; break;
     case at::kFloat8_e4m3fn: x.dtype = CP_E4M3; break;
+    case at::kByte:
+      if (k_block != Py_None && v_block != Py_None) {
+        x.dtype = CP_I4;
+        break;
+      }
+      bad_type("a cache of uint8 holds 4 bits an element and needs k_block and v_block");
     default:
       bad_type(std::string("the cache must be float32, bfloat16 or float8_e4m3fn, got ") + c10::toString(k.scalar_type()));
   }
@@ -169,22 +187,53 @@ cp_cache cache_of(Call& c, PyObject* k_cache, PyObject* v_cache, PyObject* table
     bad_value("k_cache and v_cache must share shape, strides and dtype");
   const Tensor& t = c.of_type("table", table, at::kInt);
   if (t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) bad_value("table must be [B, width], dense in its last dimension");
+  const int64_t each = x.dtype == CP_I4 ? 2 : 1;  // elements of the cache in one of the tensor
   x.k = k.data_ptr();
   x.v = v.data_ptr();
   x.pages = k.size(0);
   x.page_size = k.size(1);
   x.heads = k.size(2);
-  x.D = k.size(3);
+  x.D = k.size(3) * each;
   // strides of dimensions of one do not matter, whatever the tensor says
-  x.page_stride = x.pages > 1 ? k.stride(0) : 0;
-  x.slot_stride = x.page_size > 1 ? k.stride(1) : 0;
-  x.head_stride = x.heads > 1 ? k.stride(2) : 0;
+  x.page_stride = x.pages > 1 ? k.stride(0) * each : 0;
+  x.slot_stride = x.page_size > 1 ? k.stride(1) * each : 0;
+  x.head_stride = x.heads > 1 ? k.stride(2) * each : 0;
+  if (x.dtype == CP_I4) {
+    const Tensor& kb = blocks_of(c, "k_block", k_block, x);
+    const Tensor& vb = blocks_of(c, "v_block", v_block, x);
+    if (vb.strides() != kb.strides()) bad_value("k_block and v_block must share strides");
+    x.k_block = kb.data_ptr();
+    x.v_block = vb.data_ptr();
+    x.block_page_stride = x.pages > 1 ? kb.stride(0) : 0;
+    x.block_slot_stride = x.page_size > 1 ? kb.stride(1) : 0;
+    x.block_head_stride = x.heads > 1 ? kb.stride(2) : 0;
+  } else if (k_block != Py_None || v_block != Py_None) {
+    bad_value("k_block and v_block go with a cache of uint8");
+  }
   x.k_scale = c.optional<const float>("k_scale", k_scale, at::kFloat, {x.heads}, false);
   x.v_scale = c.optional<const float>("v_scale", v_scale, at::kFloat, {x.heads}, false);
   x.table = (const int32_t*)t.data_ptr();
   x.table_width = t.size(0) ? t.size(1) : 0;  // nothing, at no address
   x.table_stride = t.stride(0);
   return x;
+}
+
+// A cache that a call writes.
+void written_cache(const cp_cache& x, PyObject* k_cache, PyObject* v_cache, PyObject* k_block, PyObject* v_block) {
+  Call::written("k_cache", THPVariable_Unpack(k_cache));
+  Call::written("v_cache", THPVariable_Unpack(v_cache));
+  if (x.dtype != CP_I4) return;
+  Call::written("k_block", THPVariable_Unpack(k_block));
+  Call::written("v_block", THPVariable_Unpack(v_block));
+}
+
+// Weights of the keys, a row a sequence.
+const Tensor& weights_of(Call& c, const char* name, PyObject* o, int64_t B, int64_t keys) {
+  const Tensor& t = c.of_type(name, o, at::kFloat);
+  if (t.dim() != 2 || t.size(0) != B || t.size(1) < keys || (t.size(1) > 1 && t.stride(1) != 1))
+    bad_value(std::string(name) + " must be [" + std::to_string(B) + ", at least " + std::to_string(keys) +
+              "], dense in its last dimension");
+  return t;
 }
 
 // Autograd learns that a tensor of the caller's was written, and so notices where it had
@@ -296,13 +345,13 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 }
 
 // (k, v, k_cache, v_cache, table, lens, starts, pos, inv_freq, layout, scale, q, k_scale,
-// v_scale, new_lens, q_out, status) -> (new_lens, q_out)
+// v_scale, new_lens, q_out, status, k_block, v_block) -> (new_lens, q_out)
 PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
-  if (!counted(n_args, 17)) return nullptr;
+  if (!counted(n_args, 19)) return nullptr;
   return entry([&]() -> PyObject* {
     Call c;
-    const cp_cache cache = cache_of(c, a[2], a[3], a[4], a[12], a[13]);
-    Call::written("k_cache", THPVariable_Unpack(a[2]));
+    const cp_cache cache = cache_of(c, a[2], a[3], a[4], a[12], a[13], a[17], a[18]);
+    written_cache(cache, a[2], a[3], a[17], a[18]);
     const Tensor& k = c.rows("k", a[0], 3);
     const Tensor& v = c.rows("v", a[1], 3);
     const int64_t T = k.size(0), B = THPVariable_Unpack(a[4]).size(0);
@@ -342,7 +391,7 @@ PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                                      c.stream());
     });
     if (st != CP_OK) return PyLong_FromLong(st);
-    for (const int i : {2, 3, 14, 16}) changed(a[i]);  // the caches, new_lens, status
+    for (const int i : {2, 3, 14, 16, 17, 18}) changed(a[i]);  // the caches, new_lens, status, the caches' scales
     if (queries) changed(a[15]);
     PyObject* first = given_lens ? own(a[14]) : THPVariable_Wrap(lens_out);
     PyObject* second = !queries || a[15] != Py_None ? own(a[15]) : THPVariable_Wrap(q_out);
@@ -354,12 +403,12 @@ PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 }
 
 // (q, k_cache, v_cache, table, lens, scale or None, window, keep, k_scale, v_scale, lse, out, ws,
-// status) -> (out, lse or None, ws)
+// status, k_block, v_block, weight) -> (out, lse or None, ws)
 PyObject* decode_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
-  if (!counted(n_args, 14)) return nullptr;
+  if (!counted(n_args, 17)) return nullptr;
   return entry([&]() -> PyObject* {
     Call c;
-    const cp_cache cache = cache_of(c, a[1], a[2], a[3], a[8], a[9]);
+    const cp_cache cache = cache_of(c, a[1], a[2], a[3], a[8], a[9], a[14], a[15]);
     const Tensor& q = c.rows("q", a[0], 3);
     const int64_t B = THPVariable_Unpack(a[3]).size(0), Hq = q.size(1), keys = cache.table_width * cache.page_size;
     if (q.size(2) != cache.D || q.size(0) != B)
@@ -378,6 +427,8 @@ PyObject* decode_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     const float scale = a[5] == Py_None ? (float)(1.0 / std::sqrt((double)(cache.D > 0 ? cache.D : 1))) : (float)real(a[5]);
     const int64_t window = integer(a[6]);
     int32_t* status = c.word("status", a[13]);
+    const bool weigh = a[16] != Py_None;
+    if (weigh) Call::written("weight", weights_of(c, "weight", a[16], B, keys));
     const int with_lse = PyObject_IsTrue(a[10]);
     if (with_lse < 0) throw python_error();
 
@@ -385,7 +436,8 @@ PyObject* decode_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     Tensor out, lse, ws;
     if (a[12] == Py_None) {
       size_t bytes = 0;
-      const int st = coverprune_decode_workspace_size(B, Hq, &cache, &bytes);
+      const int st = weigh ? coverprune_decode_weigh_workspace_size(B, Hq, &cache, &bytes)
+                           : coverprune_decode_workspace_size(B, Hq, &cache, &bytes);
       if (st != CP_OK) return PyLong_FromLong(st);
       ws = c.made({(int64_t)bytes}, at::kByte);
     }
@@ -396,16 +448,131 @@ PyObject* decode_attention(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     if (with_lse) lse = c.made({B, Hq}, at::kFloat);
     const int64_t qs[2] = {q.stride(0), q.stride(1)}, os[2] = {to.stride(0), to.stride(1)};
     const int st = launch([&] {
+      float* to_lse = with_lse ? (float*)lse.data_ptr() : nullptr;
+      const size_t room = (size_t)work.numel() * work.element_size();
+      if (weigh) {
+        const Tensor& w = THPVariable_Unpack(a[16]);
+        return coverprune_decode_attention_weigh(q.data_ptr(), qs, dtype, B, Hq, &cache, (const int32_t*)lens.data_ptr(), keep,
+                                                 keep_stride, scale, window, to.data_ptr(), os, to_lse, (float*)w.data_ptr(),
+                                                 w.stride(0), work.data_ptr(), room, status, c.stream());
+      }
       return coverprune_decode_attention(q.data_ptr(), qs, dtype, B, Hq, &cache, (const int32_t*)lens.data_ptr(), keep,
-                                         keep_stride, scale, window, to.data_ptr(), os,
-                                         with_lse ? (float*)lse.data_ptr() : nullptr, work.data_ptr(),
-                                         (size_t)work.numel() * work.element_size(), status, c.stream());
+                                         keep_stride, scale, window, to.data_ptr(), os, to_lse, work.data_ptr(), room, status,
+                                         c.stream());
     });
     if (st != CP_OK) return PyLong_FromLong(st);
-    for (const int i : {11, 12, 13}) changed(a[i]);  // out, ws, status
+    for (const int i : {11, 12, 13, 16}) changed(a[i]);  // out, ws, status, weight
     PyObject* x = a[11] == Py_None ? THPVariable_Wrap(out) : own(a[11]);
     PyObject* y = with_lse ? THPVariable_Wrap(lse) : own(Py_None);
     PyObject* z = a[12] == Py_None ? THPVariable_Wrap(ws) : own(a[12]);
+    PyObject* all = x && y && z ? PyTuple_Pack(3, x, y, z) : nullptr;
+    Py_XDECREF(x);
+    Py_XDECREF(y);
+    Py_XDECREF(z);
+    return all;
+  });
+}
+
+// (k_cache, v_cache, table, lens, starts, tokens or None, k_scale, v_scale, k_block, v_block, float32 or
+// None, k_out, v_out, status) -> (k, v)
+PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (!counted(n_args, 14)) return nullptr;
+  return entry([&]() -> PyObject* {
+    Call c;
+    const cp_cache cache = cache_of(c, a[0], a[1], a[2], a[6], a[7], a[8], a[9]);
+    const int64_t B = THPVariable_Unpack(a[2]).size(0);
+    const Tensor& lens = c.dense("lens", a[3], at::kInt, {B}, false);
+    const int32_t* starts = c.optional<const int32_t>("starts", a[4], at::kInt, {B + 1}, false);
+    int64_t T = B;
+    if (a[5] != Py_None)
+      T = integer(a[5]);
+    else if (a[11] != Py_None)
+      T = c.rows("k_out", a[11], 3).size(0);
+    else if (a[4] != Py_None)
+      bad_value("with starts, tokens says how many rows there are");
+    if (T < 0) bad_value("tokens must not be negative, got " + std::to_string(T));
+    if (a[4] == Py_None && T != B)
+      bad_value("without starts there is one row a sequence: " + std::to_string(T) + " rows, " + std::to_string(B) + " sequences");
+    at::ScalarType type = cache.dtype == CP_F32 ? at::kFloat : at::kBFloat16;
+    if (a[10] != Py_None) {
+      const int wide = PyObject_IsTrue(a[10]);
+      if (wide < 0) throw python_error();
+      type = wide ? at::kFloat : at::kBFloat16;
+    } else if (a[11] != Py_None) {
+      type = c.rows("k_out", a[11], 3).scalar_type();
+    }
+    int32_t* status = c.word("status", a[13]);
+
+    c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.device);
+    Tensor made[2];
+    const int64_t shape[3] = {T, cache.heads, cache.D};
+    const char* const name[2] = {"k_out", "v_out"};
+    for (int i = 0; i < 2; ++i) {
+      if (a[11 + i] == Py_None) {
+        made[i] = c.made(at::IntArrayRef(shape, 3), type);
+        continue;
+      }
+      const Tensor& t = Call::written(name[i], c.rows(name[i], a[11 + i], 3));
+      if (t.sizes() != at::IntArrayRef(shape, 3) || t.scalar_type() != type)
+        bad_value(std::string(name[i]) + " must be " + text(at::IntArrayRef(shape, 3)) + " of " + c10::toString(type));
+    }
+    const Tensor& k = a[11] == Py_None ? made[0] : THPVariable_Unpack(a[11]);
+    const Tensor& v = a[12] == Py_None ? made[1] : THPVariable_Unpack(a[12]);
+    const int dtype = row_type(k);
+    const int64_t ks[2] = {k.stride(0), k.stride(1)}, vs[2] = {v.stride(0), v.stride(1)};
+    const int st = launch([&] {
+      return coverprune_cache_read(&cache, T, starts, (const int32_t*)lens.data_ptr(), B, k.data_ptr(), ks, v.data_ptr(), vs,
+                                   dtype, status, c.stream());
+    });
+    if (st != CP_OK) return PyLong_FromLong(st);
+    for (const int i : {11, 12, 13}) changed(a[i]);
+    PyObject* x = a[11] == Py_None ? THPVariable_Wrap(made[0]) : own(a[11]);
+    PyObject* y = a[12] == Py_None ? THPVariable_Wrap(made[1]) : own(a[12]);
+    PyObject* both = x && y ? PyTuple_Pack(2, x, y) : nullptr;
+    Py_XDECREF(x);
+    Py_XDECREF(y);
+    return both;
+  });
+}
+
+// (k_cache, v_cache, table, lens, weight, left, first, recent, k_block, v_block, new_lens, new_weight, kept, status)
+// -> (new_lens, new_weight, kept)
+PyObject* cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (!counted(n_args, 14)) return nullptr;
+  return entry([&]() -> PyObject* {
+    Call c;
+    const cp_cache cache = cache_of(c, a[0], a[1], a[2], Py_None, Py_None, a[8], a[9]);
+    written_cache(cache, a[0], a[1], a[8], a[9]);
+    const int64_t B = THPVariable_Unpack(a[2]).size(0), keys = cache.table_width * cache.page_size;
+    const Tensor& lens = c.dense("lens", a[3], at::kInt, {B}, false);
+    const Tensor& weight = weights_of(c, "weight", a[4], B, keys);
+    const int64_t left = integer(a[5]), first = integer(a[6]), recent = integer(a[7]);
+    if (left < 0 || first < 0 || recent < 0 || first > left || recent > left - first)
+      bad_value("of the keys that are left, " + std::to_string(left) + ", the first " + std::to_string(first) + " and the last " +
+                std::to_string(recent) + " must be parts");
+    int32_t* given_lens = c.optional<int32_t>("new_lens", a[10], at::kInt, {B}, false);
+    if (a[11] != Py_None && Call::written("new_weight", weights_of(c, "new_weight", a[11], B, keys)).sizes() != weight.sizes())
+      bad_value("new_weight must have weight's shape");
+    int32_t* given_kept = c.optional<int32_t>("kept", a[12], at::kInt, {B, left}, false);
+    int32_t* status = c.word("status", a[13]);
+
+    c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.device);
+    Tensor made_lens, made_weight, made_kept;
+    if (!given_lens) made_lens = c.like(lens);
+    if (a[11] == Py_None) made_weight = c.made(weight.sizes(), at::kFloat);
+    if (!given_kept) made_kept = c.made({B, left}, at::kInt);
+    const Tensor& to = a[11] == Py_None ? made_weight : THPVariable_Unpack(a[11]);
+    const int st = launch([&] {
+      return coverprune_cache_evict(&cache, (const int32_t*)lens.data_ptr(), B, (const float*)weight.data_ptr(), weight.stride(0),
+                                    left, first, recent, given_lens ? given_lens : (int32_t*)made_lens.data_ptr(),
+                                    (float*)to.data_ptr(), to.stride(0), to.size(1),
+                                    given_kept ? given_kept : (int32_t*)made_kept.data_ptr(), status, c.stream());
+    });
+    if (st != CP_OK) return PyLong_FromLong(st);
+    for (const int i : {0, 1, 8, 9, 10, 11, 12, 13}) changed(a[i]);
+    PyObject* x = given_lens ? own(a[10]) : THPVariable_Wrap(made_lens);
+    PyObject* y = a[11] == Py_None ? THPVariable_Wrap(made_weight) : own(a[11]);
+    PyObject* z = given_kept ? own(a[12]) : THPVariable_Wrap(made_kept);
     PyObject* all = x && y && z ? PyTuple_Pack(3, x, y, z) : nullptr;
     Py_XDECREF(x);
     Py_XDECREF(y);
@@ -418,6 +585,8 @@ PyMethodDef methods[] = {
     {"rotary", (PyCFunction)(void (*)(void))rotary, METH_FASTCALL, nullptr},
     {"cache_append", (PyCFunction)(void (*)(void))cache_append, METH_FASTCALL, nullptr},
     {"decode_attention", (PyCFunction)(void (*)(void))decode_attention, METH_FASTCALL, nullptr},
+    {"cache_read", (PyCFunction)(void (*)(void))cache_read, METH_FASTCALL, nullptr},
+    {"cache_evict", (PyCFunction)(void (*)(void))cache_evict, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "coverprune_torch", nullptr, -1, methods};
 
