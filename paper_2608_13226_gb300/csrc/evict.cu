@@ -1,13 +1,12 @@
 // Eviction from a paged cache: which keys of each sequence stay, and their rows moved up.
 //
 // k_evict_pick finds them: the weights become integers of the same order, the weight of the last key
-// that stays is found by counting digits of 8 bits from the top (radix selection), and a
-// count over the keys in their order gives each that stays its place.  Weights are read five
-// times, from L2 after the first: its latency bounds it.
+// that stays is found by counting digits of 11 bits from the top (radix selection), and a
+// count over the keys in their order gives each that stays its place.
 //
-// k_evict_move moves the rows: HBM bounds it, every row read and written once.  A block has a slice
-// of one head's rows (of keys or values) of a sequence to itself and takes them in their
-// order, some at a time: all of these are read before the first is written, and rows still
+// k_evict_move moves the rows: HBM bounds it, every row read and written once.  A block or a cluster has
+// one head's rows (of keys or values) of a sequence to itself and takes them in their
+// order, a turn of some at a time: all of these are read before the first is written, and rows still
 // to come lie behind every place that is written (the i-th row that stays comes from place i or
 // later).  So reading goes on ahead of writing without a further wait.
 #include "common.cuh"
@@ -17,9 +16,10 @@ namespace cp {
 
 // ------------------------------------------------------------------ which keys
 constexpr int kPickThreads = 1024, kPickWarps = kPickThreads / 32;
-constexpr int kMaxPick = 8;     // blocks of a cluster
-constexpr int kBins = 256;
-constexpr int kCopies = 8;      // of the counts, so that fewer lanes meet at one
+constexpr int kMaxCluster = 8;
+constexpr int kBins = 2048;        // of a digit: sign, exponent and two bits first, so that few lanes meet at one
+constexpr int kCopies = 2;         // of the counts
+constexpr int kMostHeld = 32768;   // keys that a block keeps in shared memory
 
 // Larger weights have larger numbers: a NaN 0, then -infinity to infinity, -0 as 0.
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -33,10 +33,13 @@ __device__ __forceinline__ uint32_t remote_u32(const uint32_t* p, int rank) {
   return x;
 }
 
+// A cluster of `size` blocks has a sequence.  HELD: a block's numbers fit its shared memory.
+template <bool HELD>
 __global__ void __launch_bounds__(kPickThreads) k_evict_pick(EvictArgs a, int size) {
+  extern __shared__ uint32_t s_held[];
   __shared__ uint32_t s_count[kCopies][kBins];
-  __shared__ uint32_t s_sum[kBins];           // this block's counts, for the others
-  __shared__ uint32_t s_all[kBins];           // the cluster's
+  __shared__ uint32_t s_all[kBins];           // this block's counts, for the others; then the cluster's
+  __shared__ uint32_t s_warp[kPickWarps];     // the cluster's, of a warp's bins
   __shared__ uint32_t s_above[kPickWarps], s_equal[kPickWarps];
   __shared__ uint32_t s_pair[2];              // this block's numbers above and equal
   __shared__ uint32_t s_digit, s_left;
@@ -48,73 +51,93 @@ __global__ void __launch_bounds__(kPickThreads) k_evict_pick(EvictArgs a, int si
   int32_t* kept = a.kept + (int64_t)b * a.left;
   float* to = a.new_weight ? a.new_weight + b * a.new_weight_stride : nullptr;
   const int n = min(len, a.left);
-  if (rank == 0 && threadIdx.x == 0 && a.new_lens) a.new_lens[b] = given < 0 ? given : n;
-  // what stays in any case, and what follows the last key
-  const int threads = kPickThreads * size, tid = rank * kPickThreads + threadIdx.x;
   const bool all = len <= a.left;
   const int front = all ? len : a.first, back = all ? 0 : a.recent;
-  for (int i = tid; i < front; i += threads) {
-    kept[i] = i;
-    if (to && i < a.new_weight_width) to[i] = weight[i];
-  }
-  for (int i = tid; i < back; i += threads) {
-    const int j = len - back + i, at = n - back + i;
-    kept[at] = j;
-    if (to && at < a.new_weight_width) to[at] = weight[j];
-  }
-  for (int i = n + tid; i < a.left; i += threads) kept[i] = -1;
-  if (to)
-    for (int64_t i = n + tid; i < a.new_weight_width; i += threads) to[i] = 0.0f;
+  // what stays in any case, and what follows the last key (in the end: barriers of a cluster wait for what was written)
+  auto rest = [&] {
+    const int threads = kPickThreads * size, tid = rank * kPickThreads + threadIdx.x;
+    if (tid == 0 && a.new_lens) a.new_lens[b] = given < 0 ? given : n;
+    for (int i = tid; i < front; i += threads) {
+      kept[i] = i;
+      if (to && i < a.new_weight_width) to[i] = weight[i];
+    }
+    for (int i = tid; i < back; i += threads) {
+      const int j = len - back + i, at = n - back + i;
+      kept[at] = j;
+      if (to && at < a.new_weight_width) to[at] = weight[j];
+    }
+    for (int i = n + tid; i < a.left; i += threads) kept[i] = -1;
+    if (to)
+      for (int64_t i = n + tid; i < a.new_weight_width; i += threads) to[i] = 0.0f;
+  };
   const int want = n - front - back;  // of the keys [lo, hi) between
-  if (all || want <= 0) return;       // the same in every block of the cluster
+  if (all || want <= 0) {             // the same in every block of the cluster
+    rest();
+    return;
+  }
   const int lo = a.first, hi = len - a.recent;
   // a warp's keys: [w0, w1), in the order of ranks and warps
   const int warps = kPickWarps * size, each = ((hi - lo + warps - 1) / warps + 31) / 32 * 32;
   const int w0 = (int)min((int64_t)hi, lo + (int64_t)(rank * kPickWarps + warp) * each), w1 = min(hi, w0 + each);
+  uint32_t* held = s_held + warp * each - w0;
+  if (HELD) {
+#pragma unroll 8
+    for (int j = w0 + lane; j < w1; j += 32) held[j] = order_of(weight[j]);
+  }
+  auto number = [&](int j) { return HELD ? held[j] : order_of(weight[j]); };
 
   uint32_t prefix = 0, left = (uint32_t)want;  // the digits so far; how many of the keys with them stay
-  for (int shift = 24; shift >= 0; shift -= 8) {
+#pragma unroll
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass < 2 ? 2048 : 1024;
+    const uint32_t mask = pass == 0 ? 0 : pass == 1 ? ~0u << 21 : ~0u << 10;
     for (int i = threadIdx.x; i < kCopies * kBins; i += kPickThreads) (&s_count[0][0])[i] = 0;
     __syncthreads();
-    const uint32_t mask = shift == 24 ? 0 : ~0u << (shift + 8);
+#pragma unroll 4
     for (int j = w0 + lane; j < w1; j += 32) {
-      const uint32_t u = order_of(weight[j]);
-      if ((u & mask) == prefix) atomicAdd(&s_count[warp % kCopies][u >> shift & 255], 1u);
+      const uint32_t u = number(j);
+      if ((u & mask) == prefix) atomicAdd(&s_count[warp % kCopies][u >> shift & (bins - 1)], 1u);
     }
     __syncthreads();
-    if (threadIdx.x < kBins) {
-      uint32_t x = 0;
+    // thread i has bins kBins - 1 - 2 i and the one below, so that threads go from the top
+    const int top = kBins - 1 - 2 * threadIdx.x;
+    uint32_t x = 0, y = 0;
 #pragma unroll
-      for (int i = 0; i < kCopies; ++i) x += s_count[i][threadIdx.x];
-      s_sum[threadIdx.x] = s_all[threadIdx.x] = x;
+    for (int i = 0; i < kCopies; ++i) {
+      x += s_count[i][top];
+      y += s_count[i][top - 1];
     }
     if (size > 1) {
+      s_all[top] = x;
+      s_all[top - 1] = y;
       hw_cluster_sync();
-      if (threadIdx.x < kBins) {
-        uint32_t x = 0;
-        for (int r = 0; r < size; ++r) x += remote_u32(&s_sum[threadIdx.x], r);
-        s_all[threadIdx.x] = x;
+      uint32_t xs[kMaxCluster], ys[kMaxCluster];
+#pragma unroll
+      for (int r = 0; r < kMaxCluster; ++r) {
+        xs[r] = r < size ? remote_u32(&s_all[top], r) : 0;
+        ys[r] = r < size ? remote_u32(&s_all[top - 1], r) : 0;
+      }
+      x = y = 0;
+#pragma unroll
+      for (int r = 0; r < kMaxCluster; ++r) {
+        x += xs[r];
+        y += ys[r];
       }
     }
+    // the digit in which the last key that stays falls
+    uint32_t upto = x + y;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const uint32_t z = __shfl_up_sync(~0u, upto, d);
+      if (lane >= d) upto += z;
+    }
+    if (lane == 31) s_warp[warp] = upto;
     __syncthreads();
-    if (warp == 0) {  // the digit in which the last key that stays falls: lane's 8 bins, from the top
-      uint32_t own = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) own += s_all[kBins - 1 - 8 * lane - i];
-      uint32_t upto = own;
-#pragma unroll
-      for (int d = 1; d < 32; d *= 2) {
-        const uint32_t x = __shfl_up_sync(~0u, upto, d);
-        if (lane >= d) upto += x;
-      }
-      const uint32_t before = upto - own;
-      if (before < left && upto >= left) {
-        uint32_t over = before;
-        int digit = kBins - 1 - 8 * lane;
-        while (over + s_all[digit] < left) over += s_all[digit--];
-        s_digit = (uint32_t)digit;
-        s_left = left - over;
-      }
+    const uint32_t before = __reduce_add_sync(~0u, lane < warp ? s_warp[lane] : 0) + upto - x - y;
+    if (before < left && before + x + y >= left) {
+      const bool first = before + x >= left;
+      s_digit = (uint32_t)(first ? top : top - 1);
+      s_left = left - before - (first ? 0 : x);
     }
     __syncthreads();
     prefix |= s_digit << shift;
@@ -124,8 +147,9 @@ __global__ void __launch_bounds__(kPickThreads) k_evict_pick(EvictArgs a, int si
 
   // all above `prefix` stay, and the first `left` that equal it: each warp's numbers of both
   uint32_t above = 0, equal = 0;
+#pragma unroll 4
   for (int j = w0 + lane; j < w1; j += 32) {
-    const uint32_t u = order_of(weight[j]);
+    const uint32_t u = number(j);
     above += u > prefix;
     equal += u == prefix;
   }
@@ -150,18 +174,18 @@ __global__ void __launch_bounds__(kPickThreads) k_evict_pick(EvictArgs a, int si
     }
   }
   if (size > 1) {
+    __syncwarp();
     hw_cluster_sync();
-    for (int r = 0; r < rank; ++r) {
-      before_above += remote_u32(&s_pair[0], r);
-      before_equal += remote_u32(&s_pair[1], r);
-    }
+    const uint32_t x = lane < rank ? remote_u32(&s_pair[0], lane) : 0, y = lane < rank ? remote_u32(&s_pair[1], lane) : 0;
+    before_above += __reduce_add_sync(~0u, x);
+    before_equal += __reduce_add_sync(~0u, y);
     hw_cluster_sync();  // no block ends while its numbers are read
   }
   // the place of each key that stays
+#pragma unroll 2
   for (int j0 = w0; j0 < w1; j0 += 32) {
     const int j = j0 + lane;
-    const float x = j < w1 ? weight[j] : 0.0f;
-    const uint32_t u = j < w1 ? order_of(x) : 0;
+    const uint32_t u = j < w1 ? number(j) : 0;
     const uint32_t is_above = __ballot_sync(~0u, j < w1 && u > prefix), is_equal = __ballot_sync(~0u, j < w1 && u == prefix);
     const uint32_t below = (1u << lane) - 1;
     const uint32_t equals = before_equal + __popc(is_equal & below);  // before this key
@@ -169,29 +193,109 @@ __global__ void __launch_bounds__(kPickThreads) k_evict_pick(EvictArgs a, int si
     if (stays) {
       const int at = front + (int)(before_above + __popc(is_above & below) + min(equals, left));
       kept[at] = j;
-      if (to && at < a.new_weight_width) to[at] = x;
+      if (to && at < a.new_weight_width) to[at] = weight[j];
     }
     before_above += __popc(is_above);
     before_equal += __popc(is_equal);
   }
+  rest();
 }
 
 // ------------------------------------------------------------------ their rows
 constexpr int kMoveThreads = 256;
-constexpr int kPer = 4;     // pieces of a thread in a turn
-constexpr int kStages = 4;  // turns under way
+constexpr int kPer = 4;        // pieces of a thread in a turn
+constexpr int kStages = 4;     // turns under way
+constexpr int kAhead = 2;      // turns that a trip to L2 takes, about
+constexpr int64_t kTogether = 256;  // bytes that heads side by side go together up to
+constexpr int kNotes = kStages + 1;  // turns of notes: one is written while others may still go by the oldest
 
-// Rows of one kind: codes or elements (16-byte pieces), a 4-bit row's scales (4-byte ones).
+// Rows of one kind: codes or elements, or a 4-bit row's scales.  Of a row, `parts` parts of `bytes` bytes move by
+// themselves, `part` bytes apart: a head's, or those of some heads that lie side by side.
 struct Kind {
   char *k, *v;
-  int64_t page, slot, head;  // bytes
-  int pieces;                // of a slice's row
-  int slices;
+  int64_t page, slot, part;  // bytes
+  int parts, bytes;
 };
+// Where a row comes from and where it goes, bytes; -1: it stays.
+struct Move {
+  int64_t from, to;
+};
+
+// Which rows move, found out by a thread a row: its key, then kAhead turns later the pages, and again that
+// later where it goes, so that no turn waits for a trip to L2.
+struct Moves {
+  const EvictArgs& a;
+  const Kind& kind;
+  const int32_t *kept, *table;
+  int n, stride;  // rows that stay, rows of a cluster's turn
+  int row;        // this thread's of turn 0; stride: none
+  int keys[2 * kAhead];
+  int2 pages[kAhead];
+
+  __device__ int64_t row_of(int turn) const { return row + (int64_t)turn * stride; }
+  __device__ int key_of(int turn) const { return row < stride && row_of(turn) < n ? kept[row_of(turn)] : -1; }
+  __device__ int2 pages_of(int turn, int key) const {
+    if (key < 0 || key == row_of(turn)) return make_int2(-1, -1);
+    const uint32_t size = (uint32_t)a.cache.page_size;
+    return make_int2(table[(uint32_t)key / size], table[(uint32_t)row_of(turn) / size]);
+  }
+  __device__ Move move_of(int turn, int key, int2 p) const {
+    Move m{-1, -1};
+    if (key < 0 || key == row_of(turn)) return m;
+    if (p.x >= 0 && p.x < a.cache.pages && p.y >= 0 && p.y < a.cache.pages) {
+      const uint32_t size = (uint32_t)a.cache.page_size;
+      m.from = p.x * kind.page + (int64_t)((uint32_t)key % size) * kind.slot;
+      m.to = p.y * kind.page + (int64_t)((uint32_t)row_of(turn) % size) * kind.slot;
+    } else if (a.status) {
+      set_status(a.status, CP_EINVAL);
+    }
+    return m;
+  }
+  __device__ Move at_once(int turn) const {
+    const int key = key_of(turn);
+    return move_of(turn, key, pages_of(turn, key));
+  }
+  __device__ void start(int turn) {
+#pragma unroll
+    for (int i = 0; i < 2 * kAhead; ++i) keys[i] = key_of(turn + i);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) pages[i] = pages_of(turn + i, keys[i]);
+  }
+  __device__ Move next(int turn) {
+    const Move m = move_of(turn, keys[0], pages[0]);
+#pragma unroll
+    for (int i = 0; i + 1 < kAhead; ++i) pages[i] = pages[i + 1];
+    pages[kAhead - 1] = pages_of(turn + kAhead, keys[kAhead]);
+#pragma unroll
+    for (int i = 0; i + 1 < 2 * kAhead; ++i) keys[i] = keys[i + 1];
+    keys[2 * kAhead - 1] = key_of(turn + 2 * kAhead);
+    return m;
+  }
+};
+
+// The part of a sequence's rows that a cluster of `size` blocks has: its place, how many rows stay (0: nothing moves).
+__device__ __forceinline__ int part_of(const EvictArgs& a, const Kind& kind, int size, char** base, int* b) {
+  int job = blockIdx.x / size;
+  const int part = job % kind.parts;
+  job /= kind.parts;
+  *base = (job % 2 ? kind.v : kind.k) + part * kind.part;
+  *b = job / 2;
+  const int n = min(min(max(a.lens[*b], 0), a.cache.capacity), a.left);
+  return n == 0 || a.kept[(int64_t)*b * a.left + n - 1] == n - 1 ? 0 : n;
+}
+__device__ __forceinline__ void turn_barrier(int size) {
+  // A read that has come back cannot see what is written later, so that the cluster's barrier need not order memory:
+  // doing so it would wait for every row written so far, each turn (one sequence of 200,001 keys XXX us, else XXX).
+  if (size > 1) {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+  } else {
+    __syncthreads();
+  }
+}
 template <int BYTES> struct Piece;
 template <> struct Piece<16> { using type = uint4; };
 template <> struct Piece<4> { using type = uint32_t; };
-
 template <int BYTES>
 __device__ __forceinline__ void copy_piece(uint32_t to, const void* from) {
   if (BYTES == 16)
@@ -200,119 +304,155 @@ __device__ __forceinline__ void copy_piece(uint32_t to, const void* from) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
 }
 
-// Row i of the sequence's, as a thread notes it: where it comes from and where it goes, -1: it stays.
-struct Move {
-  int64_t from, to;
-};
+// Rows that a block's threads have side by side: as many as have a thread each to find out about kPer of them.
+__host__ __device__ __forceinline__ int side_of(int pieces) {
+  return pieces < kPer ? kMoveThreads / kPer : kMoveThreads / pieces;
+}
 
+// A thread has a piece of kPer rows of every turn, which it copies to a slot of its own and takes from there.
 template <int BYTES>
-__global__ void __launch_bounds__(kMoveThreads) k_evict_move(EvictArgs a, Kind kind) {
+__global__ void __launch_bounds__(kMoveThreads) k_evict_rows(EvictArgs a, Kind kind, int size) {
   using P = typename Piece<BYTES>::type;
-  extern __shared__ __align__(16) char smem[];  // kStages turns of pieces, a thread's its own, and notes
+  extern __shared__ __align__(16) char smem[];  // kStages turns of pieces, and notes of kNotes
   wait_for_stream();
-  const Cache& ch = a.cache;
-  int job = blockIdx.x;
-  const int slice = job % kind.slices;
-  job /= kind.slices;
-  const int head = job % ch.heads;
-  job /= ch.heads;
-  char* base = job % 2 ? kind.v : kind.k;
-  const int b = job / 2;
-  const int n = min(min(max(a.lens[b], 0), ch.capacity), a.left);
-  const int32_t* kept = a.kept + (int64_t)b * a.left;
-  if (n == 0 || kept[n - 1] == n - 1) return;  // nothing moves
-  base += head * kind.head + slice * kind.pieces * BYTES;
-  const int32_t* table = ch.table + b * ch.table_stride;
-
-  P* ring = reinterpret_cast<P*>(smem);
-  const int rows = kMoveThreads * kPer / kind.pieces;  // of a turn
+  char* base;
+  int b;
+  const int n = part_of(a, kind, size, &base, &b);
+  if (n == 0) return;  // in every block of the cluster
+  const int pieces = kind.bytes / BYTES, side = side_of(pieces), rows = side * kPer;  // rows side by side, and of a turn
+  const int piece = threadIdx.x % pieces, r0 = threadIdx.x / pieces;
+  const bool works = r0 < side;
+  const int rank = size > 1 ? (int)cluster_ctarank() : 0;
+  Moves moves{a, kind, a.kept + (int64_t)b * a.left, a.cache.table + b * a.cache.table_stride, n, rows * size,
+              (int)threadIdx.x < rows ? rank * rows + (int)threadIdx.x : rows * size};
+  const int turns = (n + rows * size - 1) / (rows * size);
+  P* ring = reinterpret_cast<P*>(smem) + threadIdx.x;
   Move* notes = reinterpret_cast<Move*>(smem + kStages * kPer * kMoveThreads * sizeof(P));
-  const int turns = (n + rows - 1) / rows;
-  auto page_of = [&](int key) { return table[(uint32_t)key / (uint32_t)ch.page_size]; };
-  auto issue = [&](int turn) {
-    if (turn < turns) {
-      Move* to = notes + turn % kStages * rows;
-      for (int r = threadIdx.x; r < rows; r += kMoveThreads) {
-        const int i = turn * rows + r;
-        Move m{-1, -1};
-        if (i < n) {
-          const int j = kept[i];
-          if (j != i) {
-            const int p = page_of(j), q = page_of(i);
-            if (p >= 0 && p < ch.pages && q >= 0 && q < ch.pages) {
-              m.from = p * kind.page + (int64_t)((uint32_t)j % (uint32_t)ch.page_size) * kind.slot;
-              m.to = q * kind.page + (int64_t)((uint32_t)i % (uint32_t)ch.page_size) * kind.slot;
-            } else if (a.status) {
-              set_status(a.status, CP_EINVAL);
-            }
-          }
-        }
-        to[r] = m;
-      }
-    }
-    __syncthreads();
-    if (turn < turns) {
-      const Move* of = notes + turn % kStages * rows;
+  base += piece * BYTES;
+  auto note = [&](int turn, const Move& m) {
+    notes[turn % kNotes * kMoveThreads + threadIdx.x] = m;
+  };
+  auto load = [&](int turn) {
+    if (turn < turns && works) {
+      const Move* of = notes + turn % kNotes * kMoveThreads + r0;
+      P* to = ring + turn % kStages * (kPer * kMoveThreads);
 #pragma unroll
       for (int k = 0; k < kPer; ++k) {
-        const int x = k * kMoveThreads + threadIdx.x, r = x / kind.pieces;
-        if (r < rows && of[r].from >= 0)
-          copy_piece<BYTES>(smem_addr(ring + (turn % kStages * kPer + k) * kMoveThreads + threadIdx.x),
-                            base + of[r].from + (x - r * kind.pieces) * BYTES);
+        const int64_t from = of[k * side].from;
+        if (from >= 0) copy_piece<BYTES>(smem_addr(to + k * kMoveThreads), base + from);
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  for (int t = 0; t < kStages - 1; ++t) issue(t);
+  for (int t = 0; t < kStages - 1; ++t) note(t, moves.at_once(t));
+  moves.start(kStages - 1);
+  __syncthreads();
+  for (int t = 0; t < kStages - 1; ++t) load(t);
   for (int t = 0; t < turns; ++t) {
+    note(t + kStages - 1, moves.next(t + kStages - 1));
     asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-    __syncthreads();  // turn t has been read by every thread; its rows may be written over
-    const Move* of = notes + t % kStages * rows;
+    turn_barrier(size);  // turn t has been read by every thread of the cluster; its rows may be written over
+    if (works) {
+      const Move* of = notes + t % kNotes * kMoveThreads + r0;
+      const P* from = ring + t % kStages * (kPer * kMoveThreads);
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      const int x = k * kMoveThreads + threadIdx.x, r = x / kind.pieces;
-      if (r < rows && of[r].to >= 0)
-        *reinterpret_cast<P*>(base + of[r].to + (x - r * kind.pieces) * BYTES) =
-            ring[(t % kStages * kPer + k) * kMoveThreads + threadIdx.x];
+      for (int k = 0; k < kPer; ++k) {
+        const int64_t to = of[k * side].to;
+        if (to >= 0) *reinterpret_cast<P*>(base + to) = from[k * kMoveThreads];
+      }
     }
-    issue(t + kStages - 1);
+    load(t + kStages - 1);
   }
 }
 
 template <int BYTES>
-static int move(const EvictArgs& a, Kind kind, int row_pieces, int sms, cudaStream_t s) {
-  // whole rows of a head, or where that gives few blocks a part of 4 pieces at least
-  kind.slices = 1;
-  const int64_t jobs = (int64_t)a.B * 2 * a.cache.heads;
-  while (BYTES == 16 && jobs * kind.slices < 2 * sms && row_pieces % (2 * kind.slices) == 0 &&
-         row_pieces / (2 * kind.slices) >= 4)
-    kind.slices *= 2;
-  kind.pieces = row_pieces / kind.slices;
-  const int rows = kMoveThreads * kPer / kind.pieces;
-  const size_t smem = kStages * (kPer * kMoveThreads * BYTES + rows * sizeof(Move));
+constexpr size_t smem_of() {
+  return kMoveThreads * (kStages * kPer * (size_t)BYTES + kNotes * sizeof(Move));
+}
+
+// The largest clusters of which `jobs` run at the same time (a cluster waits for its own blocks only, so more would be
+// right as well, one after another): 1 to `most` blocks.  What the device holds is asked once a device and size.
+template <int BYTES>
+static int cluster_size(int64_t jobs, int most, int* size) {
   static std::atomic<uint64_t> allowed{0};
-  CP_TRY_STATUS(allow_smem_once((const void*)k_evict_move<BYTES>, 200 * 1024, "evict: shared memory", &allowed));
-  if (jobs * kind.slices > 0x7FFFFFFF) return CP_EUNSUPPORTED;
-  return cuda_status(launch_early(k_evict_move<BYTES>, dim3((unsigned)(jobs * kind.slices)), kMoveThreads, smem, s, a, kind),
-                     "evict: move");
+  static std::atomic<int> held[64][4];  // a device's clusters of 2^i blocks, and one more (0: not asked yet)
+  CP_TRY_STATUS(allow_smem_once((const void*)k_evict_rows<BYTES>, smem_of<BYTES>(), "evict: shared memory", &allowed));
+  int dev = 0;
+  CP_TRY_STATUS(cuda_status(cudaGetDevice(&dev), "evict: device"));
+  for (*size = most; *size > 1; *size /= 2) {
+    std::atomic<int>& known = held[dev & 63][*size >= 8 ? 3 : *size / 2];
+    int n = known.load(std::memory_order_relaxed) - 1;
+    if (n < 0) {
+      cudaLaunchAttribute with{};
+      with.id = cudaLaunchAttributeClusterDimension;
+      with.val.clusterDim = {(unsigned)*size, 1, 1};
+      cudaLaunchConfig_t cfg{};
+      cfg.gridDim = dim3((unsigned)*size);
+      cfg.blockDim = dim3(kMoveThreads);
+      cfg.dynamicSmemBytes = smem_of<BYTES>();
+      cfg.attrs = &with;
+      cfg.numAttrs = 1;
+      if (cudaOccupancyMaxActiveClusters(&n, k_evict_rows<BYTES>, &cfg) != cudaSuccess) {
+        (void)cudaGetLastError();  // a size that the device does not take
+        n = 0;
+      }
+      known.store(n + 1, std::memory_order_relaxed);
+    }
+    if (jobs <= n) break;
+  }
+  return CP_OK;
+}
+
+// Rows of `bytes` bytes a head, heads `head` bytes apart, moved up.
+template <int BYTES>
+static int move_by(const EvictArgs& a, Kind kind, cudaStream_t s) {
+  const int rows = side_of(kind.bytes / BYTES) * kPer;
+  const int64_t jobs = (int64_t)a.B * 2 * kind.parts;
+  // clusters where there are few heads and sequences, if they get some turns
+  int most = kMaxCluster, size = 1;
+  while (most > 1 && (int64_t)rows * most * 4 > a.left) most /= 2;
+  CP_TRY_STATUS(cluster_size<BYTES>(jobs, most, &size));
+  if (jobs * size > 0x7FFFFFFF) return CP_EUNSUPPORTED;
+  return cuda_status(launch_early_cluster(k_evict_rows<BYTES>, dim3((unsigned)(jobs * size)), kMoveThreads, smem_of<BYTES>(), s, size, a,
+                                          kind, size),
+                     "evict: rows");
+}
+static int move(const EvictArgs& a, Kind kind, int64_t head, int bytes, cudaStream_t s) {
+  int group = 1;  // heads that lie side by side go together
+  const int heads = a.cache.heads;
+  if (head == bytes)
+    for (int g = 2; g <= heads && (int64_t)g * bytes <= kTogether; ++g)
+      if (heads % g == 0) group = g;
+  kind.parts = heads / group;
+  kind.part = head * group;
+  kind.bytes = bytes * group;
+  const uint64_t any = (uint64_t)kind.k | (uint64_t)kind.v | (uint64_t)kind.page | (uint64_t)kind.slot | (uint64_t)kind.part |
+                       (uint64_t)kind.bytes;
+  return any % 16 == 0 ? move_by<16>(a, kind, s) : move_by<4>(a, kind, s);
 }
 
 int launch_cache_evict(const EvictArgs& a, int cache_dtype, cudaStream_t s) {
   DeviceInfo di;
   CP_TRY_STATUS(device_info(&di));
   const Cache& ch = a.cache;
+  // as many blocks of a sequence as the device has room for, of 8192 keys at least
   int size = 1;
-  while (size < kMaxPick && (int64_t)size * 16384 < ch.capacity) size *= 2;
+  while (size < kMaxCluster && (int64_t)a.B * size * 2 <= di.sm_count && (int64_t)size * 16384 <= ch.capacity) size *= 2;
   if ((int64_t)a.B * size > 0x7FFFFFFF) return CP_EUNSUPPORTED;
-  CP_TRY_STATUS(cuda_status(launch_early_cluster(k_evict_pick, dim3((unsigned)(a.B * size)), kPickThreads, 0, s, size, a, size),
+  const int64_t most = (((int64_t)ch.capacity + kPickWarps * size - 1) / (kPickWarps * size) + 31) / 32 * 32 * kPickWarps;
+  static std::atomic<uint64_t> allowed{0};
+  CP_TRY_STATUS(allow_smem_once((const void*)k_evict_pick<true>, kMostHeld * 4, "evict: shared memory", &allowed));
+  const dim3 grid((unsigned)(a.B * size));
+  CP_TRY_STATUS(cuda_status(most <= kMostHeld
+                                ? launch_early_cluster(k_evict_pick<true>, grid, kPickThreads, (size_t)most * 4, s, size, a, size)
+                                : launch_early_cluster(k_evict_pick<false>, grid, kPickThreads, 0, s, size, a, size),
                             "evict: pick"));
   if (a.left == 0 || ch.capacity <= a.left) return CP_OK;  // no row moves
-  Kind kind{(char*)ch.k, (char*)ch.v, cache_bytes(cache_dtype, ch.page_stride), cache_bytes(cache_dtype, ch.slot_stride),
-            cache_bytes(cache_dtype, ch.head_stride), 0, 1};
-  CP_TRY_STATUS(move<16>(a, kind, (int)cache_bytes(cache_dtype, ch.D) / 16, di.sm_count, s));
+  Kind kind{(char*)ch.k, (char*)ch.v, cache_bytes(cache_dtype, ch.page_stride), cache_bytes(cache_dtype, ch.slot_stride)};
+  CP_TRY_STATUS(move(a, kind, cache_bytes(cache_dtype, ch.head_stride), (int)cache_bytes(cache_dtype, ch.D), s));
   if (cache_dtype != CP_I4) return CP_OK;
-  kind = Kind{(char*)ch.k_block, (char*)ch.v_block, ch.block_page, ch.block_slot, ch.block_head, 0, 1};
-  return move<4>(a, kind, block_bytes(ch.D) / 4, di.sm_count, s);
+  kind = Kind{(char*)ch.k_block, (char*)ch.v_block, ch.block_page, ch.block_slot};
+  return move(a, kind, ch.block_head, block_bytes(ch.D), s);
 }
 
 }  // namespace cp

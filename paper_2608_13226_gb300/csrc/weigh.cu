@@ -11,11 +11,10 @@
 namespace cp {
 
 constexpr int kWeighThreads = 256;
-constexpr int kWeighKeys = 256;  // of a block's turn
-constexpr int kSide = 4;         // turns of a warp whose loads are under way together
+constexpr int kSide = 4;  // keys of a lane whose loads are under way together
 
 __global__ void __launch_bounds__(kWeighThreads) k_weigh(DecodeArgs a, float* weight, int64_t weight_stride, int lanes,
-                                                         int64_t chunks, int64_t items) {
+                                                         int chunk, int64_t chunks, int64_t items) {
   wait_for_stream();
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int keys = 32 / lanes, mine = lane / lanes, head = lane % lanes;  // keys side by side, this lane's
@@ -23,9 +22,9 @@ __global__ void __launch_bounds__(kWeighThreads) k_weigh(DecodeArgs a, float* we
     const int b = (int)(item / chunks);
     const int len = min(max(a.lens[b], 0), a.cache.capacity);
     const int first = a.window > 0 && a.window < len ? len - (int)a.window : 0;
-    const int64_t begin = first + (item - b * chunks) * kWeighKeys;
+    const int64_t begin = first + (item - b * chunks) * chunk;
     if (begin >= len) continue;
-    const int end = (int)min((int64_t)len, begin + kWeighKeys);
+    const int end = (int)min((int64_t)len, begin + chunk);
     const float* scores = a.scores + (int64_t)b * a.cache.capacity * a.Hq;
     const float* lse = a.lse + (int64_t)b * a.Hq;
     float* to = weight + b * weight_stride;
@@ -61,13 +60,16 @@ int launch_weigh(const DecodeArgs& a, float* weight, int64_t weight_stride, cuda
   int lanes = 1;
   while (lanes < 32 && lanes < a.Hq) lanes *= 2;
   const int64_t most = a.window > 0 && a.window < a.cache.capacity ? a.window : a.cache.capacity;
-  const int64_t chunks = (most + kWeighKeys - 1) / kWeighKeys, items = chunks * a.B;
-  if (items == 0) return CP_OK;
   DeviceInfo di;
   CP_TRY_STATUS(device_info(&di));
   const int64_t room = (int64_t)di.sm_count * 8;
+  // a block's keys: those that its lanes take at once, and more only where there are many
+  int chunk = kWeighThreads / lanes * kSide;
+  while (chunk < 4096 && (most + chunk - 1) / chunk * a.B > 4 * room) chunk *= 2;
+  const int64_t chunks = (most + chunk - 1) / chunk, items = chunks * a.B;
+  if (items == 0) return CP_OK;
   return cuda_status(launch_early(k_weigh, dim3((unsigned)(items < room ? items : room)), kWeighThreads, 0, s, a, weight,
-                                  weight_stride, lanes, chunks, items),
+                                  weight_stride, lanes, chunk, chunks, items),
                      "weigh");
 }
 
