@@ -604,7 +604,8 @@ int coverprune_decode_attention(const void* q, const int64_t* q_stride, int dtyp
  *   weight    device float32, rows of B sequences weight_stride >= 0 elements apart, which
  *             must not overlap; each holds the keys that the table's row does
  *   ws        coverprune_decode_weigh_workspace_size bytes: the attention's, and a float for
- *             every query head and key that the table's row holds (B * Hq * keys)
+ *             every query head and key that the table's row holds (queries of a kv head
+ *             counted to a power of two)
  */
 int coverprune_decode_weigh_workspace_size(int64_t B, int64_t Hq, const cp_cache* cache,
                                            size_t* bytes);

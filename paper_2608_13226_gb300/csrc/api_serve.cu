@@ -212,7 +212,9 @@ static Room room_of(int64_t B, int64_t Hq, const Cache& c, int cache_dtype) {
   r.decode = decode_ws_bytes(Hq, c.heads, c.D, cache_dtype);
   r.lse = up(r.decode);
   r.scores = r.lse + up(4 * (size_t)B * (size_t)Hq);
-  r.all = r.scores + 4 * (size_t)B * (size_t)Hq * (size_t)c.capacity;
+  int64_t cols = 0, pitch = 0;
+  score_shape(cache_dtype, Hq, c.heads, &cols, &pitch);
+  r.all = r.scores + 4 * (size_t)(B * cols) * (size_t)pitch * (size_t)c.capacity;
   return r;
 }
 
@@ -273,8 +275,12 @@ static int attend(const void* q, const int64_t* q_stride, int dtype, int64_t B, 
   if (!weights) return launch_decode(a, cache->dtype, (cudaStream_t)stream);
   if (!lse) a.lse = (float*)((char*)ws + room.lse);
   a.scores = (float*)((char*)ws + room.scores);
+  int64_t cols = 0, pitch = 0;
+  score_shape(cache->dtype, Hq, a.cache.heads, &cols, &pitch);
+  a.score_cols = (int)cols;
+  a.score_pitch = (int)pitch;
   CP_TRY_STATUS(launch_decode_scores(a, cache->dtype, (cudaStream_t)stream));
-  return launch_weigh(a, weight, weight_stride, (cudaStream_t)stream);
+  return launch_weigh(a, cache->dtype, weight, weight_stride, (cudaStream_t)stream);
 }
 
 int coverprune_decode_attention(const void* q, const int64_t* q_stride, int dtype, int64_t B,

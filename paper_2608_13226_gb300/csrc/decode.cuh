@@ -87,8 +87,12 @@ struct Shape {
   // 8-bit sequences 101 us with two, 115 with three; four 125.
   // Short sequences: three blocks, as registers allow, as there is more to begin
   // than to copy.
-  static constexpr int fit = (SHORT ? 64 : 100) * 1024 / (kWarps * tile);
-  static constexpr int least = SHORT ? 2 : 3;
+  // 4 bits: as many blocks as registers allow.
+  static constexpr int blocks = CT != CP_I4 ? (SHORT ? 3 : 2) : DP == 256 || (DP == 128 && QT == 16) ? 2 : DP == 128 || QT == 16 ? 3 : 4;
+  static constexpr int bound = CT == CP_I4 ? blocks : 0;  // of the registers
+  static constexpr int room = CT != CP_I4 ? (SHORT ? 64 : 100) : blocks == 4 ? 50 : blocks == 3 ? 68 : 112;  // KB of a block
+  static constexpr int fit = room * 1024 / (kWarps * tile);
+  static constexpr int least = SHORT || CT == CP_I4 ? 2 : 3;
   static constexpr int stages = fit < least ? least : fit > 8 ? 8 : fit;
   static constexpr int ring = kWarps * stages * tile;
   // float32 queries, the block's or each warp's, and each warp's weights of a tile
@@ -98,7 +102,8 @@ struct Shape {
   // (Registers allow them but for some spills, 4 to 84 bytes a thread: 16 queries and heads of
   // 256 (255 registers), an 8-bit cache's 8 queries and heads of 64, float32's of 4 queries and
   // heads of 128 and 256 and, for short sequences, of 8 and 128.)
-  static constexpr int per_sm = SHORT && smem <= 70 * 1024 ? 3 : smem <= 110 * 1024 ? 2 : 1;
+  static constexpr int per_sm = CT == CP_I4 ? blocks
+                                : SHORT && smem <= 70 * 1024 ? 3 : smem <= 110 * 1024 ? 2 : 1;
   static constexpr int part = QT * (DP + 2);  // floats of a partial result
   // What beginning and merging a segment costs, in units of 64 keys: about 3 us, in
   // which a block takes 72 KB.
@@ -127,13 +132,22 @@ __host__ __device__ constexpr int swizzle(int r) {
   return CT == CP_F32 ? (r & 1) << 2 : CPR >= 8 ? r & 7 : CPR == 4 ? (r >> 1) & 3 : (r >> 2) & 1;
 }
 
+// WHOLE: L2 fetches the 128 bytes around it, which rows of a head of at least as many fill.
+template <bool WHOLE>
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  if (WHOLE)
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+template <bool WHOLE>
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
   const int n = there ? 16 : 0;  // 0: nothing is read, zeros are written
-  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n)
-               : "memory");
+  if (WHOLE)
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n)
+                 : "memory");
+  else
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
 // 4, 8 or 16 bytes, or as many zeros.
 template <int BYTES>
@@ -177,21 +191,13 @@ __device__ __forceinline__ void e4m3_f16x2(uint32_t x, uint32_t* lo, uint32_t* h
       : "=r"(*lo), "=r"(*hi)
       : "r"(x));
 }
-// Four bits of each half of x, as 2 x 2 of them come: numbers n + 8 in bits 0-3 (LOW) or
-// 4-7 of a half become n in float16.  1024 and the bits are a float16 as they are
-// (with bits 4-7 1024 and 16 times the number); what is taken off again is exact.
-template <bool LOW>
-__device__ __forceinline__ uint32_t i4_f16x2(uint32_t x) {
+// Numbers n + 8 in bits 4-7 of each half of x become n s in float16: 64 + n + 8 is a float16 as its bits
+// are, and (72 + n) s - 72 s rounds once to what float16 holds exactly; `off` is -72 s.
+__device__ __forceinline__ uint32_t i4_f16x2(uint32_t x, uint32_t s, uint32_t off) {
   uint32_t y;
-  if (LOW) {
-    asm("{\n\t.reg .b32 a;\n\tlop3.b32 a, %1, 0x000F000F, 0x64006400, 0xEA;\n\tadd.rn.f16x2 %0, a, %2;\n\t}"
-        : "=r"(y)
-        : "r"(x), "r"(0xE408E408u));  // -1032
-  } else {
-    asm("{\n\t.reg .b32 a;\n\tlop3.b32 a, %1, 0x00F000F0, 0x64006400, 0xEA;\n\tfma.rn.f16x2 %0, a, %2, %3;\n\t}"
-        : "=r"(y)
-        : "r"(x), "r"(0x2C002C00u), "r"(0xD480D480u));  // 1 / 16, -72
-  }
+  asm("{\n\t.reg .b32 a;\n\tlop3.b32 a, %1, 0x00F000F0, 0x54005400, 0xEA;\n\tfma.rn.f16x2 %0, a, %2, %3;\n\t}"
+      : "=r"(y)
+      : "r"(x), "r"(s), "r"(off));
   return y;
 }
 __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
@@ -199,6 +205,7 @@ __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
   asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
   return y;
 }
+constexpr uint32_t kOff = 0xD480D480u;  // -72
 // Bytes of a and b picked by `sel`, as two 8-bit elements, in float16 (exact).
 __device__ __forceinline__ uint32_t scales_f16x2(uint32_t a, uint32_t b, uint32_t sel) {
   uint32_t y;
@@ -321,19 +328,28 @@ struct Keys {
 };
 
 // Where the scores of a segment's tiles go, for those who add the weights up by them:
-// `to` is key 0's and query h0's, pitch floats a key; `keys` the tile's, -1 for none.
+// `to` is key 0's, pitch floats a key (1 or even); `keys` the tile's, -1 for none.
 struct NoScores {
   static constexpr bool on = false;
 };
 struct Scores {
   static constexpr bool on = true;
   float* to;
-  int64_t pitch;
-  int nq;
+  int pitch;
   const int* keys;
   __device__ __forceinline__ void put(int row, uint32_t valid, int query, float s) const {
     const int key = keys[row];  // one on a bad page weighs nothing
-    if (key >= 0 && query < nq) to[key * pitch + query] = valid >> row & 1 ? s : -INFINITY;
+    if (key >= 0 && query < pitch) to[(int64_t)key * pitch + query] = valid >> row & 1 ? s : -INFINITY;
+  }
+  // Of an even query and the next: 8 keys and 4 such pairs of a warp fill whole sectors.
+  __device__ __forceinline__ void put(int row, uint32_t valid, int query, float s0, float s1) const {
+    const int key = keys[row];
+    if (key < 0 || query >= pitch) return;
+    if (!(valid >> row & 1)) s0 = s1 = -INFINITY;
+    if (pitch == 1)
+      to[key] = s0;
+    else
+      *reinterpret_cast<float2*>(to + (int64_t)key * pitch + query) = make_float2(s0, s1);
   }
 };
 
@@ -487,10 +503,12 @@ struct Math {
         uint32_t lo[SW], hi[SW];
         load_words<SW>(lo, at + 2 * S::tk * S::row + (16 * h + g) * S::sb);
         load_words<SW>(hi, at + 2 * S::tk * S::row + (16 * h + g + 8) * S::sb);
+        if (half_word >= 0) {
 #pragma unroll
-        for (int w = 0; w < SW; ++w) {
-          lo[w] &= w == half_word ? 0xFFFFu : ~0u;
-          hi[w] &= w == half_word ? 0xFFFFu : ~0u;
+          for (int w = 0; w < SW; ++w) {
+            lo[w] &= w == half_word ? 0xFFFFu : ~0u;
+            hi[w] &= w == half_word ? 0xFFFFu : ~0u;
+          }
         }
 #pragma unroll
         for (int c = 0; c < DP / 32; c += 2) {
@@ -500,11 +518,12 @@ struct Math {
           for (int j = 0; j < 2; ++j) {
             const uint32_t sel = (2 * j + t / 2) * 0x11;
             const uint32_t s0 = scales_f16x2(lo[c / 2], 0, sel), s1 = scales_f16x2(hi[c / 2], 0, sel);
+            const uint32_t o0 = mul_f16x2(s0, kOff), o1 = mul_f16x2(s1, kOff);
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
               const uint32_t w0 = x[2 * j] >> 8 * m, w1 = x[2 * j + 1] >> 8 * m;
-              const uint32_t a0 = mul_f16x2(i4_f16x2<true>(w0), s0), a1 = mul_f16x2(i4_f16x2<true>(w1), s1);
-              const uint32_t a2 = mul_f16x2(i4_f16x2<false>(w0), s0), a3 = mul_f16x2(i4_f16x2<false>(w1), s1);
+              const uint32_t a0 = i4_f16x2(w0 * 16, s0, o0), a1 = i4_f16x2(w1 * 16, s1, o1);
+              const uint32_t a2 = i4_f16x2(w0, s0, o0), a3 = i4_f16x2(w1, s1, o1);
 #pragma unroll
               for (int n = 0; n < NT; ++n)
                 mma_f16_16816(s[h][n], a0, a1, a2, a3, q[n][2 * (c + j) + m][0], q[n][2 * (c + j) + m][1]);
@@ -519,8 +538,8 @@ struct Math {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            scores.put(16 * h + g + 8 * (i / 2), valid, 8 * n + 2 * t + (i & 1), s[h][n][i] * sc[n][i & 1]);
+          for (int i = 0; i < 4; i += 2)
+            scores.put(16 * h + g + 4 * i, valid, 8 * n + 2 * t, s[h][n][i] * sc[n][0], s[h][n][i + 1] * sc[n][1]);
     }
     const bool full = valid == S::all;
     if (!full) {
@@ -645,11 +664,12 @@ struct Math {
             const uint32_t sel = 0x40 + (2 * j + g / 4) * 0x11;
             const uint32_t s0 = scales_f16x2(ks[0][c / 2], ks[1][c / 2], sel);
             const uint32_t s1 = scales_f16x2(ks[2][c / 2], ks[3][c / 2], sel);
+            const uint32_t o0 = mul_f16x2(s0, kOff), o1 = mul_f16x2(s1, kOff);
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
               const uint32_t w0 = x[2 * j] >> 8 * m, w1 = x[2 * j + 1] >> 8 * m;
-              const uint32_t a0 = mul_f16x2(i4_f16x2<true>(w0), s0), a1 = mul_f16x2(i4_f16x2<false>(w0), s0);
-              const uint32_t a2 = mul_f16x2(i4_f16x2<true>(w1), s1), a3 = mul_f16x2(i4_f16x2<false>(w1), s1);
+              const uint32_t a0 = i4_f16x2(w0 * 16, s0, o0), a1 = i4_f16x2(w0, s0, o0);
+              const uint32_t a2 = i4_f16x2(w1 * 16, s1, o1), a3 = i4_f16x2(w1, s1, o1);
 #pragma unroll
               for (int n = 0; n < NT; ++n) mma_f16_16816(o[n][2 * (c + j) + m], a0, a1, a2, a3, p[h][n][0], p[h][n][1]);
             }
@@ -884,9 +904,10 @@ struct Math<CP_F32, DP, QT, SHORT> {
 // its ring into `math`.
 template <int CT, int DP, int QT, bool SHORT, bool SCORES, typename K>
 __device__ __forceinline__ void math_of_keys(const DecodeArgs& a, const Rows& rows, K& keys, const int32_t* table, int lo,
-                                             int hi, int hk, int b, int h0, int nq, int warp, int lane, uint32_t ring,
+                                             int hi, int hk, int b, int col, int h0, int nq, int warp, int lane, uint32_t ring,
                                              uint32_t* s_valid, int* s_keys, char* extra, Math<CT, DP, QT, SHORT>& math) {
   using S = Shape<CT, DP, QT, SHORT>;
+  constexpr bool kWhole = true;
   const Cache& ch = a.cache;
   const int chunks = (int)cache_bytes(CT, ch.D) / 16;  // of a row that is there
   const char* kp = (const char*)ch.k + cache_bytes(CT, (int64_t)hk * ch.head_stride);
@@ -951,15 +972,15 @@ __device__ __forceinline__ void math_of_keys(const DecodeArgs& a, const Rows& ro
       };
       if (valid == S::all && chunks == S::cpr) {
         each([&](uint32_t at, uint64_t off, int, int) {
-          copy16(at, kp + off);
-          copy16(at + S::tk * S::row, vp + off);
+          copy16<kWhole>(at, kp + off);
+          copy16<kWhole>(at + S::tk * S::row, vp + off);
         });
       } else {
         each([&](uint32_t at, uint64_t off, int r, int c) {
           const bool there = valid >> r & 1;
           if (c < chunks) {
-            copy16(at, kp + (there ? off : 0), there);
-            copy16(at + S::tk * S::row, vp + (there ? off : 0), there);
+            copy16<kWhole>(at, kp + (there ? off : 0), there);
+            copy16<kWhole>(at + S::tk * S::row, vp + (there ? off : 0), there);
           }
         });
       }
@@ -981,7 +1002,8 @@ __device__ __forceinline__ void math_of_keys(const DecodeArgs& a, const Rows& ro
     const int slot = i % S::stages;
     if constexpr (SCORES)
       math.tile(ring + slot * S::tile, s_valid[slot], extra, warp, lane,
-                Scores{a.scores + (int64_t)b * ch.capacity * a.Hq + h0, a.Hq, nq, s_keys + slot * S::tk});
+                Scores{a.scores + ((int64_t)b * a.score_cols + col) * ch.capacity * a.score_pitch, a.score_pitch,
+                       s_keys + slot * S::tk});
     else
       math.tile(ring + slot * S::tile, s_valid[slot], extra, warp, lane, NoScores{});
   }
@@ -1027,7 +1049,7 @@ __device__ __forceinline__ float remote(const float* p, int rank) {
 }
 
 template <int CT, int DP, int QT, bool SCORES>
-__global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, int unit, int tiles, float* parts,
+__global__ void __launch_bounds__(kThreads, Shape<CT, DP, QT>::bound) k_decode(DecodeArgs a, Rows rows, int unit, int tiles, float* parts,
                                                      Begin* begins, int by_column) {
   using S = Shape<CT, DP, QT>;
   using Row = typename Type<CT>::Row;
@@ -1107,7 +1129,7 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
       const int nq = min(QT, G - col % tiles * QT);
       const int lo = first + k0 * unit, hi = (int)min((int64_t)len, first + (int64_t)k1 * unit);
       Math<CT, DP, QT, false> math;
-      math_of_keys<CT, DP, QT, false, SCORES>(a, rows, keys, table, lo, hi, hk, b, h0, nq, warp, lane, ring, s_valid[warp],
+      math_of_keys<CT, DP, QT, false, SCORES>(a, rows, keys, table, lo, hi, hk, b, col, h0, nq, warp, lane, ring, s_valid[warp],
                                               s_keys[warp], extra, math);
       math.finish(s_m[warp], s_l[warp]);
       copy_wait<0>();
@@ -1161,7 +1183,7 @@ __global__ void __launch_bounds__(kThreads) k_decode(DecodeArgs a, Rows rows, in
 // parts from one another's shared memory, an element a thread, so that no launch has
 // to follow.
 template <int CT, int DP, int QT, bool SCORES>
-__global__ void __launch_bounds__(kThreads) k_decode_cluster(DecodeArgs a, Rows rows, int tiles, int size) {
+__global__ void __launch_bounds__(kThreads, Shape<CT, DP, QT>::bound) k_decode_cluster(DecodeArgs a, Rows rows, int tiles, int size) {
   using S = Shape<CT, DP, QT>;
   using Row = typename Type<CT>::Row;
   extern __shared__ __align__(1024) char smem[];
@@ -1190,7 +1212,7 @@ __global__ void __launch_bounds__(kThreads) k_decode_cluster(DecodeArgs a, Rows 
   keys.queue = s_queue[warp];
   keys.keep = a.keep ? a.keep + (int64_t)b * a.keep_stride : nullptr;
   Math<CT, DP, QT, false> math;
-  math_of_keys<CT, DP, QT, false, SCORES>(a, rows, keys, ch.table + (int64_t)b * ch.table_stride, lo, hi, hk, b, h0, nq, warp,
+  math_of_keys<CT, DP, QT, false, SCORES>(a, rows, keys, ch.table + (int64_t)b * ch.table_stride, lo, hi, hk, b, col, h0, nq, warp,
                                           lane, smem_addr(smem) + warp * S::stages * S::tile, s_valid[warp], s_keys[warp],
                                           smem + S::ring, math);
   math.finish(s_m[warp], s_l[warp]);
@@ -1242,7 +1264,7 @@ __global__ void __launch_bounds__(kThreads) k_decode_cluster(DecodeArgs a, Rows 
 // Many short sequences: a warp takes a query tile alone, and then another, so that one's beginning (table, keys, queries: three trips
 // to memory) runs beside the others' and nothing is merged.
 template <int CT, int DP, int QT, bool SCORES>
-__global__ void __launch_bounds__(kThreads) k_decode_short(DecodeArgs a, Rows rows, int tiles, int64_t columns) {
+__global__ void __launch_bounds__(kThreads, Shape<CT, DP, QT, true>::bound) k_decode_short(DecodeArgs a, Rows rows, int tiles, int64_t columns) {
   using S = Shape<CT, DP, QT, true>;
   using Row = typename Type<CT>::Row;
   extern __shared__ __align__(1024) char smem[];
@@ -1265,7 +1287,7 @@ __global__ void __launch_bounds__(kThreads) k_decode_short(DecodeArgs a, Rows ro
     keys_of(a, b, &first, &len);
     keys.keep = a.keep ? a.keep + (int64_t)b * a.keep_stride : nullptr;
     Math<CT, DP, QT, true> math;
-    math_of_keys<CT, DP, QT, true, SCORES>(a, rows, keys, ch.table + (int64_t)b * ch.table_stride, first, len, hk, b, h0, nq,
+    math_of_keys<CT, DP, QT, true, SCORES>(a, rows, keys, ch.table + (int64_t)b * ch.table_stride, first, len, hk, b, col, h0, nq,
                                            warp, lane, ring, s_valid[warp], s_keys[warp], smem + S::ring, math);
     copy_wait<0>();
     math.write(

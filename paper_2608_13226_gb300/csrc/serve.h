@@ -112,7 +112,10 @@ struct DecodeArgs {
   float* lse;
   void* ws;
   int32_t* status;
-  float* scores;  // [B, capacity, Hq], in units of log 2: only where weights are added up
+  // Only where weights are added up: scores in units of log 2, [B, score_cols, capacity, score_pitch],
+  // a column for every query tile of a sequence (see score_shape).
+  float* scores;
+  int score_cols, score_pitch;
 };
 // A launch that may begin before what precedes it on the stream has ended: its
 // blocks come to the SMs and wait there (wait_for_stream, first of all), so that its
@@ -153,13 +156,20 @@ int launch_decode_bf16_scores(const DecodeArgs& a, cudaStream_t s);
 int launch_decode_e4m3_scores(const DecodeArgs& a, cudaStream_t s);
 int launch_decode_f32_scores(const DecodeArgs& a, cudaStream_t s);
 int launch_decode_i4_scores(const DecodeArgs& a, cudaStream_t s);
-int launch_weigh(const DecodeArgs& a, float* weight, int64_t weight_stride, cudaStream_t s);
+int launch_weigh(const DecodeArgs& a, int cache_dtype, float* weight, int64_t weight_stride, cudaStream_t s);
 
 // Query heads that one pass of the attention takes for groups of G, the width that a
 // head is laid out for, and the most blocks of a launch: what the workspace goes by.
 inline int decode_pass(int cache_dtype, int64_t G) {
   if (cache_dtype == CP_F32) return G <= 4 ? 4 : 8;
   return G <= 8 ? 8 : 16;
+}
+// Columns of a sequence's scores (query tiles) and floats of a key in one: a tile's queries, to a power of two.
+inline void score_shape(int cache_dtype, int64_t Hq, int64_t heads, int64_t* cols, int64_t* pitch) {
+  const int64_t G = Hq / heads, pass = decode_pass(cache_dtype, G);
+  *pitch = 1;
+  while (*pitch < G && *pitch < pass) *pitch *= 2;
+  *cols = heads * ((G + pass - 1) / pass);
 }
 inline int decode_width(int64_t D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 constexpr int kDecodeBlocks = 1024;

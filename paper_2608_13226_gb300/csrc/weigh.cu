@@ -2,75 +2,98 @@
 // sum_h exp(s_hj - lse_h) for the visible keys j, from the scores that the attention left
 // (decode.cuh, in units of log 2).
 //
-// HBM or L2 bounds it: 4 bytes a key and query head, 8 a key.  A key's scores lie side by
-// side, so lanes take its query heads (32 at most, of fewer heads several keys side by
-// side) and add them up among themselves: the same order every time, no atomics.
+// HBM or L2 bounds it: 4 bytes a key and query head, 8 a key.  A thread has a key and goes over the columns of
+// scores, whose keys lie side by side: loads are whole lines, and heads are added up in
+// the same order every time, without atomics.
 #include "common.cuh"
 #include "rope.cuh"
 
 namespace cp {
 
-constexpr int kWeighThreads = 256;
-constexpr int kSide = 4;  // keys of a lane whose loads are under way together
+constexpr int kWeighThreads = 128;
 
-__global__ void __launch_bounds__(kWeighThreads) k_weigh(DecodeArgs a, float* weight, int64_t weight_stride, int lanes,
-                                                         int chunk, int64_t chunks, int64_t items) {
-  wait_for_stream();
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int keys = 32 / lanes, mine = lane / lanes, head = lane % lanes;  // keys side by side, this lane's
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int b = (int)(item / chunks);
-    const int len = min(max(a.lens[b], 0), a.cache.capacity);
-    const int first = a.window > 0 && a.window < len ? len - (int)a.window : 0;
-    const int64_t begin = first + (item - b * chunks) * chunk;
-    if (begin >= len) continue;
-    const int end = (int)min((int64_t)len, begin + chunk);
-    const float* scores = a.scores + (int64_t)b * a.cache.capacity * a.Hq;
-    const float* lse = a.lse + (int64_t)b * a.Hq;
-    float* to = weight + b * weight_stride;
-    for (int j0 = (int)begin + warp * keys * kSide; j0 < end; j0 += kWeighThreads / 32 * keys * kSide) {
-      float sum[kSide];
-      bool seen[kSide];
+// P floats of a key in a column.
+template <int P>
+__device__ __forceinline__ void load_scores(const float* p, float (&s)[P]) {
+  if constexpr (P == 1) {
+    s[0] = *p;
+  } else if constexpr (P == 2) {
+    const float2 x = *reinterpret_cast<const float2*>(p);
+    s[0] = x.x;
+    s[1] = x.y;
+  } else {
 #pragma unroll
-      for (int i = 0; i < kSide; ++i) {
-        const int j = j0 + i * keys + mine;
-        seen[i] = j < end && (!a.keep || a.keep[b * a.keep_stride + j]);
-        sum[i] = 0.0f;
-      }
-      for (int h = head; h < a.Hq; h += lanes) {
-        const float top = lse[h];
-        float s[kSide];
-#pragma unroll
-        for (int i = 0; i < kSide; ++i)
-          s[i] = seen[i] ? scores[(int64_t)(j0 + i * keys + mine) * a.Hq + h] : -INFINITY;
-#pragma unroll
-        for (int i = 0; i < kSide; ++i)  // (a head whose scores are all -infinity has no weights)
-          if (top != -INFINITY) sum[i] += exp2f(fmaf(-top, 1.4426950408889634f, s[i]));
-      }
-#pragma unroll
-      for (int i = 0; i < kSide; ++i) {
-        for (int d = 1; d < lanes; d *= 2) sum[i] += __shfl_xor_sync(~0u, sum[i], d);
-        if (seen[i] && head == 0) to[j0 + i * keys + mine] += sum[i];
-      }
+    for (int i = 0; i < P; i += 4) {
+      const float4 x = *reinterpret_cast<const float4*>(p + i);
+      s[i] = x.x;
+      s[i + 1] = x.y;
+      s[i + 2] = x.z;
+      s[i + 3] = x.w;
     }
   }
 }
 
-int launch_weigh(const DecodeArgs& a, float* weight, int64_t weight_stride, cudaStream_t s) {
-  int lanes = 1;
-  while (lanes < 32 && lanes < a.Hq) lanes *= 2;
+template <int P>
+__global__ void __launch_bounds__(kWeighThreads) k_weigh(DecodeArgs a, float* weight, int64_t weight_stride, int tiles, int pass,
+                                                         int64_t chunks, int64_t items) {
+  constexpr int kSide = P >= 8 ? 4 : 8;  // columns whose loads are under way together
+  wait_for_stream();
+  const int G = a.Hq / a.cache.heads;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int b = (int)(item / chunks);
+    const int len = min(max(a.lens[b], 0), a.cache.capacity);
+    const int first = a.window > 0 && a.window < len ? len - (int)a.window : 0;
+    const int64_t j = first + (item - b * chunks) * kWeighThreads + threadIdx.x;
+    if (j >= len || (a.keep && !a.keep[b * a.keep_stride + j])) continue;
+    float* to = weight + b * weight_stride + j;
+    const float before = *to;
+    const float* lse = a.lse + (int64_t)b * a.Hq;
+    const int64_t apart = (int64_t)a.cache.capacity * P;
+    const float* scores = a.scores + b * a.score_cols * apart + j * P;
+    float sum = 0.0f;
+    for (int c0 = 0; c0 < a.score_cols; c0 += kSide) {
+      float s[kSide][P];
+#pragma unroll
+      for (int i = 0; i < kSide; ++i)
+        if (c0 + i < a.score_cols) load_scores<P>(scores + (c0 + i) * apart, s[i]);
+#pragma unroll
+      for (int i = 0; i < kSide; ++i) {
+        const int c = c0 + i, hk = c / tiles, tile = c - hk * tiles;
+        if (c < a.score_cols) {
+          const int n = min(pass, G - tile * pass);
+          const float* of = lse + hk * G + tile * pass;
+#pragma unroll
+          for (int q = 0; q < P; ++q)
+            if (q < n) {
+              const float top = of[q];  // (a head whose scores are all -infinity has no weights)
+              sum += top == -INFINITY ? 0.0f : exp2f(fmaf(-top, 1.4426950408889634f, s[i][q]));
+            }
+        }
+      }
+    }
+    *to = before + sum;
+  }
+}
+
+int launch_weigh(const DecodeArgs& a, int cache_dtype, float* weight, int64_t weight_stride, cudaStream_t s) {
   const int64_t most = a.window > 0 && a.window < a.cache.capacity ? a.window : a.cache.capacity;
+  const int64_t chunks = (most + kWeighThreads - 1) / kWeighThreads, items = chunks * a.B;
+  if (items == 0) return CP_OK;
+  const int pass = decode_pass(cache_dtype, a.Hq / a.cache.heads), tiles = a.score_cols / a.cache.heads;
   DeviceInfo di;
   CP_TRY_STATUS(device_info(&di));
-  const int64_t room = (int64_t)di.sm_count * 8;
-  // a block's keys: those that its lanes take at once, and more only where there are many
-  int chunk = kWeighThreads / lanes * kSide;
-  while (chunk < 4096 && (most + chunk - 1) / chunk * a.B > 4 * room) chunk *= 2;
-  const int64_t chunks = (most + chunk - 1) / chunk, items = chunks * a.B;
-  if (items == 0) return CP_OK;
-  return cuda_status(launch_early(k_weigh, dim3((unsigned)(items < room ? items : room)), kWeighThreads, 0, s, a, weight,
-                                  weight_stride, lanes, chunk, chunks, items),
-                     "weigh");
+  const int64_t room = (int64_t)di.sm_count * 16;
+  const dim3 grid((unsigned)(items < room ? items : room));
+  auto launch = [&](auto kernel) {
+    return cuda_status(launch_early(kernel, grid, kWeighThreads, 0, s, a, weight, weight_stride, tiles, pass, chunks, items), "weigh");
+  };
+  switch (a.score_pitch) {
+    case 1: return launch(k_weigh<1>);
+    case 2: return launch(k_weigh<2>);
+    case 4: return launch(k_weigh<4>);
+    case 8: return launch(k_weigh<8>);
+    default: return launch(k_weigh<16>);
+  }
 }
 
 }  // namespace cp
