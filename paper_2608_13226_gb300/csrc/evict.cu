@@ -35,11 +35,11 @@ __device__ __forceinline__ uint32_t remote_u32(const uint32_t* p, int rank) {
 
 // A cluster of `size` blocks has a sequence.  HELD: a block's numbers fit its shared memory.
 template <bool HELD>
-__global__ void __launch_bounds__(kPickThreads) k_evict_pick(EvictArgs a, int size) {
+__global__ void __launch_bounds__(kPickThreads, 1) k_evict_pick(EvictArgs a, int size) {
   extern __shared__ uint32_t s_held[];
   __shared__ uint32_t s_count[kCopies][kBins];
-  __shared__ uint32_t s_all[kBins];           // this block's counts, for the others; then the cluster's
-  __shared__ uint32_t s_warp[kPickWarps];     // the cluster's, of a warp's bins
+  __shared__ uint32_t s_all[kBins], s_warp[kPickWarps];  // this block's counts, for the others: of a bin, of a warp's 64
+  __shared__ uint32_t s_total[kPickWarps];    // the cluster's of a warp's
   __shared__ uint32_t s_above[kPickWarps], s_equal[kPickWarps];
   __shared__ uint32_t s_pair[2];              // this block's numbers above and equal
   __shared__ uint32_t s_digit, s_left;
@@ -80,10 +80,6 @@ __global__ void __launch_bounds__(kPickThreads) k_evict_pick(EvictArgs a, int si
   const int warps = kPickWarps * size, each = ((hi - lo + warps - 1) / warps + 31) / 32 * 32;
   const int w0 = (int)min((int64_t)hi, lo + (int64_t)(rank * kPickWarps + warp) * each), w1 = min(hi, w0 + each);
   uint32_t* held = s_held + warp * each - w0;
-  if (HELD) {
-#pragma unroll 8
-    for (int j = w0 + lane; j < w1; j += 32) held[j] = order_of(weight[j]);
-  }
   auto number = [&](int j) { return HELD ? held[j] : order_of(weight[j]); };
 
   uint32_t prefix = 0, left = (uint32_t)want;  // the digits so far; how many of the keys with them stay
@@ -93,13 +89,15 @@ __global__ void __launch_bounds__(kPickThreads) k_evict_pick(EvictArgs a, int si
     const uint32_t mask = pass == 0 ? 0 : pass == 1 ? ~0u << 21 : ~0u << 10;
     for (int i = threadIdx.x; i < kCopies * kBins; i += kPickThreads) (&s_count[0][0])[i] = 0;
     __syncthreads();
-#pragma unroll 4
+#pragma unroll 8
     for (int j = w0 + lane; j < w1; j += 32) {
-      const uint32_t u = number(j);
+      const uint32_t u = pass == 0 ? order_of(weight[j]) : number(j);
+      if (HELD && pass == 0) held[j] = u;
       if ((u & mask) == prefix) atomicAdd(&s_count[warp % kCopies][u >> shift & (bins - 1)], 1u);
     }
     __syncthreads();
-    // thread i has bins kBins - 1 - 2 i and the one below, so that threads go from the top
+    // The digit in which the last key that stays falls.  A thread has bins kBins - 1 - 2 i and the one below, so that
+    // they go from the top; first by what the 64 bins of a warp hold, then within the one warp's.
     const int top = kBins - 1 - 2 * threadIdx.x;
     uint32_t x = 0, y = 0;
 #pragma unroll
@@ -107,37 +105,45 @@ __global__ void __launch_bounds__(kPickThreads) k_evict_pick(EvictArgs a, int si
       x += s_count[i][top];
       y += s_count[i][top - 1];
     }
+    uint32_t total = __reduce_add_sync(~0u, x + y);
     if (size > 1) {
       s_all[top] = x;
       s_all[top - 1] = y;
+      if (lane == 0) s_warp[warp] = total;
+      __syncwarp();
       hw_cluster_sync();
-      uint32_t xs[kMaxCluster], ys[kMaxCluster];
-#pragma unroll
-      for (int r = 0; r < kMaxCluster; ++r) {
-        xs[r] = r < size ? remote_u32(&s_all[top], r) : 0;
-        ys[r] = r < size ? remote_u32(&s_all[top - 1], r) : 0;
-      }
-      x = y = 0;
-#pragma unroll
-      for (int r = 0; r < kMaxCluster; ++r) {
-        x += xs[r];
-        y += ys[r];
-      }
+      total = __reduce_add_sync(~0u, lane < size ? remote_u32(&s_warp[warp], lane) : 0);
     }
-    // the digit in which the last key that stays falls
-    uint32_t upto = x + y;
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-      const uint32_t z = __shfl_up_sync(~0u, upto, d);
-      if (lane >= d) upto += z;
-    }
-    if (lane == 31) s_warp[warp] = upto;
+    if (lane == 0) s_total[warp] = total;
     __syncthreads();
-    const uint32_t before = __reduce_add_sync(~0u, lane < warp ? s_warp[lane] : 0) + upto - x - y;
-    if (before < left && before + x + y >= left) {
-      const bool first = before + x >= left;
-      s_digit = (uint32_t)(first ? top : top - 1);
-      s_left = left - before - (first ? 0 : x);
+    const uint32_t above = __reduce_add_sync(~0u, lane < warp ? s_total[lane] : 0);
+    if (above < left && above + total >= left) {  // one warp
+      if (size > 1) {
+        uint32_t xs[kMaxCluster], ys[kMaxCluster];
+#pragma unroll
+        for (int r = 0; r < kMaxCluster; ++r) {
+          xs[r] = r < size ? remote_u32(&s_all[top], r) : 0;
+          ys[r] = r < size ? remote_u32(&s_all[top - 1], r) : 0;
+        }
+        x = y = 0;
+#pragma unroll
+        for (int r = 0; r < kMaxCluster; ++r) {
+          x += xs[r];
+          y += ys[r];
+        }
+      }
+      uint32_t upto = x + y;
+#pragma unroll
+      for (int d = 1; d < 32; d *= 2) {
+        const uint32_t z = __shfl_up_sync(~0u, upto, d);
+        if (lane >= d) upto += z;
+      }
+      const uint32_t before = above + upto - x - y;
+      if (before < left && before + x + y >= left) {  // one lane
+        const bool first = before + x >= left;
+        s_digit = (uint32_t)(first ? top : top - 1);
+        s_left = left - before - (first ? 0 : x);
+      }
     }
     __syncthreads();
     prefix |= s_digit << shift;
@@ -147,7 +153,7 @@ __global__ void __launch_bounds__(kPickThreads) k_evict_pick(EvictArgs a, int si
 
   // all above `prefix` stay, and the first `left` that equal it: each warp's numbers of both
   uint32_t above = 0, equal = 0;
-#pragma unroll 4
+#pragma unroll 8
   for (int j = w0 + lane; j < w1; j += 32) {
     const uint32_t u = number(j);
     above += u > prefix;
@@ -181,22 +187,32 @@ __global__ void __launch_bounds__(kPickThreads) k_evict_pick(EvictArgs a, int si
     before_equal += __reduce_add_sync(~0u, y);
     hw_cluster_sync();  // no block ends while its numbers are read
   }
-  // the place of each key that stays
-#pragma unroll 2
-  for (int j0 = w0; j0 < w1; j0 += 32) {
-    const int j = j0 + lane;
-    const uint32_t u = j < w1 ? number(j) : 0;
-    const uint32_t is_above = __ballot_sync(~0u, j < w1 && u > prefix), is_equal = __ballot_sync(~0u, j < w1 && u == prefix);
-    const uint32_t below = (1u << lane) - 1;
-    const uint32_t equals = before_equal + __popc(is_equal & below);  // before this key
-    const bool stays = (is_above >> lane & 1) || ((is_equal >> lane & 1) && equals < left);
-    if (stays) {
-      const int at = front + (int)(before_above + __popc(is_above & below) + min(equals, left));
-      kept[at] = j;
-      if (to && at < a.new_weight_width) to[at] = weight[j];
+  // the place of each key that stays, some groups of 32 at a time, whose loads are under way together
+  constexpr int kGroups = 4;
+  const uint32_t below = (1u << lane) - 1;
+  for (int j0 = w0; j0 < w1; j0 += 32 * kGroups) {
+    uint32_t u[kGroups];
+    float x[kGroups];
+#pragma unroll
+    for (int i = 0; i < kGroups; ++i) {
+      const int j = j0 + 32 * i + lane;
+      u[i] = j < w1 ? number(j) : 0;
+      x[i] = j < w1 && to ? weight[j] : 0.0f;
     }
-    before_above += __popc(is_above);
-    before_equal += __popc(is_equal);
+#pragma unroll
+    for (int i = 0; i < kGroups; ++i) {
+      const int j = j0 + 32 * i + lane;
+      const uint32_t is_above = __ballot_sync(~0u, j < w1 && u[i] > prefix), is_equal = __ballot_sync(~0u, j < w1 && u[i] == prefix);
+      const uint32_t equals = before_equal + __popc(is_equal & below);  // before this key
+      const bool stays = (is_above >> lane & 1) || ((is_equal >> lane & 1) && equals < left);
+      if (stays) {
+        const int at = front + (int)(before_above + __popc(is_above & below) + min(equals, left));
+        kept[at] = j;
+        if (to && at < a.new_weight_width) to[at] = x[i];
+      }
+      before_above += __popc(is_above);
+      before_equal += __popc(is_equal);
+    }
   }
   rest();
 }
@@ -209,12 +225,12 @@ constexpr int kAhead = 2;      // turns that a trip to L2 takes, about
 constexpr int64_t kTogether = 256;  // bytes that heads side by side go together up to
 constexpr int kNotes = kStages + 1;  // turns of notes: one is written while others may still go by the oldest
 
-// Rows of one kind: codes or elements, or a 4-bit row's scales.  Of a row, `parts` parts of `bytes` bytes move by
-// themselves, `part` bytes apart: a head's, or those of some heads that lie side by side.
+// Rows of one kind: codes or elements, or a 4-bit row's scales.  Of a row, `parts` x `split` pieces of `bytes` bytes
+// move by themselves: `split` of a head, or one of some heads that lie side by side, and those `part` bytes apart.
 struct Kind {
   char *k, *v;
   int64_t page, slot, part;  // bytes
-  int parts, bytes;
+  int parts, split, bytes;
 };
 // Where a row comes from and where it goes, bytes; -1: it stays.
 struct Move {
@@ -276,9 +292,9 @@ struct Moves {
 // The part of a sequence's rows that a cluster of `size` blocks has: its place, how many rows stay (0: nothing moves).
 __device__ __forceinline__ int part_of(const EvictArgs& a, const Kind& kind, int size, char** base, int* b) {
   int job = blockIdx.x / size;
-  const int part = job % kind.parts;
-  job /= kind.parts;
-  *base = (job % 2 ? kind.v : kind.k) + part * kind.part;
+  const int part = job % (kind.parts * kind.split);
+  job /= kind.parts * kind.split;
+  *base = (job % 2 ? kind.v : kind.k) + part / kind.split * kind.part + part % kind.split * kind.bytes;
   *b = job / 2;
   const int n = min(min(max(a.lens[*b], 0), a.cache.capacity), a.left);
   return n == 0 || a.kept[(int64_t)*b * a.left + n - 1] == n - 1 ? 0 : n;
@@ -407,7 +423,7 @@ static int cluster_size(int64_t jobs, int most, int* size) {
 template <int BYTES>
 static int move_by(const EvictArgs& a, Kind kind, cudaStream_t s) {
   const int rows = side_of(kind.bytes / BYTES) * kPer;
-  const int64_t jobs = (int64_t)a.B * 2 * kind.parts;
+  const int64_t jobs = (int64_t)a.B * 2 * kind.parts * kind.split;
   // clusters where there are few heads and sequences, if they get some turns
   int most = kMaxCluster, size = 1;
   while (most > 1 && (int64_t)rows * most * 4 > a.left) most /= 2;
@@ -417,7 +433,7 @@ static int move_by(const EvictArgs& a, Kind kind, cudaStream_t s) {
                                           kind, size),
                      "evict: rows");
 }
-static int move(const EvictArgs& a, Kind kind, int64_t head, int bytes, cudaStream_t s) {
+static int move(const EvictArgs& a, Kind kind, int64_t head, int bytes, int sms, cudaStream_t s) {
   int group = 1;  // heads that lie side by side go together
   const int heads = a.cache.heads;
   if (head == bytes)
@@ -426,18 +442,26 @@ static int move(const EvictArgs& a, Kind kind, int64_t head, int bytes, cudaStre
   kind.parts = heads / group;
   kind.part = head * group;
   kind.bytes = bytes * group;
+  kind.split = 1;
   const uint64_t any = (uint64_t)kind.k | (uint64_t)kind.v | (uint64_t)kind.page | (uint64_t)kind.slot | (uint64_t)kind.part |
                        (uint64_t)kind.bytes;
-  return any % 16 == 0 ? move_by<16>(a, kind, s) : move_by<4>(a, kind, s);
+  if (any % 16 != 0) return move_by<4>(a, kind, s);
+  // where clusters of whole rows would not fill the device, halves of them
+  // (one sequence of 200,001 keys and 8 heads of 128 198 us, whole rows 275; 32 sequences 54.6, whole 50.1)
+  while ((int64_t)a.B * 2 * kind.parts * kind.split * kMaxCluster < 2 * sms && kind.bytes >= 256 && kind.bytes % 32 == 0) {
+    kind.bytes /= 2;
+    kind.split *= 2;
+  }
+  return move_by<16>(a, kind, s);
 }
 
 int launch_cache_evict(const EvictArgs& a, int cache_dtype, cudaStream_t s) {
   DeviceInfo di;
   CP_TRY_STATUS(device_info(&di));
   const Cache& ch = a.cache;
-  // as many blocks of a sequence as the device has room for, of 8192 keys at least
+  // as many blocks of a sequence as the device has room for, of 4096 keys at least
   int size = 1;
-  while (size < kMaxCluster && (int64_t)a.B * size * 2 <= di.sm_count && (int64_t)size * 16384 <= ch.capacity) size *= 2;
+  while (size < kMaxCluster && (int64_t)a.B * size * 2 <= di.sm_count && (int64_t)size * 8192 <= ch.capacity) size *= 2;
   if ((int64_t)a.B * size > 0x7FFFFFFF) return CP_EUNSUPPORTED;
   const int64_t most = (((int64_t)ch.capacity + kPickWarps * size - 1) / (kPickWarps * size) + 31) / 32 * 32 * kPickWarps;
   static std::atomic<uint64_t> allowed{0};
@@ -449,10 +473,10 @@ int launch_cache_evict(const EvictArgs& a, int cache_dtype, cudaStream_t s) {
                             "evict: pick"));
   if (a.left == 0 || ch.capacity <= a.left) return CP_OK;  // no row moves
   Kind kind{(char*)ch.k, (char*)ch.v, cache_bytes(cache_dtype, ch.page_stride), cache_bytes(cache_dtype, ch.slot_stride)};
-  CP_TRY_STATUS(move(a, kind, cache_bytes(cache_dtype, ch.head_stride), (int)cache_bytes(cache_dtype, ch.D), s));
+  CP_TRY_STATUS(move(a, kind, cache_bytes(cache_dtype, ch.head_stride), (int)cache_bytes(cache_dtype, ch.D), di.sm_count, s));
   if (cache_dtype != CP_I4) return CP_OK;
   kind = Kind{(char*)ch.k_block, (char*)ch.v_block, ch.block_page, ch.block_slot};
-  return move(a, kind, ch.block_head, block_bytes(ch.D), s);
+  return move(a, kind, ch.block_head, block_bytes(ch.D), di.sm_count, s);
 }
 
 }  // namespace cp

@@ -7,14 +7,14 @@
 // is looked up once a token, angles are computed once a token for all its heads.
 // Nothing is staged: with 16 components (32 bytes of bfloat16, with their pairs' other halves 64)
 // under way a thread, full SMs have 64 KB and more on their way.
-#include <type_traits>
+#include <cuda_fp16.h>
 
 #include "rope.cuh"
 
 namespace cp {
 
 constexpr int kThreads = 256;
-constexpr int kTokens = 8;  // of a block's turn, at most
+constexpr int kTokens = 64;  // of a block's turn, at most
 
 // Where a token's rows lie: elements into the cache and bytes into its scales; there < 0: they are not.
 struct Place {
@@ -22,30 +22,48 @@ struct Place {
   int there;  // 0; -1: no place, -2: padding
 };
 
-// The place of token t, of which sequence it is (starts NULL: t itself) and at which key.
-__device__ __forceinline__ Place place_of(const Cache& ch, const int32_t* starts, const int32_t* lens, int B, int64_t t,
-                                          int32_t* status, int64_t* key) {
-  Place x{0, 0, -2};
-  *key = 0;
-  const int b = starts ? sequence_of(starts, B, t) : (int)t;
-  const int64_t i = starts && b < B ? t - starts[b] : 0;  // below 0: before the first sequence's rows
-  if (b >= B || i < 0) return x;
-  const int len = lens[b];
-  const int64_t slot = (int64_t)len + i;
-  *key = slot;
-  int page = -1;
-  if (len >= 0 && slot >= 0 && slot < ch.capacity)
-    page = ch.table[b * ch.table_stride + (uint32_t)slot / (uint32_t)ch.page_size];
-  if (page >= 0 && page < ch.pages) {
-    const int64_t r = (uint32_t)slot % (uint32_t)ch.page_size;
-    x.row = page * ch.page_stride + r * ch.slot_stride;
-    x.block = page * ch.block_page + r * ch.block_slot;
-    x.there = 0;
-  } else {
-    x.there = -1;
-    if (status) set_status(status, CP_EINVAL);
+// How many of starts[1..B] are <= t, by a warp: few of them are counted at once, of many a binary search ends.
+__device__ __forceinline__ int sequence_by_warp(const int32_t* starts, int B, int64_t t) {
+  if (B > 256) return sequence_of(starts, B, t);
+  int n = 0;
+  for (int b = threadIdx.x % 32; b < B; b += 32) n += starts[1 + b] <= t;
+  return __reduce_add_sync(~0u, n);
+}
+
+// The places of tokens t0 to t0 + n - 1, a thread each (whole warps come here): which sequence each is of (starts NULL:
+// it by itself), at which key.
+__device__ __forceinline__ void find_places(const Cache& ch, const int32_t* starts, const int32_t* lens, int B, int64_t t0, int n,
+                                            int32_t* status, Place* places, int64_t* keys) {
+  const int i0 = threadIdx.x / 32 * 32;  // the warp's first
+  if (i0 >= n) return;
+  const int64_t t = t0 + threadIdx.x;
+  int b = (int)min(t, (int64_t)B);
+  if (starts) {  // between those of the warp's first token and of its last
+    const int lo = sequence_by_warp(starts, B, t0 + i0), hi = sequence_by_warp(starts, B, t0 + min(i0 + 31, n - 1));
+    b = lo + sequence_of(starts + lo, hi - lo, t);
   }
-  return x;
+  if ((int)threadIdx.x >= n) return;
+  Place x{0, 0, -2};
+  int64_t key = 0;
+  const int64_t at = starts && b < B ? t - starts[b] : 0;  // below 0: before the first sequence's rows
+  if (b < B && at >= 0) {
+    const int len = lens[b];
+    key = (int64_t)len + at;
+    int page = -1;
+    if (len >= 0 && key >= 0 && key < ch.capacity)
+      page = ch.table[b * ch.table_stride + (uint32_t)key / (uint32_t)ch.page_size];
+    if (page >= 0 && page < ch.pages) {
+      const int64_t r = (uint32_t)key % (uint32_t)ch.page_size;
+      x.row = page * ch.page_stride + r * ch.slot_stride;
+      x.block = page * ch.block_page + r * ch.block_slot;
+      x.there = 0;
+    } else {
+      x.there = -1;
+      if (status) set_status(status, CP_EINVAL);
+    }
+  }
+  places[threadIdx.x] = x;
+  if (keys) keys[threadIdx.x] = key;
 }
 
 // N consecutive elements as float32; VEC: aligned to 16 bytes.
@@ -112,19 +130,49 @@ __device__ __forceinline__ void store_row(__nv_bfloat16* p, const float (&x)[N])
   }
 }
 
+__device__ __forceinline__ float max_nan(float a, float b) {  // a NaN is above all numbers
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+
 // 16 components to 4 bits each and their scale's byte.
 __device__ __forceinline__ uint2 to_fours(const float (&x)[16], float head, uint8_t* scale) {
-  uint32_t top = 0;  // the largest size, a NaN above all numbers
+  float top = fabsf(x[0]);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-  const __nv_fp8_e4m3 s = from_f32<__nv_fp8_e4m3>(__fdiv_rn(__uint_as_float(top), __fmul_rn(7.0f, head)));
+  for (int i = 1; i < 16; ++i) top = max_nan(top, fabsf(x[i]));
+  const float want = __fdiv_rn(top, __fmul_rn(7.0f, head));
+  const __nv_fp8_e4m3 s = from_f32<__nv_fp8_e4m3>(want);
   *scale = s.__x;
   const float step = __fmul_rn((float)s, head);
   uint32_t w[2] = {};
+  // Quotients rounded as a division rounds them: q = x r with the rounded reciprocal r, and q + (x - q step) r, whose
+  // rounding is the quotient's wherever step's significand is not all ones (Markstein 1990, Computation of elementary
+  // functions on the IBM RISC System/6000, theorem 7).  That within ranges where nothing under- or overflows and
+  // the scale is a normal number, which no quotient is above 7 (1 + 2^-4) of.  Else divisions.  38,400 tokens of
+  // 2 x 4 heads of 128 XXX us, by divisions alone XXX.
+  if (want >= 0.015625f && want <= 448.0f && step > 1e-15f && step < 1e15f && (__float_as_uint(step) & 0x7FFFFF) != 0x7FFFFF) {
+    const float r = __frcp_rn(step);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const float n = step == 0.0f ? 0.0f : fminf(fmaxf(rintf(__fdiv_rn(x[i], step)), -7.0f), 7.0f);
-    w[i / 8] |= (uint32_t)((int)n + 8) << 4 * (i % 8);
+    for (int h = 0; h < 2; ++h) {
+      // a number's bits end in n + 8 once 1.5 2^23 + 8 is added, which rounds it to nearest even; what is
+      // above them adds up to a constant
+      uint32_t all = 0, above = 0;
+#pragma unroll
+      for (int i = 7; i >= 0; --i) {
+        const float q = __fmul_rn(x[8 * h + i], r);
+        const float y = __fmaf_rn(__fmaf_rn(-q, step, x[8 * h + i]), r, q);
+        all = all * 16 + __float_as_uint(__fadd_rn(y, 12582920.0f));
+        above = above * 16 + 0x4B400000u;
+      }
+      w[h] = all - above;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float n = step == 0.0f ? 0.0f : fminf(fmaxf(rintf(__fdiv_rn(x[i], step)), -7.0f), 7.0f);
+      w[i / 8] |= (uint32_t)((int)n + 8) << 4 * (i % 8);
+    }
   }
   return make_uint2(w[0], w[1]);
 }
@@ -144,7 +192,7 @@ __device__ __forceinline__ void turn_neighbours(const Rope& r, int d0, float (&x
 
 // A piece of a query's row turned: 8 pairs of the half layout, or 16 components side by side, so that no
 // thread reads what another writes where the result goes to the query's own place.
-__device__ __forceinline__ int query_pieces(const Rope& r, int D) {
+__host__ __device__ __forceinline__ int query_pieces(const Rope& r, int D) {
   return r.interleaved ? D / 16 : (r.half + 7) / 8 + (D - 2 * r.half + 15) / 16;
 }
 template <typename T, bool VEC>
@@ -191,15 +239,45 @@ __device__ __forceinline__ void turn_query(const Rope& r, int D, const T* in, T*
   store_row<VEC>(out + d0, x);
 }
 
-// VEC: rows come in vectors of 16 bytes, and so do the halves that pairs lie apart.
+// How a block's threads share the items of one kind of a turn's tokens: `width` of a token's `count` side by side, and so
+// `side` tokens; items beyond `width` in further rounds.  What an item is, a thread works out once a round.
+struct Share {
+  int count, per_row;  // items of a token, of a row
+  int width, side;
+};
+static Share share_of(int rows, int per_row) {
+  Share x;
+  x.count = rows * per_row;
+  x.per_row = per_row;
+  const int rounds = x.count < 1 ? 1 : (x.count + kThreads - 1) / kThreads;
+  x.width = x.count < 1 ? 1 : (x.count + rounds - 1) / rounds;
+  x.side = kThreads / x.width;
+  return x;
+}
+// Tokens of a turn: few go to as many blocks as there is room for.
+static int tokens_of(int64_t T, int sms) {
+  int n = 1;
+  while (n < kTokens && n * (int64_t)sms * 4 < T) n *= 2;
+  return n;
+}
+// body(item, first, step): the tokens first, first + step, .. of an item.
+template <typename F>
+__device__ __forceinline__ void each_item(const Share& x, F body) {
+  const int first = threadIdx.x / x.width;
+  if (first < x.side)
+    for (int r = threadIdx.x - first * x.width; r < x.count; r += x.width) body(r, first, x.side);
+}
+
+// VEC: rows come in vectors of 16 bytes.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads) k_append_fours(AppendArgs a, int tokens) {
+__global__ void __launch_bounds__(kThreads, 4) k_append_fours(AppendArgs a, int tokens, Share queries, Share rows, Divisor by_half) {
   extern __shared__ __align__(16) char smem[];  // angles and speeds
   __shared__ Place s_place[kTokens];
   __shared__ int64_t s_pos[kTokens];
   wait_for_stream();
   const Cache& ch = a.cache;
   const int half = a.rope.half;
+  const bool even = half % 8 == 0;  // a pair's halves are vectors apart
   float* s_cos = reinterpret_cast<float*>(smem);
   float* s_sin = s_cos + tokens * half;
   uint64_t* s_turns = reinterpret_cast<uint64_t*>(s_sin + tokens * half);
@@ -210,82 +288,90 @@ __global__ void __launch_bounds__(kThreads) k_append_fours(AppendArgs a, int tok
       a.new_lens[b] = len < 0 ? len : (int32_t)min(n, (int64_t)ch.capacity);
     }
   for (int i = threadIdx.x; i < half; i += kThreads) s_turns[i] = rope_turns(a.rope.inv_freq[i]);
-  const int per_query = a.q.heads > 0 ? query_pieces(a.rope, ch.D) : 1, per_row = ch.D / 16;
-  const int queries = a.q.heads * per_query, per_token = queries + 2 * ch.heads * per_row;
   for (int64_t t0 = (int64_t)blockIdx.x * tokens; t0 < a.T; t0 += (int64_t)gridDim.x * tokens) {
     const int n = (int)min((int64_t)tokens, a.T - t0);
     __syncthreads();  // the tokens before are done with
-    if (threadIdx.x < n) {
-      int64_t key;
-      s_place[threadIdx.x] = place_of(ch, a.starts, a.lens, a.B, t0 + threadIdx.x, a.status, &key);
-      s_pos[threadIdx.x] = a.pos ? a.pos[t0 + threadIdx.x] : key;
-    }
+    find_places(ch, a.starts, a.lens, a.B, t0, n, a.status, s_place, a.pos ? nullptr : s_pos);
+    if (a.pos && threadIdx.x < n) s_pos[threadIdx.x] = a.pos[t0 + threadIdx.x];
     __syncthreads();
     for (int i = threadIdx.x; i < n * half; i += kThreads)
-      rope_unit(s_turns[i % half], s_pos[i / half], a.rope, s_cos + i, s_sin + i);
+      rope_unit(s_turns[i - by_half.of(i) * half], s_pos[by_half.of(i)], a.rope, s_cos + i, s_sin + i);
     if (half > 0) __syncthreads();
-    for (int i = threadIdx.x; i < n * per_token; i += kThreads) {
-      const int tok = i / per_token;
-      int r = i - tok * per_token;
-      const Place at = s_place[tok];
-      const int64_t t = t0 + tok;
-      const float* co = s_cos + tok * half;
-      const float* si = s_sin + tok * half;
-      if (r < queries) {
-        if (at.there == -2) continue;
-        const int h = r / per_query;
-        turn_query<T, VEC>(a.rope, ch.D, (const T*)a.q.in + t * a.q.in_t + h * a.q.in_h,
-                           (T*)a.q.out + t * a.q.out_t + h * a.q.out_h, r - h * per_query, co, si);
-        continue;
-      }
-      if (at.there < 0) continue;
-      r -= queries;
-      int h = r / per_row;
-      const int d0 = 16 * (r - h * per_row);
+    // 16 components from d0 on of head h's key or value
+    each_item(rows, [&](int r, int first, int step) {
+      int h = r / rows.per_row;
+      const int d0 = 16 * (r - h * rows.per_row);
       const bool key = h < ch.heads;
       if (!key) h -= ch.heads;
-      const T* in = key ? (const T*)a.k + t * a.k_t + h * a.k_h : (const T*)a.v + t * a.v_t + h * a.v_h;
-      float x[16];
-      load_row<VEC>(in + d0, x);
-      if (key && d0 < 2 * half) {
-        if (a.rope.interleaved) {
-          turn_neighbours(a.rope, d0, x, co, si);
-        } else if constexpr (VEC) {  // half is a multiple of 8
+      const T* row0 = (key ? (const T*)a.k + h * a.k_h : (const T*)a.v + h * a.v_h) + d0;
+      const int64_t apart = key ? a.k_t : a.v_t;
+      const float* scales = key ? ch.k_scale : ch.v_scale;
+      const float head = scales ? scales[h] : 1.0f;
+      char* codes = (char*)(key ? ch.k : ch.v) + (h * ch.head_stride + d0) / 2;
+      uint8_t* blocks = (key ? ch.k_block : ch.v_block) + h * ch.block_head + d0 / 16;
+      const bool turns = key && d0 < 2 * half;
+#pragma unroll 1
+      for (int tok = first; tok < n; tok += step) {
+        const T* in = row0 + (t0 + tok) * apart;
+        float x[16];
+        load_row<VEC>(in, x);
+        const Place at = s_place[tok];
+        if (at.there < 0) continue;
+        if (turns) {
+          const float* co = s_cos + tok * half;
+          const float* si = s_sin + tok * half;
+          if (a.rope.interleaved) {
+            turn_neighbours(a.rope, d0, x, co, si);
+          } else if (VEC && even) {
 #pragma unroll
-          for (int g = 0; g < 16; g += 8) {
-            const int d = d0 + g;
-            if (d < 2 * half) {
-              const bool front = d < half;
-              const int p = front ? d : d - half;
-              float y[8];
-              load_row<true>(in + (front ? d + half : d - half), y);
+            for (int g = 0; g < 16; g += 8) {
+              const int d = d0 + g;
+              if (d < 2 * half) {
+                const bool front = d < half;
+                const int p = front ? d : d - half;
+                float y[8];
+                load_row<true>(in + g + (front ? half : -half), y);
 #pragma unroll
-              for (int j = 0; j < 8; ++j)
-                x[g + j] = fmaf(y[j], front ? -si[p + j] : si[p + j], __fmul_rn(x[g + j], co[p + j]));
+                for (int j = 0; j < 8; ++j)
+                  x[g + j] = fmaf(y[j], front ? -si[p + j] : si[p + j], __fmul_rn(x[g + j], co[p + j]));
+              }
             }
-          }
-        } else {
+          } else {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const int d = d0 + j;
-            if (d < 2 * half) {
-              const bool front = d < half;
-              const int p = front ? d : d - half;
-              const float y = (float)in[front ? d + half : d - half];
-              x[j] = fmaf(y, front ? -si[p] : si[p], __fmul_rn(x[j], co[p]));
+            for (int j = 0; j < 16; ++j) {
+              const int d = d0 + j;
+              if (d < 2 * half) {
+                const bool front = d < half;
+                const int p = front ? d : d - half;
+                const float y = (float)in[j + (front ? half : -half)];
+                x[j] = fmaf(y, front ? -si[p] : si[p], __fmul_rn(x[j], co[p]));
+              }
             }
           }
         }
+        uint8_t s;
+        const uint2 w = to_fours(x, head, &s);
+        *reinterpret_cast<uint2*>(codes + at.row / 2) = w;
+        uint8_t* to = blocks + at.block;
+        *to = s;
+        if (d0 + 16 >= ch.D)  // the padding
+          for (int j = d0 / 16 + 1; j < block_bytes(ch.D); ++j) *++to = 0;
       }
-      const float* scales = key ? ch.k_scale : ch.v_scale;
-      uint8_t s;
-      const uint2 w = to_fours(x, scales ? scales[h] : 1.0f, &s);
-      *reinterpret_cast<uint2*>((char*)(key ? ch.k : ch.v) + (at.row + h * ch.head_stride + d0) / 2) = w;
-      uint8_t* to = (key ? ch.k_block : ch.v_block) + at.block + h * ch.block_head + d0 / 16;
-      *to = s;
-      if (d0 + 16 >= ch.D)  // the padding
-        for (int j = d0 / 16 + 1; j < block_bytes(ch.D); ++j) *++to = 0;
-    }
+    });
+    each_item(queries, [&](int r, int first, int step) {
+      const int h = r / queries.per_row, piece = r - h * queries.per_row;
+      const T* in = (const T*)a.q.in + h * a.q.in_h;
+      T* out = (T*)a.q.out + h * a.q.out_h;
+#pragma unroll 1
+      for (int tok = first; tok < n; tok += step) {
+        if (s_place[tok].there == -2) continue;
+        const int64_t t = t0 + tok;
+        if (VEC && (even || a.rope.interleaved))
+          turn_query<T, VEC>(a.rope, ch.D, in + t * a.q.in_t, out + t * a.q.out_t, piece, s_cos + tok * half, s_sin + tok * half);
+        else
+          turn_query<T, false>(a.rope, ch.D, in + t * a.q.in_t, out + t * a.q.out_t, piece, s_cos + tok * half, s_sin + tok * half);
+      }
+    });
   }
 }
 
@@ -294,12 +380,14 @@ static int append_fours(const AppendArgs& a, cudaStream_t s) {
   DeviceInfo di;
   CP_TRY_STATUS(device_info(&di));
   const int64_t room = (int64_t)di.sm_count * 8;
-  int tokens = 1;
-  while (tokens < kTokens && tokens * room < a.T) tokens *= 2;
+  const int tokens = tokens_of(a.T, di.sm_count);
   const int64_t turns = (a.T + tokens - 1) / tokens;
   const size_t smem = (size_t)a.rope.half * (8 * (size_t)tokens + 8);
+  static std::atomic<uint64_t> allowed{0};
+  CP_TRY_STATUS(allow_smem_once((const void*)k_append_fours<T, VEC>, 128 * (8 * kTokens + 8), "cache append: shared memory", &allowed));
   return cuda_status(launch_early(k_append_fours<T, VEC>, dim3((unsigned)(turns < 1 ? 1 : turns < room ? turns : room)), kThreads,
-                                  smem, s, a, tokens),
+                                  smem, s, a, tokens, share_of(a.q.heads, query_pieces(a.rope, a.cache.D)),
+                                  share_of(2 * a.cache.heads, a.cache.D / 16), divisor(a.rope.half)),
                      "cache append, 4 bits");
 }
 
@@ -309,7 +397,7 @@ static bool vectors(const void* p, int64_t t, int64_t h, size_t e) {
 template <typename T>
 static int append_fours_of(const AppendArgs& a, cudaStream_t s) {
   const size_t e = sizeof(T);
-  const bool vec = vectors(a.k, a.k_t, a.k_h, e) && vectors(a.v, a.v_t, a.v_h, e) && (a.rope.interleaved || a.rope.half % 8 == 0) &&
+  const bool vec = vectors(a.k, a.k_t, a.k_h, e) && vectors(a.v, a.v_t, a.v_h, e) &&
                    (a.q.heads == 0 || (vectors(a.q.in, a.q.in_t, a.q.in_h, e) && vectors(a.q.out, a.q.out_t, a.q.out_h, e)));
   return vec ? append_fours<T, true>(a, s) : append_fours<T, false>(a, s);
 }
@@ -317,83 +405,120 @@ int launch_append_fours(const AppendArgs& a, int dtype, cudaStream_t s) {
   return dtype == CP_F32 ? append_fours_of<float>(a, s) : append_fours_of<__nv_bfloat16>(a, s);
 }
 
-// 16 cached components from `at` on (8 where a row has no more), as their element says, in float32.
+// 16 cached components (8 where a row has no more), as they come.
 template <int CT>
-__device__ __forceinline__ void load_cached(const void* cache, int64_t at, uint8_t scale, float (&x)[16], bool whole) {
-  if constexpr (CT == CP_I4) {
-    const uint2 y = *reinterpret_cast<const uint2*>((const char*)cache + at / 2);
-    __nv_fp8_e4m3 s;
-    s.__x = scale;
-    const float f = (float)s;
+struct Held {
+  static constexpr int kVecs = CT == CP_F32 ? 4 : CT == CP_BF16 ? 2 : 1;
+  uint4 v[kVecs];
+  uint8_t scale;
+  // `there` of them; a row of float32 may end after 4, 8 or 12
+  __device__ __forceinline__ void load(const char* p, const uint8_t* block, int there) {
+    if constexpr (CT == CP_I4) {
+      const uint2 x = *reinterpret_cast<const uint2*>(p);
+      v[0] = make_uint4(x.x, x.y, 0, 0);
+      scale = *block;
+    } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = __fmul_rn((float)((int)((i < 8 ? y.x : y.y) >> 4 * (i % 8) & 15) - 8), f);
-  } else if constexpr (CT == CP_E4M3) {
-    const uint4 y = *reinterpret_cast<const uint4*>((const char*)cache + at);
-    const uint32_t w[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      __nv_fp8_e4m3 s;
-      s.__x = (uint8_t)(w[i / 4] >> 8 * (i % 4));
-      x[i] = (float)s;
+      for (int i = 0; i < kVecs; ++i)
+        if (i * (16 / kVecs) < there) v[i] = reinterpret_cast<const uint4*>(p)[i];
     }
-  } else {
-    using C = typename std::conditional<CT == CP_F32, float, __nv_bfloat16>::type;
-    float y[8] = {};
-    load_row<true>((const C*)cache + at, *reinterpret_cast<float(*)[8]>(&x[0]));
-    if (whole) load_row<true>((const C*)cache + at + 8, y);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[8 + i] = y[i];
   }
-}
+  __device__ __forceinline__ void floats(float (&x)[16]) const {
+    if constexpr (CT == CP_I4) {
+      // Two numbers of a word at a time, four places apart: with bits 4-7 of a half 64 + n + 8 is a float16 as it is,
+      // and (72 + n) s - 72 s rounds once to what float16 holds exactly.
+      __nv_fp8_e4m3 s;
+      s.__x = scale;
+      const __half2 f = __half2half2(__half((float)s)), off = __hmul2(f, __half2half2(__half(-72.0f)));
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t w = h ? v[0].y : v[0].x;
+        const uint32_t at[4] = {w << 4, w, w >> 4, w >> 8};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t bits = (at[i] & 0x00F000F0u) | 0x54005400u;
+          const float2 y = __half22float2(__hfma2(*reinterpret_cast<const __half2*>(&bits), f, off));
+          x[8 * h + i] = y.x;
+          x[8 * h + i + 4] = y.y;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i) {
+        const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (CT == CP_F32) {
+            x[4 * i + j] = __uint_as_float(w[j]);
+          } else if constexpr (CT == CP_BF16) {
+            x[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
+            x[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              __nv_fp8_e4m3 s;
+              s.__x = (uint8_t)(w[j] >> 8 * k);
+              x[4 * j + k] = (float)s;
+            }
+          }
+        }
+      }
+    }
+  }
+};
 
 template <int CT, typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads) k_cache_read(ReadArgs a, int tokens) {
+__global__ void __launch_bounds__(kThreads) k_cache_read(ReadArgs a, int tokens, Share rows) {
   __shared__ Place s_place[kTokens];
   wait_for_stream();
   const Cache& ch = a.cache;
-  const int per_row = (ch.D + 15) / 16, per_token = 2 * ch.heads * per_row;
   for (int64_t t0 = (int64_t)blockIdx.x * tokens; t0 < a.T; t0 += (int64_t)gridDim.x * tokens) {
     const int n = (int)min((int64_t)tokens, a.T - t0);
     __syncthreads();
-    int64_t key;
-    if (threadIdx.x < n) s_place[threadIdx.x] = place_of(ch, a.starts, a.lens, a.B, t0 + threadIdx.x, a.status, &key);
+    find_places(ch, a.starts, a.lens, a.B, t0, n, a.status, s_place, nullptr);
     __syncthreads();
-    for (int i = threadIdx.x; i < n * per_token; i += kThreads) {
-      const int tok = i / per_token, r = (i - tok * per_token) / per_row, d0 = 16 * (i - tok * per_token - r * per_row);
-      const Place at = s_place[tok];
-      const bool key = r < ch.heads;
-      const int h = key ? r : r - ch.heads;
-      if (at.there == -2) continue;
-      float x[16] = {};
-      const int there = ch.D - d0;  // a multiple of 4
-      if (at.there == 0) {
-        const int64_t e = at.row + h * ch.head_stride + d0;
-        const void* from = key ? ch.k : ch.v;
-        if (CT == CP_F32 && there < 16) {
+    each_item(rows, [&](int r, int first, int step) {
+      int h = r / rows.per_row;
+      const int d0 = 16 * (r - h * rows.per_row), there = ch.D - d0;  // `there` components at least, a multiple of 4
+      const bool key = h < ch.heads;
+      if (!key) h -= ch.heads;
+      const char* from = (const char*)(key ? ch.k : ch.v) + cache_bytes(CT, h * ch.head_stride + d0);
+      const uint8_t* block = (key ? ch.k_block : ch.v_block) + h * ch.block_head + d0 / 16;
+      const float* scales = key ? ch.k_scale : ch.v_scale;
+      const float f = scales ? scales[h] : 1.0f;
+      T* out0 = key ? (T*)a.k + h * a.k_h + d0 : (T*)a.v + h * a.v_h + d0;
+      const int64_t apart = key ? a.k_t : a.v_t;
+      // two tokens at a time: the second's loads do not wait for the first's stores
+#pragma unroll 1
+      for (int tok = first; tok < n; tok += 2 * step) {
+        Held<CT> held[2];
+        const int other = tok + step < n ? tok + step : tok;
+        const Place at[2] = {s_place[tok], s_place[other]};
 #pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (j < there) x[j] = ((const float*)from)[e + j];
-        } else {
-          uint8_t s = 0;
-          if (CT == CP_I4) s = (key ? ch.k_block : ch.v_block)[at.block + h * ch.block_head + d0 / 16];
-          load_cached<CT>(from, e, s, x, there >= 16);
-        }
-        const float* scales = key ? ch.k_scale : ch.v_scale;
-        if (scales) {
-          const float f = scales[h];
+        for (int u = 0; u < 2; ++u)
+          if (at[u].there == 0) held[u].load(from + cache_bytes(CT, at[u].row), block + at[u].block, there);
 #pragma unroll
-          for (int j = 0; j < 16; ++j) x[j] = __fmul_rn(x[j], f);
+        for (int u = 0; u < 2; ++u) {
+          if (at[u].there == -2 || (u == 1 && other == tok)) continue;
+          float x[16] = {};
+          if (at[u].there == 0) {
+            held[u].floats(x);
+            if (scales) {
+#pragma unroll
+              for (int j = 0; j < 16; ++j) x[j] = __fmul_rn(x[j], f);
+            }
+          }
+          T* out = out0 + (t0 + (u ? other : tok)) * apart;
+          if (there >= 16) {
+            store_row<VEC>(out, x);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              if (j < there) out[j] = from_f32<T>(x[j]);
+          }
         }
       }
-      T* out = key ? (T*)a.k + (t0 + tok) * a.k_t + h * a.k_h + d0 : (T*)a.v + (t0 + tok) * a.v_t + h * a.v_h + d0;
-      if (there >= 16) {
-        store_row<VEC>(out, x);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-          if (j < there) out[j] = from_f32<T>(x[j]);
-      }
-    }
+    });
   }
 }
 
@@ -402,10 +527,10 @@ static int cache_read(const ReadArgs& a, cudaStream_t s) {
   DeviceInfo di;
   CP_TRY_STATUS(device_info(&di));
   const int64_t room = (int64_t)di.sm_count * 8;
-  int tokens = 1;
-  while (tokens < kTokens && tokens * room < a.T) tokens *= 2;
+  const int tokens = tokens_of(a.T, di.sm_count);
   const int64_t turns = (a.T + tokens - 1) / tokens;
-  return cuda_status(launch_early(k_cache_read<CT, T, VEC>, dim3((unsigned)(turns < room ? turns : room)), kThreads, 0, s, a, tokens),
+  return cuda_status(launch_early(k_cache_read<CT, T, VEC>, dim3((unsigned)(turns < room ? turns : room)), kThreads, 0, s, a, tokens,
+                                  share_of(2 * a.cache.heads, (a.cache.D + 15) / 16)),
                      "cache read");
 }
 template <int CT, typename T>

@@ -86,4 +86,17 @@ __device__ __forceinline__ int sequence_of(const int32_t* starts, int B, int64_t
   return lo;
 }
 
+// n / d for 0 <= n < 2^31 by a product: with 2^l >= d, mul = ceil(2^(31 + l) / d)
+// is off by less than d / 2^(31 + l), and n times that by less than 1 / d.
+struct Divisor {
+  uint32_t d, mul, shift;
+  __device__ __forceinline__ int of(int n) const { return (int)((uint64_t)(uint32_t)n * mul >> 31 >> shift); }
+};
+inline Divisor divisor(int d) {
+  if (d < 1) d = 1;
+  uint32_t l = 0;
+  while (((int64_t)1 << l) < d) ++l;
+  return Divisor{(uint32_t)d, (uint32_t)((((uint64_t)1 << (31 + l)) + d - 1) / d), l};
+}
+
 }  // namespace cp

@@ -31,13 +31,6 @@ constexpr int kChunk = 256;  // tokens looked up at a time
 constexpr int64_t kTwoBlocks = 108 * 1024;  // dynamic shared memory of a block that leaves room for another
 constexpr size_t kMostSmem = 160 * 1024;  // more than any launch takes
 
-// n / d for 0 <= n < 2^31 by a product: with 2^l >= d, mul = ceil(2^(31 + l) / d)
-// is off by less than d / 2^(31 + l), and n times that by less than 1 / d.
-struct Divisor {
-  uint32_t d, mul, shift;
-  __device__ __forceinline__ int of(int n) const { return (int)((uint64_t)(uint32_t)n * mul >> 31 >> shift); }
-};
-
 // Sizes of a launch that the kernels share.
 struct Tiling {
   int places, wide;  // of V pairs (and then of 2 V components that pass) in a row; threads for them
@@ -497,12 +490,6 @@ static bool fits(const RowSet& r, int V, size_t e) {
   return fits(r.in, s, 3, V, e) && fits(r.out, s + 3, 3, V, e);
 }
 
-static Divisor divisor(int d) {
-  if (d < 1) d = 1;
-  uint32_t l = 0;
-  while (((int64_t)1 << l) < d) ++l;
-  return Divisor{(uint32_t)d, (uint32_t)((((uint64_t)1 << (31 + l)) + d - 1) / d), l};
-}
 static size_t slots_of(int bytes) { return bytes >= 4 ? 8 * kItems * kThreads * (size_t)bytes : 0; }
 static int places_of(int half, int D, int V) { return (half + V - 1) / V + (D - 2 * half + 2 * V - 1) / (2 * V); }
 // Whether rows come in vectors of V: in the half layout a pair's second components are
