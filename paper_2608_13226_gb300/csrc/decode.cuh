@@ -1050,7 +1050,7 @@ __device__ __forceinline__ float remote(const float* p, int rank) {
 
 template <int CT, int DP, int QT, bool SCORES>
 __global__ void __launch_bounds__(kThreads, Shape<CT, DP, QT>::bound) k_decode(DecodeArgs a, Rows rows, int unit, int tiles, float* parts,
-                                                     Begin* begins, int by_column) {
+                                                     Begin* begins, int by_column, int lines_of) {
   using S = Shape<CT, DP, QT>;
   using Row = typename Type<CT>::Row;
   extern __shared__ __align__(1024) char smem[];  // addresses of rows are put together by exclusive or
@@ -1061,7 +1061,11 @@ __global__ void __launch_bounds__(kThreads, Shape<CT, DP, QT>::bound) k_decode(D
   wait_for_stream();
   const Cache& ch = a.cache;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int G = a.Hq / ch.heads, cols = ch.heads * tiles;
+  // With `lines` a column has a line of its own, and every lines-th block: the blocks that run together
+  // then read the same keys of different heads, whose rows share what the memory gives at a time.
+  const int lines = CT == CP_I4 ? lines_of : 1;
+  const int G = a.Hq / ch.heads, every = ch.heads * tiles, cols = lines > 1 ? 1 : every;
+  const int place = (int)(blockIdx.x / lines), places = (int)(gridDim.x / lines);  // of the line
 
   // this block's units of the line
   const int64_t mine = lane < a.B ? units_of(a, lane, unit) : 0;
@@ -1073,15 +1077,15 @@ __global__ void __launch_bounds__(kThreads, Shape<CT, DP, QT>::bound) k_decode(D
   total *= cols;
   // Where blocks have many units, a query tile counts for `setup` more, so that one
   // with several short ones does not end last.
-  const int setup = total >= 8 * (int64_t)gridDim.x ? S::setup : 0;
+  const int setup = total >= 8 * (int64_t)places ? S::setup : 0;
   total += (int64_t)setup * a.B * cols;
-  const int64_t blocks = min((int64_t)gridDim.x, total);  // each of these has a unit at least
+  const int64_t blocks = min((int64_t)places, total);  // each of these has a unit at least
   if (begins && !by_column && threadIdx.x == 0) begins[blockIdx.x] = Begin{0, 0, 0, 0};
-  if (blockIdx.x >= blocks) return;
+  if (place >= blocks) return;
   // the first `longer` of them one more than the others
   const int64_t share = quotient(total, blocks), longer = total - share * blocks;
-  int64_t u = share * blockIdx.x + min((int64_t)blockIdx.x, longer);
-  const int64_t end = u + share + (blockIdx.x < longer);
+  int64_t u = share * place + min((int64_t)place, longer);
+  const int64_t end = u + share + (place < longer);
   // the sequence they start in
   int b = 0;
   int64_t before = 0;
@@ -1120,8 +1124,8 @@ __global__ void __launch_bounds__(kThreads, Shape<CT, DP, QT>::bound) k_decode(D
     const int long_nu = nu + setup;
     for (; u < end && u < before + (int64_t)long_nu * cols;) {
       // the segment: units [k0, k1) of sequence b, query tile `col`, on the line after its setup
-      const int col = (int)quotient(u - before, long_nu);
-      const int64_t at = before + (int64_t)col * long_nu + setup;  // its unit 0
+      const int turn = (int)quotient(u - before, long_nu), col = lines > 1 ? (int)(blockIdx.x % lines) : turn;
+      const int64_t at = before + (int64_t)turn * long_nu + setup;  // its unit 0
       const int k0 = (int)max(u - at, (int64_t)0), k1 = (int)min((int64_t)nu, end - at);
       u = min(end, at + nu);
       if (k1 <= 0) continue;  // the block ends before unit 0
@@ -1170,8 +1174,8 @@ __global__ void __launch_bounds__(kThreads, Shape<CT, DP, QT>::bound) k_decode(D
         // the block that has the query tile's last unit
         const int64_t last = at + nu - 1, split = longer * (share + 1);
         const int to = (int)(last < split ? quotient(last, share + 1) : longer + quotient(last - split, share));
-        begins[by_column ? b * cols + col : (int)blockIdx.x] =
-            Begin{(int)blockIdx.x, whole ? 0 : to - (int)blockIdx.x + 1, b, col};
+        begins[by_column ? b * every + col : (int)blockIdx.x] =
+            Begin{(int)blockIdx.x, whole ? 0 : to - place + 1, b, col};
       }
       __syncthreads();  // the ring and the sums are free
     }
@@ -1326,7 +1330,7 @@ __device__ __forceinline__ void load_part(const float* p, float (&x)[V]) {
 }
 template <int CT, int DP, int QT, bool SCORES>
 __global__ void __launch_bounds__(32 * kJoinWarps) k_decode_join(DecodeArgs a, int tiles, int side, const float* parts,
-                                                                 const Begin* begins) {
+                                                                 const Begin* begins, int lines_of) {
   using S = Shape<CT, DP, QT>;
   using Row = typename Type<CT>::Row;
   constexpr int V = DP / 32;
@@ -1341,7 +1345,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_decode_join(DecodeArgs a, i
   const int nq = min(QT, G - x.col % tiles * QT);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int warps = kJoinWarps / side, n = min((int)blockIdx.y * side + warp / warps, nq - 1), own = warp % warps;
-  auto part = [&](int i) { return parts + (2 * ((int64_t)x.block + i) + (i == 0)) * S::part; };
+  const int lines = CT == CP_I4 ? lines_of : 1;  // from one of a tile's blocks to the next
+  auto part = [&](int i) { return parts + (2 * ((int64_t)x.block + i * lines) + (i == 0)) * S::part; };
   float m0 = kLowest, l0 = 0.0f;  // the first 32 parts' maxima and sums are kept
   if (lane < x.blocks) {
     m0 = part(lane)[n];
@@ -1490,6 +1495,13 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   const int64_t all = grid;
   if (grid > line) grid = line;
   const int64_t columns = (int64_t)a.B * ch.heads * tiles;
+  // A 4-bit row is shorter than the 128 bytes that L2 likes, and its scales than the 32 that it fetches at least: where
+  // a token's heads lie side by side, the blocks go over them together.  XXX
+  int lines = 1;
+  if (CT == CP_I4 && ch.heads > 1 && ch.slot_stride > ch.head_stride && 4 * ch.heads * tiles <= grid) {
+    lines = ch.heads * tiles;
+    grid = grid / lines * lines;
+  }
   const bool by_column = columns <= grid;
   Begin* begins = (Begin*)a.ws;
   float* parts = (float*)((char*)a.ws + kDecodeBlocks * sizeof(Begin));
@@ -1546,7 +1558,7 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
                                             s, size, a, rows, tiles, size),
                        "decode: cluster");
   CP_TRY_STATUS(cuda_status(launch_early(k_decode<CT, DP, QT, SCORES>, dim3((unsigned)grid), kThreads, S::smem, s, a, rows, unit,
-                                         tiles, parts, cut ? begins : nullptr, (int)by_column),
+                                         tiles, parts, cut ? begins : nullptr, (int)by_column, lines),
                             "decode"));
   if (!cut) return CP_OK;
   // about so many parts a query tile, and the join's queries side by side for it
@@ -1555,7 +1567,7 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   int side = share <= 4 ? 8 : share <= 12 ? 2 : 1;
   while (side > 1 && side / 2 >= queries) side /= 2;
   const dim3 joins((unsigned)(by_column ? columns : grid), (unsigned)(queries + side - 1) / side);
-  return cuda_status(launch_early(k_decode_join<CT, DP, QT, SCORES>, joins, 32 * kJoinWarps, 0, s, a, tiles, side, parts, begins),
+  return cuda_status(launch_early(k_decode_join<CT, DP, QT, SCORES>, joins, 32 * kJoinWarps, 0, s, a, tiles, side, parts, begins, lines),
                      "decode: join");
 }
 
