@@ -497,38 +497,48 @@ struct Math {
         }
       }
     } else {
+      // scales of keys g and g + 8; a lane's word of chunk c is of components 32 c + 8 t to + 7, one scale
+      uint32_t lo[H][SW], hi[H][SW];
 #pragma unroll
       for (int h = 0; h < H; ++h) {
-        // scales of keys g and g + 8; a lane's word of chunk c is of components 32 c + 8 t to + 7, one scale
-        uint32_t lo[SW], hi[SW];
-        load_words<SW>(lo, at + 2 * S::tk * S::row + (16 * h + g) * S::sb);
-        load_words<SW>(hi, at + 2 * S::tk * S::row + (16 * h + g + 8) * S::sb);
+        load_words<SW>(lo[h], at + 2 * S::tk * S::row + (16 * h + g) * S::sb);
+        load_words<SW>(hi[h], at + 2 * S::tk * S::row + (16 * h + g + 8) * S::sb);
         if (half_word >= 0) {
 #pragma unroll
           for (int w = 0; w < SW; ++w) {
-            lo[w] &= w == half_word ? 0xFFFFu : ~0u;
-            hi[w] &= w == half_word ? 0xFFFFu : ~0u;
+            lo[h][w] &= w == half_word ? 0xFFFFu : ~0u;
+            hi[h][w] &= w == half_word ? 0xFFFFu : ~0u;
           }
         }
+      }
+      // (the groups of keys in turn, so that two products in a row do not wait for one another)
 #pragma unroll
-        for (int c = 0; c < DP / 32; c += 2) {
-          uint32_t x[4];
-          ldmatrix4(x, (at + 16 * h * S::row + k_at) ^ (16 * c));
+      for (int c = 0; c < DP / 32; c += 2) {
+        uint32_t x[H][4];
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const uint32_t sel = (2 * j + t / 2) * 0x11;
-            const uint32_t s0 = scales_f16x2(lo[c / 2], 0, sel), s1 = scales_f16x2(hi[c / 2], 0, sel);
-            const uint32_t o0 = mul_f16x2(s0, kOff), o1 = mul_f16x2(s1, kOff);
+        for (int h = 0; h < H; ++h) ldmatrix4(x[h], (at + 16 * h * S::row + k_at) ^ (16 * c));
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
-              const uint32_t w0 = x[2 * j] >> 8 * m, w1 = x[2 * j + 1] >> 8 * m;
-              const uint32_t a0 = i4_f16x2(w0 * 16, s0, o0), a1 = i4_f16x2(w1 * 16, s1, o1);
-              const uint32_t a2 = i4_f16x2(w0, s0, o0), a3 = i4_f16x2(w1, s1, o1);
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t sel = (2 * j + t / 2) * 0x11;
+          uint32_t s0[H], s1[H], o0[H], o1[H];
+#pragma unroll
+          for (int h = 0; h < H; ++h) {
+            s0[h] = scales_f16x2(lo[h][c / 2], 0, sel);
+            s1[h] = scales_f16x2(hi[h][c / 2], 0, sel);
+            o0[h] = mul_f16x2(s0[h], kOff);
+            o1[h] = mul_f16x2(s1[h], kOff);
+          }
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int h = 0; h < H; ++h) {
+              const uint32_t w0 = x[h][2 * j] >> 8 * m, w1 = x[h][2 * j + 1] >> 8 * m;
+              const uint32_t a0 = i4_f16x2(w0 * 16, s0[h], o0[h]), a1 = i4_f16x2(w1 * 16, s1[h], o1[h]);
+              const uint32_t a2 = i4_f16x2(w0, s0[h], o0[h]), a3 = i4_f16x2(w1, s1[h], o1[h]);
 #pragma unroll
               for (int n = 0; n < NT; ++n)
                 mma_f16_16816(s[h][n], a0, a1, a2, a3, q[n][2 * (c + j) + m][0], q[n][2 * (c + j) + m][1]);
             }
-          }
         }
       }
     }
