@@ -39,6 +39,7 @@ __global__ void __launch_bounds__(kWeighThreads) k_weigh(DecodeArgs a, float* we
   constexpr int kSide = P >= 8 ? 4 : 8;  // columns whose loads are under way together
   wait_for_stream();
   const int G = a.Hq / a.cache.heads;
+  const int64_t apart = (int64_t)a.cache.capacity * P;
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     const int b = (int)(item / chunks);
     const int len = min(max(a.lens[b], 0), a.cache.capacity);
@@ -47,27 +48,31 @@ __global__ void __launch_bounds__(kWeighThreads) k_weigh(DecodeArgs a, float* we
     if (j >= len || (a.keep && !a.keep[b * a.keep_stride + j])) continue;
     float* to = weight + b * weight_stride + j;
     const float before = *to;
-    const float* lse = a.lse + (int64_t)b * a.Hq;
-    const int64_t apart = (int64_t)a.cache.capacity * P;
+    const float* lse = a.lse + (int64_t)b * a.Hq;  // of the tile at hand
     const float* scores = a.scores + b * a.score_cols * apart + j * P;
     float sum = 0.0f;
+    int tile = 0;  // of its kv head
     for (int c0 = 0; c0 < a.score_cols; c0 += kSide) {
       float s[kSide][P];
 #pragma unroll
       for (int i = 0; i < kSide; ++i)
-        if (c0 + i < a.score_cols) load_scores<P>(scores + (c0 + i) * apart, s[i]);
+        if (c0 + i < a.score_cols) load_scores<P>(scores + i * apart, s[i]);
+      scores += kSide * apart;
 #pragma unroll
       for (int i = 0; i < kSide; ++i) {
-        const int c = c0 + i, hk = c / tiles, tile = c - hk * tiles;
-        if (c < a.score_cols) {
+        if (c0 + i < a.score_cols) {
           const int n = min(pass, G - tile * pass);
-          const float* of = lse + hk * G + tile * pass;
 #pragma unroll
           for (int q = 0; q < P; ++q)
             if (q < n) {
-              const float top = of[q];  // (a head whose scores are all -infinity has no weights)
-              sum += top == -INFINITY ? 0.0f : exp2f(fmaf(-top, 1.4426950408889634f, s[i][q]));
+              // exp2 off by 2^-22 of itself; a head whose scores are all -infinity has no weights
+              const float top = lse[q];
+              float w;
+              asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(fmaf(-top, 1.4426950408889634f, s[i][q])));
+              sum += top == -INFINITY ? 0.0f : w;
             }
+          lse += n;
+          if (++tile == tiles) tile = 0;
         }
       }
     }
