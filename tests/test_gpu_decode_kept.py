@@ -70,3 +70,48 @@ def test_steps_and_command(capsys):
     dk.main(["--scenes", "1", "--steps", "2"])
     lines = capsys.readouterr().out.strip().split("\n")
     assert len(lines) == 2 and lines[0].startswith("kept") and lines[1].startswith("all")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float8_e4m3fn, torch.uint8])
+def test_small_cache(dtype):
+    """Steps on a cache of 16, 8 and 4 bits that is cut to a budget: each is attention on what the cache holds, and what
+    was evicted never comes back."""
+    f, pos, fr = batch_to_dev([scene("long_video", i, N=300, D=256) for i in range(3)])
+    layer = dk.make_layer(256, 12, 3, width=64)
+    cache = dk.Cache(layer, 3, 120, dtype, budget=40)
+    every = torch.arange(90, device="cuda").expand(3, 90).contiguous()
+    dk.fill(layer, cache, f[:, :90].contiguous(), every)
+    x, scale = f[:, 90].contiguous(), {} if cache.scale is None else dict(k_scale=cache.scale, v_scale=cache.scale)
+    for i in range(40):
+        at = torch.full((3,), 90 + i, device="cuda")
+        before = cache.lens.clone()
+        got = dk.step(layer, cache, x, at)
+        n = cache.most if i else 40
+        assert cache.lens.tolist() == [n] * 3 and int(cache.status) == 0 and n < 40 + dk.SLACK
+        if cache.lens[0] > before[0]:  # nothing evicted after this step: the cache is what it attended to
+            rows = torch.arange(0, 3 * n + 1, n, dtype=torch.int32, device="cuda")
+            k, v = cp.coverprune_cache_read(cache.k, cache.v, cache.table, torch.zeros_like(cache.lens), starts=rows, tokens=3 * n,
+                                            **scale, **cache.blocks)
+            q = layer.project(x)[0].double()
+            a = at[0].double() * layer.freq
+            u, w = q.chunk(2, -1)
+            q = torch.cat([u * a.cos() - w * a.sin(), w * a.cos() + u * a.sin()], -1)
+            k, v = (t.double().view(3, n, 3, 64).repeat_interleave(4, 2) for t in (k, v))
+            s = torch.einsum("bhd,bjhd->bhj", q, k) / 8
+            o = torch.einsum("bhj,bjhd->bhd", s.softmax(-1), v)
+            want = o.flatten(1) @ layer.out.double()
+            # the query is rounded to bfloat16 before the scores and keys and values are read rounded to it (scores off by d,
+            # 2^-8 of |q| |k| for each; weights by 2 d), the output twice more
+            mag = torch.einsum("bhd,bjhd->bhj", q.abs(), k.abs()) / 8
+            d = (2.0 ** -7 * mag).amax(-1, keepdim=True)
+            off = torch.einsum("bhj,bjhd->bhd", s.softmax(-1), v.abs()) * (2 * d + 2.0 ** -8 + 2.0 ** -7)
+            tol = off.flatten(1) @ layer.out.double().abs() + 2.0 ** -8 * want.abs() + 256 * 2.0 ** -24
+            assert bool(((got.double() - want).abs() <= tol).all())
+        x = got / got.float().norm(dim=1, keepdim=True).bfloat16()
+    assert bool((cache.weight[:, cache.most:] == 0).all())
+
+
+def test_command_with_small_caches(capsys):
+    dk.main(["--scenes", "1", "--steps", "20", "--cache", "i4", "--budget", "1000"])
+    lines = capsys.readouterr().out.strip().split("\n")
+    assert len(lines) == 2 and lines[0].startswith("kept") and lines[1].startswith("all")
