@@ -546,11 +546,11 @@ int coverprune_cache_read(const cp_cache* cache, int64_t T, const int32_t* start
  *   kept      device int32 [B, left]: the index that each key left had, -1 after the
  *             last
  *   status    device int32 or NULL; set to CP_EINVAL (and otherwise not written)
- *             if a key that is left lies, or would come to lie, on a bad page: it is not
- *             moved (its new place keeps what it held).
+ *             if a key that has to move lies, or would come to lie, on a bad page: it is
+ *             not moved (its new place keeps what it held).
  * new_lens, new_weight and kept must not overlap lens, weight or one another.  Sequences
  * that share pages are the caller's mistake.  weight_stride and new_weight_stride in elements,
- * not negative.  B <= 2^24, B * left < 2^31 * 16.
+ * 0 to 2^36.  B <= 2^24, B * left < 2^31 * 16.
  */
 int coverprune_cache_evict(const cp_cache* cache, const int32_t* lens, int64_t B,
                            const float* weight, int64_t weight_stride, int64_t left,

@@ -206,16 +206,18 @@ int coverprune_cache_append(const cp_cache* cache, const void* k, const int64_t*
 struct Room {
   size_t decode, lse, scores, all;
 };
-static Room room_of(int64_t B, int64_t Hq, const Cache& c, int cache_dtype) {
+static int room_of(int64_t B, int64_t Hq, const Cache& c, int cache_dtype, Room* room) {
   const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-  Room r;
+  Room& r = *room;
   r.decode = decode_ws_bytes(Hq, c.heads, c.D, cache_dtype);
   r.lse = up(r.decode);
   r.scores = r.lse + up(4 * (size_t)B * (size_t)Hq);
   int64_t cols = 0, pitch = 0;
   score_shape(cache_dtype, Hq, c.heads, &cols, &pitch);
-  r.all = r.scores + 4 * (size_t)(B * cols) * (size_t)pitch * (size_t)c.capacity;
-  return r;
+  // (B heads <= 2^24 and tiles times pitch < 2^18 leave what is below 2^42)
+  if (c.capacity > 0 && B * cols * pitch > ((int64_t)1 << 60) / c.capacity) return CP_EUNSUPPORTED;
+  r.all = r.scores + 4 * (size_t)(B * cols * pitch) * (size_t)c.capacity;
+  return CP_OK;
 }
 
 static int check_decode(int64_t B, int64_t Hq, const cp_cache* cache, bool with_memory, Cache* c) {
@@ -253,7 +255,9 @@ static int attend(const void* q, const int64_t* q_stride, int dtype, int64_t B, 
     return CP_EINVAL;
   if (weights && ((!weight && a.cache.capacity > 0) || !aligned(weight, 4) || (B > 1 && weight_stride < a.cache.capacity)))
     return CP_EINVAL;
-  const Room room = room_of(B, Hq, a.cache, cache->dtype);
+  Room room;
+  const int st_room = room_of(B, Hq, a.cache, cache->dtype, &room);
+  if (weights) CP_TRY_STATUS(st_room);
   if (!ws || !aligned(ws, 256) || ws_bytes < (weights ? room.all : room.decode)) return CP_EWORKSPACE;
   a.q = q;
   a.q_b = q_stride[0];
@@ -297,7 +301,9 @@ int coverprune_decode_weigh_workspace_size(int64_t B, int64_t Hq, const cp_cache
   if (!bytes) return CP_EINVAL;
   Cache c;
   CP_TRY_STATUS(check_decode(B, Hq, cache, false, &c));
-  *bytes = room_of(B, Hq, c, cache->dtype).all;
+  Room room;
+  CP_TRY_STATUS(room_of(B, Hq, c, cache->dtype, &room));
+  *bytes = room.all;
   return CP_OK;
 }
 
@@ -347,8 +353,9 @@ int coverprune_cache_evict(const cp_cache* cache, const int32_t* lens, int64_t B
                            int32_t* status, cp_stream_t stream) {
   EvictArgs a{};
   CP_TRY_STATUS(cache_of(cache, true, &a.cache));
+  constexpr int64_t far = (int64_t)1 << 36;  // between rows of weights: their offsets stay within 64 bits
   if (B < 0 || B > (1 << 24) || left < 0 || first < 0 || recent < 0 || first > left || recent > left - first ||
-      weight_stride < 0 || new_weight_stride < 0 || new_weight_width < 0 || new_weight_width > kMaxSize)
+      weight_stride > far || new_weight_stride > far || weight_stride < 0 || new_weight_stride < 0 || new_weight_width < 0 || new_weight_width > kMaxSize)
     return CP_EINVAL;
   if (left > kMaxKeys || left * B > kMaxSize * 16) return CP_EUNSUPPORTED;
   if (B == 0) return CP_OK;

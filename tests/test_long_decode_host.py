@@ -66,6 +66,10 @@ def test_weigh_refuses(lib):
         assert _weigh(lib, c, ws_bytes=n.value - 1) == cp.CP_EWORKSPACE
         assert _decode(lib, c, ws_bytes=m.value - 1) == cp.CP_EWORKSPACE
     assert lib.coverprune_decode_weigh_workspace_size(1, 4, C.byref(cache()), None) == cp.CP_EINVAL
+    # a size that 64 bits do not hold is refused, not cut
+    vast = cache(heads=1, table_width=1 << 26)
+    assert lib.coverprune_decode_weigh_workspace_size(1 << 24, 1 << 16, C.byref(vast), C.byref(n)) == cp.CP_EUNSUPPORTED
+    assert _weigh(lib, vast, B=1 << 24, Hq=1 << 16, stride=1 << 30) == cp.CP_EUNSUPPORTED
     for c, want in BAD_CACHES:
         assert lib.coverprune_decode_weigh_workspace_size(1, 4, C.byref(cache(**c)), C.byref(n)) == want
 
@@ -103,7 +107,8 @@ def test_evict_refuses(lib):
     for c, want in BAD_FOURS + BAD_BLOCKS:
         assert _evict(lib, fours(**c), B=0) == want, c
     for b in (dict(B=-1), dict(left=-1), dict(first=-1), dict(recent=-1), dict(first=11), dict(first=5, recent=6), dict(first=1 << 62, recent=1 << 62),
-              dict(lens=0), dict(lens=FAKE + 1), dict(weight=0), dict(weight=FAKE + FAR + 2), dict(stride=-1), dict(new_stride=-1), dict(new_stride=127),
+              dict(lens=0), dict(lens=FAKE + 1), dict(weight=0), dict(weight=FAKE + FAR + 2), dict(stride=-1), dict(new_stride=-1), dict(new_stride=127), dict(stride=1 << 60),
+              dict(new_stride=1 << 60),
               dict(width=-1), dict(kept=0), dict(kept=FAKE + 4 * FAR + 1), dict(new_lens=FAKE), dict(new_lens=FAKE + FAR + 4), dict(new_weight=FAKE + FAR + 512),
               dict(new_weight=FAKE + FAR - 1020), dict(kept=FAKE + FAR + 1020), dict(kept=FAKE + 3 * FAR + 4), dict(kept=FAKE + 2 * FAR + 4), dict(kept=FAKE),
               dict(status=FAKE + 1)):
