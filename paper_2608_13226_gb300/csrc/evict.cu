@@ -459,9 +459,10 @@ int launch_cache_evict(const EvictArgs& a, int cache_dtype, cudaStream_t s) {
   DeviceInfo di;
   CP_TRY_STATUS(device_info(&di));
   const Cache& ch = a.cache;
-  // as many blocks of a sequence as the device has room for, of 4096 keys at least
+  // As many blocks of a sequence as the device has room for, of 8192 keys at least (one of 8192 keys 17.6 us a call, by
+  // two blocks 19.3).
   int size = 1;
-  while (size < kMaxCluster && (int64_t)a.B * size * 2 <= di.sm_count && (int64_t)size * 8192 <= ch.capacity) size *= 2;
+  while (size < kMaxCluster && (int64_t)a.B * size * 2 <= di.sm_count && (int64_t)size * 16384 <= ch.capacity) size *= 2;
   if ((int64_t)a.B * size > 0x7FFFFFFF) return CP_EUNSUPPORTED;
   const int64_t most = (((int64_t)ch.capacity + kPickWarps * size - 1) / (kPickWarps * size) + 31) / 32 * 32 * kPickWarps;
   static std::atomic<uint64_t> allowed{0};
