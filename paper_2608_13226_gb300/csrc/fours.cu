@@ -392,8 +392,8 @@ static int append_fours(const AppendArgs& a, cudaStream_t s) {
                      "cache append, 4 bits");
 }
 
-static bool vectors(const void* p, int64_t t, int64_t h, size_t e) {
-  return (uintptr_t)p % 16 == 0 && t * (int64_t)e % 16 == 0 && h * (int64_t)e % 16 == 0;
+static bool vectors(const void* p, int64_t t, int64_t h, size_t e, int bytes = 16) {
+  return (uintptr_t)p % bytes == 0 && t * (int64_t)e % bytes == 0 && h * (int64_t)e % bytes == 0;
 }
 template <typename T>
 static int append_fours_of(const AppendArgs& a, cudaStream_t s) {
@@ -404,6 +404,27 @@ static int append_fours_of(const AppendArgs& a, cudaStream_t s) {
 }
 int launch_append_fours(const AppendArgs& a, int dtype, cudaStream_t s) {
   return dtype == CP_F32 ? append_fours_of<float>(a, s) : append_fours_of<__nv_bfloat16>(a, s);
+}
+
+// The same 16 components at a multiple of 32 bytes, which a thread stores whole: by 16 bytes, a warp's stores would fill
+// half of every sector that they touch.
+__device__ __forceinline__ void store_wide(__nv_bfloat16* p, const float (&x)[16]) {
+  uint32_t w[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[j]) : "f"(x[2 * j + 1]), "f"(x[2 * j]));
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+__device__ __forceinline__ void store_wide(float* p, const float (&x)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; i += 8)
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + i), "r"(__float_as_uint(x[i])),
+                 "r"(__float_as_uint(x[i + 1])), "r"(__float_as_uint(x[i + 2])), "r"(__float_as_uint(x[i + 3])),
+                 "r"(__float_as_uint(x[i + 4])), "r"(__float_as_uint(x[i + 5])), "r"(__float_as_uint(x[i + 6])),
+                 "r"(__float_as_uint(x[i + 7]))
+                 : "memory");
 }
 
 // 16 cached components (8 where a row has no more), as they come.
@@ -468,7 +489,8 @@ struct Held {
   }
 };
 
-template <int CT, typename T, bool VEC>
+// ALIGN: bytes that the results' rows are aligned to, as far as it counts: 32, 16 or 0.
+template <int CT, typename T, int ALIGN>
 __global__ void __launch_bounds__(kThreads) k_cache_read(ReadArgs a, int tokens, Share rows) {
   __shared__ Place s_place[kTokens];
   wait_for_stream();
@@ -511,7 +533,10 @@ __global__ void __launch_bounds__(kThreads) k_cache_read(ReadArgs a, int tokens,
           }
           T* out = out0 + (t0 + (u ? other : tok)) * apart;
           if (there >= 16) {
-            store_row<VEC>(out, x);
+            if constexpr (ALIGN == 32)
+              store_wide(out, x);
+            else
+              store_row<ALIGN == 16>(out, x);
           } else {
 #pragma unroll
             for (int j = 0; j < 16; ++j)
@@ -523,21 +548,22 @@ __global__ void __launch_bounds__(kThreads) k_cache_read(ReadArgs a, int tokens,
   }
 }
 
-template <int CT, typename T, bool VEC>
+template <int CT, typename T, int ALIGN>
 static int cache_read(const ReadArgs& a, cudaStream_t s) {
   DeviceInfo di;
   CP_TRY_STATUS(device_info(&di));
   const int64_t room = (int64_t)di.sm_count * 8;
   const int tokens = tokens_of(a.T, di.sm_count);
   const int64_t turns = (a.T + tokens - 1) / tokens;
-  return cuda_status(launch_early(k_cache_read<CT, T, VEC>, dim3((unsigned)(turns < room ? turns : room)), kThreads, 0, s, a, tokens,
+  return cuda_status(launch_early(k_cache_read<CT, T, ALIGN>, dim3((unsigned)(turns < room ? turns : room)), kThreads, 0, s, a, tokens,
                                   share_of(2 * a.cache.heads, (a.cache.D + 15) / 16)),
                      "cache read");
 }
 template <int CT, typename T>
 static int cache_read_of(const ReadArgs& a, cudaStream_t s) {
-  const bool vec = vectors(a.k, a.k_t, a.k_h, sizeof(T)) && vectors(a.v, a.v_t, a.v_h, sizeof(T));
-  return vec ? cache_read<CT, T, true>(a, s) : cache_read<CT, T, false>(a, s);
+  if (vectors(a.k, a.k_t, a.k_h, sizeof(T), 32) && vectors(a.v, a.v_t, a.v_h, sizeof(T), 32)) return cache_read<CT, T, 32>(a, s);
+  if (vectors(a.k, a.k_t, a.k_h, sizeof(T)) && vectors(a.v, a.v_t, a.v_h, sizeof(T))) return cache_read<CT, T, 16>(a, s);
+  return cache_read<CT, T, 0>(a, s);
 }
 int launch_cache_read(const ReadArgs& a, int dtype, int cache_dtype, cudaStream_t s) {
   const bool wide = dtype == CP_F32;
