@@ -153,18 +153,21 @@ __device__ __forceinline__ uint2 to_fours(const float (&x)[16], float head, uint
   // above 7 (1 + 2^-4).  Else divisions.  38,400 tokens of 2 x 4 heads of 128 28.2 us, by divisions alone 46.8.
   if (want >= 0.015625f && want <= 448.0f && step > 1e-15f && step < 1e15f) {
     const float r = __frcp_rn(step);
+    const uint64_t r2 = pair(r, r), less = pair(-step, -step), magic = pair(12582920.0f, 12582920.0f);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       // a number's bits end in n + 8 once 1.5 2^23 + 8 is added, which rounds it to nearest even; what is
       // above them adds up to a constant
       uint32_t all = 0, above = 0;
 #pragma unroll
-      for (int i = 7; i >= 0; --i) {
-        float y = __fmul_rn(x[8 * h + i], r);
-        y = __fmaf_rn(__fmaf_rn(-y, step, x[8 * h + i]), r, y);
-        y = __fmaf_rn(__fmaf_rn(-y, step, x[8 * h + i]), r, y);
-        all = all * 16 + __float_as_uint(__fadd_rn(y, 12582920.0f));
-        above = above * 16 + 0x4B400000u;
+      for (int i = 6; i >= 0; i -= 2) {
+        const uint64_t v = pair(x[8 * h + i], x[8 * h + i + 1]);
+        uint64_t y = mul2(v, r2);
+        y = fma2(fma2(y, less, v), r2, y);
+        y = fma2(fma2(y, less, v), r2, y);
+        y = add2(y, magic);
+        all = (all * 16 + (uint32_t)(y >> 32)) * 16 + (uint32_t)y;
+        above = (above * 16 + 0x4B400000u) * 16 + 0x4B400000u;
       }
       w[h] = all - above;
     }

@@ -102,20 +102,6 @@ __device__ __forceinline__ void store(C* p, int at, const float (&x)[V]) {
   *reinterpret_cast<W*>(p + at) = y;
 }
 
-__device__ __forceinline__ uint64_t pair(float lo, float hi) {
-  return (uint64_t)__float_as_uint(hi) << 32 | __float_as_uint(lo);
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-
 // The two vectors of a place turned by its pairs: in the half layout a[i] with
 // b[i], interleaved neighbours within a and within b.
 template <typename T, int V, bool INTERLEAVED>
