@@ -32,7 +32,7 @@
 // term) for 8 KB: a sixth of the tensor pipe at the full rate of HBM, where
 // tcgen05's 128 rows would be 7 of 8 empty.
 //
-// A 4-bit cache is bound by instructions: of the 825 of a warp for 32 keys (head 128, 8 queries) 450 turn 4 bits and
+// A 4-bit cache is bound by instructions: of the 850 of a warp for 32 keys (head 128, 8 queries) 450 turn 4 bits and
 // scales into float16 operands (14 for 8 numbers: a mask and a fused product each two, their scale), and
 // the SM's four schedulers issue 2.4 a cycle together however many warps there are.  32 sequences of 8192 to 8704
 // keys 47.7 us (0.48 of the HBM's rate), the copies alone 34, all but the copies 43.

@@ -150,7 +150,7 @@ __device__ __forceinline__ uint2 to_fours(const float (&x)[16], float head, uint
   // place of x / step, q + (x - q step) r rounds to the quotient (Markstein 1990, Computation of elementary functions on
   // the IBM RISC System/6000).  x r alone may be two units off, and once corrected is within one.  That within ranges
   // where nothing that counts under- or overflows, and where the scale is a normal number, so that no quotient is
-  // above 7 (1 + 2^-4).  Else divisions.  38,400 tokens of 2 x 4 heads of 128 28.2 us, by divisions alone 46.8.
+  // above 7 (1 + 2^-4).  Else divisions.  38,400 tokens of 2 x 4 heads of 128 26.6 us, by divisions alone 46.8.
   if (want >= 0.015625f && want <= 448.0f && step > 1e-15f && step < 1e15f) {
     const float r = __frcp_rn(step);
     const uint64_t r2 = pair(r, r), less = pair(-step, -step), magic = pair(12582920.0f, 12582920.0f);
