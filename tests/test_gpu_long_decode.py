@@ -197,6 +197,15 @@ def test_append_many_tokens(Hq, H, D, rot):
     check_append(D + Hq, [9000, 0, 12345, 7001, 1], [3, 0, 100, 0, 77], 16, Hq, H, D, rot, BF16, scales=True)
 
 
+def test_append_and_read_many_sequences():
+    """More sequences than are counted at once, most of them empty or short, and one among them long."""
+    new = [(i * 7 % 5) * (i % 3 == 0) for i in range(900)]
+    new[417] = 333
+    check_append(1, new, [i % 4 for i in range(900)], 4, 2, 1, 32, 32, BF16, padding=5)
+    check_append(2, [0] * 256 + [1] + [0] * 40, [0] * 297, 1, 0, 1, 64, 0, F32)
+    check_append(3, [0] * 255 + [2], [3] * 256, 2, 1, 2, 32, 16, BF16)
+
+
 def test_append_specials():
     """Infinities saturate with their block, a NaN makes its 16 components NaN, what is too small becomes 0."""
     v = torch.randn(1, 1, 96, device="cuda")
@@ -526,7 +535,8 @@ def test_evict_ties_and_specials():
 
 @pytest.mark.parametrize("lens,left,page,D,H,cdt", [([50000, 30, 40001], 20000, 64, 64, 1, BF16), ([200001], 100000, 64, 32, 1, I4),
                                                     ([9000] * 9, 1229, 16, 128, 4, BF16), ([1240] * 64, 1229, 32, 128, 2, E4M3),
-                                                    ([140000, 139999], 139000, 100, 8, 1, BF16)])
+                                                    ([140000, 139999], 139000, 100, 8, 1, BF16), ([300001], 123456, 64, 8, 1, BF16),
+                                                    ([4000] * 3 + [90] * 160, 77, 7, 8, 1, BF16)])
 def test_evict_long(lens, left, page, D, H, cdt):
     """Blocks alone and clusters of them; many turns."""
     check_evict(left, lens, left, 4, 64, page, H, D, cdt, ties=True)
@@ -535,6 +545,8 @@ def test_evict_long(lens, left, page, D, H, cdt):
 def test_evict_lengths_out_of_range_and_wide_tables():
     check_evict(5, [-3, 500, 64], 60, 2, 3, 16, 2, 64, BF16)
     c, r = check_evict(6, [70, 3], 40, 0, 0, 16, 2, 64, I4, width=3000)
+    # rows of 40,000 keys of more sequences than share the device by clusters: weights are read again, not held
+    check_evict(7, [700, 3, 120] * 60, 100, 1, 2, 16, 1, 64, BF16, width=2500, ties=True)
     g = gen(3)  # a length beyond the table's row is what the row holds
     c = Cache(g, 1, 32, 16, 1, 64, BF16)
     w = torch.rand(1, 32, generator=g, device="cuda")
