@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) k_evict_pick(EvictArgs a, int
   __shared__ uint32_t s_total[kPickWarps];    // the cluster's of a warp's
   __shared__ uint32_t s_above[kPickWarps], s_equal[kPickWarps];
   __shared__ uint32_t s_pair[2];              // this block's numbers above and equal
-  __shared__ uint32_t s_digit, s_left;
+  __shared__ uint32_t s_digit, s_left, s_size;
   wait_for_stream();
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int b = blockIdx.x / size, rank = size > 1 ? (int)cluster_ctarank() : 0;
@@ -143,12 +143,21 @@ __global__ void __launch_bounds__(kPickThreads, 1) k_evict_pick(EvictArgs a, int
         const bool first = before + x >= left;
         s_digit = (uint32_t)(first ? top : top - 1);
         s_left = left - before - (first ? 0 : x);
+        s_size = first ? x : y;
       }
     }
     __syncthreads();
     prefix |= s_digit << shift;
     left = s_left;
+    const bool whole = s_left == s_size;
     if (size > 1) hw_cluster_sync();  // the others have read this block's counts
+    // All keys with these digits stay, as where there is one: those above what lies below them do, and no digit
+    // more is wanted.  (They are not all keys that there are, so there is something below.)
+    if (whole) {
+      prefix -= 1;
+      left = 0;
+      break;
+    }
   }
 
   // all above `prefix` stay, and the first `left` that equal it: each warp's numbers of both
