@@ -309,14 +309,12 @@ __device__ __forceinline__ int part_of(const EvictArgs& a, const Kind& kind, int
   return n == 0 || a.kept[(int64_t)*b * a.left + n - 1] == n - 1 ? 0 : n;
 }
 __device__ __forceinline__ void turn_barrier(int size) {
-  // A read that has come back cannot see what is written later, so that the cluster's barrier need not order memory:
-  // doing so it would wait for every row written so far, each turn (one sequence of 200,001 keys 274 us, else 378).
-  if (size > 1) {
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
-  } else {
-    __syncthreads();
-  }
+  // The notes go from thread to thread of a block, which __syncthreads orders.  Between blocks nothing is handed on but that
+  // rows have been read, and a read that has come back cannot see what is written later: the cluster's barrier
+  // need not order memory.  Doing so it would wait for every row written so far, each turn (one sequence of
+  // 200,001 keys 274 us, else 378).
+  __syncthreads();
+  if (size > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 template <int BYTES> struct Piece;
 template <> struct Piece<16> { using type = uint4; };
