@@ -240,6 +240,7 @@ struct Kind {
   char *k, *v;
   int64_t page, slot, part;  // bytes
   int parts, split, bytes;
+  int jobs;  // of all sequences: a cluster each
 };
 // Where a row comes from and where it goes, bytes; -1: it stays.
 struct Move {
@@ -299,8 +300,7 @@ struct Moves {
 };
 
 // The part of a sequence's rows that a cluster of `size` blocks has: its place, how many rows stay (0: nothing moves).
-__device__ __forceinline__ int part_of(const EvictArgs& a, const Kind& kind, int size, char** base, int* b) {
-  int job = blockIdx.x / size;
+__device__ __forceinline__ int part_of(const EvictArgs& a, const Kind& kind, int job, char** base, int* b) {
   const int part = job % (kind.parts * kind.split);
   job /= kind.parts * kind.split;
   *base = (job % 2 ? kind.v : kind.k) + part / kind.split * kind.part + part % kind.split * kind.bytes;
@@ -334,13 +334,16 @@ __host__ __device__ __forceinline__ int side_of(int pieces) {
 
 // A thread has a piece of kPer rows of every turn, which it copies to a slot of its own and takes from there.
 template <int BYTES>
-__global__ void __launch_bounds__(kMoveThreads) k_evict_rows(EvictArgs a, Kind kind, int size) {
+__global__ void __launch_bounds__(kMoveThreads) k_evict_rows(EvictArgs a, Kind rows_of, Kind scales_of, int size) {
   using P = typename Piece<BYTES>::type;
   extern __shared__ __align__(16) char smem[];  // kStages turns of pieces, and notes of kNotes
   wait_for_stream();
+  const int job = blockIdx.x / size;
+  const bool scales = job >= rows_of.jobs;
+  const Kind& kind = scales ? scales_of : rows_of;
   char* base;
   int b;
-  const int n = part_of(a, kind, size, &base, &b);
+  const int n = part_of(a, kind, scales ? job - rows_of.jobs : job, &base, &b);
   if (n == 0) return;  // in every block of the cluster
   const int pieces = kind.bytes / BYTES, side = side_of(pieces), rows = side * kPer;  // rows side by side, and of a turn
   const int piece = threadIdx.x % pieces, r0 = threadIdx.x / pieces;
@@ -426,40 +429,45 @@ static int cluster_size(int64_t jobs, int most, int* size) {
   return CP_OK;
 }
 
-// Rows of `bytes` bytes a head, heads `head` bytes apart, moved up.
+// Rows of two kinds (of the second there may be none) moved up.
 template <int BYTES>
-static int move_by(const EvictArgs& a, Kind kind, cudaStream_t s) {
-  const int rows = side_of(kind.bytes / BYTES) * kPer;
-  const int64_t jobs = (int64_t)a.B * 2 * kind.parts * kind.split;
+static int move_rows(const EvictArgs& a, const Kind& first, const Kind& second, cudaStream_t s) {
+  const int rows = side_of(first.bytes / BYTES) * kPer;
+  const int64_t jobs = (int64_t)first.jobs + second.jobs;
   // clusters where there are few heads and sequences, if they get some turns
   int most = kMaxCluster, size = 1;
   while (most > 1 && (int64_t)rows * most * 4 > a.left) most /= 2;
   CP_TRY_STATUS(cluster_size<BYTES>(jobs, most, &size));
   if (jobs * size > 0x7FFFFFFF) return CP_EUNSUPPORTED;
-  return cuda_status(launch_early_cluster(k_evict_rows<BYTES>, dim3((unsigned)(jobs * size)), kMoveThreads, smem_of<BYTES>(), s, size, a,
-                                          kind, size),
+  return cuda_status(launch_early_cluster(k_evict_rows<BYTES>, dim3((unsigned)(jobs * size)), kMoveThreads, smem_of<BYTES>(), s,
+                                          size, a, first, second, size),
                      "evict: rows");
 }
-static int move(const EvictArgs& a, Kind kind, int64_t head, int bytes, int sms, cudaStream_t s) {
+// How rows of `bytes` bytes a head move, heads `head` bytes apart: by 16 bytes (`whole`) or by 4.
+static int divide(const EvictArgs& a, Kind* kind, int64_t head, int bytes, int sms, bool* whole) {
   int group = 1;  // heads that lie side by side go together
   const int heads = a.cache.heads;
   if (head == bytes)
     for (int g = 2; g <= heads && (int64_t)g * bytes <= kTogether; ++g)
       if (heads % g == 0) group = g;
-  kind.parts = heads / group;
-  kind.part = head * group;
-  kind.bytes = bytes * group;
-  kind.split = 1;
-  const uint64_t any = (uint64_t)kind.k | (uint64_t)kind.v | (uint64_t)kind.page | (uint64_t)kind.slot | (uint64_t)kind.part |
-                       (uint64_t)kind.bytes;
-  if (any % 16 != 0) return move_by<4>(a, kind, s);
+  kind->parts = heads / group;
+  kind->part = head * group;
+  kind->bytes = bytes * group;
+  kind->split = 1;
+  const uint64_t any = (uint64_t)kind->k | (uint64_t)kind->v | (uint64_t)kind->page | (uint64_t)kind->slot | (uint64_t)kind->part |
+                       (uint64_t)kind->bytes;
+  *whole = any % 16 == 0;
   // where clusters of whole rows would not fill the device, halves of them
   // (one sequence of 200,001 keys and 8 heads of 128 198 us, whole rows 275; 32 sequences 54.6, whole 50.1)
-  while ((int64_t)a.B * 2 * kind.parts * kind.split * kMaxCluster < 2 * sms && kind.bytes >= 256 && kind.bytes % 32 == 0) {
-    kind.bytes /= 2;
-    kind.split *= 2;
+  while (*whole && (int64_t)a.B * 2 * kind->parts * kind->split * kMaxCluster < 2 * sms && kind->bytes >= 256 &&
+         kind->bytes % 32 == 0) {
+    kind->bytes /= 2;
+    kind->split *= 2;
   }
-  return move_by<16>(a, kind, s);
+  const int64_t jobs = (int64_t)a.B * 2 * kind->parts * kind->split;
+  if (jobs > 0x3FFFFFFF) return CP_EUNSUPPORTED;
+  kind->jobs = (int)jobs;
+  return CP_OK;
 }
 
 int launch_cache_evict(const EvictArgs& a, int cache_dtype, cudaStream_t s) {
@@ -480,11 +488,13 @@ int launch_cache_evict(const EvictArgs& a, int cache_dtype, cudaStream_t s) {
                                 : launch_early_cluster(k_evict_pick<false>, grid, kPickThreads, 0, s, size, a, size),
                             "evict: pick"));
   if (a.left == 0 || ch.capacity <= a.left) return CP_OK;  // no row moves
-  Kind kind{(char*)ch.k, (char*)ch.v, cache_bytes(cache_dtype, ch.page_stride), cache_bytes(cache_dtype, ch.slot_stride)};
-  CP_TRY_STATUS(move(a, kind, cache_bytes(cache_dtype, ch.head_stride), (int)cache_bytes(cache_dtype, ch.D), di.sm_count, s));
-  if (cache_dtype != CP_I4) return CP_OK;
-  kind = Kind{(char*)ch.k_block, (char*)ch.v_block, ch.block_page, ch.block_slot};
-  return move(a, kind, ch.block_head, block_bytes(ch.D), di.sm_count, s);
+  Kind rows{(char*)ch.k, (char*)ch.v, cache_bytes(cache_dtype, ch.page_stride), cache_bytes(cache_dtype, ch.slot_stride)};
+  Kind scales{(char*)ch.k_block, (char*)ch.v_block, ch.block_page, ch.block_slot}, none{};
+  bool whole = true, together = false;  // (rows of the cache are multiples of 16 bytes)
+  CP_TRY_STATUS(divide(a, &rows, cache_bytes(cache_dtype, ch.head_stride), (int)cache_bytes(cache_dtype, ch.D), di.sm_count, &whole));
+  if (cache_dtype == CP_I4) CP_TRY_STATUS(divide(a, &scales, ch.block_head, block_bytes(ch.D), di.sm_count, &together));
+  CP_TRY_STATUS(move_rows<16>(a, rows, together ? scales : none, s));
+  return cache_dtype == CP_I4 && !together ? move_rows<4>(a, scales, none, s) : CP_OK;
 }
 
 }  // namespace cp
