@@ -4,7 +4,7 @@
 // that stays is found by counting digits of 11 bits from the top (radix selection), and a
 // count over the keys in their order gives each that stays its place.
 //
-// k_evict_move moves the rows: HBM bounds it, every row read and written once.  A block or a cluster has
+// k_evict_rows moves the rows: HBM bounds it, every row read and written once.  A block or a cluster has
 // one head's rows (of keys or values) of a sequence to itself and takes them in their
 // order, a turn of some at a time: all of these are read before the first is written, and rows still
 // to come lie behind every place that is written (the i-th row that stays comes from place i or
