@@ -501,7 +501,8 @@ typedef struct {
  * stays NaN).  A 4-bit one takes for 16 components the scale
  *   s = round(min(max |x| / (7 scale), 448)) to e4m3, to nearest even,
  * and for each n = round(x / (s scale)) to nearest even, at most 7 either way, in
- * float32 (s = 0: 0; an infinity is 7; a NaN makes s and so its 16 components NaN).
+ * float32 (s = 0: 0; an infinity is 7; a NaN makes s and so its 16 components NaN), and
+ * keys and values must not lie in one place.
  * Two tokens on one row of the cache are the caller's mistake.
  */
 int coverprune_cache_append(const cp_cache* cache, const void* k, const int64_t* k_stride,
@@ -548,8 +549,8 @@ int coverprune_cache_read(const cp_cache* cache, int64_t T, const int32_t* start
  *   status    device int32 or NULL; set to CP_EINVAL (and otherwise not written)
  *             if a key that has to move lies, or would come to lie, on a bad page: it is
  *             not moved (its new place keeps what it held).
- * new_lens, new_weight and kept must not overlap lens, weight or one another.  Sequences
- * that share pages are the caller's mistake.  weight_stride and new_weight_stride in elements,
+ * new_lens, new_weight and kept must not overlap lens, weight or one another; keys and
+ * values in one place are refused.  Sequences that share pages are the caller's mistake.  weight_stride and new_weight_stride in elements,
  * 0 to 2^36.  B <= 2^24, B * left < 2^31 * 16.
  */
 int coverprune_cache_evict(const cp_cache* cache, const int32_t* lens, int64_t B,

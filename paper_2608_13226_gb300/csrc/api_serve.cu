@@ -160,6 +160,11 @@ int coverprune_rotary(const cp_rows* rows, int n, int dtype, int64_t B, int64_t 
   return launch_rotary(a, dtype, (cudaStream_t)stream);
 }
 
+// Keys and values in one place: fine where they are read, but a call that writes both would mix them up.
+static bool one_place(const Cache& c, bool fours) {
+  return (c.k && c.k == c.v) || (fours && c.k_block && c.k_block == c.v_block);
+}
+
 int coverprune_cache_append(const cp_cache* cache, const void* k, const int64_t* k_stride,
                             const void* v, const int64_t* v_stride, int dtype, int64_t T,
                             const int32_t* starts, const int32_t* lens, int64_t B,
@@ -183,6 +188,7 @@ int coverprune_cache_append(const cp_cache* cache, const void* k, const int64_t*
                 !aligned(v, size_of(dtype))))
     return CP_EINVAL;
   if (T == 0 && !new_lens) return CP_OK;
+  if (T > 0 && cache->dtype == CP_I4 && one_place(a.cache, true)) return CP_EINVAL;
   a.k = k;
   a.v = v;
   if (T > 0) {
@@ -329,7 +335,7 @@ int coverprune_cache_read(const cp_cache* cache, int64_t T, const int32_t* start
   if (!starts && T != B) return CP_EINVAL;
   if (B == 0 || T == 0) return CP_OK;
   if (!lens || !aligned(lens, 4) || !aligned(starts, 4) || !aligned(status, 4) || !k || !v || !k_stride ||
-      !v_stride || !aligned(k, size_of(dtype)) || !aligned(v, size_of(dtype)))
+      !v_stride || !aligned(k, size_of(dtype)) || !aligned(v, size_of(dtype)) || k == v)
     return CP_EINVAL;
   a.k = k;
   a.v = v;
@@ -363,6 +369,7 @@ int coverprune_cache_evict(const cp_cache* cache, const int32_t* lens, int64_t B
       !aligned(kept, 4) || !aligned(status, 4) || (left > 0 && !kept) || (a.cache.capacity > 0 && !weight))
     return CP_EINVAL;
   if (new_weight && B > 1 && new_weight_stride < new_weight_width) return CP_EINVAL;
+  if (one_place(a.cache, cache->dtype == CP_I4)) return CP_EINVAL;
   // what a block writes others still read
   const int64_t w = (B - 1) * weight_stride + a.cache.capacity, nw = (B - 1) * new_weight_stride + new_weight_width;
   const struct { const void* p; int64_t n; } in[2] = {{lens, B}, {weight, w}}, out[3] = {{new_lens, B}, {new_weight, nw}, {kept, left * B}};

@@ -128,3 +128,13 @@ def test_python_refuses_cpu_tensors():
             f()
     with pytest.raises(TypeError):
         cp.coverprune_cache_read(held, held, table, lens, dtype=torch.float16, **kw)
+
+
+def test_keys_and_values_in_one_place(lib):
+    """Writes to both would meet; before anything else is looked at that needs a device."""
+    far = FAKE + 5 * FAR
+    for c in (fours(k=far, v=far), fours(v=FAKE + FAR, k_block=far, v_block=far)):
+        assert _append(lib, c, T=3) == cp.CP_EINVAL
+        assert _evict(lib, c) == cp.CP_EINVAL
+    assert _evict(lib, cache(k=far, v=far)) == cp.CP_EINVAL
+    assert _read(lib, k=far, v=far) == cp.CP_EINVAL
