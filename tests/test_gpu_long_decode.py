@@ -197,6 +197,14 @@ def test_append_many_tokens(Hq, H, D, rot):
     check_append(D + Hq, [9000, 0, 12345, 7001, 1], [3, 0, 100, 0, 77], 16, Hq, H, D, rot, BF16, scales=True)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D,rot", [(96, 24), (32, 8), (64, 40), (128, 72), (128, 6), (96, 30), (256, 248)])
+def test_append_turns_parts(dtype, D, rot):
+    """Halves that are not vectors of 16 bytes apart, in rows that are (and of a larger tensor)."""
+    check_append(D + rot, [5, 0, 300], [0, 9, 40], 7, 6, 3, D, rot, dtype, padding=3)
+    check_append(D + rot + 1, [70, 1], [3, 16], 16, 3, 1, D, rot, dtype, True, scales=True, view=8, in_place=True)
+
+
 def test_append_and_read_many_sequences():
     """More sequences than are counted at once, most of them empty or short, and one among them long."""
     new = [(i * 7 % 5) * (i % 3 == 0) for i in range(900)]
