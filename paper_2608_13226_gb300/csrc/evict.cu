@@ -230,17 +230,17 @@ __global__ void __launch_bounds__(kPickThreads, 1) k_evict_pick(EvictArgs a, int
 constexpr int kMoveThreads = 256;
 constexpr int kPer = 4;        // pieces of a thread in a turn
 constexpr int kStages = 4;     // turns under way
-constexpr int kAhead = 2;      // turns that a trip to L2 takes, about
+constexpr int kAhead = 3;      // turns that a trip to L2 takes, about (one sequence of 200,001 keys: 2 180 us, 3 174, 4 171; 64 of 1240: 34, 35, 36)
 constexpr int64_t kTogether = 256;  // bytes that heads side by side go together up to
+constexpr int kMostLooked = 256;    // sequences that a block looks through
 constexpr int kNotes = kStages + 1;  // turns of notes: one is written while others may still go by the oldest
 
-// Rows of one kind: codes or elements, or a 4-bit row's scales.  Of a row, `parts` x `split` pieces of `bytes` bytes
-// move by themselves: `split` of a head, or one of some heads that lie side by side, and those `part` bytes apart.
+// Rows of one kind: codes or elements, or a 4-bit row's scales.  Of a row, heads that lie side by side make a part of
+// `bytes` bytes, and parts are `part` bytes apart.
 struct Kind {
   char *k, *v;
   int64_t page, slot, part;  // bytes
-  int parts, split, bytes;
-  int jobs;  // of all sequences: a cluster each
+  int parts, bytes;
 };
 // Where a row comes from and where it goes, bytes; -1: it stays.
 struct Move {
@@ -251,27 +251,27 @@ struct Move {
 // later where it goes, so that no turn waits for a trip to L2.
 struct Moves {
   const EvictArgs& a;
-  const Kind& kind;
+  const int64_t page, slot;  // bytes
+  const Divisor by_page;
   const int32_t *kept, *table;
   int n, stride;  // rows that stay, rows of a cluster's turn
   int row;        // this thread's of turn 0; stride: none
   int keys[2 * kAhead];
   int2 pages[kAhead];
 
-  __device__ int64_t row_of(int turn) const { return row + (int64_t)turn * stride; }
+  __device__ int row_of(int turn) const { return row + turn * stride; }  // n < 2^30, and a few turns more
   __device__ int key_of(int turn) const { return row < stride && row_of(turn) < n ? kept[row_of(turn)] : -1; }
   __device__ int2 pages_of(int turn, int key) const {
     if (key < 0 || key == row_of(turn)) return make_int2(-1, -1);
-    const uint32_t size = (uint32_t)a.cache.page_size;
-    return make_int2(table[(uint32_t)key / size], table[(uint32_t)row_of(turn) / size]);
+    return make_int2(table[by_page.of(key)], table[by_page.of(row_of(turn))]);
   }
   __device__ Move move_of(int turn, int key, int2 p) const {
     Move m{-1, -1};
-    if (key < 0 || key == row_of(turn)) return m;
+    const int to = row_of(turn);
+    if (key < 0 || key == to) return m;
     if (p.x >= 0 && p.x < a.cache.pages && p.y >= 0 && p.y < a.cache.pages) {
-      const uint32_t size = (uint32_t)a.cache.page_size;
-      m.from = p.x * kind.page + (int64_t)((uint32_t)key % size) * kind.slot;
-      m.to = p.y * kind.page + (int64_t)((uint32_t)row_of(turn) % size) * kind.slot;
+      m.from = p.x * page + (key - by_page.of(key) * (int)by_page.d) * slot;
+      m.to = p.y * page + (to - by_page.of(to) * (int)by_page.d) * slot;
     } else if (a.status) {
       set_status(a.status, CP_EINVAL);
     }
@@ -287,26 +287,85 @@ struct Moves {
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) pages[i] = pages_of(turn + i, keys[i]);
   }
-  __device__ Move next(int turn) {
-    const Move m = move_of(turn, keys[0], pages[0]);
-#pragma unroll
-    for (int i = 0; i + 1 < kAhead; ++i) pages[i] = pages[i + 1];
-    pages[kAhead - 1] = pages_of(turn + kAhead, keys[kAhead]);
-#pragma unroll
-    for (int i = 0; i + 1 < 2 * kAhead; ++i) keys[i] = keys[i + 1];
-    keys[2 * kAhead - 1] = key_of(turn + 2 * kAhead);
+  // u: how many calls there have been, modulo 2 kAhead, a constant where it counts: a register that is still being loaded
+  // must not be moved to another.
+  __device__ __forceinline__ Move next(int turn, int u) {
+    const Move m = move_of(turn, keys[u], pages[u % kAhead]);
+    pages[u % kAhead] = pages_of(turn + kAhead, keys[(u + kAhead) % (2 * kAhead)]);
+    keys[u] = key_of(turn + 2 * kAhead);
     return m;
   }
 };
 
-// The part of a sequence's rows that a cluster of `size` blocks has: its place, how many rows stay (0: nothing moves).
-__device__ __forceinline__ int part_of(const EvictArgs& a, const Kind& kind, int job, char** base, int* b) {
-  const int part = job % (kind.parts * kind.split);
-  job /= kind.parts * kind.split;
-  *base = (job % 2 ? kind.v : kind.k) + part / kind.split * kind.part + part % kind.split * kind.bytes;
-  *b = job / 2;
-  const int n = min(min(max(a.lens[*b], 0), a.cache.capacity), a.left);
-  return n == 0 || a.kept[(int64_t)*b * a.left + n - 1] == n - 1 ? 0 : n;
+// What a cluster has to move: `bytes` bytes of `n` rows of a sequence, from `base` on.
+struct Job {
+  char* base;
+  int b, n, bytes;
+  bool of_scales;
+};
+// Into how many pieces a row's part may be divided: of 64 bytes (a turn has no more rows of smaller ones), or of 32 where
+// those do not make it up.
+template <int BYTES>
+__host__ __device__ __forceinline__ int units_of(const Kind& rows) {
+  const int bytes = rows.bytes % 64 == 0 ? 64 : 32;
+  return BYTES == 16 && rows.bytes % bytes == 0 ? rows.bytes / bytes : 1;
+}
+// Into how many they are, so that `cut` sequences' jobs are at most `clusters` (if they are undivided).
+__host__ __device__ __forceinline__ int divided_by(int clusters, int cut, const Kind& rows, const Kind& scales, int units) {
+  const int most = (clusters / (2 * cut) - scales.parts) / rows.parts;
+  int f = most < units ? most : units;
+  while (f > 1 && units % f != 0) --f;
+  return f < 1 ? 1 : f;
+}
+// The cluster's job (n 0: none).  Sequences that keep all their keys have none; where that leaves clusters without, they take pieces
+// of the others' rows (32 sequences of 1300 to 8704 keys, a few of them above 8000, 44 us, undivided 100).  Where all are cut, rows go
+// whole as far as that fills the device (32 sequences by 128 bytes 54.6 us, by 256 50.1).
+template <int BYTES>
+__device__ __forceinline__ Job job_of(const EvictArgs& a, const Kind& rows, const Kind& scales, int id, int clusters) {
+  __shared__ uint32_t s_cut[kMostLooked / 32];  // which sequences are cut
+  const int lane = threadIdx.x % 32;
+  uint32_t word = 0;
+  int cut = a.B;
+  if (a.B <= kMostLooked) {
+    const int seq = threadIdx.x;
+    const uint32_t all = __ballot_sync(~0u, seq < a.B && min(a.lens[min(seq, a.B - 1)], a.cache.capacity) > a.left);
+    if (lane == 0) s_cut[seq / 32] = all;
+    __syncthreads();
+    word = lane < kMostLooked / 32 ? s_cut[lane] : 0;
+    cut = __reduce_add_sync(~0u, __popc(word));
+  }
+  Job x{nullptr, 0, 0, 0, false};
+  if (cut == 0) return x;
+  int f = divided_by(clusters, cut, rows, scales, units_of<BYTES>(rows));
+  const int of_rows = cut * 2 * rows.parts * f;
+  if (id >= of_rows + cut * 2 * scales.parts) return x;
+  x.of_scales = id >= of_rows;
+  const Kind& kind = x.of_scales ? scales : rows;
+  if (x.of_scales) {
+    id -= of_rows;
+    f = 1;
+  }
+  x.bytes = kind.bytes / f;
+  const int part = id % (kind.parts * f);
+  id /= kind.parts * f;
+  x.base = (id % 2 ? kind.v : kind.k) + part / f * kind.part + part % f * x.bytes;
+  int b = id / 2;  // of those that are cut
+  if (cut < a.B) {
+    int upto = __popc(word);
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const int y = __shfl_up_sync(~0u, upto, d);
+      if (lane >= d) upto += y;
+    }
+    const int at = __ffs(__ballot_sync(~0u, upto > b)) - 1;
+    b -= __shfl_sync(~0u, upto - __popc(word), at);
+    word = __shfl_sync(~0u, word, at);
+    for (; b > 0; --b) word &= word - 1;
+    b = 32 * at + __ffs(word) - 1;
+  }
+  x.b = b;
+  x.n = a.B <= kMostLooked || min(a.lens[b], a.cache.capacity) > a.left ? a.left : 0;
+  return x;
 }
 __device__ __forceinline__ void turn_barrier(int size) {
   // The notes go from thread to thread of a block, which __syncthreads orders.  Between blocks nothing is handed on but that
@@ -334,22 +393,20 @@ __host__ __device__ __forceinline__ int side_of(int pieces) {
 
 // A thread has a piece of kPer rows of every turn, which it copies to a slot of its own and takes from there.
 template <int BYTES>
-__global__ void __launch_bounds__(kMoveThreads) k_evict_rows(EvictArgs a, Kind rows_of, Kind scales_of, int size) {
+__global__ void __launch_bounds__(kMoveThreads) k_evict_rows(EvictArgs a, Kind rows_of, Kind scales_of, Divisor by_page, int size) {
   using P = typename Piece<BYTES>::type;
   extern __shared__ __align__(16) char smem[];  // kStages turns of pieces, and notes of kNotes
   wait_for_stream();
-  const int job = blockIdx.x / size;
-  const bool scales = job >= rows_of.jobs;
-  const Kind& kind = scales ? scales_of : rows_of;
-  char* base;
-  int b;
-  const int n = part_of(a, kind, scales ? job - rows_of.jobs : job, &base, &b);
+  const Job job = job_of<BYTES>(a, rows_of, scales_of, blockIdx.x / size, gridDim.x / size);
+  const int b = job.b, n = job.n;
   if (n == 0) return;  // in every block of the cluster
-  const int pieces = kind.bytes / BYTES, side = side_of(pieces), rows = side * kPer;  // rows side by side, and of a turn
+  const Kind& kind = job.of_scales ? scales_of : rows_of;
+  char* base = job.base;
+  const int pieces = job.bytes / BYTES, side = side_of(pieces), rows = side * kPer;  // rows side by side, and of a turn
   const int piece = threadIdx.x % pieces, r0 = threadIdx.x / pieces;
   const bool works = r0 < side;
   const int rank = size > 1 ? (int)cluster_ctarank() : 0;
-  Moves moves{a, kind, a.kept + (int64_t)b * a.left, a.cache.table + b * a.cache.table_stride, n, rows * size,
+  Moves moves{a, kind.page, kind.slot, by_page, a.kept + (int64_t)b * a.left, a.cache.table + b * a.cache.table_stride, n, rows * size,
               (int)threadIdx.x < rows ? rank * rows + (int)threadIdx.x : rows * size};
   const int turns = (n + rows * size - 1) / (rows * size);
   P* ring = reinterpret_cast<P*>(smem) + threadIdx.x;
@@ -374,21 +431,25 @@ __global__ void __launch_bounds__(kMoveThreads) k_evict_rows(EvictArgs a, Kind r
   moves.start(kStages - 1);
   __syncthreads();
   for (int t = 0; t < kStages - 1; ++t) load(t);
-  for (int t = 0; t < turns; ++t) {
-    note(t + kStages - 1, moves.next(t + kStages - 1));
-    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-    turn_barrier(size);  // turn t has been read by every thread of the cluster; its rows may be written over
-    if (works) {
-      const Move* of = notes + t % kNotes * kMoveThreads + r0;
-      const P* from = ring + t % kStages * (kPer * kMoveThreads);
+  for (int t0 = 0; t0 < turns; t0 += 2 * kAhead)
 #pragma unroll
-      for (int k = 0; k < kPer; ++k) {
-        const int64_t to = of[k * side].to;
-        if (to >= 0) *reinterpret_cast<P*>(base + to) = from[k * kMoveThreads];
+    for (int u = 0; u < 2 * kAhead; ++u) {
+      const int t = t0 + u;
+      if (t >= turns) break;  // in every block of the cluster
+      note(t + kStages - 1, moves.next(t + kStages - 1, u));
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+      turn_barrier(size);  // turn t has been read by every thread of the cluster; its rows may be written over
+      if (works) {
+        const Move* of = notes + t % kNotes * kMoveThreads + r0;
+        const P* from = ring + t % kStages * (kPer * kMoveThreads);
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+          const int64_t to = of[k * side].to;
+          if (to >= 0) *reinterpret_cast<P*>(base + to) = from[k * kMoveThreads];
+        }
       }
+      load(t + kStages - 1);
     }
-    load(t + kStages - 1);
-  }
 }
 
 template <int BYTES>
@@ -396,55 +457,62 @@ constexpr size_t smem_of() {
   return kMoveThreads * (kStages * kPer * (size_t)BYTES + kNotes * sizeof(Move));
 }
 
-// The largest clusters of which `jobs` run at the same time (a cluster waits for its own blocks only, so more would be
-// right as well, one after another): 1 to `most` blocks.  What the device holds is asked once a device and size.
+// How many clusters of `size` blocks (1 to kMaxCluster) run at the same time; asked once a device and size.
 template <int BYTES>
-static int cluster_size(int64_t jobs, int most, int* size) {
+static int clusters_at_once(int size, int* n) {
   static std::atomic<uint64_t> allowed{0};
-  static std::atomic<int> held[64][4];  // a device's clusters of 2^i blocks, and one more (0: not asked yet)
+  static std::atomic<int> held[64][4];  // and one more (0: not asked yet)
   CP_TRY_STATUS(allow_smem_once((const void*)k_evict_rows<BYTES>, smem_of<BYTES>(), "evict: shared memory", &allowed));
   int dev = 0;
   CP_TRY_STATUS(cuda_status(cudaGetDevice(&dev), "evict: device"));
-  for (*size = most; *size > 1; *size /= 2) {
-    std::atomic<int>& known = held[dev & 63][*size >= 8 ? 3 : *size / 2];
-    int n = known.load(std::memory_order_relaxed) - 1;
-    if (n < 0) {
-      cudaLaunchAttribute with{};
-      with.id = cudaLaunchAttributeClusterDimension;
-      with.val.clusterDim = {(unsigned)*size, 1, 1};
-      cudaLaunchConfig_t cfg{};
-      cfg.gridDim = dim3((unsigned)*size);
-      cfg.blockDim = dim3(kMoveThreads);
-      cfg.dynamicSmemBytes = smem_of<BYTES>();
-      cfg.attrs = &with;
-      cfg.numAttrs = 1;
-      if (cudaOccupancyMaxActiveClusters(&n, k_evict_rows<BYTES>, &cfg) != cudaSuccess) {
-        (void)cudaGetLastError();  // a size that the device does not take
-        n = 0;
-      }
-      known.store(n + 1, std::memory_order_relaxed);
-    }
-    if (jobs <= n) break;
+  std::atomic<int>& known = held[dev & 63][size >= 8 ? 3 : size / 2];
+  *n = known.load(std::memory_order_relaxed) - 1;
+  if (*n >= 0) return CP_OK;
+  cudaLaunchAttribute with{};
+  with.id = cudaLaunchAttributeClusterDimension;
+  with.val.clusterDim = {(unsigned)size, 1, 1};
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)size);
+  cfg.blockDim = dim3(kMoveThreads);
+  cfg.dynamicSmemBytes = smem_of<BYTES>();
+  cfg.attrs = &with;
+  cfg.numAttrs = 1;
+  if (cudaOccupancyMaxActiveClusters(n, k_evict_rows<BYTES>, &cfg) != cudaSuccess) {
+    (void)cudaGetLastError();  // a size that the device does not take
+    *n = 0;
   }
+  known.store(*n + 1, std::memory_order_relaxed);
   return CP_OK;
 }
 
 // Rows of two kinds (of the second there may be none) moved up.
 template <int BYTES>
 static int move_rows(const EvictArgs& a, const Kind& first, const Kind& second, cudaStream_t s) {
-  const int rows = side_of(first.bytes / BYTES) * kPer;
-  const int64_t jobs = (int64_t)first.jobs + second.jobs;
-  // clusters where there are few heads and sequences, if they get some turns
-  int most = kMaxCluster, size = 1;
-  while (most > 1 && (int64_t)rows * most * 4 > a.left) most /= 2;
-  CP_TRY_STATUS(cluster_size<BYTES>(jobs, most, &size));
-  if (jobs * size > 0x7FFFFFFF) return CP_EUNSUPPORTED;
-  return cuda_status(launch_early_cluster(k_evict_rows<BYTES>, dim3((unsigned)(jobs * size)), kMoveThreads, smem_of<BYTES>(), s,
-                                          size, a, first, second, size),
+  const int rows = side_of(first.bytes / BYTES) * kPer, units = units_of<BYTES>(first);
+  const int64_t jobs = (int64_t)a.B * 2 * (first.parts + second.parts);
+  // Clusters where there are few heads and sequences, if they get some turns: of the sizes of which all jobs run at the same
+  // time (a cluster waits for its own blocks only, so more would be right as well, one after another) the one that
+  // keeps most blocks busy should every sequence be cut.
+  int size = 1;
+  int64_t clusters = jobs, busy = 0;
+  for (int z = kMaxCluster; z >= 1; z /= 2) {
+    if (z > 1 && (int64_t)rows * z * 4 > a.left) continue;
+    int n = 0;
+    CP_TRY_STATUS(clusters_at_once<BYTES>(z, &n));
+    if (jobs > n && z > 1) continue;
+    const int64_t with = jobs > n ? jobs : ((int64_t)divided_by(n, a.B, first, second, units) * first.parts + second.parts) * 2 * a.B;
+    if (with * z <= busy) continue;
+    busy = with * z;
+    size = z;
+    clusters = std::max(jobs, std::min((int64_t)n, (int64_t)a.B * 2 * ((int64_t)first.parts * units + second.parts)));
+  }
+  if (clusters * size > 0x7FFFFFFF) return CP_EUNSUPPORTED;
+  return cuda_status(launch_early_cluster(k_evict_rows<BYTES>, dim3((unsigned)(clusters * size)), kMoveThreads, smem_of<BYTES>(), s,
+                                          size, a, first, second, divisor(a.cache.page_size), size),
                      "evict: rows");
 }
 // How rows of `bytes` bytes a head move, heads `head` bytes apart: by 16 bytes (`whole`) or by 4.
-static int divide(const EvictArgs& a, Kind* kind, int64_t head, int bytes, int sms, bool* whole) {
+static int divide(const EvictArgs& a, Kind* kind, int64_t head, int bytes, bool* whole) {
   int group = 1;  // heads that lie side by side go together
   const int heads = a.cache.heads;
   if (head == bytes)
@@ -453,20 +521,10 @@ static int divide(const EvictArgs& a, Kind* kind, int64_t head, int bytes, int s
   kind->parts = heads / group;
   kind->part = head * group;
   kind->bytes = bytes * group;
-  kind->split = 1;
   const uint64_t any = (uint64_t)kind->k | (uint64_t)kind->v | (uint64_t)kind->page | (uint64_t)kind->slot | (uint64_t)kind->part |
                        (uint64_t)kind->bytes;
   *whole = any % 16 == 0;
-  // where clusters of whole rows would not fill the device, halves of them
-  // (one sequence of 200,001 keys and 8 heads of 128 198 us, whole rows 275; 32 sequences 54.6, whole 50.1)
-  while (*whole && (int64_t)a.B * 2 * kind->parts * kind->split * kMaxCluster < 2 * sms && kind->bytes >= 256 &&
-         kind->bytes % 32 == 0) {
-    kind->bytes /= 2;
-    kind->split *= 2;
-  }
-  const int64_t jobs = (int64_t)a.B * 2 * kind->parts * kind->split;
-  if (jobs > 0x3FFFFFFF) return CP_EUNSUPPORTED;
-  kind->jobs = (int)jobs;
+  if ((int64_t)a.B * 2 * kind->parts > 0x3FFFFFFF) return CP_EUNSUPPORTED;
   return CP_OK;
 }
 
@@ -491,8 +549,8 @@ int launch_cache_evict(const EvictArgs& a, int cache_dtype, cudaStream_t s) {
   Kind rows{(char*)ch.k, (char*)ch.v, cache_bytes(cache_dtype, ch.page_stride), cache_bytes(cache_dtype, ch.slot_stride)};
   Kind scales{(char*)ch.k_block, (char*)ch.v_block, ch.block_page, ch.block_slot}, none{};
   bool whole = true, together = false;  // (rows of the cache are multiples of 16 bytes)
-  CP_TRY_STATUS(divide(a, &rows, cache_bytes(cache_dtype, ch.head_stride), (int)cache_bytes(cache_dtype, ch.D), di.sm_count, &whole));
-  if (cache_dtype == CP_I4) CP_TRY_STATUS(divide(a, &scales, ch.block_head, block_bytes(ch.D), di.sm_count, &together));
+  CP_TRY_STATUS(divide(a, &rows, cache_bytes(cache_dtype, ch.head_stride), (int)cache_bytes(cache_dtype, ch.D), &whole));
+  if (cache_dtype == CP_I4) CP_TRY_STATUS(divide(a, &scales, ch.block_head, block_bytes(ch.D), &together));
   CP_TRY_STATUS(move_rows<16>(a, rows, together ? scales : none, s));
   return cache_dtype == CP_I4 && !together ? move_rows<4>(a, scales, none, s) : CP_OK;
 }

@@ -523,6 +523,16 @@ def test_evict_narrow_rows(D, H, cdt):
     check_evict(D, [700, 65, 64, 63], 64, 0, 5, 16, H, D, cdt)
 
 
+@pytest.mark.parametrize("D,H,cdt,hf", [(96, 2, BF16, False), (80, 1, BF16, True), (256, 1, F32, False), (128, 4, I4, False), (64, 4, I4, True), (48, 3, E4M3, False)])
+@pytest.mark.parametrize("B,cut", [(21, [20]), (33, [0, 31, 32]), (256, [7, 255]), (257, [3, 256]), (300, [])])
+def test_evict_few_of_many(B, cut, D, H, cdt, hf):
+    """Sequences that are cut between many that are not: blocks of those help."""
+    lens = [(7 * b) % 600 + 1 for b in range(B)]
+    for i, b in enumerate(cut):
+        lens[b] = 640 + 37 * i
+    check_evict(B + D, lens, 600, 2, 50, 16, H, D, cdt, hf)
+
+
 @pytest.mark.parametrize("left,first,recent", [(0, 0, 0), (1, 0, 0), (1, 1, 0), (1, 0, 1), (50, 25, 25), (50, 0, 50), (50, 50, 0), (50, 0, 0), (999, 10, 10),
                                                (1000, 0, 0), (5000, 7, 9)])
 def test_evict_budgets(left, first, recent):
