@@ -93,10 +93,11 @@ struct Shape {
   // Short sequences: three blocks, as registers allow, as there is more to begin
   // than to copy.
   // 4 bits: instructions bound it, and 2, 3 and 4 blocks of 128 threads do 32 sequences of 8448 keys in 48.6, 47.8
-  // and 49.7 us.
+  // and 49.7 us.  (100 KB, not 112, leave two blocks of 16 queries and heads of 128 room for the keys whose scores they leave behind:
+  // 32 sequences of 8448 keys, 64 heads and weights 91 us, by one block 128.)
   static constexpr int blocks = CT != CP_I4 ? (SHORT ? 3 : 2) : DP == 256 || (DP == 128 && QT == 16) ? 2 : DP == 128 || QT == 16 ? 3 : 4;
   static constexpr int bound = CT == CP_I4 ? blocks : 0;  // of the registers
-  static constexpr int room = CT != CP_I4 ? (SHORT ? 64 : 100) : blocks == 4 ? 50 : blocks == 3 ? 68 : 112;  // KB of a block
+  static constexpr int room = CT != CP_I4 ? (SHORT ? 64 : 100) : blocks == 4 ? 50 : blocks == 3 ? 68 : DP == 256 ? 112 : 100;  // KB of a block
   static constexpr int fit = room * 1024 / (kWarps * tile);
   static constexpr int least = SHORT || CT == CP_I4 ? 2 : 3;
   static constexpr int stages = fit < least ? least : fit > 8 ? 8 : fit;
@@ -1212,9 +1213,17 @@ __global__ void __launch_bounds__(kThreads, Shape<CT, DP, QT>::bound) k_decode_c
   __shared__ int s_queue[kWarps][kQueue];
   __shared__ uint32_t s_valid[kWarps][S::stages];
   __shared__ int s_keys[kWarps][SCORES ? S::stages * S::tk : 1];
-  __shared__ float s_m[kWarps][QT], s_l[kWarps][QT], s_f[kWarps][QT];
-  __shared__ float s_top[QT], s_sum[QT];          // this block's, for the others
-  __shared__ float s_w[QT][kMaxCluster], s_all[QT];  // the blocks' weights and the whole sum
+  // the warps' maxima, sums and factors, then the blocks' weights (two blocks of 4-bit heads of 256 have no 500 bytes more)
+  __shared__ union {
+    float warps[3][kWarps][QT];
+    float blocks[QT][kMaxCluster];
+  } s_by;
+  auto& s_m = s_by.warps[0];
+  auto& s_l = s_by.warps[1];
+  auto& s_f = s_by.warps[2];
+  auto& s_w = s_by.blocks;
+  __shared__ float s_top[QT], s_sum[QT];  // this block's, for the others
+  __shared__ float s_all[QT];             // the whole sum
   wait_for_stream();
   const Cache& ch = a.cache;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
