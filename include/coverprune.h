@@ -603,7 +603,8 @@ int coverprune_decode_attention(const void* q, const int64_t* q_stride, int dtyp
  * for every visible key j (in float32, the heads in a fixed order); others are not
  * touched.  A NaN among a query head's visible scores makes its weights NaN.
  *   weight    device float32, rows of B sequences weight_stride >= 0 elements apart, which
- *             must not overlap; each holds the keys that the table's row does
+ *             must not overlap one another, nor q, out, lse, lens, keep or ws; each holds
+ *             the keys that the table's row does
  *   ws        coverprune_decode_weigh_workspace_size bytes: the attention's, and a float for
  *             every query head and key that the table's row holds (queries of a kv head
  *             counted to a power of two)

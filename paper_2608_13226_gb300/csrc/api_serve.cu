@@ -14,6 +14,44 @@ static bool overlap(const void* p, int64_t n, const void* q, int64_t m) {  // of
 }
 static size_t size_of(int dtype) { return dtype == CP_F32 ? 4 : dtype == CP_BF16 ? 2 : 1; }
 
+// `rows` rows of `bytes` bytes, `apart` bytes from one to the next (a stride of the caller's may be any number: 128 bits
+// hold what its products come to).
+struct Area {
+  __int128 at;
+  int64_t rows;
+  __int128 bytes, apart;
+};
+static Area area(const void* p, int64_t rows, __int128 bytes, __int128 apart) {
+  if (!p || rows < 1 || bytes < 1) return Area{0, 0, 0, 0};
+  Area x{(__int128)(uintptr_t)p, rows, bytes, apart};
+  if (x.apart < 0) {  // from the lowest row on
+    x.at += (x.rows - 1) * x.apart;
+    x.apart = -x.apart;
+  }
+  if (x.apart == 0) x.rows = 1;
+  return x;
+}
+static Area area(const void* p, __int128 bytes) { return area(p, 1, bytes, 0); }
+// Rows of heads, as one stretch a token or sequence.
+static Area area_of_heads(const void* p, int64_t n, const int64_t* stride, int64_t heads, int64_t D, int dtype) {
+  const __int128 e = (__int128)size_of(dtype), far = e * (heads - 1) * stride[1];
+  Area x = area(p, n, (far < 0 ? -far : far) + e * D, e * stride[0]);
+  if (x.rows > 0 && far < 0) x.at += far;
+  return x;
+}
+// Whether two share a byte.  Rows that take turns at one distance do not; of rows at two distances whose
+// ranges overlap it is taken for granted.
+static bool meet(const Area& a, const Area& b) {
+  if (a.rows == 0 || b.rows == 0) return false;
+  const auto end = [](const Area& x) { return x.at + (x.rows - 1) * x.apart + x.bytes; };
+  if (a.at >= end(b) || b.at >= end(a)) return false;
+  if (a.rows > 1 && b.rows > 1 && a.apart != b.apart) return true;
+  const __int128 apart = a.rows > 1 ? a.apart : b.rows > 1 ? b.apart : 0;
+  if (apart == 0) return true;
+  const __int128 from = ((a.at - b.at) % apart + apart) % apart;  // of a's rows, behind b's
+  return from < b.bytes || apart - from < a.bytes;
+}
+
 // Room for a call's element offsets (a stride times a size) in 64 bits.
 constexpr int64_t kMaxSize = 0x7FFFFFFF;
 // Keys of a sequence: an index a little past the last is still an int.
@@ -265,6 +303,14 @@ static int attend(const void* q, const int64_t* q_stride, int dtype, int64_t B, 
   const int st_room = room_of(B, Hq, a.cache, cache->dtype, &room);
   if (weights) CP_TRY_STATUS(st_room);
   if (!ws || !aligned(ws, 256) || ws_bytes < (weights ? room.all : room.decode)) return CP_EWORKSPACE;
+  if (weights) {  // written while others are read or written
+    const Area w = area(weight, B, 4 * (__int128)a.cache.capacity, 4 * (__int128)weight_stride);
+    const Area others[] = {area_of_heads(q, B, q_stride, Hq, a.cache.D, dtype), area_of_heads(out, B, out_stride, Hq, a.cache.D, dtype),
+                           area(lse, 4 * (__int128)B * Hq), area(lens, 4 * B), area(keep, B, a.cache.capacity, keep_stride),
+                           area(ws, room.all)};
+    for (const Area& x : others)
+      if (meet(w, x)) return CP_EINVAL;
+  }
   a.q = q;
   a.q_b = q_stride[0];
   a.q_h = q_stride[1];
