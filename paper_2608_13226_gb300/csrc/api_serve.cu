@@ -9,9 +9,6 @@
 using namespace cp;
 
 static bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
-static bool overlap(const void* p, int64_t n, const void* q, int64_t m) {  // of n and m 4-byte words
-  return p && q && (uintptr_t)p < (uintptr_t)q + 4 * (uintptr_t)m && (uintptr_t)q < (uintptr_t)p + 4 * (uintptr_t)n;
-}
 static size_t size_of(int dtype) { return dtype == CP_F32 ? 4 : dtype == CP_BF16 ? 2 : 1; }
 
 // `rows` rows of `bytes` bytes, `apart` bytes from one to the next (a stride of the caller's may be any number: 128 bits
@@ -221,7 +218,8 @@ int coverprune_cache_append(const cp_cache* cache, const void* k, const int64_t*
       !aligned(status, 4) || !aligned(pos, 8))
     return CP_EINVAL;
   // blocks read the lengths and starts while others write
-  if (overlap(new_lens, B, lens, B) || overlap(new_lens, B, starts, B + 1)) return CP_EINVAL;
+  const Area lens_out = area(new_lens, 4 * B);
+  if (meet(lens_out, area(lens, 4 * B)) || meet(lens_out, area(starts, 4 * (B + 1)))) return CP_EINVAL;
   if (T > 0 && (!k || !v || !k_stride || !v_stride || !aligned(k, size_of(dtype)) ||
                 !aligned(v, size_of(dtype))))
     return CP_EINVAL;
@@ -417,13 +415,14 @@ int coverprune_cache_evict(const cp_cache* cache, const int32_t* lens, int64_t B
   if (new_weight && B > 1 && new_weight_stride < new_weight_width) return CP_EINVAL;
   if (one_place(a.cache, cache->dtype == CP_I4)) return CP_EINVAL;
   // what a block writes others still read
-  const int64_t w = (B - 1) * weight_stride + a.cache.capacity, nw = (B - 1) * new_weight_stride + new_weight_width;
-  const struct { const void* p; int64_t n; } in[2] = {{lens, B}, {weight, w}}, out[3] = {{new_lens, B}, {new_weight, nw}, {kept, left * B}};
+  const Area in[2] = {area(lens, 4 * B), area(weight, B, 4 * (__int128)a.cache.capacity, 4 * (__int128)weight_stride)};
+  const Area out[3] = {area(new_lens, 4 * B), area(new_weight, B, 4 * (__int128)new_weight_width, 4 * (__int128)new_weight_stride),
+                       area(kept, 4 * left * B)};
   for (int i = 0; i < 3; ++i) {
-    for (const auto& x : in)
-      if (overlap(out[i].p, out[i].n, x.p, x.n)) return CP_EINVAL;
+    for (const Area& x : in)
+      if (meet(out[i], x)) return CP_EINVAL;
     for (int j = 0; j < i; ++j)
-      if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return CP_EINVAL;
+      if (meet(out[i], out[j])) return CP_EINVAL;
   }
   a.lens = lens;
   a.B = (int)B;

@@ -36,3 +36,19 @@ def test_weights_beside_and_in_place_of_others():
     both = torch.zeros(B * keys, device="cuda")
     with pytest.raises(cp.CoverPruneError):
         cp.coverprune_decode_attention(q, c.k, c.v, c.table, both.view(torch.int32)[5:5 + B], weight=both.view(B, keys))
+
+
+def test_evict_weights_between_one_anothers_rows():
+    """Old and new weights of a sequence side by side in one tensor share nothing."""
+    c, lens = Cache(gen(0), 3, 64, 16, 1, 64, BF16), ints([64, 40, 7])
+    other = Cache(gen(0), 3, 64, 16, 1, 64, BF16)
+    x = torch.rand(3, 2, c.W * 16, generator=gen(1), device="cuda")
+    w = x[:, 0].clone()
+    want = cp.coverprune_cache_evict(other.k, other.v, other.table, lens, w, 20, first=2, recent=3)
+    r = cp.coverprune_cache_evict(c.k, c.v, c.table, lens, x[:, 0], 20, first=2, recent=3, new_weight=x[:, 1])
+    assert torch.equal(x[:, 0], w) and torch.equal(x[:, 1], want["weight"]) and torch.equal(r["kept"], want["kept"])
+    assert torch.equal(c.k, other.k) and torch.equal(c.v, other.v)
+    turns = torch.rand(3, 2 * c.W * 16, device="cuda")  # rows that take turns, but a word too near
+    with pytest.raises(cp.CoverPruneError) as e:
+        cp.coverprune_cache_evict(c.k, c.v, c.table, lens, turns[:, :c.W * 16], 20, new_weight=turns[:, c.W * 16 - 1:-1])
+    assert e.value.status == cp.CP_EINVAL
