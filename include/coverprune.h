@@ -551,7 +551,7 @@ int coverprune_cache_read(const cp_cache* cache, int64_t T, const int32_t* start
  *             not moved (its new place keeps what it held).
  * new_lens, new_weight and kept must not overlap lens, weight or one another; keys and
  * values in one place are refused.  Sequences that share pages are the caller's mistake.  weight_stride and new_weight_stride in elements,
- * 0 to 2^36.  B <= 2^24, B * left < 2^31 * 16.
+ * 0 to 2^36.  B <= 2^24, B * left < 2^35.
  */
 int coverprune_cache_evict(const cp_cache* cache, const int32_t* lens, int64_t B,
                            const float* weight, int64_t weight_stride, int64_t left,

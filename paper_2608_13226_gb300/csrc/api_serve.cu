@@ -407,7 +407,7 @@ int coverprune_cache_evict(const cp_cache* cache, const int32_t* lens, int64_t B
   if (B < 0 || B > (1 << 24) || left < 0 || first < 0 || recent < 0 || first > left || recent > left - first ||
       weight_stride > far || new_weight_stride > far || weight_stride < 0 || new_weight_stride < 0 || new_weight_width < 0 || new_weight_width > kMaxSize)
     return CP_EINVAL;
-  if (left > kMaxKeys || left * B > kMaxSize * 16) return CP_EUNSUPPORTED;
+  if (left > kMaxKeys || left * B >= (int64_t)1 << 35) return CP_EUNSUPPORTED;
   if (B == 0) return CP_OK;
   if (!lens || !aligned(lens, 4) || !aligned(weight, 4) || !aligned(new_lens, 4) || !aligned(new_weight, 4) ||
       !aligned(kept, 4) || !aligned(status, 4) || (left > 0 && !kept) || (a.cache.capacity > 0 && !weight))

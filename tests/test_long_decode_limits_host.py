@@ -1,5 +1,5 @@
-"""Memory that the calls of a long decode must not share is refused before anything is launched (fake pointers, never
-dereferenced)."""
+"""Memory that the calls of a long decode must not share, and sizes at their limits: refused before anything is launched (fake
+pointers, never dereferenced)."""
 import ctypes as C
 
 import pytest
@@ -38,3 +38,13 @@ def test_weights_in_place_of_others(lib, kw):
 def test_weights_in_the_workspace_end(lib):
     _, n = _weigh(lib, weight=Q)
     assert _weigh(lib, weight=WS + n - 4)[0] == cp.CP_EINVAL
+
+
+def test_most_keys_that_evictions_leave(lib):
+    """B * left < 2^35, as the header says: the largest is looked at further (and lacks its lengths), the next one is too much."""
+    def evict(B, left):
+        return lib.coverprune_cache_evict(C.byref(cache()), None, B, P(WEIGHT), KEYS, left, 0, 0, None, None, 0, 0, P(OUT), None, None)
+
+    assert 279527 * 122921 == 2 ** 35 - 1
+    assert evict(279527, 122921) == cp.CP_EINVAL
+    assert evict(1 << 15, 1 << 20) == cp.CP_EUNSUPPORTED and evict(1 << 24, 1 << 30) == cp.CP_EUNSUPPORTED
