@@ -1524,9 +1524,11 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   const int64_t columns = (int64_t)a.B * ch.heads * tiles;
   // A 4-bit row is shorter than the 128 bytes that L2 likes, and its scales than the 32 that it fetches at least: where
   // a token's heads lie side by side, the blocks go over them together.  32 sequences of 8448 keys and 4 heads of 128
-  // 47.7 us, head by head 58.9 (and 295 MB read for 156); of 20 heads of 64 123, 201.
+  // 47.5 us, head by head 57.7 (and 295 MB read for 156), in pages of one row 50.7, 59.5; of 20 heads of 64 126, 184.
   int lines = 1;
-  if (CT == CP_I4 && ch.heads > 1 && ch.slot_stride > ch.head_stride && 4 * ch.heads * tiles <= grid) {
+  // from a token to the next: pages of one row have no second slot
+  const int64_t token = ch.page_size > 1 ? ch.slot_stride : ch.page_stride;
+  if (CT == CP_I4 && ch.heads > 1 && token > ch.head_stride && 4 * ch.heads * tiles <= grid) {
     lines = ch.heads * tiles;
     grid = grid / lines * lines;
   }

@@ -52,3 +52,21 @@ def test_evict_weights_between_one_anothers_rows():
     with pytest.raises(cp.CoverPruneError) as e:
         cp.coverprune_cache_evict(c.k, c.v, c.table, lens, turns[:, :c.W * 16], 20, new_weight=turns[:, c.W * 16 - 1:-1])
     assert e.value.status == cp.CP_EINVAL
+
+
+# ------------------------------------------------------------------ one memory, two descriptions
+@pytest.mark.parametrize("Hq,H,D", [(28, 4, 128), (20, 20, 64), (64, 4, 128)])
+def test_pages_of_one_row(Hq, H, D):
+    """The rows of pages of 16 are pages of one as well: the same memory in the same order, dealt out alike, and so the same bits."""
+    B, keys = 9, 4096
+    c = Cache(gen(D), B, keys, 16, H, D, I4)
+    lens, q = ints([keys - 100 * b for b in range(B)]), randn(gen(1), B, Hq, D, dtype=BF16)
+    single = (c.table[:, :, None] * 16 + torch.arange(16, device="cuda", dtype=torch.int32)).reshape(B, -1)
+    # the dimension of one has no stride that counts, whatever the tensor's says
+    k, v, kb, vb = (t.reshape(-1, 1, *t.shape[2:]) for t in (c.k, c.v, c.kb, c.vb))
+    w, w1 = torch.zeros(2, B, keys, device="cuda")
+    for weight in (False, True):
+        want = cp.coverprune_decode_attention(q, c.k, c.v, c.table, lens, lse=True, weight=w if weight else None, **c.kw)
+        got = cp.coverprune_decode_attention(q, k, v, single, lens, lse=True, weight=w1 if weight else None, k_block=kb, v_block=vb)
+        assert torch.equal(bits(got["out"]), bits(want["out"])) and torch.equal(got["lse"], want["lse"])
+    assert torch.equal(w, w1)
