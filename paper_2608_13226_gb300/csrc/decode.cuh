@@ -141,22 +141,13 @@ __host__ __device__ constexpr int swizzle(int r) {
   return CT == CP_F32 ? (r & 1) << 2 : CPR >= 8 ? r & 7 : CPR == 4 ? (r >> 1) & 3 : (r >> 2) & 1;
 }
 
-// WHOLE: L2 fetches the 128 bytes around it, which rows of a head of at least as many fill.
-template <bool WHOLE>
+// 16 bytes of a row; L2 fetches the 128 around them.
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-  if (WHOLE)
-    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-  else
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-template <bool WHOLE>
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
   const int n = there ? 16 : 0;  // 0: nothing is read, zeros are written
-  if (WHOLE)
-    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n)
-                 : "memory");
-  else
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
 // 4, 8 or 16 bytes, or as many zeros.
 template <int BYTES>
@@ -926,7 +917,6 @@ __device__ __forceinline__ void math_of_keys(const DecodeArgs& a, const Rows& ro
                                              int hi, int hk, int b, int col, int h0, int nq, int warp, int lane, uint32_t ring,
                                              uint32_t* s_valid, int* s_keys, char* extra, Math<CT, DP, QT, SHORT>& math) {
   using S = Shape<CT, DP, QT, SHORT>;
-  constexpr bool kWhole = true;
   const Cache& ch = a.cache;
   const int chunks = (int)cache_bytes(CT, ch.D) / 16;  // of a row that is there
   const char* kp = (const char*)ch.k + cache_bytes(CT, (int64_t)hk * ch.head_stride);
@@ -991,15 +981,15 @@ __device__ __forceinline__ void math_of_keys(const DecodeArgs& a, const Rows& ro
       };
       if (valid == S::all && chunks == S::cpr) {
         each([&](uint32_t at, uint64_t off, int, int) {
-          copy16<kWhole>(at, kp + off);
-          copy16<kWhole>(at + S::tk * S::row, vp + off);
+          copy16(at, kp + off);
+          copy16(at + S::tk * S::row, vp + off);
         });
       } else {
         each([&](uint32_t at, uint64_t off, int r, int c) {
           const bool there = valid >> r & 1;
           if (c < chunks) {
-            copy16<kWhole>(at, kp + (there ? off : 0), there);
-            copy16<kWhole>(at + S::tk * S::row, vp + (there ? off : 0), there);
+            copy16(at, kp + (there ? off : 0), there);
+            copy16(at + S::tk * S::row, vp + (there ? off : 0), there);
           }
         });
       }
