@@ -1345,7 +1345,7 @@ __device__ __forceinline__ void load_part(const float* p, float (&x)[V]) {
     }
   }
 }
-template <int CT, int DP, int QT, bool SCORES>
+template <int CT, int DP, int QT>
 __global__ void __launch_bounds__(32 * kJoinWarps) k_decode_join(DecodeArgs a, int tiles, int side, const float* parts,
                                                                  const Begin* begins, int lines_of) {
   using S = Shape<CT, DP, QT>;
@@ -1423,6 +1423,19 @@ __global__ void __launch_bounds__(32 * kJoinWarps) k_decode_join(DecodeArgs a, i
     if (V * lane + j < a.cache.D) out[V * lane + j] = from_f32<Row>(sum == 0.0f ? 0.0f : o[j] * by);
   if (lane == 0 && a.lse) a.lse[(int64_t)x.b * a.Hq + h0 + n] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
+
+template <int CT, int DP, int QT>
+int launch_join(const DecodeArgs& a, dim3 joins, int tiles, int side, const float* parts, const Begin* begins, int lines, cudaStream_t s) {
+  return cuda_status(launch_early(k_decode_join<CT, DP, QT>, joins, 32 * kJoinWarps, 0, s, a, tiles, side, parts, begins, lines),
+                     "decode: join");
+}
+// The joins of a type are compiled in one of its translation units (WHERE: nothing) and used from the other, whose variants leave
+// the scores behind (WHERE: extern).
+#define CP_JOIN(WHERE, CT, DP, QT) \
+  WHERE template int launch_join<CT, DP, QT>(const DecodeArgs&, dim3, int, int, const float*, const Begin*, int, cudaStream_t);
+#define CP_JOINS(WHERE, CT, FEW, MANY)                                                                             \
+  CP_JOIN(WHERE, CT, 64, FEW) CP_JOIN(WHERE, CT, 64, MANY) CP_JOIN(WHERE, CT, 128, FEW) CP_JOIN(WHERE, CT, 128, MANY) \
+  CP_JOIN(WHERE, CT, 256, FEW) CP_JOIN(WHERE, CT, 256, MANY)
 
 // The largest clusters of which `columns` run at the same time, 2 to kMaxCluster blocks
 // (1: there are none): at most `all` blocks, and no more clusters than the device
@@ -1587,8 +1600,7 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   int side = share <= 4 ? 8 : share <= 12 ? 2 : 1;
   while (side > 1 && side / 2 >= queries) side /= 2;
   const dim3 joins((unsigned)(by_column ? columns : grid), (unsigned)(queries + side - 1) / side);
-  return cuda_status(launch_early(k_decode_join<CT, DP, QT, SCORES>, joins, 32 * kJoinWarps, 0, s, a, tiles, side, parts, begins, lines),
-                     "decode: join");
+  return launch_join<CT, DP, QT>(a, joins, tiles, side, parts, begins, lines, s);
 }
 
 template <int CT, int DP, bool SCORES>

@@ -3,6 +3,8 @@
 
 namespace cp {
 
+CP_JOINS(extern, CP_BF16, 8, 16)
+
 int launch_decode_bf16_scores(const DecodeArgs& a, cudaStream_t s) { return launch_type<CP_BF16, true>(a, s); }
 
 }  // namespace cp

@@ -3,6 +3,8 @@
 
 namespace cp {
 
+CP_JOINS(extern, CP_F32, 4, 8)
+
 int launch_decode_f32_scores(const DecodeArgs& a, cudaStream_t s) { return launch_type<CP_F32, true>(a, s); }
 
 }  // namespace cp

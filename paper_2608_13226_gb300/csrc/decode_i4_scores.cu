@@ -3,6 +3,8 @@
 
 namespace cp {
 
+CP_JOINS(extern, CP_I4, 8, 16)
+
 int launch_decode_i4_scores(const DecodeArgs& a, cudaStream_t s) { return launch_type<CP_I4, true>(a, s); }
 
 }  // namespace cp
