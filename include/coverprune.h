@@ -538,8 +538,9 @@ int coverprune_cache_read(const cp_cache* cache, int64_t T, const int32_t* start
  *   lens      device int32 [B]; negative is 0, more than the table's row holds is
  *             what it holds.  A sequence of at most `left` keys keeps them all.
  *   weight    device float32, weight[b * weight_stride + j] of key j (of
- *             coverprune_decode_attention_weigh, say); read for the keys between
- *             only.  A NaN counts as less than any number, -0 as 0.
+ *             coverprune_decode_attention_weigh, say).  Those of the keys between are
+ *             compared; where new_weight is given, those of all keys left are read and
+ *             copied, and so have to be set.  A NaN counts as less than any number, -0 as 0.
  *   left      >= 0;  first, recent >= 0 with first + recent <= left
  *   new_lens  device int32 [B] or NULL: the keys left; a negative lens[b] stays
  *   new_weight  device float32 or NULL, row b at b * new_weight_stride: the weights of the keys
@@ -600,8 +601,9 @@ int coverprune_decode_attention(const void* q, const int64_t* q_stride, int dtyp
 /*
  * coverprune_decode_attention_weigh -- the same, with what weight each key got added up:
  *   weight[b * weight_stride + j] += sum over the query heads h of exp(s_hj - lse_h)
- * for every visible key j (in float32, the heads in a fixed order); others are not
- * touched.  A NaN among a query head's visible scores makes its weights NaN.
+ * for every visible key j (in float32, the heads in a fixed order; a weight off by some
+ * (1 + |s| + |lse|) 2^-22 of itself, below 2^-126 0); others are not touched.  A NaN
+ * among a query head's visible scores makes its weights NaN.
  *   weight    device float32, rows of B sequences weight_stride >= 0 elements apart, which
  *             must not overlap one another, nor q, out, lse, lens, keep or ws; each holds
  *             the keys that the table's row does

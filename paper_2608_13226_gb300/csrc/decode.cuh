@@ -106,15 +106,17 @@ struct Shape {
   static constexpr int queries = SHORT ? kWarps : 1;
   static constexpr int extra = CT == CP_F32 ? (queries * QT * DP + kWarps * tk * QT) * 4 : 0;
   static constexpr int smem = ring + extra;
-  // (Registers allow them but for some spills, 4 to 84 bytes a thread: 16 queries and heads of
-  // 256 (255 registers), an 8-bit cache's 8 queries and heads of 64, float32's of 4 queries and
-  // heads of 128 and 256 and, for short sequences, of 8 and 128.)
+  // (Registers allow them but for some spills, 4 to 32 bytes of stores a thread: 4 and 8 bits' heads of
+  // 64, float32's of 128 and 256, 4 bits' of 256 with weights.  Heads of 256 with 16 queries, whose outputs
+  // and queries are 192 registers, spill more: 16 to 108 bytes of 16 or 8 bits, of 4 bits, where decoding
+  // needs its own, 248 to 516, and wait for that: 16 sequences of 8448 keys and 2 heads 52 us, with 8 queries 31.)
   static constexpr int per_sm = CT == CP_I4 ? blocks
                                 : SHORT && smem <= 70 * 1024 ? 3 : smem <= 110 * 1024 ? 2 : 1;
   static constexpr int part = QT * (DP + 2);  // floats of a partial result
   // What beginning and merging a segment costs, in units of 64 keys: about 3 us, in
   // which a block takes 72 KB (of 4 bits, which take longer to decode, less: 128 ragged
-  // sequences with 0, 2, 4 and 9 units 84.4, 82.6, 81.4, 83.1 us).
+  // sequences of heads of 128 with 0, 2, 4 and 9 units 84.4, 82.6, 81.4, 83.1 us; of 4 heads of 64 117, 111, 108, 103, of
+  // 8 with 2 queries each 192, 188, 187, 189).
   static constexpr int setup = CT == CP_I4 ? (DP == 64 ? 9 : 4) : 72 * 1024 / (2 * kUnit * row) < 1 ? 1 : 72 * 1024 / (2 * kUnit * row);
   static constexpr int pitch = DP + 4;        // floats of a query in the merge: the lanes' banks differ
   static_assert(SHORT || (kWarps * pitch + DP) * QT * 4 <= ring, "the merge reuses the ring");
@@ -141,7 +143,8 @@ __host__ __device__ constexpr int swizzle(int r) {
   return CT == CP_F32 ? (r & 1) << 2 : CPR >= 8 ? r & 7 : CPR == 4 ? (r >> 1) & 3 : (r >> 2) & 1;
 }
 
-// 16 bytes of a row; L2 fetches the 128 around them.
+// 16 bytes of a row; L2 fetches the 128 around them (which marked keys of 32-byte rows do not fill, at no cost: 2 sequences of
+// 180,876 keys with 15% marked 36 us with the hint and without).
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -1529,6 +1532,8 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   // a token's heads lie side by side, the blocks go over them together.  32 sequences of 8448 keys and 4 heads of 128
   // 47.5 us, head by head 57.7 (and 295 MB read for 156), in pages of one row 50.7, 59.5; of 20 heads of 64 126, 184.
   int lines = 1;
+  // (Blocks that are no multiple of the heads are left out: 61 heads of 64 and 16 sequences 212 us on 549 of 608, head by head
+  // 477; 2 sequences of 30,000 keys 99 and 98.)
   // from a token to the next: pages of one row have no second slot
   const int64_t token = ch.page_size > 1 ? ch.slot_stride : ch.page_stride;
   if (CT == CP_I4 && ch.heads > 1 && token > ch.head_stride && 4 * ch.heads * tiles <= grid) {
@@ -1553,6 +1558,10 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   // 1000 tiles of up to 1000 keys 31 / 16, 50 / 48, 8 bits 30 / 14, 45 / 35, float32 of up
   // to 600 41 / 24, 89 / 81; beyond it what some gain others lose: 1000 of up to 2000 37 /
   // 31, 76 / 90, float32 of up to 1000 50 / 34, 122 / 129.
+  // 4 bits, 7 queries a head of 128: 320 tiles of 150 to 300 keys 16.5 / 15.4, of 250 to 500 18.2 / 22.9; 640 23.2 / 19.6, 26.3 /
+  // 30.0; 1600 44.5 / 23.1, 53.2 / 33.6, of 500 to 1000 71.3 / 58.9; half marked 640 24.5 / 14.2, 23.6 / 18.9, of 500 to 1000
+  // 32.1 / 33.9.  (The rule leaves warps out at 320 tiles where half of up to 300 keys are marked, 18.6 / 11.5, and
+  // of heads of 64, 15.8 / 11.3.)
   // Few tiles too, when two tiles of keys (one of float32) are all there is: one sequence
   // of 4 tiles and 16 keys 5.5 / 3.8, of 50 5.5 / 6.2; 60 of 4, 16 keys 6.5 / 4.1, 50 keys
   // 7.2 / 6.5; float32, 8 keys 8.9 / 7.4, 16 keys 9.0 / 8.6 and, for one sequence, 7.9 /
@@ -1577,6 +1586,8 @@ static int launch(const DecodeArgs& a, cudaStream_t s) {
   // 7.5 / 6.0, of 1500 7.7 / 6.7, of 8000 15.2 / 11.1, of 16000 16.2 / 17.3; 64 of 1500
   // 15.4 / 11.3, of 4000 29.9 / 26.2, of 8000 with 15% marked 19.8 / 16.2; 128 of 1229
   // to 1741 24.1 / 22.8.
+  // 4 bits, as one line / with clusters: 4 tiles of 500 keys 9.3 / 7.4, of 8000 15.8 / 10.5; 64 of 1500 14.0 / 12.7, of
+  // 4000 20.5 / 22.2, with 15% marked 16.4 / 11.7; 128 of 1500 19.6 / 19.0.
   // float32 computes longer on a unit: half of the longest one's time and a quarter of
   // what idles; 64 tiles of 500 to 3000 keys 46 / 67 (heads of 256), 27 / 34 (128), 19 /
   // 25 (64), of 1500 41 / 40, 23.2 / 21.4, 17.4 / 15.7; 4 of 4000 16.1 / 19.5, 12.3 / 12.6,

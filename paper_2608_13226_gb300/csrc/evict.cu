@@ -318,8 +318,9 @@ __host__ __device__ __forceinline__ int divided_by(int clusters, int cut, const 
   return f < 1 ? 1 : f;
 }
 // The cluster's job (n 0: none).  Sequences that keep all their keys have none; where that leaves clusters without, they take pieces
-// of the others' rows (32 sequences of 1300 to 8704 keys, a few of them above 8000, 44 us, undivided 100).  Where all are cut, rows go
-// whole as far as that fills the device (32 sequences by 128 bytes 54.6 us, by 256 50.1).
+// of the others' rows (32 sequences of 1300 to 8704 keys, a few of them above 8000, 44 us, undivided 96; one of
+// 200,001 keys 174, 254).  Where all are cut, rows go whole as far as that fills the device (32 sequences by 128 bytes
+// 54.6 us, by 256 50.1, in an earlier version).
 template <int BYTES>
 __device__ __forceinline__ Job job_of(const EvictArgs& a, const Kind& rows, const Kind& scales, int id, int clusters) {
   __shared__ uint32_t s_cut[kMostLooked / 32];  // which sequences are cut
@@ -371,7 +372,7 @@ __device__ __forceinline__ void turn_barrier(int size) {
   // The notes go from thread to thread of a block, which __syncthreads orders.  Between blocks nothing is handed on but that
   // rows have been read, and a read that has come back cannot see what is written later: the cluster's barrier
   // need not order memory.  Doing so it would wait for every row written so far, each turn (one sequence of
-  // 200,001 keys 274 us, else 378).
+  // 200,001 keys 174 us, else 279).
   __syncthreads();
   if (size > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
@@ -532,8 +533,8 @@ int launch_cache_evict(const EvictArgs& a, int cache_dtype, cudaStream_t s) {
   DeviceInfo di;
   CP_TRY_STATUS(device_info(&di));
   const Cache& ch = a.cache;
-  // As many blocks of a sequence as the device has room for, of 8192 keys at least (one of 8192 keys 17.6 us a call, by
-  // two blocks 19.3).
+  // As many blocks of a sequence as the device has room for, of 8192 keys at least (one of 8192 keys 14.2 us a call, by
+  // two blocks 15.0).
   int size = 1;
   while (size < kMaxCluster && (int64_t)a.B * size * 2 <= di.sm_count && (int64_t)size * 16384 <= ch.capacity) size *= 2;
   if ((int64_t)a.B * size > 0x7FFFFFFF) return CP_EUNSUPPORTED;

@@ -263,7 +263,7 @@ __device__ __forceinline__ void turn_query(const Rope& r, int D, const T* in, T*
 
 // The same for rows in vectors of 16 bytes, with halves of the layout that are not vectors apart: pairs go four by four where
 // that divides them, and of what passes 16 components from a multiple of 16 on, but for the first.
-// (38,400 tokens of 28 + 2 x 4 heads of 96 with 24 turned 172 us, one by one 675.)
+// (38,400 tokens of 28 + 2 x 4 heads of 96 with 24 turned 154 us, one by one 675.)
 template <typename T>
 __device__ __forceinline__ void turn_query_apart(const Rope& r, const T* in, T* out, int piece, const float* co, const float* si) {
   const int apart = (r.half + 7) / 8;
