@@ -10,7 +10,8 @@ tokens' own indices in the scene (coverprune_cache_append).  Every further token
 is then one projection, one append with its query's rotation and one attention
 over the cache (coverprune_decode_attention).  The cache holds 16, 8 or 4 bits.  With a budget the
 attention adds up what weight each key gets, and every few tokens the lightest keys are evicted
-(coverprune_cache_evict).  Weights are random: what is shown is the
+(coverprune_cache_evict); a prompt over the budget is cut after its first token already, by that one's
+weights.  Weights of the layer are random: what is shown is the
 path and what pruning saves, the cache's size and the attention's time beside
 those of the unpruned scenes.
 """
